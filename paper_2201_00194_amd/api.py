@@ -477,3 +477,233 @@ def unpack_colblock64(x: torch.Tensor, n_rows: int, n_features: int) -> np.ndarr
     tiles = (n_rows + 63) // 64
     a = x[: tiles * n_features * 64].cpu().numpy().reshape(tiles, n_features, 64)
     return np.ascontiguousarray(a.transpose(0, 2, 1).reshape(tiles * 64, n_features)[:n_rows])
+
+
+# ---- mixtures of family models (familyseer_mixture.h) ---------------------------------------------
+
+FS_F32, FS_BF16, FS_F16 = 0, 1, 2
+FS_ID_I32, FS_ID_I64, FS_ID_U16 = 0, 1, 2
+FS_SCORE_SOFTMAX, FS_SCORE_SIGMOID = 0, 1
+FS_MAX_EXPERTS = 1024
+FS_MAX_CHOICES = 16
+
+_ELEMENT = {torch.float32: FS_F32, torch.bfloat16: FS_BF16, torch.float16: FS_F16}
+_ID = {torch.int32: FS_ID_I32, torch.int64: FS_ID_I64, torch.int16: FS_ID_U16, torch.uint16: FS_ID_U16}
+
+
+class _FsRouteParams(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("k", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("renormalise", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+                ("group_best", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+_i32, _i64, _vp, _sz, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
+for _name, _result, _args in (
+        ("fs_route", ctypes.c_int, [ctypes.POINTER(_FsRouteParams), _i64, _vp, _i32, _i64, _vp, _vp, _vp, _vp]),
+        ("fs_route_backward", ctypes.c_int,
+         [ctypes.POINTER(_FsRouteParams), _i64, _vp, _i32, _i64, _vp, _vp, _vp, _i64, _vp]),
+        ("fs_expert_plan_workspace_bytes", _sz, [_i64, _i32, _i32]),
+        ("fs_expert_plan", ctypes.c_int, [_i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+        ("fs_expert_gather", ctypes.c_int, [_i64, _i32, _i32, _i32, _vp, _i32, _i64, _vp, _vp, _vp, _i64, _vp]),
+        ("fs_expert_combine", ctypes.c_int, [_i64, _i32, _i32, _vp, _i32, _i64, _vp, _vp, _vp, _i64, _vp]),
+        ("fs_expert_combine_backward", ctypes.c_int,
+         [_i64, _i32, _i32, _i32, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp]),
+        ("fs_embed", ctypes.c_int, [_i32, _i32, _vp, _i32, _i64, _i64, _i32, _vp, _i32, _vp, _f32, _vp, _i32, _i64, _vp]),
+        ("fs_embed_backward_workspace_bytes", _sz, [_i32, _i32, _i64, _i32]),
+        ("fs_embed_backward", ctypes.c_int,
+         [_i32, _i32, _vp, _i32, _i64, _i64, _i32, _vp, _i32, _vp, _f32, _i32, _vp, _i32, _i64, _vp, _sz, _vp])):
+    getattr(_lib, _name).restype = _result
+    getattr(_lib, _name).argtypes = _args
+
+
+def _matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optional[int] = None,
+            dtype: Optional[torch.dtype] = None):
+    """(pointer, element type, row stride) of a matrix argument whose rows' elements are adjacent."""
+    if t.dim() != 2 or t.dtype not in _ELEMENT:
+        raise FsError(FS_EINVAL, f"{what} is not a matrix of fp32, bf16 or fp16")
+    if (width is not None and t.shape[1] != width) or (rows is not None and t.shape[0] != rows):
+        raise FsError(FS_EINVAL, f"{what} is {tuple(t.shape)}, not {(rows, width)}")
+    if dtype is not None and t.dtype != dtype:
+        raise FsError(FS_EINVAL, f"{what} is {t.dtype}, not {dtype}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise FsError(FS_EINVAL, f"{what}: the elements of a row are not adjacent")
+    return t.data_ptr(), _ELEMENT[t.dtype], (t.stride(0) if t.shape[0] > 1 else max(1, t.shape[1]))
+
+
+def _array(t: Optional[torch.Tensor], what: str, n: int, dtype: torch.dtype) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise FsError(FS_EINVAL, f"{what} is not a contiguous array of {n} {dtype}")
+    return t.data_ptr()
+
+
+class _Place:
+    """Where a call runs: results and working memory are allocated for its stream."""
+
+    def __init__(self, like: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+        if not like.is_cuda:
+            raise FsError(FS_EINVAL, "the tensors are not on the GPU")
+        self.device, self.stream = like.device, stream
+        self.ptr = torch.cuda.current_stream(like.device).cuda_stream if stream is None else stream.cuda_stream
+
+    def empty(self, shape, dtype: torch.dtype) -> torch.Tensor:
+        if self.stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+
+def route_params(n_experts: int, k: int, score: int = FS_SCORE_SOFTMAX, renormalise: bool = True, n_groups: int = 1,
+                 top_groups: int = 1, group_best: int = 1, scale: float = 1.0) -> _FsRouteParams:
+    return _FsRouteParams(n_experts, k, score, int(renormalise), n_groups, top_groups, group_best, scale)
+
+
+def fs_route(params: _FsRouteParams, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
+             expert: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None):
+    """(expert, weight), int32 and fp32 of [tokens, k], of logits [tokens, n_experts]."""
+    at = _Place(logits, stream)
+    ptr, typ, stride = _matrix(logits, "logits", params.n_experts)
+    n, k = logits.shape[0], params.k
+    if expert is None:
+        expert = at.empty((n, max(k, 0)), torch.int32)
+    if weight is None:
+        weight = at.empty((n, max(k, 0)), torch.float32)
+    _check(_lib.fs_route(params, n, ptr, typ, stride, _array(bias, "bias", params.n_experts, torch.float32),
+                         _array(expert, "expert", n * k, torch.int32), _array(weight, "weight", n * k, torch.float32), at.ptr))
+    return expert, weight
+
+
+def fs_route_backward(params: _FsRouteParams, logits: torch.Tensor, expert: torch.Tensor, d_weight: torch.Tensor,
+                      d_logits: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    at = _Place(logits, stream)
+    ptr, typ, stride = _matrix(logits, "logits", params.n_experts)
+    n, k = logits.shape[0], params.k
+    if d_logits is None:
+        d_logits = at.empty((n, params.n_experts), logits.dtype)
+    d_ptr, _, d_stride = _matrix(d_logits, "d_logits", params.n_experts, n, logits.dtype)
+    _check(_lib.fs_route_backward(params, n, ptr, typ, stride, _array(expert, "expert", n * k, torch.int32),
+                                  _array(d_weight, "d_weight", n * k, torch.float32), d_ptr, d_stride, at.ptr))
+    return d_logits
+
+
+class ExpertPlan:
+    """Which slot every choice of `expert` [tokens, k] takes: first [n_experts+1], order [tokens*k], place [tokens, k]."""
+
+    def __init__(self, first: torch.Tensor, order: torch.Tensor, place: torch.Tensor):
+        self.first, self.order, self.place = first, order, place
+        self.n_experts = first.shape[0] - 1
+        self.n_tokens, self.k = place.shape
+
+
+def fs_expert_plan(expert: torch.Tensor, n_experts: int, plan: Optional[ExpertPlan] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> ExpertPlan:
+    """`plan`: an ExpertPlan of the same shape whose tensors are written again."""
+    at = _Place(expert, stream)
+    if expert.dim() != 2:
+        raise FsError(FS_EINVAL, "expert is not [tokens, k]")
+    n, k = expert.shape
+    src = _array(expert, "expert", n * k, torch.int32)
+    if plan is None:
+        plan = ExpertPlan(at.empty((max(n_experts, 0) + 1,), torch.int32), at.empty((n * k,), torch.int32),
+                          at.empty((n, k), torch.int32))
+    need = _lib.fs_expert_plan_workspace_bytes(n, k, n_experts)
+    work = at.empty((need,), torch.uint8) if need else None
+    _check(_lib.fs_expert_plan(n, k, n_experts, src, _array(plan.first, "first", n_experts + 1, torch.int32),
+                               _array(plan.order, "order", n * k, torch.int32), _array(plan.place, "place", n * k, torch.int32),
+                               _ptr(work), need, at.ptr))
+    return plan
+
+
+def fs_expert_gather(x: torch.Tensor, plan: ExpertPlan, out: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Rows x [tokens, width] in the experts' slots: [tokens*k, width]."""
+    at = _Place(x, stream)
+    ptr, typ, stride = _matrix(x, "x", rows=plan.n_tokens)
+    width = x.shape[1]
+    if out is None:
+        out = at.empty((plan.n_tokens * plan.k, width), x.dtype)
+    o_ptr, _, o_stride = _matrix(out, "out", width, plan.n_tokens * plan.k, x.dtype)
+    _check(_lib.fs_expert_gather(plan.n_tokens, plan.k, plan.n_experts, width, ptr, typ, stride, _ptr(plan.first),
+                                 _ptr(plan.place), o_ptr, o_stride, at.ptr))
+    return out
+
+
+def fs_expert_combine(y: torch.Tensor, plan: ExpertPlan, weight: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The slots' rows y [tokens*k, width], weighted, at their tokens: [tokens, width]."""
+    at = _Place(y, stream)
+    ptr, typ, stride = _matrix(y, "y", rows=plan.n_tokens * plan.k)
+    width = y.shape[1]
+    if out is None:
+        out = at.empty((plan.n_tokens, width), y.dtype)
+    o_ptr, _, o_stride = _matrix(out, "out", width, plan.n_tokens, y.dtype)
+    _check(_lib.fs_expert_combine(plan.n_tokens, plan.k, width, ptr, typ, stride, _ptr(plan.place),
+                                  _array(weight, "weight", plan.n_tokens * plan.k, torch.float32), o_ptr, o_stride, at.ptr))
+    return out
+
+
+def fs_expert_combine_backward(d_out: torch.Tensor, y: torch.Tensor, plan: ExpertPlan, weight: torch.Tensor,
+                               d_y: Optional[torch.Tensor] = None, d_weight: Optional[torch.Tensor] = None,
+                               stream: Optional[torch.cuda.Stream] = None):
+    """(d_y, d_weight) of a weighted fs_expert_combine."""
+    at = _Place(d_out, stream)
+    n, k, width = plan.n_tokens, plan.k, d_out.shape[-1]
+    ptr, typ, stride = _matrix(d_out, "d_out", rows=n)
+    y_ptr, _, y_stride = _matrix(y, "y", width, n * k, d_out.dtype)
+    if d_y is None:
+        d_y = at.empty((n * k, width), d_out.dtype)
+    if d_weight is None:
+        d_weight = at.empty((n, k), torch.float32)
+    o_ptr, _, o_stride = _matrix(d_y, "d_y", width, n * k, d_out.dtype)
+    _check(_lib.fs_expert_combine_backward(n, k, plan.n_experts, width, ptr, typ, stride, y_ptr, y_stride, _ptr(plan.first),
+                                           _ptr(plan.place), _array(weight, "weight", n * k, torch.float32), o_ptr, o_stride,
+                                           _array(d_weight, "d_weight", n * k, torch.float32), at.ptr))
+    return d_y, d_weight
+
+
+def _id_array(ids: torch.Tensor, col_base: Optional[torch.Tensor]):
+    """(rows, columns, pointer, type, base pointer): ids [rows] are single tokens, [rows, columns] bags."""
+    if ids.dim() not in (1, 2) or ids.dtype not in _ID:
+        raise FsError(FS_EINVAL, "ids is not [rows] or [rows, columns] of int32, int64 or 16-bit leaf ids")
+    if not ids.is_contiguous():
+        raise FsError(FS_EINVAL, "ids is not contiguous")
+    rows, cols = ids.shape[0], (ids.shape[1] if ids.dim() == 2 else 1)
+    return rows, cols, ids.data_ptr(), _ID[ids.dtype], _array(col_base, "col_base", cols, torch.int32)
+
+
+def fs_embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, col_base: Optional[torch.Tensor] = None,
+             out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """[rows, width]: the scaled rows of `table` that ids [rows] name, or the scaled sums of those that ids [rows, columns]
+    name.  The result is of the table's type unless `out` (of that type or fp32) is given."""
+    at = _Place(table, stream)
+    t_ptr, typ, t_stride = _matrix(table, "table")
+    rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base)
+    vocab, width = table.shape
+    if out is None:
+        out = at.empty((rows, width), table.dtype)
+    o_ptr, o_typ, o_stride = _matrix(out, "out", width, rows)
+    _check(_lib.fs_embed(vocab, width, t_ptr, typ, t_stride, rows, cols, i_ptr, i_typ, base, scale, o_ptr, o_typ, o_stride, at.ptr))
+    return out
+
+
+def fs_embed_backward(d_out: torch.Tensor, ids: torch.Tensor, n_vocab: int, scale: float = 1.0,
+                      col_base: Optional[torch.Tensor] = None, d_table: Optional[torch.Tensor] = None, accumulate: bool = False,
+                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The table's gradient [n_vocab, width]: fp32 unless `d_table` (of that type or d_out's) is given; `accumulate` adds to
+    what `d_table` holds."""
+    at = _Place(d_out, stream)
+    rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base)
+    ptr, typ, stride = _matrix(d_out, "d_out", rows=rows)
+    width = d_out.shape[1]
+    if d_table is None:
+        if accumulate:
+            raise FsError(FS_EINVAL, "accumulate needs a d_table to add to")
+        d_table = at.empty((max(n_vocab, 0), width), torch.float32)
+    t_ptr, t_typ, t_stride = _matrix(d_table, "d_table", width, n_vocab)
+    need = _lib.fs_embed_backward_workspace_bytes(n_vocab, width, rows, cols)
+    work = at.empty((need,), torch.uint8) if need else None
+    _check(_lib.fs_embed_backward(n_vocab, width, ptr, typ, stride, rows, cols, i_ptr, i_typ, base, scale, int(accumulate), t_ptr,
+                                  t_typ, t_stride, _ptr(work), need, at.ptr))
+    return d_table

@@ -1,0 +1,269 @@
+"""fs_route and fs_route_backward against the definition in 64 bits: choices equal, weights and gradients within what
+fp32 arithmetic may be off.
+
+An exponent's argument x - max is rounded twice, each time by 2^-24 of it, an exponential, a sum of up to 1024 terms added
+as a tree, a quotient and a factor come on top: with D the largest such argument, 2^-24 * (4 D + 64) of the value."""
+import numpy as np
+import pytest
+
+from oracle import mixture_oracle as MO
+
+pytestmark = pytest.mark.gpu
+TYPES = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}       # half a step, relative
+
+
+@pytest.fixture(scope="module")
+def api():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    from paper_2201_00194_amd import api as A
+    return A
+
+
+def torch_type(name):
+    import torch
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[name]
+
+
+def spread(x):
+    """The largest argument of an exponential in each row."""
+    x = np.where(np.isnan(x), -np.inf, np.minimum(x, MO.BIG))
+    fine = np.where(x > -np.inf, x, 0.0)
+    top = np.where(x > -np.inf, x, -np.inf).max(axis=1, keepdims=True, initial=-np.inf)
+    top = np.where(np.isfinite(top), top, 0.0)
+    far = np.maximum(np.abs(fine), np.abs(np.where(x > -np.inf, x - top, 0.0)))
+    return np.minimum(far, 110.0).max(axis=1, keepdims=True, initial=0.0)        # beyond it everything is 0 in fp32
+
+
+def check(api, logits, k, d_weight=None, stride=None, bias=None, **kw):
+    """logits: a torch CPU tensor of its type.  Returns the chosen experts."""
+    import torch
+    tokens, experts = logits.shape
+    stride = stride or experts
+    wide = torch.full((tokens, stride), 9.0, dtype=logits.dtype)
+    wide[:, :experts] = logits
+    dev = wide.cuda()[:, :experts]
+    score = kw.get("score", "softmax")
+    params = api.route_params(experts, k, **{**kw, "score": api.FS_SCORE_SIGMOID if score == "sigmoid" else api.FS_SCORE_SOFTMAX})
+    b = None if bias is None else torch.tensor(bias, dtype=torch.float32)
+    e, w = api.fs_route(params, dev, None if b is None else b.cuda())
+    torch.cuda.synchronize()
+    x = logits.double().numpy()
+    ee, ew = MO.route(x, k, bias=None if b is None else b.double().numpy(), **kw)
+    e, w = e.cpu().numpy(), w.cpu().double().numpy()
+    assert np.array_equal(e, ee), np.argwhere(e != ee)[:5]
+    tol = 2.0 ** -24 * (4 * spread(x) + 64)
+    assert np.all(np.abs(w - ew) <= tol * np.abs(ew) + 1e-36)
+    if d_weight is None:
+        d_weight = np.random.default_rng(1).standard_normal((tokens, k)).astype(np.float32)
+    d_weight = d_weight.copy()
+    d_weight[ee < 0] = np.nan                                   # skipped, whatever it holds
+    out = torch.full((tokens, stride + 1), 7.0, dtype=logits.dtype).cuda()
+    d = api.fs_route_backward(params, dev, torch.from_numpy(ee).cuda(), torch.from_numpy(d_weight).cuda(), out[:, :experts])
+    torch.cuda.synchronize()
+    got = d.cpu().double().numpy()
+    bkw = {n: v for n, v in kw.items() if n in ("score", "renormalise", "scale")}
+    ed, size = MO.route_backward(x, ee, d_weight, **bkw)
+    half = {torch.float32: TYPES["fp32"], torch.bfloat16: TYPES["bf16"], torch.float16: TYPES["fp16"]}[logits.dtype]
+    tiny = 2.0 ** -25 if logits.dtype == torch.float16 else 1e-36      # half the smallest step
+    assert np.all(np.abs(got - ed) <= tol * size + half * np.abs(ed) + tiny), np.abs(got - ed).max()
+    assert np.all(out[:, experts:].cpu().numpy() == 7.0) if logits.dtype != torch.bfloat16 else torch.all(out[:, experts:] == 7)
+    return ee
+
+
+def normal(seed, tokens, experts, typ="fp32", scale=1.5):
+    import torch
+    return (torch.from_numpy(np.random.default_rng(seed).standard_normal((tokens, experts)).astype(np.float32)) * scale).to(torch_type(typ))
+
+
+@pytest.mark.parametrize("typ", list(TYPES))
+@pytest.mark.parametrize("tokens,experts,k", [(1, 1, 1), (1, 2, 2), (3, 7, 3), (65, 8, 2), (64, 8, 8), (129, 16, 4), (33, 17, 5), (257, 30, 4),
+                                              (64, 32, 1), (70, 64, 8), (63, 65, 6), (31, 128, 8), (17, 255, 7), (5, 256, 16),
+                                              (9, 500, 9), (6, 1000, 16), (3, 1024, 12)])
+def test_shapes(api, typ, tokens, experts, k):
+    for score in ("softmax", "sigmoid"):
+        for renormalise in (True, False):
+            check(api, normal(tokens + experts, tokens, experts, typ), k, score=score, renormalise=renormalise, scale=2.5)
+            check(api, normal(tokens + experts, tokens, experts, typ), k, score=score, renormalise=renormalise, stride=experts + 3,
+                  bias=np.random.default_rng(k).standard_normal(experts) * 0.1)
+
+
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups,top,best,k", [(64, 8, 4, 2, 8), (256, 8, 4, 2, 8), (160, 8, 3, 1, 6), (30, 5, 2, 2, 4), (8, 8, 3, 2, 3),
+                                                       (12, 4, 4, 1, 5), (1000, 8, 2, 2, 16), (1024, 1024, 7, 1, 7), (66, 33, 5, 2, 9),
+                                                       (9, 3, 1, 1, 7), (255, 3, 2, 2, 8), (7, 1, 1, 1, 3)])
+def test_groups(api, typ, score, experts, groups, top, best, k):
+    for bias in (None, np.random.default_rng(2).standard_normal(experts) * 0.05):
+        e = check(api, normal(experts + groups, 37, experts, typ), k, score=score, bias=bias, n_groups=groups, top_groups=top,
+                  group_best=best, renormalise=True)
+        if k > top * (experts // groups):
+            assert np.all(e[:, top * (experts // groups):] == -1)
+
+
+def special(experts):
+    """Rows of masks and extreme values."""
+    low, inf, nan = float(np.finfo(np.float32).min), np.inf, np.nan
+    rng = np.random.default_rng(experts)
+    rows = [np.full(experts, -inf), np.full(experts, nan), np.full(experts, low), np.full(experts, inf), np.zeros(experts)]
+    for at, v in ((0, 0.5), (experts - 1, -3.0)):
+        r = np.full(experts, -inf)
+        r[at] = v
+        rows.append(r)
+    r = rng.standard_normal(experts)
+    rows.append(np.where(rng.random(experts) < 0.5, -inf, r))
+    rows.append(np.where(rng.random(experts) < 0.5, nan, r))
+    rows.append(np.where(rng.random(experts) < 0.5, low, r))
+    rows.append(np.where(rng.random(experts) < 0.3, inf, r))
+    rows.append(np.where(np.arange(experts) % 2 == 0, inf, -inf))
+    rows.append(np.where(np.arange(experts) == experts // 2, nan, low))
+    rows.append(np.linspace(-100, 25, experts))
+    rows.append(-80 - np.arange(experts) / 8)
+    rows.append(np.round(r))                                     # many equal logits
+    rows.append(np.where(r > 0, 0.0, -0.0))
+    return np.array(rows)
+
+
+@pytest.mark.parametrize("experts", [8, 30, 64, 100, 256, 1024])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalise", [True, False])
+def test_masks_ties_and_extremes(api, experts, score, renormalise):
+    import torch
+    x = torch.from_numpy(special(experts).astype(np.float32))
+    for k in (1, 2, 8):
+        check(api, x, k, score=score, renormalise=renormalise)
+        check(api, x, k, score=score, renormalise=renormalise, n_groups=2, top_groups=1, group_best=2)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts", [8, 64, 255])
+def test_bias_extremes_and_ties(api, score, experts):
+    import torch
+    x = torch.from_numpy(special(experts).astype(np.float32))
+    rng = np.random.default_rng(3)
+    for bias in (np.zeros(experts), np.full(experts, -0.5), np.where(np.arange(experts) % 3 == 0, np.nan, 0.25),
+                 np.where(np.arange(experts) % 3 == 0, -np.inf, rng.standard_normal(experts)),
+                 np.where(np.arange(experts) % 4 == 1, np.inf, rng.standard_normal(experts)), np.full(experts, -np.inf)):
+        check(api, x, 6, score=score, bias=bias)
+    q = torch.from_numpy(np.round(rng.standard_normal((40, experts)) * 2).astype(np.float32) / 2)
+    check(api, q, 8, score=score, bias=np.round(rng.standard_normal(experts) * 4) / 64)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups", [(16, 1), (64, 1), (64, 8), (250, 1)])
+def test_keys_that_differ_by_less_than_fp32_shows(api, score, experts, groups):
+    """Logits a few steps of fp32 apart under one bias: the keys, in fp32, would be equal or in any order."""
+    import torch
+    rng = np.random.default_rng(4)
+    base = np.float32(0.7)
+    most = 9 if groups == 1 else 1 << 17            # sums of two keys in even steps would meet in 64 bits too
+    near = (base.view(np.int32) + rng.integers(-most, most + 1, (50, experts)).astype(np.int32)).view(np.float32)
+    check(api, torch.from_numpy(near), 8, score=score, bias=np.full(experts, 0.3), n_groups=groups, top_groups=max(1, groups // 2),
+          group_best=2)
+    high = (20 + rng.integers(0, 400, (50, experts)) / 100).astype(np.float32)          # sigmoids next to 1
+    check(api, torch.from_numpy(high), 8, score="sigmoid", bias=np.full(experts, 0.25))
+    low = (-22 - rng.integers(0, 400, (50, experts)) / 100).astype(np.float32)          # next to 0
+    check(api, torch.from_numpy(low), 8, score="sigmoid", bias=np.zeros(experts))
+
+
+def test_a_choice_of_ones_own(api):
+    """The gradient takes any choice: fewer experts than k, entries outside the experts, an expert twice, a masked one."""
+    import torch
+    x = normal(8, 5, 12)
+    x[4, 3] = -np.inf
+    expert = np.array([[0, 1, 2], [5, -1, 99], [-1, -1, -7], [4, 4, 2], [3, 1, 0]], np.int32)
+    dw = np.random.default_rng(8).standard_normal((5, 3)).astype(np.float32)
+    for score in ("softmax", "sigmoid"):
+        for renormalise in (True, False):
+            p = api.route_params(12, 3, score=api.FS_SCORE_SIGMOID if score == "sigmoid" else api.FS_SCORE_SOFTMAX, renormalise=renormalise)
+            d = api.fs_route_backward(p, x.cuda(), torch.from_numpy(expert).cuda(), torch.from_numpy(dw).cuda()).cpu().double().numpy()
+            ed, size = MO.route_backward(x.double().numpy(), expert, dw, score=score, renormalise=renormalise)
+            assert np.all(np.abs(d - ed) <= 2.0 ** -24 * 90 * size + 1e-36)
+
+
+def test_gradient_against_differences_of_the_forward_pass(api):
+    """Central differences of the library's own weights, h = 2^-6: the third derivative of a weight is at most 1 here
+    (weights below 1), so they are h^2 / 6 off, and 2^-23 / h for the weights' own rounding, per choice."""
+    import torch
+    x = normal(9, 40, 24)
+    dw = np.random.default_rng(9).standard_normal((40, 5)).astype(np.float32)
+    h = 2.0 ** -6
+    for score in (0, 1):
+        for renormalise in (True, False):
+            p = api.route_params(24, 5, score=score, renormalise=renormalise)
+            e, _ = api.fs_route(p, x.cuda())
+            d = api.fs_route_backward(p, x.cuda(), e, torch.from_numpy(dw).cuda()).cpu().double().numpy()
+            en = e.cpu().numpy()
+            for i in range(0, 24, 5):
+                sums = []
+                for sign in (1, -1):
+                    z = x.clone()
+                    z[:, i] += sign * h
+                    ez, wz = api.fs_route(p, z.cuda())
+                    ez, wz = ez.cpu().numpy(), wz.cpu().double().numpy()
+                    same = [set(a) == set(b) for a, b in zip(ez, en)]
+                    by = np.array([[wz[t][list(ez[t]).index(v)] if same[t] else 0.0 for v in en[t]] for t in range(40)])
+                    sums.append((np.sum(by * dw, axis=1), np.array(same)))
+                fine = sums[0][1] & sums[1][1]
+                assert fine.sum() >= 20
+                diff = (sums[0][0] - sums[1][0]) / (2 * h)
+                allowed = np.abs(dw).sum(axis=1) * (h * h / 6 + 2.0 ** -23 / h * 4)
+                assert np.all(np.abs(diff - d[:, i])[fine] <= allowed[fine])
+
+
+def test_other_streams_and_graphs(api):
+    import torch
+    p = api.route_params(64, 4)
+    x = normal(10, 300, 64).cuda()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    e1, w1 = api.fs_route(p, x)
+    e2, w2 = api.fs_route(p, x, stream=s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(e1, e2) and torch.equal(w1, w2)
+    dw = torch.randn(300, 4, device="cuda")
+    d = torch.empty_like(x)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        api.fs_route(p, x, expert=e2, weight=w2)
+        api.fs_route_backward(p, x, e2, dw, d)
+    for seed in (11, 12, 13):
+        x.copy_(normal(seed, 300, 64))
+        dw.copy_(torch.randn(300, 4))
+        g.replay()
+        torch.cuda.synchronize()
+        e, w = api.fs_route(p, x)
+        assert torch.equal(e, e2) and torch.equal(w, w2) and torch.equal(d, api.fs_route_backward(p, x, e, dw))
+
+
+def test_no_tokens(api):
+    import torch
+    e, w = api.fs_route(api.route_params(8, 2), torch.zeros(0, 8, device="cuda"))
+    assert e.shape == (0, 2) and w.shape == (0, 2)
+    d = api.fs_route_backward(api.route_params(8, 2), torch.zeros(0, 8, device="cuda"), e, w)
+    assert d.shape == (0, 8)
+
+
+def test_refusals_reach_the_caller(api):
+    import torch
+    x = torch.zeros(4, 8, device="cuda")
+    for params in (api.route_params(8, 9), api.route_params(8, 0), api.route_params(8, 2, n_groups=3), api.route_params(9, 2)):
+        with pytest.raises(api.FsError):
+            api.fs_route(params, x)
+    with pytest.raises(api.FsError):
+        api.fs_route(api.route_params(8, 2), x, bias=torch.zeros(7, device="cuda"))
+    with pytest.raises(api.FsError):
+        api.fs_route(api.route_params(8, 2), x.t())
+
+
+def test_many_tokens(api):
+    """More than 65535 workgroups, and the same result twice."""
+    import torch
+    x = torch.randn(1100003, 8, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    p = api.route_params(8, 2, renormalise=False)
+    e, w = api.fs_route(p, x)
+    v, i = torch.softmax(x.double(), 1).sort(dim=1, descending=True, stable=True)
+    assert torch.equal(e.long(), i[:, :2]) and float((w.double() / v[:, :2] - 1).abs().max()) < 2.0 ** -24 * 120
+    e2, w2 = api.fs_route(p, x)
+    assert torch.equal(e, e2) and torch.equal(w, w2)
