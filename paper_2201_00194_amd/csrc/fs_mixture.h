@@ -66,6 +66,61 @@ inline int launched(const char *what)
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? FS_OK : fail_hip(e, what);
 }
+
+// ---- lanes --------------------------------------------------------------------------------------
+// What this wavefront has done in LDS is done.
+__device__ __forceinline__ void lds_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// 1 << ll neighbouring lanes work on one row.  Step s < ll of a reduction over them meets a lane whose 1 << s neighbours
+// this lane's have not met yet: within sixteen lanes by data-parallel moves (pairs, quads swapped, then mirrored halves and
+// rows, as all lanes of a quad and of a half hold the same by then).
+template <int STEP>
+__device__ __forceinline__ int met_int(int v)
+{
+    if constexpr (STEP == 0)
+        return __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true);     // quad_perm 1 0 3 2
+    else if constexpr (STEP == 1)
+        return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true);     // quad_perm 2 3 0 1
+    else if constexpr (STEP == 2)
+        return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true);    // row_half_mirror
+    else if constexpr (STEP == 3)
+        return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true);    // row_mirror
+    else
+        return __shfl_xor(v, STEP == 4 ? 16 : 32);
+}
+template <int STEP> __device__ __forceinline__ float met(float v) { return __int_as_float(met_int<STEP>(__float_as_int(v))); }
+template <int STEP> __device__ __forceinline__ int met(int v) { return met_int<STEP>(v); }
+template <int STEP> __device__ __forceinline__ double met(double v)
+{
+    return __hiloint2double(met_int<STEP>(__double2hiint(v)), met_int<STEP>(__double2loint(v)));
+}
+// f(this lane's, the met lane's) over the 1 << ll lanes of a row, ll the same in the whole wavefront; f is symmetric, so all lanes
+// of a row get the same.
+template <class T, class F>
+__device__ __forceinline__ T row_reduce(T v, int ll, F f)
+{
+    if (ll > 0) v = f(v, met<0>(v));
+    if (ll > 1) v = f(v, met<1>(v));
+    if (ll > 2) v = f(v, met<2>(v));
+    if (ll > 3) v = f(v, met<3>(v));
+    if (ll > 4) v = f(v, met<4>(v));
+    if (ll > 5) v = f(v, met<5>(v));
+    return v;
+}
+template <class T> __device__ __forceinline__ T row_sum(T v, int ll) { return row_reduce(v, ll, [](T a, T b) { return a + b; }); }
+__device__ __forceinline__ float row_max(float v, int ll) { return row_reduce(v, ll, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ int row_or(int v, int ll) { return row_reduce(v, ll, [](int a, int b) { return a | b; }); }
+
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f); }
+
+// The hardware's reciprocal, one step off at most.
+__device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }
+
 #define FS_TRY(call)               \
     do {                           \
         const int fs_rc_ = (call); \

@@ -1,9 +1,24 @@
 // Routing: logits to the k chosen experts of a token and their weights, and the logits' gradient.
+//
+// A row of E logits lies in 1 << ll neighbouring lanes, 16 a lane, so that a wavefront works on 64 >> ll rows and one
+// step of a reduction takes one move between lanes.  The choice goes by 42 bits: a key's 32, made to compare like whole
+// numbers, and the expert's number, turned round so that of equal keys the lower expert wins.  They stand in the mantissa of a double
+// between 1 and 2, because a compare and exchange of doubles is two instructions at full rate, of 64-bit integers
+// six.  Every lane sorts its keys in lists of KP >= k with Batcher's network, and two lists become the best KP of both by
+// KP maxima (the one against the other turned round) and a bitonic merge, in the lane first, between lanes then.
+//
+// Keys with a bias (score + bias) and the sums of groups have to compare as in 64 bits.  They are computed in 32, with a bound
+// on their error; a row where two keys or sums that matter are nearer than the bounds say, and not equal by their inputs, is
+// taken again by the whole wavefront in 64 bits.
 #include "fs_mixture.h"
 
 #include <math.h>
 
 namespace fs {
+
+constexpr int kRouteWaves = 4;           // of a workgroup
+constexpr int kRoutePer = 16;            // experts of a lane
+constexpr int kRouteMostGroups = 32;     // more groups than a word has bits: every row in 64 bits
 
 struct RouteArgs {
     fs_route_params p;
@@ -15,6 +30,9 @@ struct RouteArgs {
     const int32_t *chosen;
     const float *d_weight;
     void *d_logits;
+    int32_t ll, group_size;
+    int32_t exact;                       // 1: every row in 64 bits
+    int32_t wave_lds;                    // bytes
 };
 
 // NaN masks an expert as -infinity does; +infinity counts as the largest float.
@@ -23,18 +41,10 @@ __device__ __forceinline__ float route_logit(float l)
     return l != l ? -__builtin_inff() : fminf(l, 3.402823466e38f);
 }
 
-__device__ __forceinline__ double wave_max(double v)
-{
-    for (int o = 32; o; o >>= 1)
-        v = fmax(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ __forceinline__ double wave_sum(double v)
-{
-    for (int o = 32; o; o >>= 1)
-        v += __shfl_xor(v, o);
-    return v;
-}
+// ---- a row in 64 bits ---------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ double wave_max(double v) { return row_reduce(v, 6, [](double a, double b) { return fmax(a, b); }); }
+__device__ __forceinline__ double wave_sum(double v) { return row_sum(v, 6); }
 // The largest of n values in LDS, the first of equal ones; -1 if all are -infinity.
 __device__ __forceinline__ int wave_argmax(const double *v, int n, int lane)
 {
@@ -56,16 +66,13 @@ __device__ __forceinline__ double log_score(double x, double top, double log_sum
     return score == FS_SCORE_SOFTMAX ? x - top - log_sum : fmin(x, 0.0) - log1p(exp(-fabs(x)));
 }
 
-// One wavefront a token, everything in 64 bits.
-template <int TYPE>
-__global__ void __launch_bounds__(64)
-route_kernel(RouteArgs a)
+template <class T>
+__device__ void route_exact(const RouteArgs &a, int64_t row, double *key, int lane)
 {
-    typedef typename Element<TYPE>::type T;
-    __shared__ double key[FS_MAX_EXPERTS], group[FS_MAX_EXPERTS];
-    const int lane = threadIdx.x, n = a.p.n_experts, k = a.p.k;
+    const int n = a.p.n_experts, k = a.p.k;
     const double none = -__builtin_inf();
-    const T *logits = (const T *)a.logits + (int64_t)blockIdx.x * a.stride;
+    const T *logits = (const T *)a.logits + row * a.stride;
+    double *group = key + n;
     double top = none, sum = 0.0;
     for (int e = lane; e < n; e += 64)
         top = fmax(top, (double)route_logit((float)logits[e]));
@@ -75,7 +82,7 @@ route_kernel(RouteArgs a)
     for (int e = lane; e < n; e += 64)
         sum += exp((double)route_logit((float)logits[e]) - top);
     const double log_sum = log(wave_sum(sum));
-    const int per = n / a.p.n_groups;
+    lds_sync();
     for (int e = lane; e < n; e += 64) {
         const double x = route_logit((float)logits[e]);
         double v = x;
@@ -86,8 +93,9 @@ route_kernel(RouteArgs a)
         }
         key[e] = v > none ? v : none;
     }
-    __syncthreads();
+    lds_sync();
     if (a.p.n_groups > 1) {
+        const int per = a.group_size;
         for (int g = lane; g < a.p.n_groups; g += 64) {
             double first = none, second = none;
             for (int e = g * per; e < (g + 1) * per; ++e) {
@@ -99,13 +107,13 @@ route_kernel(RouteArgs a)
             }
             group[g] = a.p.group_best == 2 && second > none ? first + second : first;
         }
-        __syncthreads();
+        lds_sync();
         for (int r = 0; r < a.p.top_groups; ++r) {
             const int g = wave_argmax(group, a.p.n_groups, lane);
-            __syncthreads();
+            lds_sync();
             if (g >= 0 && lane == 0)
                 group[g] = __builtin_nan("");                 // taken
-            __syncthreads();
+            lds_sync();
         }
         for (int e = lane; e < n; e += 64) {
             const double t = group[e / per];
@@ -114,17 +122,17 @@ route_kernel(RouteArgs a)
             else if (!a.bias && key[e] > none)
                 key[e] = route_logit((float)logits[e]);
         }
-        __syncthreads();
+        lds_sync();
     }
     int mine = -1;
     for (int j = 0; j < k; ++j) {
         const int e = wave_argmax(key, n, lane);
-        __syncthreads();
+        lds_sync();
         if (e >= 0 && lane == 0)
             key[e] = none;
         if (lane == j)
             mine = e;
-        __syncthreads();
+        lds_sync();
     }
     double s = none, w;
     if (mine >= 0) {
@@ -140,70 +148,511 @@ route_kernel(RouteArgs a)
         w = mine < 0 ? 0.0 : exp(s);
     }
     if (lane < k) {
-        a.expert[(int64_t)blockIdx.x * k + lane] = mine;
-        a.weight[(int64_t)blockIdx.x * k + lane] = (float)(w * (double)a.p.scale);
+        a.expert[row * k + lane] = mine;
+        a.weight[row * k + lane] = (float)(w * (double)a.p.scale);
     }
 }
 
+// ---- keys and lists -------------------------------------------------------------------------------------------------------
+
+// The key and the expert as a double in [1, 2); 0 is nobody.
+__device__ __forceinline__ double packed(float key, int e)
+{
+    const int bits = __float_as_int(key);
+    const uint32_t order = (uint32_t)bits ^ ((uint32_t)(bits >> 31) | 0x80000000u);
+    return __hiloint2double((int)(0x3ff00000u | (order >> 12)), (int)((order << 20) | (uint32_t)(1023 - e)));
+}
+__device__ __forceinline__ int expert_of(double v) { return 1023 - (__double2loint(v) & 1023); }
+__device__ __forceinline__ float key_of(double v)
+{
+    const uint32_t order = ((uint32_t)__double2hiint(v) << 12) | ((uint32_t)__double2loint(v) >> 20);
+    return __uint_as_float(order ^ ((uint32_t)((int)~order >> 31) | 0x80000000u));
+}
+
+// __builtin_fmax would first make signalling NaNs quiet; there are none.
+__device__ __forceinline__ double larger(double a, double b)
+{
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ double smaller(double a, double b)
+{
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ void in_order(double &a, double &b)
+{
+    const double hi = larger(a, b), lo = smaller(a, b);
+    a = hi, b = lo;
+}
+// Largest first: Batcher's odd-even merge sort of N = 2^i values from `at` on.
+template <int N>
+struct SortNetwork {
+    int n = 0, first[N * 4] = {}, second[N * 4] = {};
+    constexpr SortNetwork()
+    {
+        for (int p = 1; p < N; p *= 2)
+            for (int q = p; q >= 1; q /= 2)
+                for (int j = q % p; j + q < N; j += 2 * q)
+                    for (int i = 0; i < q && i + j + q < N; ++i)
+                        if ((i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+                            first[n] = i + j;
+                            second[n++] = i + j + q;
+                        }
+    }
+};
+template <int N, int M>
+__device__ __forceinline__ void sort_list(double (&v)[M], int at)
+{
+    constexpr SortNetwork<N> kNetwork;
+#pragma unroll
+    for (int i = 0; i < kNetwork.n; ++i)
+        in_order(v[at + kNetwork.first[i]], v[at + kNetwork.second[i]]);
+}
+// list becomes the best KP of itself and other, both sorted.
+template <int KP>
+__device__ __forceinline__ void merge_list(double (&list)[KP], const double (&other)[KP])
+{
+#pragma unroll
+    for (int i = 0; i < KP; ++i)
+        list[i] = larger(list[i], other[KP - 1 - i]);
+#pragma unroll
+    for (int q = KP / 2; q >= 1; q /= 2)
+#pragma unroll
+        for (int i = 0; i < KP; ++i)
+            if ((i & q) == 0)
+                in_order(list[i], list[i + q]);
+}
+template <int STEP, int KP>
+__device__ __forceinline__ void merge_met(double (&list)[KP])
+{
+    double other[KP];
+#pragma unroll
+    for (int i = 0; i < KP; ++i)
+        other[i] = met<STEP>(list[i]);
+    merge_list<KP>(list, other);
+}
+
+// ---- the kernel -----------------------------------------------------------------------------------------------------------
+
+template <class T> constexpr int kChunk = 16 / (int)sizeof(T);       // elements of a load
+
+// x[u]: expert expert_at(u) of the row, -infinity past the last.
+template <class T>
+__device__ __forceinline__ int expert_at(int u, int ll, int h) { return (((u / kChunk<T>) << ll) + h) * kChunk<T> + u % kChunk<T>; }
+
+template <class T>
+__device__ __forceinline__ void load_row(const T *logits, int n, int ll, int h, float (&x)[kRoutePer])
+{
+    typedef T Chunk __attribute__((ext_vector_type(kChunk<T>), aligned(sizeof(T))));
+#pragma unroll
+    for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
+        const int e = expert_at<T>(c * kChunk<T>, ll, h);
+        if (e + kChunk<T> <= n) {
+            const Chunk v = *(const Chunk *)(logits + e);
+#pragma unroll
+            for (int i = 0; i < kChunk<T>; ++i)
+                x[c * kChunk<T> + i] = route_logit((float)v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kChunk<T>; ++i)
+                x[c * kChunk<T> + i] = -__builtin_inff();
+            if (e < n) {
+                T v[kChunk<T>];
+#pragma unroll
+                for (int i = 0; i < kChunk<T>; ++i)
+                    v[i] = logits[min(e + i, n - 1)];
+#pragma unroll
+                for (int i = 0; i < kChunk<T>; ++i)
+                    x[c * kChunk<T> + i] = e + i < n ? route_logit((float)v[i]) : -__builtin_inff();
+            }
+        }
+    }
+}
+
+// Choices i * (1 << LL) + h of the row's list are this lane's: their experts and weights go out.
+template <class T, int KP, int LL>
+__device__ __forceinline__ void finish(const RouteArgs &a, int64_t row, const T *logits, const double (&list)[KP], int h, float top, float sum,
+                                       bool write)
+{
+    constexpr int kLanes = (1 << LL) < KP ? 1 << LL : KP, kMine = KP / kLanes;
+    const float none = -__builtin_inff();
+    float s[kMine];
+    int expert[kMine];
+    float high = none;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        double from[kLanes];
+#pragma unroll
+        for (int l = 0; l < kLanes; ++l)
+            from[l] = list[i * kLanes + l];
+#pragma unroll
+        for (int half = kLanes / 2; half >= 1; half /= 2)
+#pragma unroll
+            for (int l = 0; l < half; ++l) {
+                const double low = from[l], high_l = from[l + half];
+                from[l] = (h & half) ? high_l : low;
+            }
+        const int j = i * kLanes + h;
+        const bool there = h < kLanes && j < a.p.k && from[0] > 0.0;
+        expert[i] = there ? expert_of(from[0]) : -1;
+        s[i] = none;
+        if (there) {
+            const float x = route_logit((float)logits[expert[i]]);
+            if (a.p.score == FS_SCORE_SOFTMAX)
+                s[i] = x;
+            else if (a.p.renormalise)
+                s[i] = fminf(x, 0.0f) - __logf(1.0f + exp_of(-fabsf(x)));
+            else
+                s[i] = x;
+        }
+        high = fmaxf(high, s[i]);
+    }
+    if (a.p.renormalise) {
+        high = row_max(high, a.ll);
+        float all = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            s[i] = expert[i] < 0 ? 0.0f : exp_of(s[i] - high);
+            all += s[i];
+        }
+        all = row_sum(all, a.ll);
+        const float factor = all > 0.0f ? a.p.scale * inverse(all) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+            s[i] *= factor;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (expert[i] < 0)
+                s[i] = 0.0f;
+            else if (a.p.score == FS_SCORE_SOFTMAX)
+                s[i] = exp_of(s[i] - top) * inverse(sum) * a.p.scale;
+            else
+                s[i] = a.p.scale * inverse(1.0f + exp_of(-s[i]));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int j = i * kLanes + h;
+        if (write && h < kLanes && j < a.p.k) {
+            a.expert[row * a.p.k + j] = expert[i];
+            a.weight[row * a.p.k + j] = s[i];
+        }
+    }
+}
+
+template <int TYPE, int KP, bool EXACT>
+__global__ void __launch_bounds__(kRouteWaves * 64)
+route_kernel(RouteArgs a)
+{
+    typedef typename Element<TYPE>::type T;
+    extern __shared__ double lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ll = a.ll, h = lane & ((1 << ll) - 1);
+    const int n = a.p.n_experts;
+    const float none = -__builtin_inff();
+    const int64_t row0 = ((int64_t)blockIdx.x * kRouteWaves + wave) << (6 - ll);
+    if (row0 >= a.n_tokens)
+        return;
+    const bool there = row0 + (lane >> ll) < a.n_tokens;
+    const int64_t row = there ? row0 + (lane >> ll) : a.n_tokens - 1;
+    double *const own = lds + wave * (a.wave_lds / 8);
+    bool again = EXACT && a.exact;                                  // this lane's row goes through 64 bits
+    if (!(EXACT && a.exact)) {
+        const T *logits = (const T *)a.logits + row * a.stride;
+        float x[kRoutePer];
+        load_row<T>(logits, n, ll, h, x);
+        float top = 0.0f, sum = 1.0f;
+        if (a.p.score == FS_SCORE_SOFTMAX && (EXACT || !a.p.renormalise)) {
+            top = none;
+#pragma unroll
+            for (int u = 0; u < kRoutePer; ++u)
+                top = fmaxf(top, x[u]);
+            top = row_max(top, ll);
+            top = top == none ? 0.0f : top;
+            sum = 0.0f;
+#pragma unroll
+            for (int u = 0; u < kRoutePer; ++u)
+                sum += exp_of(x[u] - top);
+            sum = row_sum(sum, ll);
+        }
+        // Keys.  Bounds on the error of a score in fp32: with d = top - x, an exponential is off by (2 d + 4) 2^-24 of itself and
+        // d exp(-d) < 0.37, a quotient and a sum of up to 1024 as a tree add 40: 48 * 2^-24 / sum; a sigmoid, by the same way
+        // (s (1 - s) d < 0.23), 8 * 2^-24.  The sum with the bias rounds once more.
+        constexpr float kStep = 5.9604645e-8f;                      // 2^-24
+        float key[kRoutePer], off = 0.0f;
+        if constexpr (EXACT) {
+            const float over = inverse(sum);
+            off = a.p.score == FS_SCORE_SOFTMAX ? 48.0f * kStep * over : 8.0f * kStep;
+#pragma unroll
+            for (int u = 0; u < kRoutePer; ++u) {
+                const int e = expert_at<T>(u, ll, h);
+                const float s = a.p.score == FS_SCORE_SOFTMAX ? exp_of(x[u] - top) * over : inverse(1.0f + exp_of(-x[u]));
+                float v = a.bias && e < n ? s + a.bias[e] : s;
+                key[u] = x[u] > none && v == v ? v : none;
+            }
+            if (a.p.n_groups > 1) {
+                // A lane ranks groups h, h + (1 << ll), ... of its row; keys and sums meet in LDS.
+                float *keys = (float *)own + (lane >> ll) * n, *sums = (float *)own + ((n << (6 - ll)) + (lane >> ll) * a.p.n_groups);
+#pragma unroll
+                for (int u = 0; u < kRoutePer; ++u) {
+                    const int e = expert_at<T>(u, ll, h);
+                    if (e < n)
+                        keys[e] = key[u];
+                }
+                lds_sync();
+                for (int g = h; g < a.p.n_groups; g += 1 << ll) {
+                    float first = none, second = none;
+                    for (int i = 0; i < a.group_size; ++i) {
+                        const float v = keys[g * a.group_size + i];
+                        second = fmaxf(second, fminf(first, v));
+                        first = fmaxf(first, v);
+                    }
+                    sums[g] = a.p.group_best == 2 && second > none ? first + second : first;
+                }
+                lds_sync();
+                int taken = 0;
+                for (int g = h; g < a.p.n_groups; g += 1 << ll) {
+                    const float mine = sums[g];
+                    if (mine == none)
+                        continue;
+                    int surely = 0, maybe = -1;                     // groups before this one; it is one of the second
+                    for (int o = 0; o < a.p.n_groups; ++o) {
+                        const float v = sums[o], near = 4.0f * off + 4.0f * kStep * (fabsf(mine) + fabsf(v));
+                        surely += v - mine > near;
+                        maybe += !(mine - v > near);
+                    }
+                    if (maybe < a.p.top_groups)
+                        taken |= 1 << g;
+                    else if (surely < a.p.top_groups)
+                        again = true;
+                }
+                taken = row_or(taken, ll);
+#pragma unroll
+                for (int u = 0; u < kRoutePer; ++u) {
+                    const int e = expert_at<T>(u, ll, h);
+                    if (e < n && !(taken >> (e / a.group_size) & 1))
+                        key[u] = none;
+                    else if (!a.bias && key[u] > none)
+                        key[u] = x[u];
+                }
+            } else if (!a.bias) {
+#pragma unroll
+                for (int u = 0; u < kRoutePer; ++u)
+                    key[u] = x[u];
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < kRoutePer; ++u)
+                key[u] = x[u];
+        }
+        double v[kRoutePer], list[KP];
+#pragma unroll
+        for (int u = 0; u < kRoutePer; ++u)
+            v[u] = key[u] > none ? packed(key[u] + 0.0f, expert_at<T>(u, ll, h)) : 0.0;
+#pragma unroll
+        for (int u = 0; u < kRoutePer; u += KP)
+            sort_list<KP>(v, u);
+#pragma unroll
+        for (int i = 0; i < KP; ++i)
+            list[i] = v[i];
+#pragma unroll
+        for (int u = KP; u < kRoutePer; u += KP) {
+            double other[KP];
+#pragma unroll
+            for (int i = 0; i < KP; ++i)
+                other[i] = v[u + i];
+            merge_list<KP>(list, other);
+        }
+        if (ll > 0) merge_met<0, KP>(list);
+        if (ll > 1) merge_met<1, KP>(list);
+        if (ll > 2) merge_met<2, KP>(list);
+        if (ll > 3) merge_met<3, KP>(list);
+        if (ll > 4) merge_met<4, KP>(list);
+        if (ll > 5) merge_met<5, KP>(list);
+        if constexpr (EXACT) {
+            if (a.bias) {
+                // Neighbours in the list, and what stayed outside against the last: too near to tell, unless the same logit
+                // and bias made both keys.
+                float last = none;
+                int last_e = 0;
+#pragma unroll
+                for (int j = 0; j < KP; ++j) {
+                    if (j < a.p.k) {
+                        last = list[j] > 0.0 ? key_of(list[j]) : none;
+                        last_e = expert_of(list[j]);
+                    }
+                    if (j + 1 < KP && j + 1 < a.p.k && list[j + 1 < KP ? j + 1 : j] > 0.0) {
+                        const double next = list[j + 1 < KP ? j + 1 : j];
+                        const float other = key_of(next), near = 2.0f * off + 2.0f * kStep * (fabsf(last) + fabsf(other));
+                        if (!(last - other > near)) {
+                            const int e = last_e, o = expert_of(next);
+                            again |= !(route_logit((float)logits[e]) == route_logit((float)logits[o]) && a.bias[e] == a.bias[o]);
+                        }
+                    }
+                }
+                if (last > none) {
+#pragma unroll
+                    for (int u = 0; u < kRoutePer; ++u) {
+                        const int e = expert_at<T>(u, ll, h);
+                        const float near = 2.0f * off + 2.0f * kStep * (fabsf(last) + fabsf(key[u]));
+                        if (key[u] > none && !(last - key[u] > near) && (key[u] < last || (key[u] == last && e > last_e)))
+                            again |= !(route_logit((float)logits[last_e]) == x[u] && a.bias[last_e] == a.bias[e]);
+                    }
+                }
+            }
+            again = row_or(again, ll);
+        }
+        const bool write = there && !again;
+        if (ll == 0)
+            finish<T, KP, 0>(a, row, logits, list, h, top, sum, write);
+        else if (ll == 1)
+            finish<T, KP, 1>(a, row, logits, list, h, top, sum, write);
+        else if (ll == 2)
+            finish<T, KP, 2>(a, row, logits, list, h, top, sum, write);
+        else if (ll == 3)
+            finish<T, KP, 3>(a, row, logits, list, h, top, sum, write);
+        else
+            finish<T, KP, 4>(a, row, logits, list, h, top, sum, write);
+    }
+    if constexpr (EXACT) {
+        uint64_t rows = __ballot(again && there && h == 0);
+        while (rows) {
+            const int l = __builtin_ctzll(rows);
+            rows &= rows - 1;
+            route_exact<T>(a, row0 + (l >> ll), own, lane);
+        }
+    }
+}
+
+// ---- the gradient ---------------------------------------------------------------------------------------------------------
+
+// The choices' gradients go to the row's logits through LDS; a row's experts lie in its lanes as above.
 template <int TYPE>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(kRouteWaves * 64)
 route_backward_kernel(RouteArgs a)
 {
     typedef typename Element<TYPE>::type T;
-    __shared__ double grad[FS_MAX_EXPERTS];
-    const int lane = threadIdx.x, n = a.p.n_experts, k = a.p.k;
-    const double none = -__builtin_inf();
-    const T *logits = (const T *)a.logits + (int64_t)blockIdx.x * a.stride;
-    T *out = (T *)a.d_logits + (int64_t)blockIdx.x * a.d_stride;
-    for (int e = lane; e < n; e += 64)
-        grad[e] = 0.0;
-    __syncthreads();
-    int mine = lane < k ? a.chosen[(int64_t)blockIdx.x * k + lane] : -1;
-    if (mine < 0 || mine >= n)
-        mine = -1;
-    const double dw = mine < 0 ? 0.0 : (double)a.d_weight[(int64_t)blockIdx.x * k + lane];
-    double g = dw;
+    typedef T Chunk __attribute__((ext_vector_type(kChunk<T>), aligned(sizeof(T))));
+    __shared__ float lds[kRouteWaves * 64 * kRoutePer];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ll = a.ll, h = lane & ((1 << ll) - 1);
+    const int n = a.p.n_experts, k = a.p.k;
+    const float none = -__builtin_inff();
+    const int64_t row0 = ((int64_t)blockIdx.x * kRouteWaves + wave) << (6 - ll);
+    if (row0 >= a.n_tokens)
+        return;
+    const bool there = row0 + (lane >> ll) < a.n_tokens;
+    const int64_t row = there ? row0 + (lane >> ll) : a.n_tokens - 1;
+    const T *logits = (const T *)a.logits + row * a.stride;
+    float *const grad = lds + wave * 64 * kRoutePer + ((lane >> ll) << ll) * kRoutePer;      // of this row
+    float x[kRoutePer];
+    load_row<T>(logits, n, ll, h, x);
+#pragma unroll
+    for (int u = 0; u < kRoutePer; ++u)
+        grad[expert_at<T>(u, ll, h)] = 0.0f;
+    // renormalised: weight_j = exp(s_j) / sum exp(s_i), s the logit or the logarithm of its sigmoid
+    float high = none, all = 0.0f, mean = 0.0f;
     if (a.p.renormalise) {
-        const double x = mine < 0 ? none : (double)route_logit((float)logits[mine]);
-        const double s = mine < 0 ? none : a.p.score == FS_SCORE_SOFTMAX ? x : fmin(x, 0.0) - log1p(exp(-fabs(x)));
-        const double high = wave_max(s);
-        double q = s > none ? exp(s - high) : 0.0;
-        const double all = wave_sum(q);
-        q = all > 0.0 ? q / all : 0.0;
-        const double mean = wave_sum(q > 0.0 ? q * dw : 0.0);
-        g = q > 0.0 ? q * (dw - mean) : 0.0;
-        if (a.p.score == FS_SCORE_SIGMOID)
-            g *= 1.0 / (1.0 + exp(x));
-    }
-    for (int j = 0; j < k; ++j) {
-        if (lane == j && mine >= 0)
-            grad[mine] += g;
-        __syncthreads();
-    }
-    double top = none, sum = 0.0, dot = 0.0;
-    if (!a.p.renormalise && a.p.score == FS_SCORE_SOFTMAX) {
-        for (int e = lane; e < n; e += 64)
-            top = fmax(top, (double)route_logit((float)logits[e]));
-        top = wave_max(top);
-        if (top == none)
-            top = 0.0;
-        for (int e = lane; e < n; e += 64) {
-            const double v = exp((double)route_logit((float)logits[e]) - top);
-            sum += v;
-            dot += v * grad[e];
+        for (int j = h; j < k; j += 1 << ll) {
+            const int e = a.chosen[row * k + j];
+            if (e >= 0 && e < n) {
+                const float l = route_logit((float)logits[e]);
+                high = fmaxf(high, a.p.score == FS_SCORE_SOFTMAX ? l : fminf(l, 0.0f) - __logf(1.0f + exp_of(-fabsf(l))));
+            }
         }
-        sum = wave_sum(sum);
-        dot = wave_sum(dot) / sum;
+        high = row_max(high, ll);
+        for (int j = h; j < k; j += 1 << ll) {
+            const int e = a.chosen[row * k + j];
+            if (e >= 0 && e < n) {
+                const float l = route_logit((float)logits[e]);
+                const float s = a.p.score == FS_SCORE_SOFTMAX ? l : fminf(l, 0.0f) - __logf(1.0f + exp_of(-fabsf(l)));
+                const float q = s > none ? exp_of(s - high) : 0.0f;
+                all += q;
+                mean += q > 0.0f ? q * a.d_weight[row * k + j] : 0.0f;
+            }
+        }
+        all = row_sum(all, ll);
+        mean = row_sum(mean, ll);
+        all = all > 0.0f ? inverse(all) : 0.0f;
+        mean *= all;
     }
-    for (int e = lane; e < n; e += 64) {
-        const double x = route_logit((float)logits[e]);
-        double d = grad[e];
-        if (!(x > none))
-            d = 0.0;
-        else if (!a.p.renormalise)
-            d = a.p.score == FS_SCORE_SOFTMAX ? exp(x - top) / sum * (d - dot) : d / ((1.0 + exp(x)) * (1.0 + exp(-x)));
-        out[e] = (T)(float)(d * (double)a.p.scale);
+    lds_sync();
+    for (int j = 0; j < k; ++j) {          // one after the other: an expert may have been named twice
+        const int e = a.chosen[row * k + j];
+        if (h == (j & ((1 << ll) - 1)) && e >= 0 && e < n) {
+            float g = a.d_weight[row * k + j];
+            if (a.p.renormalise) {
+                const float l = route_logit((float)logits[e]);
+                const float s = a.p.score == FS_SCORE_SOFTMAX ? l : fminf(l, 0.0f) - __logf(1.0f + exp_of(-fabsf(l)));
+                const float q = s > none ? exp_of(s - high) * all : 0.0f;
+                g = q > 0.0f ? q * (g - mean) : 0.0f;
+                if (a.p.score == FS_SCORE_SIGMOID)
+                    g *= inverse(1.0f + exp_of(l));
+            }
+            grad[e] += g;
+        }
+        lds_sync();
     }
+    float g[kRoutePer];
+#pragma unroll
+    for (int u = 0; u < kRoutePer; ++u)
+        g[u] = grad[expert_at<T>(u, ll, h)];
+    if (!a.p.renormalise && a.p.score == FS_SCORE_SOFTMAX) {
+        float top = none, sum = 0.0f, dot = 0.0f;
+#pragma unroll
+        for (int u = 0; u < kRoutePer; ++u)
+            top = fmaxf(top, x[u]);
+        top = row_max(top, ll);
+        top = top == none ? 0.0f : top;
+#pragma unroll
+        for (int u = 0; u < kRoutePer; ++u) {
+            const float p = exp_of(x[u] - top);
+            sum += p;
+            dot += p > 0.0f ? p * g[u] : 0.0f;
+        }
+        sum = row_sum(sum, ll);
+        dot = row_sum(dot, ll);
+        const float factor = inverse(sum);
+        dot *= factor;
+#pragma unroll
+        for (int u = 0; u < kRoutePer; ++u)
+            g[u] = exp_of(x[u] - top) * factor * (g[u] - dot);
+    } else if (!a.p.renormalise) {
+#pragma unroll
+        for (int u = 0; u < kRoutePer; ++u)      // s (1 - s), the smaller factor first
+            g[u] = g[u] * inverse(1.0f + exp_of(fabsf(x[u]))) * inverse(1.0f + exp_of(-fabsf(x[u])));
+    }
+    if (!there)
+        return;
+    T *out = (T *)a.d_logits + row * a.d_stride;
+#pragma unroll
+    for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
+        const int e = expert_at<T>(c * kChunk<T>, ll, h);
+        Chunk v;
+#pragma unroll
+        for (int i = 0; i < kChunk<T>; ++i) {
+            const int u = c * kChunk<T> + i;
+            v[i] = (T)(x[u] > none ? g[u] * a.p.scale : 0.0f);
+        }
+        if (e + kChunk<T> <= n) {
+            *(Chunk *)(out + e) = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kChunk<T>; ++i)
+                if (e + i < n)
+                    out[e + i] = v[i];
+        }
+    }
+}
+
+static int lanes_log(int n_experts)
+{
+    int ll = 0;
+    while ((kRoutePer << ll) < n_experts)
+        ++ll;
+    return ll;
 }
 
 static int check_route(const char *who, const fs_route_params *p, int64_t n_tokens, const void *logits, int32_t type, int64_t stride)
@@ -247,10 +696,28 @@ extern "C" int fs_route(const fs_route_params *params, int64_t n_tokens, const v
     FS_TRY(check_array(who, "weight", weight, n_tokens, 4));
     if (n_tokens == 0)
         return FS_OK;
-    RouteArgs a = {*params, n_tokens, logit_stride, 0, logits, bias, expert, weight, nullptr, nullptr, nullptr};
+    const int n = params->n_experts, groups = params->n_groups, ll = lanes_log(n);
+    const bool exact = bias || groups > 1;
+    size_t wave_lds = 0;
+    if (exact) {
+        const size_t wide = (size_t)(n + (groups > 1 ? groups : 0)) * 8, rows = groups > 1 ? ((size_t)(n + groups) << (6 - ll)) * 4 : 0;
+        wave_lds = ((wide > rows && wide > 0 ? wide : rows) + 15) / 16 * 16;
+    }
+    RouteArgs a = {*params, n_tokens, logit_stride, 0, logits, bias, expert, weight, nullptr, nullptr, nullptr, ll, n / groups,
+                   exact && groups > kRouteMostGroups, (int32_t)wave_lds};
+    const dim3 grid((unsigned)((n_tokens + ((int64_t)kRouteWaves << (6 - ll)) - 1) / ((int64_t)kRouteWaves << (6 - ll))));
     prof_start(kKernTopk, stream);
     with_type(logit_type, [&](auto t) {
-        hipLaunchKernelGGL(route_kernel<decltype(t)::value>, dim3((unsigned)n_tokens), dim3(64), 0, stream, a);
+        constexpr int type = decltype(t)::value;
+        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kRouteWaves * 64), kRouteWaves * wave_lds, stream, a); };
+        if (params->k <= 2)
+            exact ? go(route_kernel<type, 2, true>) : go(route_kernel<type, 2, false>);
+        else if (params->k <= 4)
+            exact ? go(route_kernel<type, 4, true>) : go(route_kernel<type, 4, false>);
+        else if (params->k <= 8)
+            exact ? go(route_kernel<type, 8, true>) : go(route_kernel<type, 8, false>);
+        else
+            exact ? go(route_kernel<type, 16, true>) : go(route_kernel<type, 16, false>);
     });
     prof_stop(stream);
     return launched("route kernel launch");
@@ -267,10 +734,13 @@ extern "C" int fs_route_backward(const fs_route_params *params, int64_t n_tokens
     FS_TRY(check_matrix(who, "d_logits", d_logits, n_tokens, params->n_experts, logit_type, d_logit_stride));
     if (n_tokens == 0)
         return FS_OK;
-    RouteArgs a = {*params, n_tokens, logit_stride, d_logit_stride, logits, nullptr, nullptr, nullptr, expert, d_weight, d_logits};
+    RouteArgs a = {*params, n_tokens, logit_stride, d_logit_stride, logits, nullptr, nullptr, nullptr, expert, d_weight, d_logits,
+                   lanes_log(params->n_experts), 0, 0, 0};
+    const int64_t rows = (int64_t)kRouteWaves << (6 - a.ll);
     prof_start(kKernTrainOther, stream);
     with_type(logit_type, [&](auto t) {
-        hipLaunchKernelGGL(route_backward_kernel<decltype(t)::value>, dim3((unsigned)n_tokens), dim3(64), 0, stream, a);
+        hipLaunchKernelGGL(route_backward_kernel<decltype(t)::value>, dim3((unsigned)((n_tokens + rows - 1) / rows)), dim3(kRouteWaves * 64), 0,
+                           stream, a);
     });
     prof_stop(stream);
     return launched("route gradient kernel launch");
