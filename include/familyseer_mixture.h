@@ -53,7 +53,8 @@ enum {
 };
 
 #define FS_MAX_EXPERTS 1024
-#define FS_MAX_CHOICES 16      /* experts of a token */
+#define FS_MAX_CHOICES 16      /* experts of a token                                             */
+#define FS_MAX_WIDTH 1048576   /* elements of a row that travels or is looked up                 */
 
 /* ---- routing ------------------------------------------------------------------------------ */
 
@@ -132,8 +133,8 @@ int fs_expert_combine_backward(int64_t n_tokens, int32_t k, int32_t n_experts, i
 /* ---- embedding ----------------------------------------------------------------------------- */
 
 /*
- * out[r] = scale * sum over c ascending of table[col_base[c] + ids[r*n_cols + c]], c < n_cols.  One column is the
- * plain lookup; without col_base its entries count as 0.  Leaves of an ensemble: FS_ID_U16 ids with
+ * out[r] = scale * sum over c of table[col_base[c] + ids[r*n_cols + c]], c < n_cols, in an order that depends on the
+ * sizes alone.  One column is the plain lookup; without col_base its entries count as 0.  Leaves of an ensemble: FS_ID_U16 ids with
  * col_base = the tree_off of fs_model_create, n_cols = n_trees.  Ids whose row is outside
  * [0, n_vocab) add nothing (use -1 for padding).  out_type is the table's type or FS_F32.
  * n_rows*n_cols < 2^31.

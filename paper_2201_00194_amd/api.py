@@ -486,6 +486,7 @@ FS_ID_I32, FS_ID_I64, FS_ID_U16 = 0, 1, 2
 FS_SCORE_SOFTMAX, FS_SCORE_SIGMOID = 0, 1
 FS_MAX_EXPERTS = 1024
 FS_MAX_CHOICES = 16
+FS_MAX_WIDTH = 1048576
 
 _ELEMENT = {torch.float32: FS_F32, torch.bfloat16: FS_BF16, torch.float16: FS_F16}
 _ID = {torch.int32: FS_ID_I32, torch.int64: FS_ID_I64, torch.int16: FS_ID_U16, torch.uint16: FS_ID_U16}

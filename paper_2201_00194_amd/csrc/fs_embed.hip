@@ -1,16 +1,29 @@
 // Embedding: tokens, or bags of tokens, to scaled sums of a table's rows, and the table's gradient by sorted tokens.
+//
+// The gradient of a table's row is the sum over the places that named it.  The (token, row) pairs are sorted by token,
+// stably, a digit at a time; then the sorted list is cut in chunks, and the lanes that hold a row add a chunk's rows run by run.
+// A run inside a chunk is a finished row of the table; what a chunk has of a run that goes on at either end is a partial sum,
+// two a chunk at most, and the partial sums are a sorted list themselves, of 2 / chunk the length: they go the same way
+// again until one chunk is left.  So a token named everywhere costs no more than others, and the order of additions depends on the
+// ids alone.
 #include "fs_slots.h"
 
 #include <math.h>
 
 namespace fs {
 
+constexpr int kEmbedWaves = 4;            // of a workgroup
+constexpr int kEmbedAhead = 8;            // rows on their way at once
+constexpr int kEmbedFewWaves = 2048;
+constexpr int kSumMostChunk = 256, kSumLeastChunk = 16;   // pairs a chunk
+constexpr int kSumNextChunk = 64;                         // partial sums a chunk
+
 struct EmbedIds {
     const void *ids;
     const int32_t *col_base;
     int32_t id_type, n_cols, n_vocab;
-    // The table's row of entry i, or -1.
-    __device__ __forceinline__ int64_t row(int64_t i) const
+    // The table's row that entry i, of column c, names, or -1.
+    __device__ __forceinline__ int row(int64_t i, int c) const
     {
         int64_t v = id_type == FS_ID_I32 ? (int64_t)((const int32_t *)ids)[i]
                     : id_type == FS_ID_I64 ? ((const int64_t *)ids)[i]
@@ -18,111 +31,264 @@ struct EmbedIds {
         if (v < -2147483648ll || v > 2147483647ll)
             return -1;
         if (col_base)
-            v += col_base[i % n_cols];
-        return v >= 0 && v < n_vocab ? v : -1;
+            v += col_base[c];
+        return v >= 0 && v < n_vocab ? (int)v : -1;
     }
 };
 
 struct EmbedArgs {
     EmbedIds ids;
-    const void *in;            // the table, or the gradient of the sums
+    const void *in;            // the table
     int64_t in_stride, out_stride, n_rows;
-    int32_t width, accumulate;
+    int32_t width, ll, split;  // a row of the result in 1 << (ll + split) lanes, the bag in 1 << split parts
     float scale;
     void *out;
-    const int32_t *token, *entry;   // sorted
+    int64_t block0;            // of this launch
 };
 
 template <int IN, int OUT>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(kEmbedWaves * 64)
 embed_kernel(EmbedArgs a)
 {
     typedef typename Element<IN>::type In;
     typedef typename Element<OUT>::type Out;
-    const int64_t r = blockIdx.x;
-    for (int c = threadIdx.x; c < a.width; c += 64) {
-        float sum = 0.0f;
-        for (int j = 0; j < a.ids.n_cols; ++j) {
-            const int64_t v = a.ids.row(r * a.ids.n_cols + j);
-            if (v >= 0)
-                sum += (float)((const In *)a.in)[v * a.in_stride + c];
+    constexpr int N = kChunk<In>;
+    const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1), part = (lane >> ll) & ((1 << a.split) - 1);
+    const int64_t row0 = ((a.block0 + blockIdx.x) * kEmbedWaves + (threadIdx.x >> 6)) << (6 - ll - a.split);
+    if (row0 >= a.n_rows)
+        return;
+    const bool there = row0 + (lane >> (ll + a.split)) < a.n_rows;
+    const int64_t row = there ? row0 + (lane >> (ll + a.split)) : a.n_rows - 1;
+    const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
+    const int cols = a.ids.n_cols, per = (cols + (1 << a.split) - 1) >> a.split;
+    const int begin = min(part * per, cols), end = min(begin + per, cols);
+    const In *const in = (const In *)a.in + c;
+    float sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        sum[i] = 0.0f;
+    for (int j0 = 0; j0 < per; j0 += kEmbedAhead) {          // the same number of times in all lanes
+        int v[kEmbedAhead];
+        if (ll >= 3) {                                       // eight lanes fetch an id each
+            const int j = begin + j0 + (h & 7);
+            const int id = j < end ? a.ids.row(row * cols + j, j) : -1;
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u)
+                v[u] = __shfl(id, (lane & ~7) + u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u) {
+                const int j = begin + j0 + u;
+                v[u] = j < end ? a.ids.row(row * cols + j, j) : -1;
+            }
         }
-        ((Out *)a.out)[r * a.out_stride + c] = (Out)(sum * a.scale);
+        float x[kEmbedAhead][N];
+#pragma unroll
+        for (int u = 0; u < kEmbedAhead; ++u)
+            load_chunk<N>(in + (int64_t)max(v[u], 0) * a.in_stride, v[u] >= 0 ? n : 0, x[u]);
+#pragma unroll
+        for (int u = 0; u < kEmbedAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                sum[i] += x[u][i];
     }
+    for (int s = 0; s < a.split; ++s)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            sum[i] += __shfl_xor(sum[i], 1 << (ll + s));
+    if (!there || part != 0)
+        return;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        sum[i] *= a.scale;
+    store_chunk<N>((Out *)a.out + row * a.out_stride + c, n, sum);
 }
 
-// Sorting the entries by token, a digit at a time: the first pass takes ids, the others what the pass before left.
+// ---- sorting by token: the first pass takes ids, the others what the pass before left -----------------------------------
+
+struct Pair {
+    int32_t token, row;
+};
 struct DigitOfId {
     EmbedIds ids;
     int32_t mask;
     __device__ __forceinline__ int token(int64_t i) const
     {
-        const int64_t v = ids.row(i);
-        return v < 0 ? ids.n_vocab : (int)v;
+        const int v = ids.row(i, ids.n_cols == 1 ? 0 : (int)((uint32_t)i % (uint32_t)ids.n_cols));
+        return v < 0 ? ids.n_vocab : v;
     }
     __device__ __forceinline__ int operator()(int64_t i) const { return token(i) & mask; }
 };
-struct DigitOfToken {
-    const int32_t *from;
+struct DigitOfPair {
+    const Pair *from;
     int32_t shift, mask;
-    __device__ __forceinline__ int operator()(int64_t i) const { return (from[i] >> shift) & mask; }
+    __device__ __forceinline__ int operator()(int64_t i) const { return (from[i].token >> shift) & mask; }
 };
 struct PutId {
     DigitOfId of;
-    int32_t *token, *entry;
+    Pair *to;
+    __device__ __forceinline__ void start(int, int) const {}
     __device__ __forceinline__ void operator()(int64_t i, int, int slot) const
     {
-        token[slot] = of.token(i);
-        entry[slot] = (int32_t)i;
+        to[slot] = Pair{of.token(i), (int32_t)((uint32_t)i / (uint32_t)of.ids.n_cols)};
     }
 };
-struct PutToken {
-    const int32_t *from_token, *from_entry;
-    int32_t *token, *entry;
-    __device__ __forceinline__ void operator()(int64_t i, int, int slot) const
-    {
-        token[slot] = from_token[i];
-        entry[slot] = from_entry[i];
-    }
+struct PutPair {
+    const Pair *from;
+    Pair *to;
+    __device__ __forceinline__ void start(int, int) const {}
+    __device__ __forceinline__ void operator()(int64_t i, int, int slot) const { to[slot] = from[i]; }
 };
 
-__device__ __forceinline__ int64_t first_not_below(const int32_t *token, int64_t n, int v)
-{
-    int64_t lo = 0, hi = n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (token[mid] < v)
-            lo = mid + 1;
-        else
-            hi = mid;
-    }
-    return lo;
-}
+// ---- sums of the runs -----------------------------------------------------------------------------------------------------
 
-template <int IN, int OUT>
-__global__ void __launch_bounds__(64)
-embed_backward_kernel(EmbedArgs a, int64_t n)
+struct SumArgs {
+    const Pair *pairs;             // the list, or
+    const uint32_t *token;         // partial sums: token * 2, + 1 where there is nothing to add
+    const void *in;
+    int64_t in_stride, out_stride, n;
+    int32_t width, ll, chunk, n_vocab, accumulate;
+    float scale;
+    void *out;
+    uint32_t *next_token;          // two a chunk
+    float *next;
+    int64_t next_stride;
+};
+
+template <int IN, int OUT, bool PAIRS>
+__global__ void __launch_bounds__(kEmbedWaves * 64)
+embed_sum_kernel(SumArgs a)
 {
     typedef typename Element<IN>::type In;
     typedef typename Element<OUT>::type Out;
-    const int v = blockIdx.x;
-    const int64_t begin = first_not_below(a.token, n, v), end = first_not_below(a.token, n, v + 1);
-    for (int c = threadIdx.x; c < a.width; c += 64) {
-        double sum = 0.0;
-        for (int64_t i = begin; i < end; ++i)
-            sum += (double)(float)((const In *)a.in)[(int64_t)(a.entry[i] / a.ids.n_cols) * a.in_stride + c];
-        Out &out = ((Out *)a.out)[(int64_t)v * a.out_stride + c];
-        const double add = sum * (double)a.scale;
-        out = (Out)(float)(a.accumulate ? (double)(float)out + add : add);
+    constexpr int N = kChunk<In>;
+    const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
+    const int64_t at = (((int64_t)blockIdx.x * kEmbedWaves + (threadIdx.x >> 6)) << (6 - ll)) + (lane >> ll);
+    const int64_t begin = at * a.chunk, end = min(begin + a.chunk, a.n);
+    if (begin >= a.n)
+        return;
+    const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
+    const In *const in = (const In *)a.in + c;
+    const auto token_at = [&](int64_t i) -> int { return PAIRS ? a.pairs[i].token : (int)(a.token[i] >> 1); };
+    const int before = begin > 0 ? token_at(begin - 1) : -1, behind = end < a.n ? token_at(end) : -1;
+    float sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        sum[i] = 0.0f;
+    int now = token_at(begin);
+    bool first = true, some = false;
+    const auto mark = [&](int which, bool partial) {
+        if (h == 0 && blockIdx.y == 0)
+            a.next_token[2 * at + which] = (uint32_t)now * 2u + (partial ? 0u : 1u);
+        if (partial)
+            store_chunk<N>(a.next + (2 * at + which) * a.next_stride + c, n, sum);
+    };
+    const auto done = [&](bool last) {                       // the run of `now` ends here, or the chunk does
+        const bool left = first && before == now, right = last && behind == now;
+        if (!left && !right && some) {
+            Out *const out = (Out *)a.out + (int64_t)now * a.out_stride + c;
+            float had[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                had[i] = 0.0f;
+            if (a.accumulate)
+                load_chunk<N>(out, n, had);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                had[i] += sum[i] * a.scale;
+            store_chunk<N>(out, n, had);
+        }
+        if (first)
+            mark(0, (left || right) && some);
+        if (last)
+            mark(1, !first && right && some);
+    };
+    for (int64_t i0 = begin; i0 < end; i0 += kEmbedAhead) {
+        int token[kEmbedAhead];
+        bool add[kEmbedAhead];
+        int64_t from[kEmbedAhead];
+#pragma unroll
+        for (int u = 0; u < kEmbedAhead; ++u) {
+            const int64_t i = min(i0 + u, end - 1);
+            if constexpr (PAIRS) {
+                const Pair p = a.pairs[i];
+                token[u] = p.token;
+                from[u] = p.row;
+                add[u] = i0 + u < end && p.token < a.n_vocab;
+            } else {
+                const uint32_t t = a.token[i];
+                token[u] = (int)(t >> 1);
+                from[u] = i;
+                add[u] = i0 + u < end && !(t & 1);
+            }
+        }
+        float x[kEmbedAhead][N];
+#pragma unroll
+        for (int u = 0; u < kEmbedAhead; ++u)
+            load_chunk<N>(in + from[u] * a.in_stride, add[u] ? n : 0, x[u]);
+#pragma unroll
+        for (int u = 0; u < kEmbedAhead; ++u) {
+            if (token[u] != now) {
+                done(false);
+                first = false;
+                some = false;
+                now = token[u];
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    sum[i] = 0.0f;
+            }
+            if (add[u]) {
+                some = true;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    sum[i] += x[u][i];
+            }
+        }
     }
+    done(true);
+}
+
+// Rows that nobody names are 0.
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+embed_clear_kernel(void *table, int64_t n_rows, int32_t width, int64_t stride, int32_t ll)
+{
+    typedef typename Element<TYPE>::type T;
+    constexpr int N = kChunk<T>;
+    const int lane = threadIdx.x & 63, h = lane & ((1 << ll) - 1);
+    const int c = ((int)blockIdx.y * 64 + h) * N;
+    const float zero[N] = {};
+    for (int64_t r = (((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) << (6 - ll)) + (lane >> ll); r < n_rows; r += ((int64_t)gridDim.x * 4) << (6 - ll))
+        store_chunk<N>((T *)table + r * stride + c, width - c, zero);
+}
+
+struct SumPlan {
+    int64_t n[2];                  // rows of partial sums behind the first and the second sum
+    int64_t stride;
+    int32_t chunk;
+};
+// More, shorter chunks where there are few pairs to a wavefront: down to kSumLeastChunk for 4096 wavefronts.
+static SumPlan sum_plan(int64_t n, int32_t width)
+{
+    SumPlan p;
+    const int64_t lanes = (width + 3) / 4;           // of 16 bytes in fp32
+    p.chunk = kSumMostChunk;
+    while (p.chunk > kSumLeastChunk && n / p.chunk * lanes < 4096 * 64)
+        p.chunk /= 2;
+    p.stride = (width + 3) / 4 * 4;
+    const int64_t chunks = (n + p.chunk - 1) / p.chunk;
+    p.n[0] = chunks > 1 ? 2 * chunks : 2;
+    p.n[1] = 2 * ((p.n[0] + kSumNextChunk - 1) / kSumNextChunk);
+    return p;
 }
 
 struct SortPlan {
     int passes, bits;
     SlotShape shape;
-    size_t list_bytes, bytes;
+    SumPlan sum;
+    size_t list_bytes, token_bytes[2], sum_bytes[2], bytes;
 };
-static SortPlan sort_plan(int32_t n_vocab, int64_t n)
+static SortPlan sort_plan(int32_t n_vocab, int32_t width, int64_t n)
 {
     SortPlan p;
     int bits = 1;                                  // of 0 .. n_vocab
@@ -131,8 +297,14 @@ static SortPlan sort_plan(int32_t n_vocab, int64_t n)
     p.passes = (bits + 9) / 10;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.shape = slot_shape(n, 1 << p.bits);
-    p.list_bytes = ((size_t)n * 4 + 255) / 256 * 256;
-    p.bytes = 4 * p.list_bytes + slot_count_bytes(p.shape);
+    p.sum = sum_plan(n, width);
+    p.list_bytes = ((size_t)n * sizeof(Pair) + 255) / 256 * 256;
+    p.bytes = 2 * p.list_bytes + slot_count_bytes(p.shape);
+    for (int i = 0; i < 2; ++i) {
+        p.token_bytes[i] = ((size_t)p.sum.n[i] * 4 + 255) / 256 * 256;
+        p.sum_bytes[i] = ((size_t)p.sum.n[i] * p.sum.stride * 4 + 255) / 256 * 256;
+        p.bytes += p.token_bytes[i] + p.sum_bytes[i];
+    }
     return p;
 }
 
@@ -140,8 +312,7 @@ static int check_embed(const char *who, int32_t n_vocab, int32_t width, int64_t 
 {
     if (n_vocab < 1 || n_vocab == 2147483647)
         return fail(FS_EINVAL, "%s: n_vocab %d outside [1, 2^31 - 2]", who, n_vocab);
-    if (width < 1)
-        return fail(FS_EINVAL, "%s: width %d", who, width);
+    FS_TRY(check_width(who, width));
     if (n_cols < 1)
         return fail(FS_EINVAL, "%s: n_cols %d", who, n_cols);
     if (n_rows < 0 || n_rows >= ((int64_t)1 << 31) || n_rows * n_cols >= ((int64_t)1 << 31))
@@ -192,10 +363,18 @@ extern "C" int fs_embed(int32_t n_vocab, int32_t width, const void *table, int32
     FS_TRY(check_out_type(who, "out", table_type, out_type));
     if (n_rows == 0)
         return FS_OK;
-    EmbedArgs a = {{ids, col_base, id_type, n_cols, n_vocab}, table, table_stride, out_stride, n_rows, width, 0, scale, out, nullptr, nullptr};
+    const int chunk = 16 / (int)type_bytes(table_type), ll = row_lanes_log(width, chunk), blocks = column_blocks(width, chunk);
+    int split = 0;                 // a long bag of few rows: its parts in neighbouring lanes, down to four ids each
+    while (split < 6 - ll && (n_cols >> (split + 1)) >= 4 && (((n_rows * blocks) << (ll + split)) >> 6) < kEmbedFewWaves)
+        ++split;
+    EmbedArgs a = {{ids, col_base, id_type, n_cols, n_vocab}, table, table_stride, out_stride, n_rows, width, ll, split, scale, out, 0};
+    const int64_t rows = (int64_t)kEmbedWaves << (6 - ll - split);
     prof_start(kKernPack, stream);
     with_types(table_type, out_type, [&](auto i, auto o) {
-        hipLaunchKernelGGL((embed_kernel<decltype(i)::value, decltype(o)::value>), dim3((unsigned)n_rows), dim3(64), 0, stream, a);
+        in_pieces((n_rows + rows - 1) / rows, [&](int64_t at, unsigned n) {
+            a.block0 = at;
+            hipLaunchKernelGGL((embed_kernel<decltype(i)::value, decltype(o)::value>), dim3(n, (unsigned)blocks), dim3(kEmbedWaves * 64), 0, stream, a);
+        });
     });
     prof_stop(stream);
     return launched("embedding kernel launch");
@@ -205,7 +384,7 @@ extern "C" size_t fs_embed_backward_workspace_bytes(int32_t n_vocab, int32_t wid
 {
     if (check_embed("fs_embed_backward_workspace_bytes", n_vocab, width, n_rows, n_cols) != FS_OK)
         return 0;
-    return sort_plan(n_vocab, n_rows * n_cols).bytes;
+    return sort_plan(n_vocab, width, n_rows * n_cols).bytes;
 }
 
 extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_out, int32_t d_out_type, int64_t d_out_stride, int64_t n_rows,
@@ -222,31 +401,67 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
     if (accumulate != 0 && accumulate != 1)
         return fail(FS_EINVAL, "%s: accumulate is %d", who, accumulate);
     const int64_t n = n_rows * n_cols;
-    const SortPlan p = sort_plan(n_vocab, n);
+    const SortPlan p = sort_plan(n_vocab, width, n);
     FS_TRY(check_array(who, "work", work, (int64_t)p.bytes, 256));
     if (work_bytes < p.bytes)
         return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, p.bytes);
-    int32_t *token[2], *entry[2];
+    char *at = (char *)work;
+    const auto take = [&](size_t bytes) {
+        char *const here = at;
+        at += bytes;
+        return here;
+    };
+    Pair *list[2];
+    uint32_t *token[2];
+    float *sum[2];
     for (int i = 0; i < 2; ++i) {
-        token[i] = (int32_t *)((char *)work + (2 * i) * p.list_bytes);
-        entry[i] = (int32_t *)((char *)work + (2 * i + 1) * p.list_bytes);
+        list[i] = (Pair *)take(p.list_bytes);
+        token[i] = (uint32_t *)take(p.token_bytes[i]);
+        sum[i] = (float *)take(p.sum_bytes[i]);
     }
-    int32_t *count = (int32_t *)((char *)work + 4 * p.list_bytes);
+    int32_t *const count = (int32_t *)at;
     prof_start(kKernTrainOther, stream);
-    const EmbedIds e = {ids, col_base, id_type, n_cols, n_vocab};
-    const int mask = (1 << p.bits) - 1;
-    int at = 0;
+    if (!accumulate)
+        with_type(d_table_type, [&](auto t) {
+            typedef typename Element<decltype(t)::value>::type T;
+            const int ll = row_lanes_log(width, kChunk<T>);
+            const int64_t rows = (int64_t)4 << (6 - ll), blocks = (n_vocab + rows - 1) / rows;
+            hipLaunchKernelGGL(embed_clear_kernel<decltype(t)::value>,
+                               dim3((unsigned)(blocks < 8192 ? blocks : 8192), (unsigned)column_blocks(width, kChunk<T>)), dim3(256), 0, stream, d_table,
+                               (int64_t)n_vocab, width, d_table_stride, ll);
+        });
     if (n > 0) {
-        const DigitOfId of = {e, mask};
-        launch_slots(of, PutId{of, token[0], entry[0]}, p.shape, count, stream);
-        for (int pass = 1; pass < p.passes; ++pass, at ^= 1)
-            launch_slots(DigitOfToken{token[at], pass * p.bits, mask}, PutToken{token[at], entry[at], token[at ^ 1], entry[at ^ 1]},
-                         p.shape, count, stream);
+        const int mask = (1 << p.bits) - 1;
+        const DigitOfId of = {{ids, col_base, id_type, n_cols, n_vocab}, mask};
+        launch_slots(of, PutId{of, list[0]}, p.shape, count, stream);
+        int now = 0;
+        for (int pass = 1; pass < p.passes; ++pass, now ^= 1)
+            launch_slots(DigitOfPair{list[now], pass * p.bits, mask}, PutPair{list[now], list[now ^ 1]}, p.shape, count, stream);
+        SumArgs a = {list[now], nullptr, d_out, d_out_stride, d_table_stride, n, width, 0, p.sum.chunk, n_vocab, accumulate, scale, d_table,
+                     token[0], sum[0], p.sum.stride};
+        const auto grid_of = [&](int chunk_elements) {
+            a.ll = row_lanes_log(width, chunk_elements);
+            const int64_t chunks = (a.n + a.chunk - 1) / a.chunk, each = (int64_t)kEmbedWaves << (6 - a.ll);
+            return dim3((unsigned)((chunks + each - 1) / each), (unsigned)column_blocks(width, chunk_elements));
+        };
+        with_types(d_out_type, d_table_type, [&](auto i, auto o) {
+            constexpr int in = decltype(i)::value, out = decltype(o)::value;
+            dim3 grid = grid_of(kChunk<typename Element<in>::type>);
+            hipLaunchKernelGGL((embed_sum_kernel<in, out, true>), grid, dim3(kEmbedWaves * 64), 0, stream, a);
+            for (int from = 0; a.n > a.chunk; from ^= 1) {
+                a.n = 2 * ((a.n + a.chunk - 1) / a.chunk);
+                a.chunk = kSumNextChunk;
+                a.pairs = nullptr;
+                a.token = token[from];
+                a.in = sum[from];
+                a.in_stride = p.sum.stride;
+                a.next_token = token[from ^ 1];
+                a.next = sum[from ^ 1];
+                grid = grid_of(kChunk<float>);
+                hipLaunchKernelGGL((embed_sum_kernel<FS_F32, out, false>), grid, dim3(kEmbedWaves * 64), 0, stream, a);
+            }
+        });
     }
-    EmbedArgs a = {e, d_out, d_out_stride, d_table_stride, n_rows, width, accumulate, scale, d_table, token[at], entry[at]};
-    with_types(d_out_type, d_table_type, [&](auto i, auto o) {
-        hipLaunchKernelGGL((embed_backward_kernel<decltype(i)::value, decltype(o)::value>), dim3((unsigned)n_vocab), dim3(64), 0, stream, a, n);
-    });
     prof_stop(stream);
     return launched("embedding gradient kernels launch");
 }

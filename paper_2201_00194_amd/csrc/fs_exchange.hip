@@ -13,8 +13,9 @@ struct ChoiceNumber {
     }
 };
 struct ChoicePut {
-    int32_t *order, *place;
+    int32_t *first, *order, *place;
     int32_t n_experts;
+    __device__ __forceinline__ void start(int e, int slot) const { first[e] = slot; }
     __device__ __forceinline__ void operator()(int64_t i, int e, int slot) const
     {
         order[slot] = e < n_experts ? (int32_t)i : -1;
@@ -22,11 +23,12 @@ struct ChoicePut {
     }
 };
 
+// No choices: no slots.
 __global__ void __launch_bounds__(256)
-expert_first_kernel(const int32_t *count, SlotShape s, int32_t *first)
+expert_none_kernel(int32_t n_experts, int32_t *first)
 {
-    for (int e = threadIdx.x; e < s.buckets; e += 256)
-        first[e] = s.stretches ? count[(int64_t)e * s.stretches] : 0;
+    for (int e = threadIdx.x; e <= n_experts; e += 256)
+        first[e] = 0;
 }
 
 struct ExchangeArgs {
@@ -109,10 +111,6 @@ expert_combine_backward_kernel(ExchangeArgs a)
     clear_slots_behind<T>(a, t, threadIdx.x);
 }
 
-static int check_width(const char *who, int32_t width)
-{
-    return width < 1 ? fail(FS_EINVAL, "%s: width %d", who, width) : FS_OK;
-}
 static int check_experts(const char *who, int32_t n_experts)
 {
     if (n_experts < 1 || n_experts > FS_MAX_EXPERTS)
@@ -151,8 +149,9 @@ extern "C" int fs_expert_plan(int64_t n_tokens, int32_t k, int32_t n_experts, co
     int32_t *count = (int32_t *)work;
     prof_start(kKernPack, stream);
     if (s.n > 0)
-        launch_slots(ChoiceNumber{expert, n_experts}, ChoicePut{order, place, n_experts}, s, count, stream);
-    hipLaunchKernelGGL(expert_first_kernel, dim3(1), dim3(256), 0, stream, (const int32_t *)count, s, first);
+        launch_slots(ChoiceNumber{expert, n_experts}, ChoicePut{first, order, place, n_experts}, s, count, stream);
+    else
+        hipLaunchKernelGGL(expert_none_kernel, dim3(1), dim3(256), 0, stream, n_experts, first);
     prof_stop(stream);
     return launched("expert plan kernels launch");
 }

@@ -45,6 +45,12 @@ inline int check_matrix(const char *who, const char *what, const void *p, int64_
         return fail(FS_EINVAL, "%s: %s is not aligned to its elements", who, what);
     return FS_OK;
 }
+inline int check_width(const char *who, int32_t width)
+{
+    if (width < 1 || width > FS_MAX_WIDTH)
+        return fail(width < 1 ? FS_EINVAL : FS_EUNSUPPORTED, "%s: width %d outside [1, %d]", who, width, FS_MAX_WIDTH);
+    return FS_OK;
+}
 inline int check_array(const char *who, const char *what, const void *p, int64_t n, size_t bytes)
 {
     if (n > 0 && !p)
@@ -118,8 +124,75 @@ __device__ __forceinline__ int row_or(int v, int ll) { return row_reduce(v, ll, 
 
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f); }
 
+// ---- rows of a matrix ---------------------------------------------------------------------------
+// A row's elements lie in 1 << ll neighbouring lanes, 16 bytes of them a lane; wider rows take several column blocks of a
+// wavefront's 1 KB.  Rows need not be aligned to more than their elements: unaligned loads are loads all the same.
+template <class T> constexpr int kChunk = 16 / (int)sizeof(T);
+inline int row_lanes_log(int width, int chunk)
+{
+    int ll = 0;
+    while (ll < 6 && (chunk << ll) < width)
+        ++ll;
+    return ll;
+}
+inline int column_blocks(int width, int chunk) { return (width + chunk * 64 - 1) / (chunk * 64); }
+
+template <class T, int N>
+struct ChunkOf {
+    typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+// N elements, n of them there: the others are 0, and nothing behind the n-th is read.
+template <int N, class T>
+__device__ __forceinline__ void load_chunk(const T *p, int n, float (&v)[N])
+{
+    if (n >= N) {
+        const typename ChunkOf<T, N>::type c = *(const typename ChunkOf<T, N>::type *)p;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = (float)c[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = 0.0f;
+        if (n > 0) {
+            T c[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                c[i] = p[i < n ? i : n - 1];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                v[i] = i < n ? (float)c[i] : 0.0f;
+        }
+    }
+}
+template <int N, class T>
+__device__ __forceinline__ void store_chunk(T *p, int n, const float (&v)[N])
+{
+    if (n >= N) {
+        typename ChunkOf<T, N>::type c;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            c[i] = (T)v[i];
+        *(typename ChunkOf<T, N>::type *)p = c;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n)
+                p[i] = (T)v[i];
+    }
+}
+
 // The hardware's reciprocal, one step off at most.
 __device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }
+
+// A launch has at most 2^32 - 1 threads: f(first block, blocks) for pieces of 2^22 workgroups.
+template <class F>
+void in_pieces(int64_t blocks, F f)
+{
+    constexpr int64_t kMost = (int64_t)1 << 22;
+    for (int64_t at = 0; at < blocks; at += kMost)
+        f(at, (unsigned)(blocks - at < kMost ? blocks - at : kMost));
+}
 
 #define FS_TRY(call)               \
     do {                           \

@@ -33,6 +33,7 @@ struct RouteArgs {
     int32_t ll, group_size;
     int32_t exact;                       // 1: every row in 64 bits
     int32_t wave_lds;                    // bytes
+    int64_t block0;                      // of this launch
 };
 
 // NaN masks an expert as -infinity does; +infinity counts as the largest float.
@@ -237,8 +238,6 @@ __device__ __forceinline__ void merge_met(double (&list)[KP])
 
 // ---- the kernel -----------------------------------------------------------------------------------------------------------
 
-template <class T> constexpr int kChunk = 16 / (int)sizeof(T);       // elements of a load
-
 // x[u]: expert expert_at(u) of the row, -infinity past the last.
 template <class T>
 __device__ __forceinline__ int expert_at(int u, int ll, int h) { return (((u / kChunk<T>) << ll) + h) * kChunk<T> + u % kChunk<T>; }
@@ -246,29 +245,14 @@ __device__ __forceinline__ int expert_at(int u, int ll, int h) { return (((u / k
 template <class T>
 __device__ __forceinline__ void load_row(const T *logits, int n, int ll, int h, float (&x)[kRoutePer])
 {
-    typedef T Chunk __attribute__((ext_vector_type(kChunk<T>), aligned(sizeof(T))));
 #pragma unroll
     for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
         const int e = expert_at<T>(c * kChunk<T>, ll, h);
-        if (e + kChunk<T> <= n) {
-            const Chunk v = *(const Chunk *)(logits + e);
+        float v[kChunk<T>];
+        load_chunk<kChunk<T>>(logits + e, n - e, v);
 #pragma unroll
-            for (int i = 0; i < kChunk<T>; ++i)
-                x[c * kChunk<T> + i] = route_logit((float)v[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kChunk<T>; ++i)
-                x[c * kChunk<T> + i] = -__builtin_inff();
-            if (e < n) {
-                T v[kChunk<T>];
-#pragma unroll
-                for (int i = 0; i < kChunk<T>; ++i)
-                    v[i] = logits[min(e + i, n - 1)];
-#pragma unroll
-                for (int i = 0; i < kChunk<T>; ++i)
-                    x[c * kChunk<T> + i] = e + i < n ? route_logit((float)v[i]) : -__builtin_inff();
-            }
-        }
+        for (int i = 0; i < kChunk<T>; ++i)
+            x[c * kChunk<T> + i] = e + i < n ? route_logit(v[i]) : -__builtin_inff();
     }
 }
 
@@ -353,7 +337,7 @@ route_kernel(RouteArgs a)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ll = a.ll, h = lane & ((1 << ll) - 1);
     const int n = a.p.n_experts;
     const float none = -__builtin_inff();
-    const int64_t row0 = ((int64_t)blockIdx.x * kRouteWaves + wave) << (6 - ll);
+    const int64_t row0 = ((a.block0 + blockIdx.x) * kRouteWaves + wave) << (6 - ll);
     if (row0 >= a.n_tokens)
         return;
     const bool there = row0 + (lane >> ll) < a.n_tokens;
@@ -535,12 +519,11 @@ __global__ void __launch_bounds__(kRouteWaves * 64)
 route_backward_kernel(RouteArgs a)
 {
     typedef typename Element<TYPE>::type T;
-    typedef T Chunk __attribute__((ext_vector_type(kChunk<T>), aligned(sizeof(T))));
     __shared__ float lds[kRouteWaves * 64 * kRoutePer];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ll = a.ll, h = lane & ((1 << ll) - 1);
     const int n = a.p.n_experts, k = a.p.k;
     const float none = -__builtin_inff();
-    const int64_t row0 = ((int64_t)blockIdx.x * kRouteWaves + wave) << (6 - ll);
+    const int64_t row0 = ((a.block0 + blockIdx.x) * kRouteWaves + wave) << (6 - ll);
     if (row0 >= a.n_tokens)
         return;
     const bool there = row0 + (lane >> ll) < a.n_tokens;
@@ -630,20 +613,13 @@ route_backward_kernel(RouteArgs a)
 #pragma unroll
     for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
         const int e = expert_at<T>(c * kChunk<T>, ll, h);
-        Chunk v;
+        float v[kChunk<T>];
 #pragma unroll
         for (int i = 0; i < kChunk<T>; ++i) {
             const int u = c * kChunk<T> + i;
-            v[i] = (T)(x[u] > none ? g[u] * a.p.scale : 0.0f);
+            v[i] = x[u] > none ? g[u] * a.p.scale : 0.0f;
         }
-        if (e + kChunk<T> <= n) {
-            *(Chunk *)(out + e) = v;
-        } else {
-#pragma unroll
-            for (int i = 0; i < kChunk<T>; ++i)
-                if (e + i < n)
-                    out[e + i] = v[i];
-        }
+        store_chunk<kChunk<T>>(out + e, n - e, v);
     }
 }
 
@@ -704,12 +680,17 @@ extern "C" int fs_route(const fs_route_params *params, int64_t n_tokens, const v
         wave_lds = ((wide > rows && wide > 0 ? wide : rows) + 15) / 16 * 16;
     }
     RouteArgs a = {*params, n_tokens, logit_stride, 0, logits, bias, expert, weight, nullptr, nullptr, nullptr, ll, n / groups,
-                   exact && groups > kRouteMostGroups, (int32_t)wave_lds};
-    const dim3 grid((unsigned)((n_tokens + ((int64_t)kRouteWaves << (6 - ll)) - 1) / ((int64_t)kRouteWaves << (6 - ll))));
+                   exact && groups > kRouteMostGroups, (int32_t)wave_lds, 0};
+    const int64_t rows = (int64_t)kRouteWaves << (6 - ll);
     prof_start(kKernTopk, stream);
     with_type(logit_type, [&](auto t) {
         constexpr int type = decltype(t)::value;
-        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kRouteWaves * 64), kRouteWaves * wave_lds, stream, a); };
+        const auto go = [&](auto kernel) {
+            in_pieces((n_tokens + rows - 1) / rows, [&](int64_t at, unsigned blocks) {
+                a.block0 = at;
+                hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kRouteWaves * 64), kRouteWaves * wave_lds, stream, a);
+            });
+        };
         if (params->k <= 2)
             exact ? go(route_kernel<type, 2, true>) : go(route_kernel<type, 2, false>);
         else if (params->k <= 4)
@@ -735,12 +716,14 @@ extern "C" int fs_route_backward(const fs_route_params *params, int64_t n_tokens
     if (n_tokens == 0)
         return FS_OK;
     RouteArgs a = {*params, n_tokens, logit_stride, d_logit_stride, logits, nullptr, nullptr, nullptr, expert, d_weight, d_logits,
-                   lanes_log(params->n_experts), 0, 0, 0};
+                   lanes_log(params->n_experts), 0, 0, 0, 0};
     const int64_t rows = (int64_t)kRouteWaves << (6 - a.ll);
     prof_start(kKernTrainOther, stream);
     with_type(logit_type, [&](auto t) {
-        hipLaunchKernelGGL(route_backward_kernel<decltype(t)::value>, dim3((unsigned)((n_tokens + rows - 1) / rows)), dim3(kRouteWaves * 64), 0,
-                           stream, a);
+        in_pieces((n_tokens + rows - 1) / rows, [&](int64_t at, unsigned blocks) {
+            a.block0 = at;
+            hipLaunchKernelGGL(route_backward_kernel<decltype(t)::value>, dim3(blocks), dim3(kRouteWaves * 64), 0, stream, a);
+        });
     });
     prof_stop(stream);
     return launched("route gradient kernel launch");
