@@ -31,84 +31,166 @@ expert_none_kernel(int32_t n_experts, int32_t *first)
         first[e] = 0;
 }
 
+constexpr int kExchangeWaves = 4;      // of a workgroup
+constexpr int kExchangeAhead = 8;      // rows on their way at once
+
 struct ExchangeArgs {
     int64_t n_tokens, in_stride, y_stride, out_stride;
-    int32_t k, n_experts, width;
+    int32_t k, n_experts, width, ll;
     const void *in;                  // x, or the gradient of the tokens' results
     const void *y;
     const int32_t *first, *place;
     const float *weight;
     void *out;
     float *d_weight;
+    int64_t block0;                  // of this launch
+};
+// Lanes (1 << ll) to a token.
+struct TokenLanes {
+    int h;
+    int64_t token;
+    __device__ __forceinline__ explicit TokenLanes(const ExchangeArgs &a)
+    {
+        const int lane = threadIdx.x & 63;
+        h = lane & ((1 << a.ll) - 1);
+        token = (((a.block0 + blockIdx.x) * kExchangeWaves + (threadIdx.x >> 6)) << (6 - a.ll)) + (lane >> a.ll);
+    }
 };
 
-// The slots behind the last expert's: n_tokens wavefronts share them.
+// The slots behind the last expert's: the tokens' lanes share them.
 template <class T>
-__device__ __forceinline__ void clear_slots_behind(const ExchangeArgs &a, int64_t token, int lane)
+__device__ __forceinline__ void clear_slots_behind(const ExchangeArgs &a, int64_t token, int c, int n)
 {
+    RawChunk<T> zero;
+    zero.clear();
     const int64_t slots = a.n_tokens * a.k;
     for (int64_t s = max(a.first[a.n_experts], 0) + token; s < slots; s += a.n_tokens)
-        for (int c = lane; c < a.width; c += 64)
-            ((T *)a.out)[s * a.out_stride + c] = (T)0.0f;
+        zero.store((T *)a.out + s * a.out_stride + c, n);
 }
 
+// A row is read once and written k times.
 template <int TYPE>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(kExchangeWaves * 64)
 expert_gather_kernel(ExchangeArgs a)
 {
     typedef typename Element<TYPE>::type T;
-    const int64_t t = blockIdx.x, slots = a.n_tokens * a.k;
-    const T *in = (const T *)a.in + t * a.in_stride;
+    const TokenLanes l(a);
+    if (l.token >= a.n_tokens)
+        return;
+    const int c = ((int)blockIdx.y * 64 + l.h) * kChunk<T>, n = a.width - c;
+    const int64_t slots = a.n_tokens * a.k;
+    RawChunk<T> x;
+    x.load((const T *)a.in + l.token * a.in_stride + c, n);
+    const int32_t *const place = a.place + l.token * a.k;
     for (int j = 0; j < a.k; ++j) {
-        const int p = a.place[t * a.k + j];
+        const int p = place[j];
         if (p >= 0 && p < slots)
-            for (int c = threadIdx.x; c < a.width; c += 64)
-                ((T *)a.out)[(int64_t)p * a.out_stride + c] = in[c];
+            x.store((T *)a.out + (int64_t)p * a.out_stride + c, n);
     }
-    clear_slots_behind<T>(a, t, threadIdx.x);
+    clear_slots_behind<T>(a, l.token, c, n);
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(kExchangeWaves * 64)
 expert_combine_kernel(ExchangeArgs a)
 {
     typedef typename Element<TYPE>::type T;
-    const int64_t t = blockIdx.x, slots = a.n_tokens * a.k;
-    for (int c = threadIdx.x; c < a.width; c += 64) {
-        float sum = 0.0f;
-        for (int j = 0; j < a.k; ++j) {
-            const int p = a.place[t * a.k + j];
-            if (p >= 0 && p < slots)
-                sum = fmaf(a.weight ? a.weight[t * a.k + j] : 1.0f, (float)((const T *)a.y)[(int64_t)p * a.y_stride + c], sum);
+    constexpr int N = kChunk<T>;
+    const TokenLanes l(a);
+    if (l.token >= a.n_tokens)
+        return;
+    const int c = ((int)blockIdx.y * 64 + l.h) * N, n = a.width - c;
+    const int64_t slots = a.n_tokens * a.k;
+    const T *const y = (const T *)a.y + c;
+    float sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        sum[i] = 0.0f;
+    for (int j0 = 0; j0 < a.k; j0 += kExchangeAhead) {
+        float x[kExchangeAhead][N], w[kExchangeAhead];
+#pragma unroll
+        for (int u = 0; u < kExchangeAhead; ++u) {
+            const int j = min(j0 + u, a.k - 1), p = a.place[l.token * a.k + j];
+            const bool there = j0 + u < a.k && p >= 0 && p < slots;
+            w[u] = !there ? 0.0f : a.weight ? a.weight[l.token * a.k + j] : 1.0f;
+            load_chunk<N>(y + (int64_t)(there ? p : 0) * a.y_stride, there ? n : 0, x[u]);
         }
-        ((T *)a.out)[t * a.out_stride + c] = (T)sum;
+#pragma unroll
+        for (int u = 0; u < kExchangeAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                sum[i] = fmaf(w[u], x[u][i], sum[i]);
     }
+    store_chunk<N>((T *)a.out + l.token * a.out_stride + c, n, sum);
 }
 
+// The products need a token's whole width, so that its lanes go over the column blocks themselves.
 template <int TYPE>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(kExchangeWaves * 64)
 expert_combine_backward_kernel(ExchangeArgs a)
 {
     typedef typename Element<TYPE>::type T;
-    const int64_t t = blockIdx.x, slots = a.n_tokens * a.k;
-    const T *in = (const T *)a.in + t * a.in_stride;
-    for (int j = 0; j < a.k; ++j) {
-        const int p = a.place[t * a.k + j];
-        float dot = 0.0f;
-        if (p >= 0 && p < slots) {
-            const float w = a.weight[t * a.k + j];
-            for (int c = threadIdx.x; c < a.width; c += 64) {
-                const float g = (float)in[c];
-                dot = fmaf(g, (float)((const T *)a.y)[(int64_t)p * a.y_stride + c], dot);
-                ((T *)a.out)[(int64_t)p * a.out_stride + c] = (T)(w * g);
-            }
-            for (int o = 32; o; o >>= 1)
-                dot += __shfl_xor(dot, o);
+    constexpr int N = kChunk<T>;
+    const TokenLanes l(a);
+    const bool there = l.token < a.n_tokens;
+    const int64_t slots = a.n_tokens * a.k, token = there ? l.token : a.n_tokens - 1;
+    if (__ballot(there) == 0)
+        return;
+    for (int j0 = 0; j0 < a.k; j0 += kExchangeAhead) {
+        int p[kExchangeAhead];
+        float w[kExchangeAhead], dot[kExchangeAhead];
+#pragma unroll
+        for (int u = 0; u < kExchangeAhead; ++u) {
+            const int j = min(j0 + u, a.k - 1);
+            p[u] = a.place[token * a.k + j];
+            if (!there || j0 + u >= a.k || p[u] < 0 || p[u] >= slots)
+                p[u] = -1;
+            w[u] = a.weight[token * a.k + j];
+            dot[u] = 0.0f;
         }
-        if (threadIdx.x == 0)
-            a.d_weight[t * a.k + j] = dot;
+        for (int c = l.h * N; c < a.width; c += 64 * N) {
+            const int n = a.width - c;
+            float g[N], y[kExchangeAhead][N];
+            load_chunk<N>((const T *)a.in + token * a.in_stride + c, n, g);
+#pragma unroll
+            for (int u = 0; u < kExchangeAhead; ++u)
+                load_chunk<N>((const T *)a.y + (int64_t)max(p[u], 0) * a.y_stride + c, p[u] >= 0 ? n : 0, y[u]);
+#pragma unroll
+            for (int u = 0; u < kExchangeAhead; ++u) {
+                if (p[u] < 0)
+                    continue;
+                float d[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    dot[u] = fmaf(g[i], y[u][i], dot[u]);
+                    d[i] = w[u] * g[i];
+                }
+                store_chunk<N>((T *)a.out + (int64_t)p[u] * a.out_stride + c, n, d);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kExchangeAhead; ++u) {
+            const float all = row_sum(dot[u], a.ll);
+            if (there && l.h == 0 && j0 + u < a.k)
+                a.d_weight[token * a.k + j0 + u] = all;
+        }
     }
-    clear_slots_behind<T>(a, t, threadIdx.x);
+    if (there)
+        for (int c = l.h * N; c < a.width; c += 64 * N)
+            clear_slots_behind<T>(a, token, c, a.width - c);
+}
+
+// f(workgroups' columns) launches what one launch holds; a.ll and a.block0 are set.
+template <class F>
+void over_tokens(ExchangeArgs &a, int32_t type, F f)
+{
+    const int chunk = 16 / (int)type_bytes(type);
+    a.ll = row_lanes_log(a.width, chunk);
+    const int64_t tokens = (int64_t)kExchangeWaves << (6 - a.ll);
+    in_pieces((a.n_tokens + tokens - 1) / tokens, [&](int64_t at, unsigned blocks) {
+        a.block0 = at;
+        f(blocks, (unsigned)column_blocks(a.width, chunk));
+    });
 }
 
 static int check_experts(const char *who, int32_t n_experts)
@@ -170,10 +252,12 @@ extern "C" int fs_expert_gather(int64_t n_tokens, int32_t k, int32_t n_experts, 
     FS_TRY(check_array(who, "place", place, n_tokens, 4));
     if (n_tokens == 0)
         return FS_OK;
-    ExchangeArgs a = {n_tokens, x_stride, 0, xs_stride, k, n_experts, width, x, nullptr, first, place, nullptr, xs, nullptr};
+    ExchangeArgs a = {n_tokens, x_stride, 0, xs_stride, k, n_experts, width, 0, x, nullptr, first, place, nullptr, xs, nullptr, 0};
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
-        hipLaunchKernelGGL(expert_gather_kernel<decltype(t)::value>, dim3((unsigned)n_tokens), dim3(64), 0, stream, a);
+        over_tokens(a, type, [&](unsigned blocks, unsigned columns) {
+            hipLaunchKernelGGL(expert_gather_kernel<decltype(t)::value>, dim3(blocks, columns), dim3(kExchangeWaves * 64), 0, stream, a);
+        });
     });
     prof_stop(stream);
     return launched("expert gather kernel launch");
@@ -192,10 +276,12 @@ extern "C" int fs_expert_combine(int64_t n_tokens, int32_t k, int32_t width, con
     FS_TRY(check_array(who, "weight", weight, 0, 4));
     if (n_tokens == 0)
         return FS_OK;
-    ExchangeArgs a = {n_tokens, 0, y_stride, out_stride, k, 0, width, nullptr, y, nullptr, place, weight, out, nullptr};
+    ExchangeArgs a = {n_tokens, 0, y_stride, out_stride, k, 0, width, 0, nullptr, y, nullptr, place, weight, out, nullptr, 0};
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
-        hipLaunchKernelGGL(expert_combine_kernel<decltype(t)::value>, dim3((unsigned)n_tokens), dim3(64), 0, stream, a);
+        over_tokens(a, type, [&](unsigned blocks, unsigned columns) {
+            hipLaunchKernelGGL(expert_combine_kernel<decltype(t)::value>, dim3(blocks, columns), dim3(kExchangeWaves * 64), 0, stream, a);
+        });
     });
     prof_stop(stream);
     return launched("expert combine kernel launch");
@@ -219,10 +305,12 @@ extern "C" int fs_expert_combine_backward(int64_t n_tokens, int32_t k, int32_t n
     FS_TRY(check_array(who, "d_weight", d_weight, n_tokens, 4));
     if (n_tokens == 0)
         return FS_OK;
-    ExchangeArgs a = {n_tokens, d_out_stride, y_stride, d_y_stride, k, n_experts, width, d_out, y, first, place, weight, d_y, d_weight};
+    ExchangeArgs a = {n_tokens, d_out_stride, y_stride, d_y_stride, k, n_experts, width, 0, d_out, y, first, place, weight, d_y, d_weight, 0};
     prof_start(kKernTrainOther, stream);
     with_type(type, [&](auto t) {
-        hipLaunchKernelGGL(expert_combine_backward_kernel<decltype(t)::value>, dim3((unsigned)n_tokens), dim3(64), 0, stream, a);
+        over_tokens(a, type, [&](unsigned blocks, unsigned ) {
+            hipLaunchKernelGGL(expert_combine_backward_kernel<decltype(t)::value>, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
+        });
     });
     prof_stop(stream);
     return launched("expert combine gradient kernel launch");

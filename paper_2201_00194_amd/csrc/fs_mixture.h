@@ -182,6 +182,47 @@ __device__ __forceinline__ void store_chunk(T *p, int n, const float (&v)[N])
     }
 }
 
+// The same elements as they are.
+template <class T>
+struct RawChunk {
+    static constexpr int N = kChunk<T>;
+    T v[N];
+    __device__ __forceinline__ void load(const T *p, int n)
+    {
+        if (n >= N) {
+            const typename ChunkOf<T, N>::type c = *(const typename ChunkOf<T, N>::type *)p;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                v[i] = c[i];
+        } else if (n > 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                v[i] = p[i < n ? i : n - 1];
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = (T)0.0f;
+    }
+    __device__ __forceinline__ void store(T *p, int n) const
+    {
+        if (n >= N) {
+            typename ChunkOf<T, N>::type c;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                c[i] = v[i];
+            *(typename ChunkOf<T, N>::type *)p = c;
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < n)
+                    p[i] = v[i];
+        }
+    }
+};
+
 // The hardware's reciprocal, one step off at most.
 __device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }
 
