@@ -104,41 +104,87 @@ embed_kernel(EmbedArgs a)
     store_chunk<N>((Out *)a.out + row * a.out_stride + c, n, sum);
 }
 
-// ---- sorting by token: the first pass takes ids, the others what the pass before left -----------------------------------
+// ---- sorting by token, the lowest digit first: the first pass takes ids, the others what the pass before left ------------
 
 struct Pair {
     int32_t token, row;
 };
-struct DigitOfId {
+struct IdDigit {
+    typedef Pair Item;
     EmbedIds ids;
+    Pair *to;
     int32_t mask;
-    __device__ __forceinline__ int token(int64_t i) const
+    __device__ __forceinline__ Pair load(int64_t i) const
     {
-        const int v = ids.row(i, ids.n_cols == 1 ? 0 : (int)((uint32_t)i % (uint32_t)ids.n_cols));
-        return v < 0 ? ids.n_vocab : v;
+        const uint32_t row = ids.n_cols == 1 ? (uint32_t)i : (uint32_t)i / (uint32_t)ids.n_cols;
+        const int v = ids.row(i, (int)((uint32_t)i - row * (uint32_t)ids.n_cols));
+        return Pair{v < 0 ? ids.n_vocab : v, (int32_t)row};
     }
-    __device__ __forceinline__ int operator()(int64_t i) const { return token(i) & mask; }
+    __device__ __forceinline__ int number(const Pair &p) const { return p.token & mask; }
+    __device__ __forceinline__ void start(int, int) const {}
+    __device__ __forceinline__ void put(const Pair &p, int64_t, int, int slot) const { to[slot] = p; }
 };
-struct DigitOfPair {
+struct PairDigit {
+    typedef Pair Item;
     const Pair *from;
+    Pair *to;
     int32_t shift, mask;
-    __device__ __forceinline__ int operator()(int64_t i) const { return (from[i].token >> shift) & mask; }
-};
-struct PutId {
-    DigitOfId of;
-    Pair *to;
+    __device__ __forceinline__ Pair load(int64_t i) const { return from[i]; }
+    __device__ __forceinline__ int number(const Pair &p) const { return (p.token >> shift) & mask; }
     __device__ __forceinline__ void start(int, int) const {}
-    __device__ __forceinline__ void operator()(int64_t i, int, int slot) const
-    {
-        to[slot] = Pair{of.token(i), (int32_t)((uint32_t)i / (uint32_t)of.ids.n_cols)};
+    __device__ __forceinline__ void put(const Pair &p, int64_t, int, int slot) const { to[slot] = p; }
+};
+
+// All digits of up to kSlotFew entries in one workgroup.  LDS holds the tokens where the entries are and the entries' numbers
+// in the order so far, which a pass takes to registers and puts back.
+constexpr int kFewDigitBits = 9;
+__global__ void __launch_bounds__(kSlotFewWaves * 64)
+embed_sort_few_kernel(IdDigit source, int32_t n, int32_t bits)
+{
+    __shared__ int32_t token[kSlotFew], c[kSlotFewWaves << kFewDigitBits], wave_total[kSlotFewWaves];
+    __shared__ uint16_t order[kSlotFew];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int steps = (n + kSlotFewWaves * 64 - 1) / (kSlotFewWaves * 64);
+    const int begin = wave * steps * 64 + lane;
+#pragma unroll
+    for (int u = 0; u < kSlotFewPer; ++u) {
+        const int i = begin + u * 64;
+        if (u < steps && i < n) {
+            token[i] = source.load(i).token;
+            order[i] = (uint16_t)i;
+        }
     }
-};
-struct PutPair {
-    const Pair *from;
-    Pair *to;
-    __device__ __forceinline__ void start(int, int) const {}
-    __device__ __forceinline__ void operator()(int64_t i, int, int slot) const { to[slot] = from[i]; }
-};
+    const int passes = (bits + kFewDigitBits - 1) / kFewDigitBits, digit = (bits + passes - 1) / passes, buckets = 1 << digit;
+    for (int shift = 0; shift < bits; shift += digit) {
+        for (int b = threadIdx.x; b < kSlotFewWaves * buckets; b += kSlotFewWaves * 64)
+            c[b] = 0;
+        __syncthreads();
+        uint16_t mine[kSlotFewPer];
+        int number[kSlotFewPer];
+#pragma unroll
+        for (int u = 0; u < kSlotFewPer; ++u)
+            if (u < steps && begin + u * 64 < n) {
+                mine[u] = order[begin + u * 64];
+                number[u] = (token[mine[u]] >> shift) & (buckets - 1);
+                atomicAdd(&c[wave * buckets + number[u]], 1);
+            }
+        __syncthreads();
+        first_slots(c, buckets, wave_total, [](int, int) {});
+#pragma unroll
+        for (int u = 0; u < kSlotFewPer; ++u)
+            if (u < steps) {
+                const bool there = begin + u * 64 < n;
+                const int slot = take_slot(c + wave * buckets, there ? number[u] : 0, digit, there);
+                if (there)
+                    order[slot] = mine[u];
+            }
+        __syncthreads();
+    }
+    for (int s = threadIdx.x; s < n; s += kSlotFewWaves * 64) {
+        const int i = order[s];
+        source.to[s] = Pair{token[i], (int32_t)((uint32_t)i / (uint32_t)source.ids.n_cols)};
+    }
+}
 
 // ---- sums of the runs -----------------------------------------------------------------------------------------------------
 
@@ -283,7 +329,7 @@ static SumPlan sum_plan(int64_t n, int32_t width)
 }
 
 struct SortPlan {
-    int passes, bits;
+    int token_bits, passes, bits;      // of all digits, of one
     SlotShape shape;
     SumPlan sum;
     size_t list_bytes, token_bytes[2], sum_bytes[2], bytes;
@@ -294,6 +340,7 @@ static SortPlan sort_plan(int32_t n_vocab, int32_t width, int64_t n)
     int bits = 1;                                  // of 0 .. n_vocab
     while (((int64_t)1 << bits) <= n_vocab)
         ++bits;
+    p.token_bits = bits;
     p.passes = (bits + 9) / 10;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.shape = slot_shape(n, 1 << p.bits);
@@ -432,11 +479,15 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
         });
     if (n > 0) {
         const int mask = (1 << p.bits) - 1;
-        const DigitOfId of = {{ids, col_base, id_type, n_cols, n_vocab}, mask};
-        launch_slots(of, PutId{of, list[0]}, p.shape, count, stream);
+        const IdDigit of = {{ids, col_base, id_type, n_cols, n_vocab}, list[0], mask};
         int now = 0;
-        for (int pass = 1; pass < p.passes; ++pass, now ^= 1)
-            launch_slots(DigitOfPair{list[now], pass * p.bits, mask}, PutPair{list[now], list[now ^ 1]}, p.shape, count, stream);
+        if (n <= kSlotFew) {
+            hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n, p.token_bits);
+        } else {
+            launch_slots(of, p.shape, count, stream);
+            for (int pass = 1; pass < p.passes; ++pass, now ^= 1)
+                launch_slots(PairDigit{list[now], list[now ^ 1], pass * p.bits, mask}, p.shape, count, stream);
+        }
         SumArgs a = {list[now], nullptr, d_out, d_out_stride, d_table_stride, n, width, 0, p.sum.chunk, n_vocab, accumulate, scale, d_table,
                      token[0], sum[0], p.sum.stride};
         const auto grid_of = [&](int chunk_elements) {

@@ -3,20 +3,15 @@
 
 namespace fs {
 
-struct ChoiceNumber {
+struct Choices {
+    typedef int32_t Item;
     const int32_t *expert;
-    int32_t n_experts;
-    __device__ __forceinline__ int operator()(int64_t i) const
-    {
-        const int e = expert[i];
-        return e >= 0 && e < n_experts ? e : n_experts;
-    }
-};
-struct ChoicePut {
     int32_t *first, *order, *place;
     int32_t n_experts;
+    __device__ __forceinline__ int32_t load(int64_t i) const { return expert[i]; }
+    __device__ __forceinline__ int number(int32_t e) const { return e >= 0 && e < n_experts ? e : n_experts; }
     __device__ __forceinline__ void start(int e, int slot) const { first[e] = slot; }
-    __device__ __forceinline__ void operator()(int64_t i, int e, int slot) const
+    __device__ __forceinline__ void put(int32_t, int64_t i, int e, int slot) const
     {
         order[slot] = e < n_experts ? (int32_t)i : -1;
         place[i] = e < n_experts ? slot : -1;
@@ -36,7 +31,7 @@ constexpr int kExchangeAhead = 8;      // rows on their way at once
 
 struct ExchangeArgs {
     int64_t n_tokens, in_stride, y_stride, out_stride;
-    int32_t k, n_experts, width, ll;
+    int32_t k, n_experts, width, ll, columns;
     const void *in;                  // x, or the gradient of the tokens' results
     const void *y;
     const int32_t *first, *place;
@@ -45,15 +40,17 @@ struct ExchangeArgs {
     float *d_weight;
     int64_t block0;                  // of this launch
 };
-// Lanes (1 << ll) to a token.
+// Lanes (1 << ll) to a token; of a wide row, `columns` neighbouring wavefronts, so that they read a row at one time.
 struct TokenLanes {
-    int h;
+    int h, column;
     int64_t token;
     __device__ __forceinline__ explicit TokenLanes(const ExchangeArgs &a)
     {
         const int lane = threadIdx.x & 63;
         h = lane & ((1 << a.ll) - 1);
-        token = (((a.block0 + blockIdx.x) * kExchangeWaves + (threadIdx.x >> 6)) << (6 - a.ll)) + (lane >> a.ll);
+        const int64_t wave = (a.block0 + blockIdx.x) * kExchangeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        column = a.columns == 1 ? 0 : (int)(wave % a.columns);
+        token = a.columns == 1 ? (wave << (6 - a.ll)) + (lane >> a.ll) : wave / a.columns;
     }
 };
 
@@ -77,7 +74,7 @@ expert_gather_kernel(ExchangeArgs a)
     const TokenLanes l(a);
     if (l.token >= a.n_tokens)
         return;
-    const int c = ((int)blockIdx.y * 64 + l.h) * kChunk<T>, n = a.width - c;
+    const int c = (l.column * 64 + l.h) * kChunk<T>, n = a.width - c;
     const int64_t slots = a.n_tokens * a.k;
     RawChunk<T> x;
     x.load((const T *)a.in + l.token * a.in_stride + c, n);
@@ -99,7 +96,7 @@ expert_combine_kernel(ExchangeArgs a)
     const TokenLanes l(a);
     if (l.token >= a.n_tokens)
         return;
-    const int c = ((int)blockIdx.y * 64 + l.h) * N, n = a.width - c;
+    const int c = (l.column * 64 + l.h) * N, n = a.width - c;
     const int64_t slots = a.n_tokens * a.k;
     const T *const y = (const T *)a.y + c;
     float sum[N];
@@ -107,13 +104,14 @@ expert_combine_kernel(ExchangeArgs a)
     for (int i = 0; i < N; ++i)
         sum[i] = 0.0f;
     for (int j0 = 0; j0 < a.k; j0 += kExchangeAhead) {
-        float x[kExchangeAhead][N], w[kExchangeAhead];
+        RawChunk<T> x[kExchangeAhead];
+        float w[kExchangeAhead];
 #pragma unroll
         for (int u = 0; u < kExchangeAhead; ++u) {
             const int j = min(j0 + u, a.k - 1), p = a.place[l.token * a.k + j];
             const bool there = j0 + u < a.k && p >= 0 && p < slots;
             w[u] = !there ? 0.0f : a.weight ? a.weight[l.token * a.k + j] : 1.0f;
-            load_chunk<N>(y + (int64_t)(there ? p : 0) * a.y_stride, there ? n : 0, x[u]);
+            x[u].load(y + (int64_t)(there ? p : 0) * a.y_stride, there ? n : 0);
         }
 #pragma unroll
         for (int u = 0; u < kExchangeAhead; ++u)
@@ -150,11 +148,11 @@ expert_combine_backward_kernel(ExchangeArgs a)
         }
         for (int c = l.h * N; c < a.width; c += 64 * N) {
             const int n = a.width - c;
-            float g[N], y[kExchangeAhead][N];
-            load_chunk<N>((const T *)a.in + token * a.in_stride + c, n, g);
+            RawChunk<T> g, y[kExchangeAhead];
+            g.load((const T *)a.in + token * a.in_stride + c, n);
 #pragma unroll
             for (int u = 0; u < kExchangeAhead; ++u)
-                load_chunk<N>((const T *)a.y + (int64_t)max(p[u], 0) * a.y_stride + c, p[u] >= 0 ? n : 0, y[u]);
+                y[u].load((const T *)a.y + (int64_t)max(p[u], 0) * a.y_stride + c, p[u] >= 0 ? n : 0);
 #pragma unroll
             for (int u = 0; u < kExchangeAhead; ++u) {
                 if (p[u] < 0)
@@ -180,16 +178,17 @@ expert_combine_backward_kernel(ExchangeArgs a)
             clear_slots_behind<T>(a, token, c, a.width - c);
 }
 
-// f(workgroups' columns) launches what one launch holds; a.ll and a.block0 are set.
+// f(workgroups) launches what one launch holds; a's numbers of lanes, columns and workgroups are set.
 template <class F>
-void over_tokens(ExchangeArgs &a, int32_t type, F f)
+void over_tokens(ExchangeArgs &a, int32_t type, bool whole_rows, F f)
 {
     const int chunk = 16 / (int)type_bytes(type);
     a.ll = row_lanes_log(a.width, chunk);
-    const int64_t tokens = (int64_t)kExchangeWaves << (6 - a.ll);
-    in_pieces((a.n_tokens + tokens - 1) / tokens, [&](int64_t at, unsigned blocks) {
+    a.columns = whole_rows ? 1 : column_blocks(a.width, chunk);
+    const int64_t waves = (a.n_tokens * a.columns + ((int64_t)1 << (6 - a.ll)) - 1) >> (6 - a.ll);
+    in_pieces((waves + kExchangeWaves - 1) / kExchangeWaves, [&](int64_t at, unsigned blocks) {
         a.block0 = at;
-        f(blocks, (unsigned)column_blocks(a.width, chunk));
+        f(blocks);
     });
 }
 
@@ -230,8 +229,11 @@ extern "C" int fs_expert_plan(int64_t n_tokens, int32_t k, int32_t n_experts, co
         return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, need);
     int32_t *count = (int32_t *)work;
     prof_start(kKernPack, stream);
-    if (s.n > 0)
-        launch_slots(ChoiceNumber{expert, n_experts}, ChoicePut{first, order, place, n_experts}, s, count, stream);
+    const Choices choices = {expert, first, order, place, n_experts};
+    if (s.n > kSlotFew)
+        launch_slots(choices, s, count, stream);
+    else if (s.n > 0)
+        launch_few_slots(choices, s, stream);
     else
         hipLaunchKernelGGL(expert_none_kernel, dim3(1), dim3(256), 0, stream, n_experts, first);
     prof_stop(stream);
@@ -252,11 +254,11 @@ extern "C" int fs_expert_gather(int64_t n_tokens, int32_t k, int32_t n_experts, 
     FS_TRY(check_array(who, "place", place, n_tokens, 4));
     if (n_tokens == 0)
         return FS_OK;
-    ExchangeArgs a = {n_tokens, x_stride, 0, xs_stride, k, n_experts, width, 0, x, nullptr, first, place, nullptr, xs, nullptr, 0};
+    ExchangeArgs a = {n_tokens, x_stride, 0, xs_stride, k, n_experts, width, 0, 1, x, nullptr, first, place, nullptr, xs, nullptr, 0};
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
-        over_tokens(a, type, [&](unsigned blocks, unsigned columns) {
-            hipLaunchKernelGGL(expert_gather_kernel<decltype(t)::value>, dim3(blocks, columns), dim3(kExchangeWaves * 64), 0, stream, a);
+        over_tokens(a, type, false, [&](unsigned blocks) {
+            hipLaunchKernelGGL(expert_gather_kernel<decltype(t)::value>, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
         });
     });
     prof_stop(stream);
@@ -276,11 +278,11 @@ extern "C" int fs_expert_combine(int64_t n_tokens, int32_t k, int32_t width, con
     FS_TRY(check_array(who, "weight", weight, 0, 4));
     if (n_tokens == 0)
         return FS_OK;
-    ExchangeArgs a = {n_tokens, 0, y_stride, out_stride, k, 0, width, 0, nullptr, y, nullptr, place, weight, out, nullptr, 0};
+    ExchangeArgs a = {n_tokens, 0, y_stride, out_stride, k, 0, width, 0, 1, nullptr, y, nullptr, place, weight, out, nullptr, 0};
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
-        over_tokens(a, type, [&](unsigned blocks, unsigned columns) {
-            hipLaunchKernelGGL(expert_combine_kernel<decltype(t)::value>, dim3(blocks, columns), dim3(kExchangeWaves * 64), 0, stream, a);
+        over_tokens(a, type, false, [&](unsigned blocks) {
+            hipLaunchKernelGGL(expert_combine_kernel<decltype(t)::value>, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
         });
     });
     prof_stop(stream);
@@ -305,10 +307,10 @@ extern "C" int fs_expert_combine_backward(int64_t n_tokens, int32_t k, int32_t n
     FS_TRY(check_array(who, "d_weight", d_weight, n_tokens, 4));
     if (n_tokens == 0)
         return FS_OK;
-    ExchangeArgs a = {n_tokens, d_out_stride, y_stride, d_y_stride, k, n_experts, width, 0, d_out, y, first, place, weight, d_y, d_weight, 0};
+    ExchangeArgs a = {n_tokens, d_out_stride, y_stride, d_y_stride, k, n_experts, width, 0, 1, d_out, y, first, place, weight, d_y, d_weight, 0};
     prof_start(kKernTrainOther, stream);
     with_type(type, [&](auto t) {
-        over_tokens(a, type, [&](unsigned blocks, unsigned ) {
+        over_tokens(a, type, true, [&](unsigned blocks) {
             hipLaunchKernelGGL(expert_combine_backward_kernel<decltype(t)::value>, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
         });
     });

@@ -182,43 +182,43 @@ __device__ __forceinline__ void store_chunk(T *p, int n, const float (&v)[N])
     }
 }
 
-// The same elements as they are.
+// The same elements as they are: a quarter or half of the registers of load_chunk's, for what is on its way for long.
 template <class T>
 struct RawChunk {
     static constexpr int N = kChunk<T>;
-    T v[N];
+    typedef typename ChunkOf<T, N>::type Chunk;
+    Chunk c;
     __device__ __forceinline__ void load(const T *p, int n)
     {
         if (n >= N) {
-            const typename ChunkOf<T, N>::type c = *(const typename ChunkOf<T, N>::type *)p;
+            c = *(const Chunk *)p;
+        } else {
+            clear();
+            if (n > 0) {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                v[i] = c[i];
-        } else if (n > 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                v[i] = p[i < n ? i : n - 1];
+                for (int i = 0; i < N; ++i) {
+                    const T v = p[i < n ? i : n - 1];
+                    c[i] = i < n ? v : (T)0.0f;
+                }
+            }
         }
     }
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            v[i] = (T)0.0f;
+            c[i] = (T)0.0f;
     }
+    __device__ __forceinline__ float operator[](int i) const { return (float)c[i]; }
     __device__ __forceinline__ void store(T *p, int n) const
     {
         if (n >= N) {
-            typename ChunkOf<T, N>::type c;
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                c[i] = v[i];
-            *(typename ChunkOf<T, N>::type *)p = c;
+            *(Chunk *)p = c;
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (i < n)
-                    p[i] = v[i];
+                    p[i] = c[i];
         }
     }
 };

@@ -1,6 +1,10 @@
-// A stable counting sort of n entries by a number below `buckets`, in three kernels: every wavefront counts the numbers in
-// its stretch of entries; a number's counts are summed along the stretches; every wavefront places its stretch's entries.
-// No atomics on memory, and the same result whatever runs first.  Used for the slots of experts and for the table's gradient.
+// A stable counting sort of n entries by a number below `buckets`.  Long lists take three kernels: every wavefront counts the
+// numbers in its stretch of entries; a number's counts are summed along the stretches; every wavefront places its stretch's
+// entries.  Up to kSlotFew entries are one workgroup's, in one kernel.  No atomics on memory, and the same result
+// whatever runs first.  Used for the slots of experts and for the table's gradient.
+//
+// A Source says what the entries are: Item load(i), int number(item), put(item, i, number, slot), and start(number, slot of its
+// first), called once for every number.
 #ifndef FS_SLOTS_H
 #define FS_SLOTS_H
 
@@ -13,21 +17,31 @@ constexpr int kSlotMostBuckets = 1025;      // experts, and one for choices with
 constexpr int kSlotMostStretches = 4096;
 constexpr int kSlotScanThreads = 256;
 constexpr int kSlotScanPer = kSlotMostStretches / kSlotScanThreads;
+constexpr int kSlotAhead = 8;               // loads of a lane on their way at once
+constexpr int kSlotFew = 16384;
+constexpr int kSlotFewWaves = 16;
+constexpr int kSlotFewPer = kSlotFew / (kSlotFewWaves * 64);
 
 struct SlotShape {
     int32_t n, buckets, stretch, stretches;
 };
+// Stretches as short as 128 entries, for as many wavefronts, but not shorter than the numbers are many: the counts then
+// are no more than the entries.
 inline SlotShape slot_shape(int64_t n, int buckets)
 {
-    SlotShape s = {(int32_t)n, buckets, 1024, 0};
-    const int64_t least = (n + kSlotMostStretches - 1) / kSlotMostStretches;
-    if (least > s.stretch)
-        s.stretch = (int32_t)((least + 63) / 64 * 64);
+    SlotShape s = {(int32_t)n, buckets, 0, 0};
+    int64_t stretch = (n + kSlotMostStretches - 1) / kSlotMostStretches;
+    stretch = stretch < buckets ? buckets : stretch;
+    stretch = stretch < 128 ? 128 : stretch;
+    s.stretch = (int32_t)((stretch + 63) / 64 * 64);
     s.stretches = (int32_t)((n + s.stretch - 1) / s.stretch);
     return s;
 }
 // The counts, and behind them every number's total.
-inline size_t slot_count_bytes(const SlotShape &s) { return s.n == 0 ? 0 : ((size_t)s.buckets * (s.stretches + 1) * 4 + 255) / 256 * 256; }
+inline size_t slot_count_bytes(const SlotShape &s)
+{
+    return s.n <= kSlotFew ? 0 : ((size_t)s.buckets * (s.stretches + 1) * 4 + 255) / 256 * 256;
+}
 
 // The lanes whose number is this lane's, among the lanes that are there.
 __device__ __forceinline__ uint64_t same_number(int number, int bits, bool there)
@@ -47,27 +61,23 @@ __host__ __device__ inline int bits_of(int n)        // of numbers below n
         ++b;
     return b;
 }
-
-// count[number * stretches + stretch]
-template <class Number>
-__global__ void __launch_bounds__(kSlotWaves * 64)
-slot_count_kernel(Number number, SlotShape s, int32_t *count)
+__device__ __forceinline__ int lanes_before(uint64_t lanes)
 {
-    __shared__ int32_t lds[kSlotWaves * kSlotMostBuckets];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int mine = (int)blockIdx.x * kSlotWaves + wave;
-    int32_t *c = lds + wave * s.buckets;
-    for (int b = lane; b < s.buckets; b += 64)
-        c[b] = 0;
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
+}
+// The slot of this lane's number: next[number] and up, in the order of the lanes; next moves on.
+__device__ __forceinline__ int take_slot(int32_t *next, int number, int bits, bool there)
+{
+    const uint64_t same = same_number(number, bits, there);
+    const int before = lanes_before(same);
+    int slot = 0;
+    if (there)
+        slot = next[number] + before;
     lds_sync();
-    if (mine >= s.stretches)
-        return;
-    const int64_t begin = (int64_t)mine * s.stretch, end = min(begin + s.stretch, (int64_t)s.n);
-    for (int64_t i = begin + lane; i < end; i += 64)
-        atomicAdd(&c[number(i)], 1);
+    if (there && before == 0)
+        next[number] = slot + __popcll(same);
     lds_sync();
-    for (int b = lane; b < s.buckets; b += 64)
-        count[(int64_t)b * s.stretches + mine] = c[b];
+    return slot;
 }
 
 __device__ __forceinline__ int32_t wave_inclusive_sum(int32_t v, int lane)
@@ -79,6 +89,38 @@ __device__ __forceinline__ int32_t wave_inclusive_sum(int32_t v, int lane)
             v += t;
     }
     return v;
+}
+
+// count[number * stretches + stretch]
+template <class Source>
+__global__ void __launch_bounds__(kSlotWaves * 64)
+slot_count_kernel(Source source, SlotShape s, int32_t *count)
+{
+    __shared__ int32_t lds[kSlotWaves * kSlotMostBuckets];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int mine = (int)blockIdx.x * kSlotWaves + wave;
+    int32_t *c = lds + wave * s.buckets;
+    for (int b = lane; b < s.buckets; b += 64)
+        c[b] = 0;
+    lds_sync();
+    if (mine >= s.stretches)
+        return;
+    const int64_t begin = (int64_t)mine * s.stretch, end = min(begin + s.stretch, (int64_t)s.n);
+    for (int64_t i0 = begin; i0 < end; i0 += kSlotAhead * 64) {
+        int number[kSlotAhead];
+#pragma unroll
+        for (int u = 0; u < kSlotAhead; ++u) {
+            const int64_t i = i0 + u * 64 + lane;
+            number[u] = i < end ? source.number(source.load(i)) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kSlotAhead; ++u)
+            if (number[u] >= 0)
+                atomicAdd(&c[number[u]], 1);
+    }
+    lds_sync();
+    for (int b = lane; b < s.buckets; b += 64)
+        count[(int64_t)b * s.stretches + mine] = c[b];
 }
 
 // A workgroup a number: its counts become the sums of those before them, and their total goes behind all counts.
@@ -115,10 +157,9 @@ slot_scan_kernel(int32_t *count, SlotShape s)
         count[(int64_t)s.buckets * s.stretches + blockIdx.x] = total;
 }
 
-// put(i, number, slot) for every entry; put.start(number, slot of its first), once for every number.
-template <class Number, class Put>
+template <class Source>
 __global__ void __launch_bounds__(kSlotWaves * 64)
-slot_place_kernel(Number number, Put put, SlotShape s, const int32_t *count)
+slot_place_kernel(Source source, SlotShape s, const int32_t *count)
 {
     constexpr int kThreads = kSlotWaves * 64, kPer = (kSlotMostBuckets + kThreads - 1) / kThreads;
     __shared__ int32_t lds[kSlotWaves * kSlotMostBuckets], base[kSlotMostBuckets], wave_total[kSlotWaves];
@@ -145,7 +186,7 @@ slot_place_kernel(Number number, Put put, SlotShape s, const int32_t *count)
         if (first + i < s.buckets) {
             base[first + i] = at;
             if (blockIdx.x == 0)
-                put.start(first + i, at);
+                source.start(first + i, at);
         }
         at += v[i];
     }
@@ -158,31 +199,106 @@ slot_place_kernel(Number number, Put put, SlotShape s, const int32_t *count)
     lds_sync();
     const int bits = bits_of(s.buckets);
     const int64_t begin = (int64_t)mine * s.stretch, end = min(begin + s.stretch, (int64_t)s.n);
-    for (int64_t i0 = begin; i0 < end; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const bool there = i < end;
-        const int m = there ? number(i) : 0;
-        const uint64_t same = same_number(m, bits, there);
-        const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
-        int slot = 0;
-        if (there)
-            slot = next[m] + before;
-        lds_sync();
-        if (there && before == 0)
-            next[m] = slot + __popcll(same);
-        lds_sync();
-        if (there)
-            put(i, m, slot);
+    for (int64_t i0 = begin; i0 < end; i0 += kSlotAhead * 64) {
+        typename Source::Item item[kSlotAhead];
+#pragma unroll
+        for (int u = 0; u < kSlotAhead; ++u)
+            item[u] = source.load(min(i0 + u * 64 + lane, end - 1));
+#pragma unroll
+        for (int u = 0; u < kSlotAhead; ++u) {
+            const int64_t i = i0 + u * 64 + lane;
+            if (i0 + u * 64 < end) {
+                const int number = source.number(item[u]);
+                const int slot = take_slot(next, number, bits, i < end);
+                if (i < end)
+                    source.put(item[u], i, number, slot);
+            }
+        }
     }
 }
 
-template <class Number, class Put>
-void launch_slots(const Number &number, const Put &put, const SlotShape &s, int32_t *count, hipStream_t stream)
+// ---- few entries: one workgroup ----------------------------------------------------------------------------------------
+
+// Sixteen wavefronts' counts (c[wave * buckets + number]) become every wavefront's first slot of a number; start(number, slot).
+// All threads of the workgroup call it, after a barrier; it ends with one.
+template <class F>
+__device__ __forceinline__ void first_slots(int32_t *c, int buckets, int32_t *wave_total, F start)
+{
+    constexpr int kThreads = kSlotFewWaves * 64, kPer = (kSlotMostBuckets + kThreads - 1) / kThreads;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int per = (buckets + kThreads - 1) / kThreads, first = threadIdx.x * per;      // 1 or 2 numbers a thread
+    int32_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (i < per && first + i < buckets)
+            for (int w = 0; w < kSlotFewWaves; ++w)
+                sum += c[w * buckets + first + i];
+    const int32_t upto = wave_inclusive_sum(sum, lane);
+    if (lane == 63)
+        wave_total[wave] = upto;
+    __syncthreads();
+    int32_t at = upto - sum;
+    for (int w = 0; w < wave; ++w)
+        at += wave_total[w];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (i < per && first + i < buckets) {
+            start(first + i, at);
+            for (int w = 0; w < kSlotFewWaves; ++w) {
+                const int32_t n = c[w * buckets + first + i];
+                c[w * buckets + first + i] = at;
+                at += n;
+            }
+        }
+    __syncthreads();
+}
+
+template <class Source>
+__global__ void __launch_bounds__(kSlotFewWaves * 64)
+slot_few_kernel(Source source, int32_t n, int32_t buckets)
+{
+    __shared__ int32_t c[kSlotFewWaves * kSlotMostBuckets], wave_total[kSlotFewWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int steps = (n + kSlotFewWaves * 64 - 1) / (kSlotFewWaves * 64);       // of a wavefront, at most kSlotFewPer
+    const int begin = wave * steps * 64 + lane;
+    typename Source::Item item[kSlotFewPer];
+#pragma unroll
+    for (int u = 0; u < kSlotFewPer; ++u)
+        if (u < steps)
+            item[u] = source.load(min(begin + u * 64, n - 1));
+    for (int b = threadIdx.x; b < kSlotFewWaves * buckets; b += kSlotFewWaves * 64)
+        c[b] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSlotFewPer; ++u)
+        if (u < steps && begin + u * 64 < n)
+            atomicAdd(&c[wave * buckets + source.number(item[u])], 1);
+    __syncthreads();
+    first_slots(c, buckets, wave_total, [&](int number, int slot) { source.start(number, slot); });
+    const int bits = bits_of(buckets);
+#pragma unroll
+    for (int u = 0; u < kSlotFewPer; ++u)
+        if (u < steps) {
+            const bool there = begin + u * 64 < n;
+            const int number = source.number(item[u]);
+            const int slot = take_slot(c + wave * buckets, number, bits, there);
+            if (there)
+                source.put(item[u], begin + u * 64, number, slot);
+        }
+}
+
+template <class Source>
+void launch_few_slots(const Source &source, const SlotShape &s, hipStream_t stream)
+{
+    hipLaunchKernelGGL(slot_few_kernel<Source>, dim3(1), dim3(kSlotFewWaves * 64), 0, stream, source, s.n, s.buckets);
+}
+template <class Source>
+void launch_slots(const Source &source, const SlotShape &s, int32_t *count, hipStream_t stream)
 {
     const dim3 grid((unsigned)((s.stretches + kSlotWaves - 1) / kSlotWaves)), block(kSlotWaves * 64);
-    hipLaunchKernelGGL(slot_count_kernel<Number>, grid, block, 0, stream, number, s, count);
+    hipLaunchKernelGGL(slot_count_kernel<Source>, grid, block, 0, stream, source, s, count);
     hipLaunchKernelGGL(slot_scan_kernel, dim3((unsigned)s.buckets), dim3(kSlotScanThreads), 0, stream, count, s);
-    hipLaunchKernelGGL((slot_place_kernel<Number, Put>), grid, block, 0, stream, number, put, s, (const int32_t *)count);
+    hipLaunchKernelGGL(slot_place_kernel<Source>, grid, block, 0, stream, source, s, (const int32_t *)count);
 }
 
 }  // namespace fs

@@ -48,7 +48,7 @@ int main(void) {
     if (fs_route(&p, 1, x, FS_F32, 8, NULL, NULL, NULL, NULL) != FS_EINVAL) return 1;
     if (strlen(fs_last_error()) == 0) return 2;
     if (fs_expert_plan_workspace_bytes(-1, 1, 1) != 0) return 3;
-    if (fs_expert_plan_workspace_bytes(100, 2, 8) == 0) return 4;
+    if (fs_expert_plan_workspace_bytes(100000, 2, 8) == 0) return 4;
     if (fs_embed_backward_workspace_bytes(100, 8, 10, 2) == 0) return 5;
     printf("ok %d\n", FS_MAX_EXPERTS);
     return 0;
@@ -114,7 +114,7 @@ def test_route_backward_refuses_bad_arguments(api, at, value, word):
     (2, 1025, EUNSUPPORTED, "n_experts"), (3, None, EINVAL, "expert"), (4, None, EINVAL, "first"), (5, None, EINVAL, "order"),
     (6, None, EINVAL, "place"), (7, None, EINVAL, "work"), (7, ctypes.c_void_p(4100), EINVAL, "work"), (8, 0, EINVAL, "working memory")])
 def test_plan_refuses_bad_arguments(api, at, value, code, word):
-    args = [1000, 2, 8, P, P, P, P, P, 1 << 30, None]
+    args = [100000, 2, 8, P, P, P, P, P, 1 << 30, None]
     args[at] = value
     refused(api, code, word, api._lib.fs_expert_plan(*args))
 
