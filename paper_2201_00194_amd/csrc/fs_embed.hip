@@ -15,38 +15,82 @@ namespace fs {
 constexpr int kEmbedWaves = 4;            // of a workgroup
 constexpr int kEmbedAhead = 8;            // rows on their way at once
 constexpr int kEmbedFewWaves = 2048;
+constexpr int kLookupRows = 4;            // rows of a lane
 constexpr int kSumMostChunk = 256, kSumLeastChunk = 16;   // pairs a chunk
 constexpr int kSumNextChunk = 64;                         // partial sums a chunk
+
+template <int ID> struct IdOf;
+template <> struct IdOf<FS_ID_I32> { typedef int32_t type; };
+template <> struct IdOf<FS_ID_I64> { typedef int64_t type; };
+template <> struct IdOf<FS_ID_U16> { typedef uint16_t type; };
+template <class F>
+void with_id_type(int32_t type, F f)
+{
+    if (type == FS_ID_I32)
+        f(TypeTag<FS_ID_I32>());
+    else if (type == FS_ID_I64)
+        f(TypeTag<FS_ID_I64>());
+    else
+        f(TypeTag<FS_ID_U16>());
+}
 
 struct EmbedIds {
     const void *ids;
     const int32_t *col_base;
-    int32_t id_type, n_cols, n_vocab;
-    // The table's row that entry i, of column c, names, or -1.
-    __device__ __forceinline__ int row(int64_t i, int c) const
+    int32_t n_cols, n_vocab;
+    uint32_t magic, shift;       // i / n_cols = (i * magic >> 32) >> shift for i < 2^31, n_cols > 1
+    // The table's rows that N entries name, or -1.  All ids are on their way before the first is looked at.
+    template <int ID, int N, class Entry, class Column>
+    __device__ __forceinline__ void rows(int (&row)[N], Entry entry, Column column) const
     {
-        int64_t v = id_type == FS_ID_I32 ? (int64_t)((const int32_t *)ids)[i]
-                    : id_type == FS_ID_I64 ? ((const int64_t *)ids)[i]
-                                           : (int64_t)((const uint16_t *)ids)[i];
-        if (v < -2147483648ll || v > 2147483647ll)
-            return -1;
+        typename IdOf<ID>::type id[N];
+        int32_t base[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            id[u] = ((const typename IdOf<ID>::type *)ids)[entry(u)];
+            base[u] = 0;
+        }
         if (col_base)
-            v += col_base[c];
-        return v >= 0 && v < n_vocab ? (int)v : -1;
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+                base[u] = col_base[column(u)];
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            int64_t v = (int64_t)id[u];
+            bool fits = true;
+            if constexpr (ID == FS_ID_I64)
+                fits = v == (int64_t)(int32_t)v;
+            v = (int64_t)(int32_t)v + base[u];
+            row[u] = fits && v >= 0 && v < n_vocab ? (int)v : -1;
+        }
     }
+    __device__ __forceinline__ uint32_t row_of(uint32_t i) const { return n_cols == 1 ? i : __umulhi(i, magic) >> shift; }
 };
+// n_cols = d > 1, s the bits of d - 1: magic = floor(2^(31 + s) / d) + 1 is i / d times 2^(31 + s) with an error that stays below
+// 1 / d for i < 2^31.
+static EmbedIds embed_ids(const void *ids, const int32_t *col_base, int32_t n_cols, int32_t n_vocab)
+{
+    EmbedIds e = {ids, col_base, n_cols, n_vocab, 0, 0};
+    if (n_cols > 1) {
+        const int s = bits_of(n_cols);
+        e.magic = (uint32_t)((((uint64_t)1 << (31 + s)) / (uint32_t)n_cols) + 1);
+        e.shift = (uint32_t)(s - 1);
+    }
+    return e;
+}
 
 struct EmbedArgs {
     EmbedIds ids;
     const void *in;            // the table
     int64_t in_stride, out_stride, n_rows;
-    int32_t width, ll, split;  // a row of the result in 1 << (ll + split) lanes, the bag in 1 << split parts
+    int32_t width, ll, split;  // a row of the result in 1 << (ll + split) lanes, the bag in 1 << split parts;
+    int32_t columns;           // of a wide row, `columns` neighbouring wavefronts
     float scale;
     void *out;
     int64_t block0;            // of this launch
 };
 
-template <int IN, int OUT>
+template <int IN, int OUT, int ID>
 __global__ void __launch_bounds__(kEmbedWaves * 64)
 embed_kernel(EmbedArgs a)
 {
@@ -54,12 +98,13 @@ embed_kernel(EmbedArgs a)
     typedef typename Element<OUT>::type Out;
     constexpr int N = kChunk<In>;
     const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1), part = (lane >> ll) & ((1 << a.split) - 1);
-    const int64_t row0 = ((a.block0 + blockIdx.x) * kEmbedWaves + (threadIdx.x >> 6)) << (6 - ll - a.split);
+    const int64_t wave = (a.block0 + blockIdx.x) * kEmbedWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row0 = a.columns == 1 ? wave << (6 - ll - a.split) : wave / a.columns;
     if (row0 >= a.n_rows)
         return;
     const bool there = row0 + (lane >> (ll + a.split)) < a.n_rows;
     const int64_t row = there ? row0 + (lane >> (ll + a.split)) : a.n_rows - 1;
-    const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
+    const int c = ((a.columns == 1 ? 0 : (int)(wave % a.columns)) * 64 + h) * N, n = a.width - c;
     const int cols = a.ids.n_cols, per = (cols + (1 << a.split) - 1) >> a.split;
     const int begin = min(part * per, cols), end = min(begin + per, cols);
     const In *const in = (const In *)a.in + c;
@@ -70,22 +115,23 @@ embed_kernel(EmbedArgs a)
     for (int j0 = 0; j0 < per; j0 += kEmbedAhead) {          // the same number of times in all lanes
         int v[kEmbedAhead];
         if (ll >= 3) {                                       // eight lanes fetch an id each
-            const int j = begin + j0 + (h & 7);
-            const int id = j < end ? a.ids.row(row * cols + j, j) : -1;
+            int id[1];
+            const int j = min(begin + j0 + (h & 7), cols - 1);
+            a.ids.template rows<ID>(id, [&](int) { return row * cols + j; }, [&](int) { return j; });
 #pragma unroll
             for (int u = 0; u < kEmbedAhead; ++u)
-                v[u] = __shfl(id, (lane & ~7) + u);
+                v[u] = __shfl(id[0], (lane & ~7) + u);
         } else {
-#pragma unroll
-            for (int u = 0; u < kEmbedAhead; ++u) {
-                const int j = begin + j0 + u;
-                v[u] = j < end ? a.ids.row(row * cols + j, j) : -1;
-            }
+            const auto j = [&](int u) { return min(begin + j0 + u, cols - 1); };
+            a.ids.template rows<ID>(v, [&](int u) { return row * cols + j(u); }, j);
         }
-        float x[kEmbedAhead][N];
 #pragma unroll
         for (int u = 0; u < kEmbedAhead; ++u)
-            load_chunk<N>(in + (int64_t)max(v[u], 0) * a.in_stride, v[u] >= 0 ? n : 0, x[u]);
+            v[u] = begin + j0 + u < end ? v[u] : -1;
+        RawChunk<In> x[kEmbedAhead];
+#pragma unroll
+        for (int u = 0; u < kEmbedAhead; ++u)
+            x[u].load(in + (int64_t)max(v[u], 0) * a.in_stride, v[u] >= 0 ? n : 0);
 #pragma unroll
         for (int u = 0; u < kEmbedAhead; ++u)
 #pragma unroll
@@ -104,21 +150,58 @@ embed_kernel(EmbedArgs a)
     store_chunk<N>((Out *)a.out + row * a.out_stride + c, n, sum);
 }
 
+// One id a row: kLookupRows of them a lane.
+template <int IN, int OUT, int ID>
+__global__ void __launch_bounds__(kEmbedWaves * 64)
+embed_lookup_kernel(EmbedArgs a)
+{
+    typedef typename Element<IN>::type In;
+    typedef typename Element<OUT>::type Out;
+    constexpr int N = kChunk<In>;
+    const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
+    const int64_t wave = (a.block0 + blockIdx.x) * kEmbedWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row0 = ((a.columns == 1 ? wave : wave / a.columns) * kLookupRows) << (6 - ll);
+    if (row0 >= a.n_rows)
+        return;
+    const int c = ((a.columns == 1 ? 0 : (int)(wave % a.columns)) * 64 + h) * N, n = a.width - c;
+    const In *const in = (const In *)a.in + c;
+    const auto row = [&](int u) { return row0 + (u << (6 - ll)) + (lane >> ll); };
+    int v[kLookupRows];
+    a.ids.template rows<ID>(v, [&](int u) { return min(row(u), a.n_rows - 1); }, [](int) { return 0; });
+    RawChunk<In> x[kLookupRows];
+#pragma unroll
+    for (int u = 0; u < kLookupRows; ++u)
+        x[u].load(in + (int64_t)max(v[u], 0) * a.in_stride, v[u] >= 0 ? n : 0);
+#pragma unroll
+    for (int u = 0; u < kLookupRows; ++u) {
+        float y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            y[i] = x[u][i] * a.scale;
+        store_chunk<N>((Out *)a.out + row(u) * a.out_stride + c, row(u) < a.n_rows ? n : 0, y);
+    }
+}
+
 // ---- sorting by token, the lowest digit first: the first pass takes ids, the others what the pass before left ------------
 
 struct Pair {
     int32_t token, row;
 };
+template <int ID>
 struct IdDigit {
     typedef Pair Item;
     EmbedIds ids;
     Pair *to;
     int32_t mask;
-    __device__ __forceinline__ Pair load(int64_t i) const
+    template <int N>
+    __device__ __forceinline__ void load(Pair (&item)[N], int64_t i, int64_t end) const
     {
-        const uint32_t row = ids.n_cols == 1 ? (uint32_t)i : (uint32_t)i / (uint32_t)ids.n_cols;
-        const int v = ids.row(i, (int)((uint32_t)i - row * (uint32_t)ids.n_cols));
-        return Pair{v < 0 ? ids.n_vocab : v, (int32_t)row};
+        int row[N];
+        const auto entry = [&](int u) { return (uint32_t)min(i + u * 64, end - 1); };
+        ids.template rows<ID>(row, entry, [&](int u) { return entry(u) - ids.row_of(entry(u)) * (uint32_t)ids.n_cols; });
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            item[u] = Pair{row[u] < 0 ? ids.n_vocab : row[u], (int32_t)ids.row_of(entry(u))};
     }
     __device__ __forceinline__ int number(const Pair &p) const { return p.token & mask; }
     __device__ __forceinline__ void start(int, int) const {}
@@ -129,7 +212,13 @@ struct PairDigit {
     const Pair *from;
     Pair *to;
     int32_t shift, mask;
-    __device__ __forceinline__ Pair load(int64_t i) const { return from[i]; }
+    template <int N>
+    __device__ __forceinline__ void load(Pair (&item)[N], int64_t i, int64_t end) const
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            item[u] = from[min(i + u * 64, end - 1)];
+    }
     __device__ __forceinline__ int number(const Pair &p) const { return (p.token >> shift) & mask; }
     __device__ __forceinline__ void start(int, int) const {}
     __device__ __forceinline__ void put(const Pair &p, int64_t, int, int slot) const { to[slot] = p; }
@@ -138,19 +227,22 @@ struct PairDigit {
 // All digits of up to kSlotFew entries in one workgroup.  LDS holds the tokens where the entries are and the entries' numbers
 // in the order so far, which a pass takes to registers and puts back.
 constexpr int kFewDigitBits = 9;
+template <int ID>
 __global__ void __launch_bounds__(kSlotFewWaves * 64)
-embed_sort_few_kernel(IdDigit source, int32_t n, int32_t bits)
+embed_sort_few_kernel(IdDigit<ID> source, int32_t n, int32_t bits)
 {
     __shared__ int32_t token[kSlotFew], c[kSlotFewWaves << kFewDigitBits], wave_total[kSlotFewWaves];
     __shared__ uint16_t order[kSlotFew];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int steps = (n + kSlotFewWaves * 64 - 1) / (kSlotFewWaves * 64);
     const int begin = wave * steps * 64 + lane;
+    Pair item[kSlotFewPer];
+    source.load(item, begin, n);
 #pragma unroll
     for (int u = 0; u < kSlotFewPer; ++u) {
         const int i = begin + u * 64;
         if (u < steps && i < n) {
-            token[i] = source.load(i).token;
+            token[i] = item[u].token;
             order[i] = (uint16_t)i;
         }
     }
@@ -182,7 +274,7 @@ embed_sort_few_kernel(IdDigit source, int32_t n, int32_t bits)
     }
     for (int s = threadIdx.x; s < n; s += kSlotFewWaves * 64) {
         const int i = order[s];
-        source.to[s] = Pair{token[i], (int32_t)((uint32_t)i / (uint32_t)source.ids.n_cols)};
+        source.to[s] = Pair{token[i], (int32_t)source.ids.row_of((uint32_t)i)};
     }
 }
 
@@ -414,13 +506,20 @@ extern "C" int fs_embed(int32_t n_vocab, int32_t width, const void *table, int32
     int split = 0;                 // a long bag of few rows: its parts in neighbouring lanes, down to four ids each
     while (split < 6 - ll && (n_cols >> (split + 1)) >= 4 && (((n_rows * blocks) << (ll + split)) >> 6) < kEmbedFewWaves)
         ++split;
-    EmbedArgs a = {{ids, col_base, id_type, n_cols, n_vocab}, table, table_stride, out_stride, n_rows, width, ll, split, scale, out, 0};
-    const int64_t rows = (int64_t)kEmbedWaves << (6 - ll - split);
+    EmbedArgs a = {embed_ids(ids, col_base, n_cols, n_vocab), table, table_stride, out_stride, n_rows, width, ll, split, blocks, scale, out, 0};
+    const int64_t rows = ((int64_t)(n_cols == 1 ? kLookupRows : 1)) << (6 - ll - split);       // of a wavefront
+    const int64_t waves = (n_rows + rows - 1) / rows * blocks;
     prof_start(kKernPack, stream);
     with_types(table_type, out_type, [&](auto i, auto o) {
-        in_pieces((n_rows + rows - 1) / rows, [&](int64_t at, unsigned n) {
-            a.block0 = at;
-            hipLaunchKernelGGL((embed_kernel<decltype(i)::value, decltype(o)::value>), dim3(n, (unsigned)blocks), dim3(kEmbedWaves * 64), 0, stream, a);
+        with_id_type(id_type, [&](auto d) {
+            constexpr int in = decltype(i)::value, to = decltype(o)::value, id = decltype(d)::value;
+            in_pieces((waves + kEmbedWaves - 1) / kEmbedWaves, [&](int64_t at, unsigned n) {
+                a.block0 = at;
+                if (n_cols == 1)
+                    hipLaunchKernelGGL((embed_lookup_kernel<in, to, id>), dim3(n), dim3(kEmbedWaves * 64), 0, stream, a);
+                else
+                    hipLaunchKernelGGL((embed_kernel<in, to, id>), dim3(n), dim3(kEmbedWaves * 64), 0, stream, a);
+            });
         });
     });
     prof_stop(stream);
@@ -479,15 +578,18 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
         });
     if (n > 0) {
         const int mask = (1 << p.bits) - 1;
-        const IdDigit of = {{ids, col_base, id_type, n_cols, n_vocab}, list[0], mask};
         int now = 0;
-        if (n <= kSlotFew) {
-            hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n, p.token_bits);
-        } else {
-            launch_slots(of, p.shape, count, stream);
+        with_id_type(id_type, [&](auto type) {
+            constexpr int id = decltype(type)::value;
+            const IdDigit<id> of = {embed_ids(ids, col_base, n_cols, n_vocab), list[0], mask};
+            if (n <= kSlotFew)
+                hipLaunchKernelGGL(embed_sort_few_kernel<id>, dim3(1), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n, p.token_bits);
+            else
+                launch_slots(of, p.shape, count, stream);
+        });
+        if (n > kSlotFew)
             for (int pass = 1; pass < p.passes; ++pass, now ^= 1)
                 launch_slots(PairDigit{list[now], list[now ^ 1], pass * p.bits, mask}, p.shape, count, stream);
-        }
         SumArgs a = {list[now], nullptr, d_out, d_out_stride, d_table_stride, n, width, 0, p.sum.chunk, n_vocab, accumulate, scale, d_table,
                      token[0], sum[0], p.sum.stride};
         const auto grid_of = [&](int chunk_elements) {

@@ -8,7 +8,13 @@ struct Choices {
     const int32_t *expert;
     int32_t *first, *order, *place;
     int32_t n_experts;
-    __device__ __forceinline__ int32_t load(int64_t i) const { return expert[i]; }
+    template <int N>
+    __device__ __forceinline__ void load(int32_t (&item)[N], int64_t i, int64_t end) const
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            item[u] = expert[min(i + u * 64, end - 1)];
+    }
     __device__ __forceinline__ int number(int32_t e) const { return e >= 0 && e < n_experts ? e : n_experts; }
     __device__ __forceinline__ void start(int e, int slot) const { first[e] = slot; }
     __device__ __forceinline__ void put(int32_t, int64_t i, int e, int slot) const

@@ -3,8 +3,8 @@
 // entries.  Up to kSlotFew entries are one workgroup's, in one kernel.  No atomics on memory, and the same result
 // whatever runs first.  Used for the slots of experts and for the table's gradient.
 //
-// A Source says what the entries are: Item load(i), int number(item), put(item, i, number, slot), and start(number, slot of its
-// first), called once for every number.
+// A Source says what the entries are: load(items, i) takes entries i, i + 64, ... (the last one, where that is past it), int
+// number(item), put(item, i, number, slot), and start(number, slot of its first), called once for every number.
 #ifndef FS_SLOTS_H
 #define FS_SLOTS_H
 
@@ -14,6 +14,7 @@ namespace fs {
 
 constexpr int kSlotWaves = 4;               // of a workgroup
 constexpr int kSlotMostBuckets = 1025;      // experts, and one for choices without a slot
+constexpr int kSlotMostBits = 11;
 constexpr int kSlotMostStretches = 4096;
 constexpr int kSlotScanThreads = 256;
 constexpr int kSlotScanPer = kSlotMostStretches / kSlotScanThreads;
@@ -44,15 +45,21 @@ inline size_t slot_count_bytes(const SlotShape &s)
 }
 
 // The lanes whose number is this lane's, among the lanes that are there.
+// Four instructions a bit: its sign, a compare, two three-way bit operations.
 __device__ __forceinline__ uint64_t same_number(int number, int bits, bool there)
 {
-    uint64_t same = __ballot(there);
-    for (int b = 0; b < bits; ++b) {
-        const bool set = (number >> b) & 1;
-        const uint64_t with = __ballot(set);
-        same &= set ? with : ~with;
+    const uint64_t all = __ballot(there);
+    uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+#pragma unroll
+    for (int b = 0; b < kSlotMostBits; ++b) {
+        if (b < bits) {
+            const int mine = (int)((uint32_t)number << (31 - b)) >> 31;
+            const uint64_t with = __ballot(mine != 0);
+            lo &= ~((uint32_t)with ^ (uint32_t)mine);
+            hi &= ~((uint32_t)(with >> 32) ^ (uint32_t)mine);
+        }
     }
-    return same;
+    return (uint64_t)hi << 32 | lo;
 }
 __host__ __device__ inline int bits_of(int n)        // of numbers below n
 {
@@ -107,16 +114,12 @@ slot_count_kernel(Source source, SlotShape s, int32_t *count)
         return;
     const int64_t begin = (int64_t)mine * s.stretch, end = min(begin + s.stretch, (int64_t)s.n);
     for (int64_t i0 = begin; i0 < end; i0 += kSlotAhead * 64) {
-        int number[kSlotAhead];
-#pragma unroll
-        for (int u = 0; u < kSlotAhead; ++u) {
-            const int64_t i = i0 + u * 64 + lane;
-            number[u] = i < end ? source.number(source.load(i)) : -1;
-        }
+        typename Source::Item item[kSlotAhead];
+        source.load(item, i0 + lane, end);
 #pragma unroll
         for (int u = 0; u < kSlotAhead; ++u)
-            if (number[u] >= 0)
-                atomicAdd(&c[number[u]], 1);
+            if (i0 + u * 64 + lane < end)
+                atomicAdd(&c[source.number(item[u])], 1);
     }
     lds_sync();
     for (int b = lane; b < s.buckets; b += 64)
@@ -201,9 +204,7 @@ slot_place_kernel(Source source, SlotShape s, const int32_t *count)
     const int64_t begin = (int64_t)mine * s.stretch, end = min(begin + s.stretch, (int64_t)s.n);
     for (int64_t i0 = begin; i0 < end; i0 += kSlotAhead * 64) {
         typename Source::Item item[kSlotAhead];
-#pragma unroll
-        for (int u = 0; u < kSlotAhead; ++u)
-            item[u] = source.load(min(i0 + u * 64 + lane, end - 1));
+        source.load(item, i0 + lane, end);
 #pragma unroll
         for (int u = 0; u < kSlotAhead; ++u) {
             const int64_t i = i0 + u * 64 + lane;
@@ -262,10 +263,7 @@ slot_few_kernel(Source source, int32_t n, int32_t buckets)
     const int steps = (n + kSlotFewWaves * 64 - 1) / (kSlotFewWaves * 64);       // of a wavefront, at most kSlotFewPer
     const int begin = wave * steps * 64 + lane;
     typename Source::Item item[kSlotFewPer];
-#pragma unroll
-    for (int u = 0; u < kSlotFewPer; ++u)
-        if (u < steps)
-            item[u] = source.load(min(begin + u * 64, n - 1));
+    source.load(item, begin, n);
     for (int b = threadIdx.x; b < kSlotFewWaves * buckets; b += kSlotFewWaves * 64)
         c[b] = 0;
     __syncthreads();
