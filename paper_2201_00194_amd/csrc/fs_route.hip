@@ -31,6 +31,7 @@ struct RouteArgs {
     const float *d_weight;
     void *d_logits;
     int32_t ll, group_size;
+    uint32_t group_magic;                // e / group_size = e * group_magic >> 22 for e < 1024
     int32_t exact;                       // 1: every row in 64 bits
     int32_t wave_lds;                    // bytes
     int64_t block0;                      // of this launch
@@ -156,17 +157,19 @@ __device__ void route_exact(const RouteArgs &a, int64_t row, double *key, int la
 
 // ---- keys and lists -------------------------------------------------------------------------------------------------------
 
-// The key and the expert as a double in [1, 2); 0 is nobody.
+// The key (not -0) and the expert as a double in [1, 2).
 __device__ __forceinline__ double packed(float key, int e)
 {
     const int bits = __float_as_int(key);
     const uint32_t order = (uint32_t)bits ^ ((uint32_t)(bits >> 31) | 0x80000000u);
-    return __hiloint2double((int)(0x3ff00000u | (order >> 12)), (int)((order << 20) | (uint32_t)(1023 - e)));
+    return __hiloint2double((int)__builtin_amdgcn_alignbit(0x3ffu, order, 12), (int)((order << 20) | (uint32_t)(1023 - e)));
 }
+// Nobody: an expert whose key is -infinity.
+__device__ __forceinline__ bool somebody(double v) { return __double2hiint(v) > 0x3ff007ff; }
 __device__ __forceinline__ int expert_of(double v) { return 1023 - (__double2loint(v) & 1023); }
 __device__ __forceinline__ float key_of(double v)
 {
-    const uint32_t order = ((uint32_t)__double2hiint(v) << 12) | ((uint32_t)__double2loint(v) >> 20);
+    const uint32_t order = __builtin_amdgcn_alignbit((uint32_t)__double2hiint(v), (uint32_t)__double2loint(v), 20);
     return __uint_as_float(order ^ ((uint32_t)((int)~order >> 31) | 0x80000000u));
 }
 
@@ -236,6 +239,18 @@ __device__ __forceinline__ void merge_met(double (&list)[KP])
     merge_list<KP>(list, other);
 }
 
+template <int KP>
+__device__ __forceinline__ int last_expert(const double (&list)[KP], int k)
+{
+    int e = 0;
+#pragma unroll
+    for (int j = 0; j < KP; ++j) {
+        const int low = __double2loint(list[j]);
+        e = j < k ? low + 0 : e;
+    }
+    return 1023 - (e & 1023);
+}
+
 // ---- the kernel -----------------------------------------------------------------------------------------------------------
 
 // x[u]: expert expert_at(u) of the row, -infinity past the last.
@@ -280,7 +295,7 @@ __device__ __forceinline__ void finish(const RouteArgs &a, int64_t row, const T 
                 from[l] = (h & half) ? high_l : low;
             }
         const int j = i * kLanes + h;
-        const bool there = h < kLanes && j < a.p.k && from[0] > 0.0;
+        const bool there = h < kLanes && j < a.p.k && somebody(from[0]);
         expert[i] = there ? expert_of(from[0]) : -1;
         s[i] = none;
         if (there) {
@@ -368,29 +383,64 @@ route_kernel(RouteArgs a)
         constexpr float kStep = 5.9604645e-8f;                      // 2^-24
         float key[kRoutePer], off = 0.0f;
         if constexpr (EXACT) {
-            const float over = inverse(sum);
-            off = a.p.score == FS_SCORE_SOFTMAX ? 48.0f * kStep * over : 8.0f * kStep;
+            if (a.p.score == FS_SCORE_SOFTMAX) {
+                const float over = inverse(sum);
+                off = 48.0f * kStep * over;
 #pragma unroll
-            for (int u = 0; u < kRoutePer; ++u) {
-                const int e = expert_at<T>(u, ll, h);
-                const float s = a.p.score == FS_SCORE_SOFTMAX ? exp_of(x[u] - top) * over : inverse(1.0f + exp_of(-x[u]));
-                float v = a.bias && e < n ? s + a.bias[e] : s;
-                key[u] = x[u] > none && v == v ? v : none;
+                for (int u = 0; u < kRoutePer; ++u)
+                    key[u] = exp_of(x[u] - top) * over;
+            } else {
+                off = 8.0f * kStep;
+#pragma unroll
+                for (int u = 0; u < kRoutePer; ++u)
+                    key[u] = inverse(1.0f + exp_of(-x[u]));
             }
-            if (a.p.n_groups > 1) {
-                // A lane ranks groups h, h + (1 << ll), ... of its row; keys and sums meet in LDS.
-                float *keys = (float *)own + (lane >> ll) * n, *sums = (float *)own + ((n << (6 - ll)) + (lane >> ll) * a.p.n_groups);
+            if (a.bias) {
 #pragma unroll
-                for (int u = 0; u < kRoutePer; ++u) {
-                    const int e = expert_at<T>(u, ll, h);
-                    if (e < n)
-                        keys[e] = key[u];
+                for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
+                    const int e = expert_at<T>(c * kChunk<T>, ll, h);
+                    float b[kChunk<T>];
+                    load_chunk<kChunk<T>>(a.bias + e, n - e, b);
+#pragma unroll
+                    for (int i = 0; i < kChunk<T>; ++i)
+                        key[c * kChunk<T> + i] += b[i];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kRoutePer; ++u)
+                key[u] = x[u] > none && key[u] == key[u] ? key[u] : none;
+            if (a.p.n_groups > 1) {
+                // A lane ranks groups h, h + (1 << ll), ... of its row.  What they are made of meets in LDS: of groups of whole
+                // chunks every chunk's best two keys, else all keys; then their sums.
+                const bool whole = a.group_size % kChunk<T> == 0;
+                const int width = whole ? n / kChunk<T> * 2 : n, per = width / a.p.n_groups;      // per: of a group
+                float *keys = (float *)own + (lane >> ll) * width, *sums = (float *)own + ((n << (6 - ll)) + (lane >> ll) * a.p.n_groups);
+                if (whole) {
+#pragma unroll
+                    for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
+                        const int e = expert_at<T>(c * kChunk<T>, ll, h);
+                        float first = key[c * kChunk<T>], second = none;
+#pragma unroll
+                        for (int i = 1; i < kChunk<T>; ++i) {
+                            second = fmaxf(second, fminf(first, key[c * kChunk<T> + i]));
+                            first = fmaxf(first, key[c * kChunk<T> + i]);
+                        }
+                        if (e < n)
+                            *(float2 *)(keys + e / kChunk<T> * 2) = make_float2(first, second);
+                    }
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kRoutePer; ++u) {
+                        const int e = expert_at<T>(u, ll, h);
+                        if (e < n)
+                            keys[e] = key[u];
+                    }
                 }
                 lds_sync();
                 for (int g = h; g < a.p.n_groups; g += 1 << ll) {
                     float first = none, second = none;
-                    for (int i = 0; i < a.group_size; ++i) {
-                        const float v = keys[g * a.group_size + i];
+                    for (int i = 0; i < per; ++i) {
+                        const float v = keys[g * per + i];
                         second = fmaxf(second, fminf(first, v));
                         first = fmaxf(first, v);
                     }
@@ -400,42 +450,49 @@ route_kernel(RouteArgs a)
                 int taken = 0;
                 for (int g = h; g < a.p.n_groups; g += 1 << ll) {
                     const float mine = sums[g];
-                    if (mine == none)
-                        continue;
                     int surely = 0, maybe = -1;                     // groups before this one; it is one of the second
                     for (int o = 0; o < a.p.n_groups; ++o) {
                         const float v = sums[o], near = 4.0f * off + 4.0f * kStep * (fabsf(mine) + fabsf(v));
                         surely += v - mine > near;
                         maybe += !(mine - v > near);
                     }
-                    if (maybe < a.p.top_groups)
-                        taken |= 1 << g;
-                    else if (surely < a.p.top_groups)
-                        again = true;
+                    if (mine > none) {
+                        if (maybe < a.p.top_groups)
+                            taken |= 1 << g;
+                        else if (surely < a.p.top_groups)
+                            again = true;
+                    }
                 }
                 taken = row_or(taken, ll);
+                if (whole) {
 #pragma unroll
-                for (int u = 0; u < kRoutePer; ++u) {
-                    const int e = expert_at<T>(u, ll, h);
-                    if (e < n && !(taken >> (e / a.group_size) & 1))
-                        key[u] = none;
-                    else if (!a.bias && key[u] > none)
-                        key[u] = x[u];
+                    for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
+                        const bool in = taken >> ((uint32_t)expert_at<T>(c * kChunk<T>, ll, h) * a.group_magic >> 22 & 31) & 1;
+#pragma unroll
+                        for (int i = 0; i < kChunk<T>; ++i)
+                            key[c * kChunk<T> + i] = in ? key[c * kChunk<T> + i] : none;
+                    }
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kRoutePer; ++u) {
+                        const bool in = taken >> ((uint32_t)expert_at<T>(u, ll, h) * a.group_magic >> 22 & 31) & 1;
+                        key[u] = in ? key[u] : none;
+                    }
                 }
-            } else if (!a.bias) {
+            }
+            if (!a.bias)
 #pragma unroll
                 for (int u = 0; u < kRoutePer; ++u)
-                    key[u] = x[u];
-            }
+                    key[u] = key[u] > none ? x[u] + 0.0f : none;
         } else {
 #pragma unroll
             for (int u = 0; u < kRoutePer; ++u)
-                key[u] = x[u];
+                key[u] = x[u] + 0.0f;
         }
         double v[kRoutePer], list[KP];
 #pragma unroll
         for (int u = 0; u < kRoutePer; ++u)
-            v[u] = key[u] > none ? packed(key[u] + 0.0f, expert_at<T>(u, ll, h)) : 0.0;
+            v[u] = packed(key[u], expert_at<T>(u, ll, h));
 #pragma unroll
         for (int u = 0; u < kRoutePer; u += KP)
             sort_list<KP>(v, u);
@@ -458,32 +515,46 @@ route_kernel(RouteArgs a)
         if (ll > 5) merge_met<5, KP>(list);
         if constexpr (EXACT) {
             if (a.bias) {
-                // Neighbours in the list, and what stayed outside against the last: too near to tell, unless the same logit
-                // and bias made both keys.
-                float last = none;
-                int last_e = 0;
+                // Two of the list's keys nearer than this may be in the wrong order, and one that stayed outside may belong in
+                // the place of the last.
+                float size = 0.0f, last = none;
 #pragma unroll
-                for (int j = 0; j < KP; ++j) {
+                for (int j = 0; j < KP; ++j)
                     if (j < a.p.k) {
-                        last = list[j] > 0.0 ? key_of(list[j]) : none;
-                        last_e = expert_of(list[j]);
+                        last = key_of(list[j]);
+                        size = somebody(list[j]) ? fmaxf(size, fabsf(last)) : size;
                     }
-                    if (j + 1 < KP && j + 1 < a.p.k && list[j + 1 < KP ? j + 1 : j] > 0.0) {
-                        const double next = list[j + 1 < KP ? j + 1 : j];
-                        const float other = key_of(next), near = 2.0f * off + 2.0f * kStep * (fabsf(last) + fabsf(other));
-                        if (!(last - other > near)) {
-                            const int e = last_e, o = expert_of(next);
+                const float near = 2.0f * off + 4.0f * kStep * size;
+                const float border = last > none ? last - 1.0001f * near : __builtin_inff();      // nobody: all are in the list
+                bool doubt = !(near < __builtin_inff());
+#pragma unroll
+                for (int j = 0; j + 1 < KP; ++j)
+                    if (j + 1 < a.p.k)
+                        doubt |= somebody(list[j + 1]) && !(key_of(list[j]) - key_of(list[j + 1]) > near);
+                int above = 0;
+#pragma unroll
+                for (int u = 0; u < kRoutePer; ++u)
+                    above += key[u] >= border;
+                doubt |= row_sum(above, ll) > a.p.k;
+                // Unless the same logit and bias made both keys, which is the same key then.
+                if (__ballot(doubt)) {
+                    const int last_e = last_expert<KP>(list, a.p.k);
+                    const bool finite = near < __builtin_inff();
+                    again |= !finite;
+#pragma unroll
+                    for (int j = 0; j + 1 < KP; ++j)
+                        if (j + 1 < a.p.k && doubt && finite && somebody(list[j + 1]) && !(key_of(list[j]) - key_of(list[j + 1]) > near)) {
+                            const int e = expert_of(list[j]), o = expert_of(list[j + 1]);
                             again |= !(route_logit((float)logits[e]) == route_logit((float)logits[o]) && a.bias[e] == a.bias[o]);
                         }
-                    }
-                }
-                if (last > none) {
+                    if (doubt && finite && last > none) {
+                        const float last_x = route_logit((float)logits[last_e]), last_b = a.bias[last_e];
 #pragma unroll
-                    for (int u = 0; u < kRoutePer; ++u) {
-                        const int e = expert_at<T>(u, ll, h);
-                        const float near = 2.0f * off + 2.0f * kStep * (fabsf(last) + fabsf(key[u]));
-                        if (key[u] > none && !(last - key[u] > near) && (key[u] < last || (key[u] == last && e > last_e)))
-                            again |= !(route_logit((float)logits[last_e]) == x[u] && a.bias[last_e] == a.bias[e]);
+                        for (int u = 0; u < kRoutePer; ++u) {
+                            const int e = expert_at<T>(u, ll, h);
+                            if (key[u] >= border && (key[u] < last || (key[u] == last && e > last_e)))
+                                again |= !(last_x == x[u] && last_b == a.bias[e]);
+                        }
                     }
                 }
             }
@@ -513,111 +584,147 @@ route_kernel(RouteArgs a)
 
 // ---- the gradient ---------------------------------------------------------------------------------------------------------
 
-// The choices' gradients go to the row's logits through LDS; a row's experts lie in its lanes as above.
-template <int TYPE>
+// The choices' gradients go to the row's logits through LDS; a row's experts lie in its lanes as above, its choices j in lane
+// j mod (1 << LL).
+template <int TYPE, int LL>
 __global__ void __launch_bounds__(kRouteWaves * 64)
 route_backward_kernel(RouteArgs a)
 {
     typedef typename Element<TYPE>::type T;
+    constexpr int kMine = LL < 4 ? 16 >> LL : 1;
     __shared__ float lds[kRouteWaves * 64 * kRoutePer];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ll = a.ll, h = lane & ((1 << ll) - 1);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane & ((1 << LL) - 1);
     const int n = a.p.n_experts, k = a.p.k;
     const float none = -__builtin_inff();
-    const int64_t row0 = ((a.block0 + blockIdx.x) * kRouteWaves + wave) << (6 - ll);
+    const int64_t row0 = ((a.block0 + blockIdx.x) * kRouteWaves + wave) << (6 - LL);
     if (row0 >= a.n_tokens)
         return;
-    const bool there = row0 + (lane >> ll) < a.n_tokens;
-    const int64_t row = there ? row0 + (lane >> ll) : a.n_tokens - 1;
+    const bool there = row0 + (lane >> LL) < a.n_tokens;
+    const int64_t row = there ? row0 + (lane >> LL) : a.n_tokens - 1;
     const T *logits = (const T *)a.logits + row * a.stride;
-    float *const grad = lds + wave * 64 * kRoutePer + ((lane >> ll) << ll) * kRoutePer;      // of this row
+    float *const grad = lds + wave * 64 * kRoutePer + ((lane >> LL) << LL) * kRoutePer;      // of this row
+    int expert[kMine];
+    float g[kMine], l[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int j = (i << LL) + h;
+        expert[i] = -1;
+        g[i] = 0.0f;
+        if (j < k) {
+            expert[i] = a.chosen[row * k + j];
+            g[i] = a.d_weight[row * k + j];
+        }
+    }
     float x[kRoutePer];
-    load_row<T>(logits, n, ll, h, x);
+    load_row<T>(logits, n, LL, h, x);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const bool fits = expert[i] >= 0 && expert[i] < n;
+        expert[i] = fits ? expert[i] : -1;
+        g[i] = fits ? g[i] : 0.0f;
+        l[i] = fits ? route_logit((float)logits[expert[i]]) : none;
+    }
 #pragma unroll
     for (int u = 0; u < kRoutePer; ++u)
-        grad[expert_at<T>(u, ll, h)] = 0.0f;
-    // renormalised: weight_j = exp(s_j) / sum exp(s_i), s the logit or the logarithm of its sigmoid
-    float high = none, all = 0.0f, mean = 0.0f;
-    if (a.p.renormalise) {
-        for (int j = h; j < k; j += 1 << ll) {
-            const int e = a.chosen[row * k + j];
-            if (e >= 0 && e < n) {
-                const float l = route_logit((float)logits[e]);
-                high = fmaxf(high, a.p.score == FS_SCORE_SOFTMAX ? l : fminf(l, 0.0f) - __logf(1.0f + exp_of(-fabsf(l))));
-            }
+        grad[expert_at<T>(u, LL, h)] = 0.0f;
+    if (a.p.renormalise) {        // weight_j = exp(s_j) / sum exp(s_i), s the logit or the logarithm of its sigmoid
+        float q[kMine], high = none, all = 0.0f, mean = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            q[i] = a.p.score == FS_SCORE_SOFTMAX ? l[i] : fminf(l[i], 0.0f) - __logf(1.0f + exp_of(-fabsf(l[i])));
+            q[i] = l[i] > none ? q[i] : none;
+            high = fmaxf(high, q[i]);
         }
-        high = row_max(high, ll);
-        for (int j = h; j < k; j += 1 << ll) {
-            const int e = a.chosen[row * k + j];
-            if (e >= 0 && e < n) {
-                const float l = route_logit((float)logits[e]);
-                const float s = a.p.score == FS_SCORE_SOFTMAX ? l : fminf(l, 0.0f) - __logf(1.0f + exp_of(-fabsf(l)));
-                const float q = s > none ? exp_of(s - high) : 0.0f;
-                all += q;
-                mean += q > 0.0f ? q * a.d_weight[row * k + j] : 0.0f;
-            }
+        high = row_max(high, LL);
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            q[i] = q[i] > none ? exp_of(q[i] - high) : 0.0f;
+            all += q[i];
+            mean += q[i] > 0.0f ? q[i] * g[i] : 0.0f;
         }
-        all = row_sum(all, ll);
-        mean = row_sum(mean, ll);
+        all = row_sum(all, LL);
         all = all > 0.0f ? inverse(all) : 0.0f;
-        mean *= all;
-    }
-    lds_sync();
-    for (int j = 0; j < k; ++j) {          // one after the other: an expert may have been named twice
-        const int e = a.chosen[row * k + j];
-        if (h == (j & ((1 << ll) - 1)) && e >= 0 && e < n) {
-            float g = a.d_weight[row * k + j];
-            if (a.p.renormalise) {
-                const float l = route_logit((float)logits[e]);
-                const float s = a.p.score == FS_SCORE_SOFTMAX ? l : fminf(l, 0.0f) - __logf(1.0f + exp_of(-fabsf(l)));
-                const float q = s > none ? exp_of(s - high) * all : 0.0f;
-                g = q > 0.0f ? q * (g - mean) : 0.0f;
-                if (a.p.score == FS_SCORE_SIGMOID)
-                    g *= inverse(1.0f + exp_of(l));
-            }
-            grad[e] += g;
+        mean = row_sum(mean, LL) * all;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            g[i] = q[i] > 0.0f ? q[i] * all * (g[i] - mean) : 0.0f;
+            if (a.p.score == FS_SCORE_SIGMOID)
+                g[i] *= inverse(1.0f + exp_of(l[i]));
         }
+    }
+    // An expert that a row names once (fs_route names no other way) gets its number, then its gradient.  Where numbers are
+    // lost, the choices are added one after the other.
+    lds_sync();
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+        if (expert[i] >= 0)
+            grad[expert[i]] = (float)((i << LL) + h + 1);
+    lds_sync();
+    bool twice = false;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+        twice |= expert[i] >= 0 && grad[max(expert[i], 0)] != (float)((i << LL) + h + 1);
+    lds_sync();
+    if (__ballot(twice)) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+            if (expert[i] >= 0)
+                grad[expert[i]] = 0.0f;
+        lds_sync();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+            for (int o = 0; o < 1 << LL; ++o) {
+                if (h == o && expert[i] >= 0)
+                    grad[expert[i]] += g[i];
+                lds_sync();
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+            if (expert[i] >= 0)
+                grad[expert[i]] = g[i];
         lds_sync();
     }
-    float g[kRoutePer];
+    float d[kRoutePer];
 #pragma unroll
     for (int u = 0; u < kRoutePer; ++u)
-        g[u] = grad[expert_at<T>(u, ll, h)];
+        d[u] = grad[expert_at<T>(u, LL, h)];
     if (!a.p.renormalise && a.p.score == FS_SCORE_SOFTMAX) {
-        float top = none, sum = 0.0f, dot = 0.0f;
+        float top = none, sum = 0.0f, dot = 0.0f, p[kRoutePer];
 #pragma unroll
         for (int u = 0; u < kRoutePer; ++u)
             top = fmaxf(top, x[u]);
-        top = row_max(top, ll);
+        top = row_max(top, LL);
         top = top == none ? 0.0f : top;
 #pragma unroll
         for (int u = 0; u < kRoutePer; ++u) {
-            const float p = exp_of(x[u] - top);
-            sum += p;
-            dot += p > 0.0f ? p * g[u] : 0.0f;
+            p[u] = exp_of(x[u] - top);
+            sum += p[u];
+            dot += p[u] > 0.0f ? p[u] * d[u] : 0.0f;
         }
-        sum = row_sum(sum, ll);
-        dot = row_sum(dot, ll);
-        const float factor = inverse(sum);
-        dot *= factor;
+        const float factor = inverse(row_sum(sum, LL));
+        dot = row_sum(dot, LL) * factor;
 #pragma unroll
         for (int u = 0; u < kRoutePer; ++u)
-            g[u] = exp_of(x[u] - top) * factor * (g[u] - dot);
+            d[u] = p[u] * factor * (d[u] - dot);
     } else if (!a.p.renormalise) {
 #pragma unroll
-        for (int u = 0; u < kRoutePer; ++u)      // s (1 - s), the smaller factor first
-            g[u] = g[u] * inverse(1.0f + exp_of(fabsf(x[u]))) * inverse(1.0f + exp_of(-fabsf(x[u])));
+        for (int u = 0; u < kRoutePer; ++u) {    // s (1 - s) = 1 / (1 + exp(|x|)) * 1 / (1 + exp(-|x|))
+            const float small = exp_of(-fabsf(x[u])), over = inverse(1.0f + small);
+            d[u] *= small * over * over;
+        }
     }
     if (!there)
         return;
     T *out = (T *)a.d_logits + row * a.d_stride;
 #pragma unroll
     for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
-        const int e = expert_at<T>(c * kChunk<T>, ll, h);
+        const int e = expert_at<T>(c * kChunk<T>, LL, h);
         float v[kChunk<T>];
 #pragma unroll
         for (int i = 0; i < kChunk<T>; ++i) {
             const int u = c * kChunk<T> + i;
-            v[i] = x[u] > none ? g[u] * a.p.scale : 0.0f;
+            v[i] = x[u] > none ? d[u] * a.p.scale : 0.0f;
         }
         store_chunk<kChunk<T>>(out + e, n - e, v);
     }
@@ -680,6 +787,7 @@ extern "C" int fs_route(const fs_route_params *params, int64_t n_tokens, const v
         wave_lds = ((wide > rows && wide > 0 ? wide : rows) + 15) / 16 * 16;
     }
     RouteArgs a = {*params, n_tokens, logit_stride, 0, logits, bias, expert, weight, nullptr, nullptr, nullptr, ll, n / groups,
+                   (uint32_t)((1 << 22) / (n / groups) + 1),
                    exact && groups > kRouteMostGroups, (int32_t)wave_lds, 0};
     const int64_t rows = (int64_t)kRouteWaves << (6 - ll);
     prof_start(kKernTopk, stream);
@@ -716,14 +824,26 @@ extern "C" int fs_route_backward(const fs_route_params *params, int64_t n_tokens
     if (n_tokens == 0)
         return FS_OK;
     RouteArgs a = {*params, n_tokens, logit_stride, d_logit_stride, logits, nullptr, nullptr, nullptr, expert, d_weight, d_logits,
-                   lanes_log(params->n_experts), 0, 0, 0, 0};
+                   lanes_log(params->n_experts), 0, 0, 0, 0, 0};
     const int64_t rows = (int64_t)kRouteWaves << (6 - a.ll);
     prof_start(kKernTrainOther, stream);
     with_type(logit_type, [&](auto t) {
-        in_pieces((n_tokens + rows - 1) / rows, [&](int64_t at, unsigned blocks) {
-            a.block0 = at;
-            hipLaunchKernelGGL(route_backward_kernel<decltype(t)::value>, dim3(blocks), dim3(kRouteWaves * 64), 0, stream, a);
-        });
+        constexpr int type = decltype(t)::value;
+        const auto go = [&](auto kernel) {
+            in_pieces((n_tokens + rows - 1) / rows, [&](int64_t at, unsigned blocks) {
+                a.block0 = at;
+                hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kRouteWaves * 64), 0, stream, a);
+            });
+        };
+        switch (a.ll) {
+        case 0: go(route_backward_kernel<type, 0>); break;
+        case 1: go(route_backward_kernel<type, 1>); break;
+        case 2: go(route_backward_kernel<type, 2>); break;
+        case 3: go(route_backward_kernel<type, 3>); break;
+        case 4: go(route_backward_kernel<type, 4>); break;
+        case 5: go(route_backward_kernel<type, 5>); break;
+        default: go(route_backward_kernel<type, 6>); break;
+        }
     });
     prof_stop(stream);
     return launched("route gradient kernel launch");
