@@ -141,9 +141,9 @@ template <class T, int N>
 struct ChunkOf {
     typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
-// N elements, n of them there: the others are 0, and nothing behind the n-th is read.
+// N elements, n of them there: the others are `rest`, and nothing behind the n-th is read.
 template <int N, class T>
-__device__ __forceinline__ void load_chunk(const T *p, int n, float (&v)[N])
+__device__ __forceinline__ void load_chunk(const T *p, int n, float (&v)[N], float rest = 0.0f)
 {
     if (n >= N) {
         const typename ChunkOf<T, N>::type c = *(const typename ChunkOf<T, N>::type *)p;
@@ -153,7 +153,7 @@ __device__ __forceinline__ void load_chunk(const T *p, int n, float (&v)[N])
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            v[i] = 0.0f;
+            v[i] = rest;
         if (n > 0) {
             T c[N];
 #pragma unroll
@@ -161,7 +161,7 @@ __device__ __forceinline__ void load_chunk(const T *p, int n, float (&v)[N])
                 c[i] = p[i < n ? i : n - 1];
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                v[i] = i < n ? (float)c[i] : 0.0f;
+                v[i] = i < n ? (float)c[i] : rest;
         }
     }
 }

@@ -37,11 +37,16 @@ struct RouteArgs {
     int64_t block0;                      // of this launch
 };
 
-// NaN masks an expert as -infinity does; +infinity counts as the largest float.
-__device__ __forceinline__ float route_logit(float l)
+// The value between -infinity and `most`; -infinity for a quiet NaN, as the instruction is defined.  (The compiler's own
+// median lets a NaN be anything.)
+__device__ __forceinline__ float bounded(float v, float most)
 {
-    return l != l ? -__builtin_inff() : fminf(l, 3.402823466e38f);
+    float r;
+    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(v), "v"(-__builtin_inff()), "s"(most));
+    return r;
 }
+// NaN masks an expert as -infinity does; +infinity counts as the largest float.
+__device__ __forceinline__ float route_logit(float l) { return bounded(__builtin_canonicalizef(l), 3.402823466e38f); }
 
 // ---- a row in 64 bits ---------------------------------------------------------------------------------------------------
 
@@ -173,6 +178,12 @@ __device__ __forceinline__ float key_of(double v)
     return __uint_as_float(order ^ ((uint32_t)((int)~order >> 31) | 0x80000000u));
 }
 
+// Two of the largest so far, and another value.
+__device__ __forceinline__ void best_two(float &first, float &second, float v)
+{
+    asm("v_med3_f32 %0, %1, %0, %2" : "+v"(second) : "v"(first), "v"(v));
+    asm("v_max_f32 %0, %0, %1" : "+v"(first) : "v"(v));
+}
 // __builtin_fmax would first make signalling NaNs quiet; there are none.
 __device__ __forceinline__ double larger(double a, double b)
 {
@@ -239,23 +250,63 @@ __device__ __forceinline__ void merge_met(double (&list)[KP])
     merge_list<KP>(list, other);
 }
 
-template <int KP>
-__device__ __forceinline__ int last_expert(const double (&list)[KP], int k)
-{
-    int e = 0;
-#pragma unroll
-    for (int j = 0; j < KP; ++j) {
-        const int low = __double2loint(list[j]);
-        e = j < k ? low + 0 : e;
-    }
-    return 1023 - (e & 1023);
-}
-
-// ---- the kernel -----------------------------------------------------------------------------------------------------------
-
 // x[u]: expert expert_at(u) of the row, -infinity past the last.
 template <class T>
 __device__ __forceinline__ int expert_at(int u, int ll, int h) { return (((u / kChunk<T>) << ll) + h) * kChunk<T> + u % kChunk<T>; }
+
+template <int KP>
+__device__ __forceinline__ double entry_at(const double (&list)[KP], int j)
+{
+    int lo = __double2loint(list[0]), hi = __double2hiint(list[0]);
+#pragma unroll
+    for (int i = 1; i < KP; ++i) {
+        lo = j == i ? __double2loint(list[i]) : lo + 0;
+        hi = j == i ? __double2hiint(list[i]) : hi + 0;
+    }
+    return __hiloint2double(hi, lo);
+}
+template <int KP>
+__device__ __forceinline__ float key_at(const double (&list)[KP], int j) { return key_of(j == KP - 1 ? list[KP - 1] + 0.0 : entry_at<KP>(list, j)); }
+
+// Whether two keys of this lane's row that matter are too near to be told apart by what they are in fp32 (each off by at most
+// `off`, the sum's rounding on top), unless the same logit and bias made both: that is one key then, and the lower expert goes
+// first.
+template <class T, int KP>
+__device__ __forceinline__ bool in_doubt(const RouteArgs &a, const T *logits, const double (&list)[KP], const float (&x)[kRoutePer],
+                                         const float (&key)[kRoutePer], float off, int ll, int h)
+{
+    constexpr float kStep = 5.9604645e-8f;
+    float size = 0.0f;
+    bool again = false;
+#pragma unroll
+    for (int j = 0; j < KP; ++j)
+        if (j < a.p.k && somebody(list[j]))
+            size = fmaxf(size, fabsf(key_of(list[j])));
+    if (!(size < __builtin_inff()))
+        return true;
+    const float near = 2.0f * off + 4.0f * kStep * size;
+#pragma unroll
+    for (int j = 0; j + 1 < KP; ++j)
+        if (j + 1 < a.p.k && somebody(list[j + 1]) && !(key_of(list[j]) - key_of(list[j + 1]) > near)) {
+            const int e = expert_of(list[j]), o = expert_of(list[j + 1]);
+            again |= !(route_logit((float)logits[e]) == route_logit((float)logits[o]) && a.bias[e] == a.bias[o]);
+        }
+    const double end = entry_at<KP>(list, a.p.k - 1);
+    if (somebody(end)) {
+        const float last = key_of(end), border = last - 1.0001f * near;
+        const int last_e = expert_of(end);
+        const float last_x = route_logit((float)logits[last_e]), last_b = a.bias[last_e];
+#pragma unroll
+        for (int u = 0; u < kRoutePer; ++u) {
+            const int e = expert_at<T>(u, ll, h);
+            if (key[u] >= border && (key[u] < last || (key[u] == last && e > last_e)))
+                again |= !(last_x == x[u] && last_b == a.bias[e]);
+        }
+    }
+    return again;
+}
+
+// ---- the kernel -----------------------------------------------------------------------------------------------------------
 
 template <class T>
 __device__ __forceinline__ void load_row(const T *logits, int n, int ll, int h, float (&x)[kRoutePer])
@@ -264,10 +315,10 @@ __device__ __forceinline__ void load_row(const T *logits, int n, int ll, int h, 
     for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
         const int e = expert_at<T>(c * kChunk<T>, ll, h);
         float v[kChunk<T>];
-        load_chunk<kChunk<T>>(logits + e, n - e, v);
+        load_chunk<kChunk<T>>(logits + e, n - e, v, -__builtin_inff());
 #pragma unroll
         for (int i = 0; i < kChunk<T>; ++i)
-            x[c * kChunk<T> + i] = e + i < n ? route_logit(v[i]) : -__builtin_inff();
+            x[c * kChunk<T> + i] = route_logit(v[i]);
     }
 }
 
@@ -407,8 +458,10 @@ route_kernel(RouteArgs a)
                 }
             }
 #pragma unroll
-            for (int u = 0; u < kRoutePer; ++u)
-                key[u] = x[u] > none && key[u] == key[u] ? key[u] : none;
+            for (int u = 0; u < kRoutePer; ++u) {    // a NaN becomes -infinity
+                const float v = bounded(key[u], __builtin_inff());
+                key[u] = x[u] > none ? v : none;
+            }
             if (a.p.n_groups > 1) {
                 // A lane ranks groups h, h + (1 << ll), ... of its row.  What they are made of meets in LDS: of groups of whole
                 // chunks every chunk's best two keys, else all keys; then their sums.
@@ -421,10 +474,8 @@ route_kernel(RouteArgs a)
                         const int e = expert_at<T>(c * kChunk<T>, ll, h);
                         float first = key[c * kChunk<T>], second = none;
 #pragma unroll
-                        for (int i = 1; i < kChunk<T>; ++i) {
-                            second = fmaxf(second, fminf(first, key[c * kChunk<T> + i]));
-                            first = fmaxf(first, key[c * kChunk<T> + i]);
-                        }
+                        for (int i = 1; i < kChunk<T>; ++i)
+                            best_two(first, second, key[c * kChunk<T> + i]);
                         if (e < n)
                             *(float2 *)(keys + e / kChunk<T> * 2) = make_float2(first, second);
                     }
@@ -437,24 +488,25 @@ route_kernel(RouteArgs a)
                     }
                 }
                 lds_sync();
+                float size = 0.0f;                                  // of the sums
                 for (int g = h; g < a.p.n_groups; g += 1 << ll) {
                     float first = none, second = none;
-                    for (int i = 0; i < per; ++i) {
-                        const float v = keys[g * per + i];
-                        second = fmaxf(second, fminf(first, v));
-                        first = fmaxf(first, v);
-                    }
-                    sums[g] = a.p.group_best == 2 && second > none ? first + second : first;
+                    for (int i = 0; i < per; ++i)
+                        best_two(first, second, keys[g * per + i]);
+                    first = a.p.group_best == 2 && second > none ? first + second : first;
+                    sums[g] = first;
+                    size = first > none ? fmaxf(size, fabsf(first)) : size;
                 }
                 lds_sync();
+                size = row_max(size, ll);
+                const float near = 4.0f * off + 8.0f * kStep * size;
                 int taken = 0;
                 for (int g = h; g < a.p.n_groups; g += 1 << ll) {
-                    const float mine = sums[g];
+                    const float mine = sums[g], high = mine + near, low = mine - near;
                     int surely = 0, maybe = -1;                     // groups before this one; it is one of the second
                     for (int o = 0; o < a.p.n_groups; ++o) {
-                        const float v = sums[o], near = 4.0f * off + 4.0f * kStep * (fabsf(mine) + fabsf(v));
-                        surely += v - mine > near;
-                        maybe += !(mine - v > near);
+                        surely += sums[o] > high;
+                        maybe += !(sums[o] < low);
                     }
                     if (mine > none) {
                         if (maybe < a.p.top_groups)
@@ -515,48 +567,23 @@ route_kernel(RouteArgs a)
         if (ll > 5) merge_met<5, KP>(list);
         if constexpr (EXACT) {
             if (a.bias) {
-                // Two of the list's keys nearer than this may be in the wrong order, and one that stayed outside may belong in
-                // the place of the last.
-                float size = 0.0f, last = none;
-#pragma unroll
-                for (int j = 0; j < KP; ++j)
-                    if (j < a.p.k) {
-                        last = key_of(list[j]);
-                        size = somebody(list[j]) ? fmaxf(size, fabsf(last)) : size;
-                    }
-                const float near = 2.0f * off + 4.0f * kStep * size;
-                const float border = last > none ? last - 1.0001f * near : __builtin_inff();      // nobody: all are in the list
-                bool doubt = !(near < __builtin_inff());
+                // Two of the list's keys nearer than `near` may be in the wrong order, and one that stayed outside may belong in
+                // the place of the last: then more keys reach the border than the list has, over all rows of the wavefront.
+                const float best = somebody(list[0]) ? key_of(list[0]) : 0.0f, last = key_at<KP>(list, a.p.k - 1);
+                const bool full = last > none;
+                const float near = 2.0f * off + 4.0f * kStep * fmaxf(fabsf(best), full ? fabsf(last) : 0.0f);
+                const float border = full ? last - 1.0001f * near : __builtin_inff();
+                bool doubt = !full || !(near < __builtin_inff());
 #pragma unroll
                 for (int j = 0; j + 1 < KP; ++j)
                     if (j + 1 < a.p.k)
-                        doubt |= somebody(list[j + 1]) && !(key_of(list[j]) - key_of(list[j + 1]) > near);
+                        doubt |= !(key_of(list[j]) - key_of(list[j + 1]) > near);
                 int above = 0;
 #pragma unroll
                 for (int u = 0; u < kRoutePer; ++u)
-                    above += key[u] >= border;
-                doubt |= row_sum(above, ll) > a.p.k;
-                // Unless the same logit and bias made both keys, which is the same key then.
-                if (__ballot(doubt)) {
-                    const int last_e = last_expert<KP>(list, a.p.k);
-                    const bool finite = near < __builtin_inff();
-                    again |= !finite;
-#pragma unroll
-                    for (int j = 0; j + 1 < KP; ++j)
-                        if (j + 1 < a.p.k && doubt && finite && somebody(list[j + 1]) && !(key_of(list[j]) - key_of(list[j + 1]) > near)) {
-                            const int e = expert_of(list[j]), o = expert_of(list[j + 1]);
-                            again |= !(route_logit((float)logits[e]) == route_logit((float)logits[o]) && a.bias[e] == a.bias[o]);
-                        }
-                    if (doubt && finite && last > none) {
-                        const float last_x = route_logit((float)logits[last_e]), last_b = a.bias[last_e];
-#pragma unroll
-                        for (int u = 0; u < kRoutePer; ++u) {
-                            const int e = expert_at<T>(u, ll, h);
-                            if (key[u] >= border && (key[u] < last || (key[u] == last && e > last_e)))
-                                again |= !(last_x == x[u] && last_b == a.bias[e]);
-                        }
-                    }
-                }
+                    above += __popcll(__ballot(key[u] >= border));
+                if (__ballot(doubt) || above != __popcll(__ballot(full && h == 0)) * a.p.k)
+                    again |= in_doubt<T, KP>(a, logits, list, x, key, off, ll, h);
             }
             again = row_or(again, ll);
         }
