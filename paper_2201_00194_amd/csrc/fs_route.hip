@@ -48,9 +48,14 @@ __device__ __forceinline__ float bounded(float v, float most)
 // NaN masks an expert as -infinity does; +infinity counts as the largest float.
 __device__ __forceinline__ float route_logit(float l) { return bounded(__builtin_canonicalizef(l), 3.402823466e38f); }
 
+// The logarithm of a score, but for a term that is the same for all of a row: it falls out of weights that are renormalised.
+__device__ __forceinline__ float chosen_log(const RouteArgs &a, float x)
+{
+    return a.p.score == FS_SCORE_SOFTMAX ? x : fminf(x, 0.0f) - __logf(1.0f + exp_of(-fabsf(x)));
+}
+
 // ---- a row in 64 bits ---------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ double wave_max(double v) { return row_reduce(v, 6, [](double a, double b) { return fmax(a, b); }); }
 __device__ __forceinline__ double wave_sum(double v) { return row_sum(v, 6); }
 // The largest of n values in LDS, the first of equal ones; -1 if all are -infinity.
 __device__ __forceinline__ int wave_argmax(const double *v, int n, int lane)
@@ -68,11 +73,7 @@ __device__ __forceinline__ int wave_argmax(const double *v, int n, int lane)
     }
     return at == 1 << 30 ? -1 : at;
 }
-__device__ __forceinline__ double log_score(double x, double top, double log_sum, int score)
-{
-    return score == FS_SCORE_SOFTMAX ? x - top - log_sum : fmin(x, 0.0) - log1p(exp(-fabs(x)));
-}
-
+// The choice by 64-bit keys, in LDS; its weights as everywhere.
 template <class T>
 __device__ void route_exact(const RouteArgs &a, int64_t row, double *key, int lane)
 {
@@ -80,31 +81,34 @@ __device__ void route_exact(const RouteArgs &a, int64_t row, double *key, int la
     const double none = -__builtin_inf();
     const T *logits = (const T *)a.logits + row * a.stride;
     double *group = key + n;
-    double top = none, sum = 0.0;
+    const bool softmax = a.p.score == FS_SCORE_SOFTMAX;
+    float top = -__builtin_inff();
+#pragma nounroll
     for (int e = lane; e < n; e += 64)
-        top = fmax(top, (double)route_logit((float)logits[e]));
-    top = wave_max(top);
-    if (top == none)
-        top = 0.0;
-    for (int e = lane; e < n; e += 64)
-        sum += exp((double)route_logit((float)logits[e]) - top);
-    const double log_sum = log(wave_sum(sum));
+        top = fmaxf(top, route_logit((float)logits[e]));
+    top = row_max(top, 6);
+    top = top == -__builtin_inff() ? 0.0f : top;
+    double sum = 0.0;
     lds_sync();
+#pragma nounroll
     for (int e = lane; e < n; e += 64) {
-        const double x = route_logit((float)logits[e]);
-        double v = x;
-        if (x > none && (a.bias || a.p.n_groups > 1)) {
-            v = exp(log_score(x, top, log_sum, a.p.score));
-            if (a.bias)
-                v += (double)a.bias[e];
-        }
-        key[e] = v > none ? v : none;
+        const double x = route_logit((float)logits[e]), v = exp(softmax ? x - (double)top : -x);
+        key[e] = softmax ? v : 1.0 / (1.0 + v);
+        sum += v;
+    }
+    sum = wave_sum(sum);
+#pragma nounroll
+    for (int e = lane; e < n; e += 64) {
+        const double s = softmax ? key[e] / sum : key[e], v = a.bias ? s + (double)a.bias[e] : s;
+        key[e] = route_logit((float)logits[e]) > -__builtin_inff() && v > none ? v : none;
     }
     lds_sync();
     if (a.p.n_groups > 1) {
         const int per = a.group_size;
+#pragma nounroll
         for (int g = lane; g < a.p.n_groups; g += 64) {
             double first = none, second = none;
+#pragma nounroll
             for (int e = g * per; e < (g + 1) * per; ++e) {
                 const double v = key[e];
                 if (v > first)
@@ -115,6 +119,7 @@ __device__ void route_exact(const RouteArgs &a, int64_t row, double *key, int la
             group[g] = a.p.group_best == 2 && second > none ? first + second : first;
         }
         lds_sync();
+#pragma nounroll
         for (int r = 0; r < a.p.top_groups; ++r) {
             const int g = wave_argmax(group, a.p.n_groups, lane);
             lds_sync();
@@ -122,6 +127,7 @@ __device__ void route_exact(const RouteArgs &a, int64_t row, double *key, int la
                 group[g] = __builtin_nan("");                 // taken
             lds_sync();
         }
+#pragma nounroll
         for (int e = lane; e < n; e += 64) {
             const double t = group[e / per];
             if (t == t)
@@ -132,6 +138,7 @@ __device__ void route_exact(const RouteArgs &a, int64_t row, double *key, int la
         lds_sync();
     }
     int mine = -1;
+#pragma nounroll
     for (int j = 0; j < k; ++j) {
         const int e = wave_argmax(key, n, lane);
         lds_sync();
@@ -141,22 +148,19 @@ __device__ void route_exact(const RouteArgs &a, int64_t row, double *key, int la
             mine = e;
         lds_sync();
     }
-    double s = none, w;
-    if (mine >= 0) {
-        const double x = route_logit((float)logits[mine]);
-        s = a.p.renormalise && a.p.score == FS_SCORE_SOFTMAX ? x : log_score(x, top, log_sum, a.p.score);
-    }
-    if (a.p.renormalise) {                 // the softmax over the chosen: a common term of their logarithms falls out
-        const double high = wave_max(s);
-        w = mine < 0 ? 0.0 : exp(s - high);
-        const double all = wave_sum(w);
-        w = all > 0.0 ? w / all : 0.0;
+    const float x = mine < 0 ? 0.0f : route_logit((float)logits[mine]);
+    float w;
+    if (a.p.renormalise) {
+        const float s = mine < 0 ? -__builtin_inff() : chosen_log(a, x), high = row_max(s, 6);
+        w = mine < 0 ? 0.0f : exp_of(s - high);
+        const float all = row_sum(w, 6);
+        w = all > 0.0f ? w * inverse(all) : 0.0f;
     } else {
-        w = mine < 0 ? 0.0 : exp(s);
+        w = mine < 0 ? 0.0f : softmax ? exp_of(x - top) * inverse((float)sum) : inverse(1.0f + exp_of(-x));
     }
     if (lane < k) {
         a.expert[row * k + lane] = mine;
-        a.weight[row * k + lane] = (float)(w * (double)a.p.scale);
+        a.weight[row * k + lane] = w * a.p.scale;
     }
 }
 
@@ -272,8 +276,8 @@ __device__ __forceinline__ float key_at(const double (&list)[KP], int j) { retur
 // `off`, the sum's rounding on top), unless the same logit and bias made both: that is one key then, and the lower expert goes
 // first.
 template <class T, int KP>
-__device__ __forceinline__ bool in_doubt(const RouteArgs &a, const T *logits, const double (&list)[KP], const float (&x)[kRoutePer],
-                                         const float (&key)[kRoutePer], float off, int ll, int h)
+__device__ __forceinline__ bool in_doubt(const RouteArgs &a, const T *logits, const double (&list)[KP], const float (&key)[kRoutePer], float off,
+                                         int ll, int h)
 {
     constexpr float kStep = 5.9604645e-8f;
     float size = 0.0f;
@@ -300,7 +304,7 @@ __device__ __forceinline__ bool in_doubt(const RouteArgs &a, const T *logits, co
         for (int u = 0; u < kRoutePer; ++u) {
             const int e = expert_at<T>(u, ll, h);
             if (key[u] >= border && (key[u] < last || (key[u] == last && e > last_e)))
-                again |= !(last_x == x[u] && last_b == a.bias[e]);
+                again |= !(last_x == route_logit((float)logits[e]) && last_b == a.bias[e]);
         }
     }
     return again;
@@ -351,12 +355,7 @@ __device__ __forceinline__ void finish(const RouteArgs &a, int64_t row, const T 
         s[i] = none;
         if (there) {
             const float x = route_logit((float)logits[expert[i]]);
-            if (a.p.score == FS_SCORE_SOFTMAX)
-                s[i] = x;
-            else if (a.p.renormalise)
-                s[i] = fminf(x, 0.0f) - __logf(1.0f + exp_of(-fabsf(x)));
-            else
-                s[i] = x;
+            s[i] = a.p.renormalise ? chosen_log(a, x) : x;
         }
         high = fmaxf(high, s[i]);
     }
@@ -395,7 +394,7 @@ __device__ __forceinline__ void finish(const RouteArgs &a, int64_t row, const T 
 }
 
 template <int TYPE, int KP, bool EXACT>
-__global__ void __launch_bounds__(kRouteWaves * 64)
+__global__ void __launch_bounds__(kRouteWaves * 64, KP > 8 ? 4 : EXACT ? 5 : 8)
 route_kernel(RouteArgs a)
 {
     typedef typename Element<TYPE>::type T;
@@ -583,7 +582,7 @@ route_kernel(RouteArgs a)
                 for (int u = 0; u < kRoutePer; ++u)
                     above += __popcll(__ballot(key[u] >= border));
                 if (__ballot(doubt) || above != __popcll(__ballot(full && h == 0)) * a.p.k)
-                    again |= in_doubt<T, KP>(a, logits, list, x, key, off, ll, h);
+                    again |= in_doubt<T, KP>(a, logits, list, key, off, ll, h);
             }
             again = row_or(again, ll);
         }
@@ -658,8 +657,7 @@ route_backward_kernel(RouteArgs a)
         float q[kMine], high = none, all = 0.0f, mean = 0.0f;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-            q[i] = a.p.score == FS_SCORE_SOFTMAX ? l[i] : fminf(l[i], 0.0f) - __logf(1.0f + exp_of(-fabsf(l[i])));
-            q[i] = l[i] > none ? q[i] : none;
+            q[i] = l[i] > none ? chosen_log(a, l[i]) : none;
             high = fmaxf(high, q[i]);
         }
         high = row_max(high, LL);
