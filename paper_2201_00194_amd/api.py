@@ -8,6 +8,7 @@ fallback: if the library has not been built, importing this module raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import List, Optional, Sequence
 
@@ -518,8 +519,10 @@ for _name, _result, _args in (
 
 
 def _matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optional[int] = None,
-            dtype: Optional[torch.dtype] = None):
-    """(pointer, element type, row stride) of a matrix argument whose rows' elements are adjacent."""
+            dtype: Optional[torch.dtype] = None, on: Optional[int] = None):
+    """(pointer, element type, row stride) of a matrix argument whose rows' elements are adjacent; `on`: the call's GPU."""
+    if on is not None and t.get_device() != on:
+        raise FsError(FS_EINVAL, f"{what} is not on the call's GPU")
     if t.dim() != 2 or t.dtype not in _ELEMENT:
         raise FsError(FS_EINVAL, f"{what} is not a matrix of fp32, bf16 or fp16")
     if (width is not None and t.shape[1] != width) or (rows is not None and t.shape[0] != rows):
@@ -531,28 +534,51 @@ def _matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optio
     return t.data_ptr(), _ELEMENT[t.dtype], (t.stride(0) if t.shape[0] > 1 else max(1, t.shape[1]))
 
 
-def _array(t: Optional[torch.Tensor], what: str, n: int, dtype: torch.dtype) -> Optional[int]:
+def _array(t: Optional[torch.Tensor], what: str, n: int, dtype: torch.dtype, on: Optional[int] = None) -> Optional[int]:
     if t is None:
         return None
+    if on is not None and t.get_device() != on:
+        raise FsError(FS_EINVAL, f"{what} is not on the call's GPU")
     if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise FsError(FS_EINVAL, f"{what} is not a contiguous array of {n} {dtype}")
     return t.data_ptr()
 
 
+# The current stream's handle without the object around it (0.1 us instead of 2, of 11 that a call takes).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class _Place:
     """Where a call runs: results and working memory are allocated for its stream."""
+
+    __slots__ = ("device", "index", "stream", "ptr")
 
     def __init__(self, like: torch.Tensor, stream: Optional[torch.cuda.Stream]):
         if not like.is_cuda:
             raise FsError(FS_EINVAL, "the tensors are not on the GPU")
         self.device, self.stream = like.device, stream
-        self.ptr = torch.cuda.current_stream(like.device).cuda_stream if stream is None else stream.cuda_stream
+        self.index = self.device.index
+        self.ptr = _raw_stream(self.index) if stream is None else stream.cuda_stream
 
     def empty(self, shape, dtype: torch.dtype) -> torch.Tensor:
         if self.stream is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def matrix(self, out: Optional[torch.Tensor], what: str, rows: int, width: int, dtype: torch.dtype):
+        """(the tensor, its pointer, its row stride): `out`, checked, or a new one."""
+        if out is None:
+            out = self.empty((rows, width), dtype)
+            return out, out.data_ptr(), max(1, width)
+        ptr, _, stride = _matrix(out, what, width, rows, dtype, self.index)
+        return out, ptr, stride
+
+    def array(self, out: Optional[torch.Tensor], what: str, shape, dtype: torch.dtype):
+        if out is None:
+            out = self.empty(shape, dtype)
+            return out, out.data_ptr()
+        return out, _array(out, what, math.prod(shape), dtype, self.index)
 
 
 def route_params(n_experts: int, k: int, score: int = FS_SCORE_SOFTMAX, renormalise: bool = True, n_groups: int = 1,
@@ -565,27 +591,23 @@ def fs_route(params: _FsRouteParams, logits: torch.Tensor, bias: Optional[torch.
              stream: Optional[torch.cuda.Stream] = None):
     """(expert, weight), int32 and fp32 of [tokens, k], of logits [tokens, n_experts]."""
     at = _Place(logits, stream)
-    ptr, typ, stride = _matrix(logits, "logits", params.n_experts)
+    ptr, typ, stride = _matrix(logits, "logits", params.n_experts, on=at.index)
     n, k = logits.shape[0], params.k
-    if expert is None:
-        expert = at.empty((n, max(k, 0)), torch.int32)
-    if weight is None:
-        weight = at.empty((n, max(k, 0)), torch.float32)
-    _check(_lib.fs_route(params, n, ptr, typ, stride, _array(bias, "bias", params.n_experts, torch.float32),
-                         _array(expert, "expert", n * k, torch.int32), _array(weight, "weight", n * k, torch.float32), at.ptr))
+    expert, e_ptr = at.array(expert, "expert", (n, max(k, 0)), torch.int32)
+    weight, w_ptr = at.array(weight, "weight", (n, max(k, 0)), torch.float32)
+    _check(_lib.fs_route(params, n, ptr, typ, stride, _array(bias, "bias", params.n_experts, torch.float32, at.index), e_ptr, w_ptr,
+                         at.ptr))
     return expert, weight
 
 
 def fs_route_backward(params: _FsRouteParams, logits: torch.Tensor, expert: torch.Tensor, d_weight: torch.Tensor,
                       d_logits: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     at = _Place(logits, stream)
-    ptr, typ, stride = _matrix(logits, "logits", params.n_experts)
+    ptr, typ, stride = _matrix(logits, "logits", params.n_experts, on=at.index)
     n, k = logits.shape[0], params.k
-    if d_logits is None:
-        d_logits = at.empty((n, params.n_experts), logits.dtype)
-    d_ptr, _, d_stride = _matrix(d_logits, "d_logits", params.n_experts, n, logits.dtype)
-    _check(_lib.fs_route_backward(params, n, ptr, typ, stride, _array(expert, "expert", n * k, torch.int32),
-                                  _array(d_weight, "d_weight", n * k, torch.float32), d_ptr, d_stride, at.ptr))
+    d_logits, d_ptr, d_stride = at.matrix(d_logits, "d_logits", n, params.n_experts, logits.dtype)
+    _check(_lib.fs_route_backward(params, n, ptr, typ, stride, _array(expert, "expert", n * k, torch.int32, at.index),
+                                  _array(d_weight, "d_weight", n * k, torch.float32, at.index), d_ptr, d_stride, at.ptr))
     return d_logits
 
 
@@ -597,6 +619,11 @@ class ExpertPlan:
         self.n_experts = first.shape[0] - 1
         self.n_tokens, self.k = place.shape
 
+    def _lists(self, at: _Place):
+        """The pointers of first and place."""
+        return (_array(self.first, "first", self.n_experts + 1, torch.int32, at.index),
+                _array(self.place, "place", self.n_tokens * self.k, torch.int32, at.index))
+
 
 def fs_expert_plan(expert: torch.Tensor, n_experts: int, plan: Optional[ExpertPlan] = None,
                    stream: Optional[torch.cuda.Stream] = None) -> ExpertPlan:
@@ -605,29 +632,25 @@ def fs_expert_plan(expert: torch.Tensor, n_experts: int, plan: Optional[ExpertPl
     if expert.dim() != 2:
         raise FsError(FS_EINVAL, "expert is not [tokens, k]")
     n, k = expert.shape
-    src = _array(expert, "expert", n * k, torch.int32)
-    if plan is None:
-        plan = ExpertPlan(at.empty((max(n_experts, 0) + 1,), torch.int32), at.empty((n * k,), torch.int32),
-                          at.empty((n, k), torch.int32))
+    src = _array(expert, "expert", n * k, torch.int32, at.index)
+    old = (None, None, None) if plan is None else (plan.first, plan.order, plan.place)
+    first, f_ptr = at.array(old[0], "first", (max(n_experts, 0) + 1,), torch.int32)
+    order, o_ptr = at.array(old[1], "order", (n * k,), torch.int32)
+    place, p_ptr = at.array(old[2], "place", (n, k), torch.int32)
     need = _lib.fs_expert_plan_workspace_bytes(n, k, n_experts)
     work = at.empty((need,), torch.uint8) if need else None
-    _check(_lib.fs_expert_plan(n, k, n_experts, src, _array(plan.first, "first", n_experts + 1, torch.int32),
-                               _array(plan.order, "order", n * k, torch.int32), _array(plan.place, "place", n * k, torch.int32),
-                               _ptr(work), need, at.ptr))
-    return plan
+    _check(_lib.fs_expert_plan(n, k, n_experts, src, f_ptr, o_ptr, p_ptr, _ptr(work), need, at.ptr))
+    return ExpertPlan(first, order, place) if plan is None else plan
 
 
 def fs_expert_gather(x: torch.Tensor, plan: ExpertPlan, out: Optional[torch.Tensor] = None,
                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Rows x [tokens, width] in the experts' slots: [tokens*k, width]."""
     at = _Place(x, stream)
-    ptr, typ, stride = _matrix(x, "x", rows=plan.n_tokens)
+    ptr, typ, stride = _matrix(x, "x", rows=plan.n_tokens, on=at.index)
     width = x.shape[1]
-    if out is None:
-        out = at.empty((plan.n_tokens * plan.k, width), x.dtype)
-    o_ptr, _, o_stride = _matrix(out, "out", width, plan.n_tokens * plan.k, x.dtype)
-    _check(_lib.fs_expert_gather(plan.n_tokens, plan.k, plan.n_experts, width, ptr, typ, stride, _ptr(plan.first),
-                                 _ptr(plan.place), o_ptr, o_stride, at.ptr))
+    out, o_ptr, o_stride = at.matrix(out, "out", plan.n_tokens * plan.k, width, x.dtype)
+    _check(_lib.fs_expert_gather(plan.n_tokens, plan.k, plan.n_experts, width, ptr, typ, stride, *plan._lists(at), o_ptr, o_stride, at.ptr))
     return out
 
 
@@ -635,13 +658,11 @@ def fs_expert_combine(y: torch.Tensor, plan: ExpertPlan, weight: Optional[torch.
                       out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The slots' rows y [tokens*k, width], weighted, at their tokens: [tokens, width]."""
     at = _Place(y, stream)
-    ptr, typ, stride = _matrix(y, "y", rows=plan.n_tokens * plan.k)
+    ptr, typ, stride = _matrix(y, "y", rows=plan.n_tokens * plan.k, on=at.index)
     width = y.shape[1]
-    if out is None:
-        out = at.empty((plan.n_tokens, width), y.dtype)
-    o_ptr, _, o_stride = _matrix(out, "out", width, plan.n_tokens, y.dtype)
-    _check(_lib.fs_expert_combine(plan.n_tokens, plan.k, width, ptr, typ, stride, _ptr(plan.place),
-                                  _array(weight, "weight", plan.n_tokens * plan.k, torch.float32), o_ptr, o_stride, at.ptr))
+    out, o_ptr, o_stride = at.matrix(out, "out", plan.n_tokens, width, y.dtype)
+    _check(_lib.fs_expert_combine(plan.n_tokens, plan.k, width, ptr, typ, stride, plan._lists(at)[1],
+                                  _array(weight, "weight", plan.n_tokens * plan.k, torch.float32, at.index), o_ptr, o_stride, at.ptr))
     return out
 
 
@@ -651,27 +672,25 @@ def fs_expert_combine_backward(d_out: torch.Tensor, y: torch.Tensor, plan: Exper
     """(d_y, d_weight) of a weighted fs_expert_combine."""
     at = _Place(d_out, stream)
     n, k, width = plan.n_tokens, plan.k, d_out.shape[-1]
-    ptr, typ, stride = _matrix(d_out, "d_out", rows=n)
-    y_ptr, _, y_stride = _matrix(y, "y", width, n * k, d_out.dtype)
-    if d_y is None:
-        d_y = at.empty((n * k, width), d_out.dtype)
-    if d_weight is None:
-        d_weight = at.empty((n, k), torch.float32)
-    o_ptr, _, o_stride = _matrix(d_y, "d_y", width, n * k, d_out.dtype)
-    _check(_lib.fs_expert_combine_backward(n, k, plan.n_experts, width, ptr, typ, stride, y_ptr, y_stride, _ptr(plan.first),
-                                           _ptr(plan.place), _array(weight, "weight", n * k, torch.float32), o_ptr, o_stride,
-                                           _array(d_weight, "d_weight", n * k, torch.float32), at.ptr))
+    ptr, typ, stride = _matrix(d_out, "d_out", rows=n, on=at.index)
+    y_ptr, _, y_stride = _matrix(y, "y", width, n * k, d_out.dtype, at.index)
+    d_y, o_ptr, o_stride = at.matrix(d_y, "d_y", n * k, width, d_out.dtype)
+    d_weight, w_ptr = at.array(d_weight, "d_weight", (n, k), torch.float32)
+    _check(_lib.fs_expert_combine_backward(n, k, plan.n_experts, width, ptr, typ, stride, y_ptr, y_stride, *plan._lists(at),
+                                           _array(weight, "weight", n * k, torch.float32, at.index), o_ptr, o_stride, w_ptr, at.ptr))
     return d_y, d_weight
 
 
-def _id_array(ids: torch.Tensor, col_base: Optional[torch.Tensor]):
+def _id_array(ids: torch.Tensor, col_base: Optional[torch.Tensor], on: Optional[int] = None):
     """(rows, columns, pointer, type, base pointer): ids [rows] are single tokens, [rows, columns] bags."""
     if ids.dim() not in (1, 2) or ids.dtype not in _ID:
         raise FsError(FS_EINVAL, "ids is not [rows] or [rows, columns] of int32, int64 or 16-bit leaf ids")
     if not ids.is_contiguous():
         raise FsError(FS_EINVAL, "ids is not contiguous")
+    if on is not None and ids.get_device() != on:
+        raise FsError(FS_EINVAL, "ids is not on the call's GPU")
     rows, cols = ids.shape[0], (ids.shape[1] if ids.dim() == 2 else 1)
-    return rows, cols, ids.data_ptr(), _ID[ids.dtype], _array(col_base, "col_base", cols, torch.int32)
+    return rows, cols, ids.data_ptr(), _ID[ids.dtype], _array(col_base, "col_base", cols, torch.int32, on)
 
 
 def fs_embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, col_base: Optional[torch.Tensor] = None,
@@ -679,12 +698,11 @@ def fs_embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, col_bas
     """[rows, width]: the scaled rows of `table` that ids [rows] name, or the scaled sums of those that ids [rows, columns]
     name.  The result is of the table's type unless `out` (of that type or fp32) is given."""
     at = _Place(table, stream)
-    t_ptr, typ, t_stride = _matrix(table, "table")
-    rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base)
+    t_ptr, typ, t_stride = _matrix(table, "table", on=at.index)
+    rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base, at.index)
     vocab, width = table.shape
-    if out is None:
-        out = at.empty((rows, width), table.dtype)
-    o_ptr, o_typ, o_stride = _matrix(out, "out", width, rows)
+    out, o_ptr, o_stride = at.matrix(out, "out", rows, width, table.dtype if out is None else out.dtype)
+    o_typ = _ELEMENT[out.dtype]
     _check(_lib.fs_embed(vocab, width, t_ptr, typ, t_stride, rows, cols, i_ptr, i_typ, base, scale, o_ptr, o_typ, o_stride, at.ptr))
     return out
 
@@ -695,14 +713,14 @@ def fs_embed_backward(d_out: torch.Tensor, ids: torch.Tensor, n_vocab: int, scal
     """The table's gradient [n_vocab, width]: fp32 unless `d_table` (of that type or d_out's) is given; `accumulate` adds to
     what `d_table` holds."""
     at = _Place(d_out, stream)
-    rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base)
-    ptr, typ, stride = _matrix(d_out, "d_out", rows=rows)
+    rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base, at.index)
+    ptr, typ, stride = _matrix(d_out, "d_out", rows=rows, on=at.index)
     width = d_out.shape[1]
-    if d_table is None:
-        if accumulate:
-            raise FsError(FS_EINVAL, "accumulate needs a d_table to add to")
-        d_table = at.empty((max(n_vocab, 0), width), torch.float32)
-    t_ptr, t_typ, t_stride = _matrix(d_table, "d_table", width, n_vocab)
+    if d_table is None and accumulate:
+        raise FsError(FS_EINVAL, "accumulate needs a d_table to add to")
+    kind = torch.float32 if d_table is None else d_table.dtype
+    d_table, t_ptr, t_stride = at.matrix(d_table, "d_table", max(n_vocab, 0), width, kind)
+    t_typ = _ELEMENT[d_table.dtype]
     need = _lib.fs_embed_backward_workspace_bytes(n_vocab, width, rows, cols)
     work = at.empty((need,), torch.uint8) if need else None
     _check(_lib.fs_embed_backward(n_vocab, width, ptr, typ, stride, rows, cols, i_ptr, i_typ, base, scale, int(accumulate), t_ptr,

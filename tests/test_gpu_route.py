@@ -267,3 +267,23 @@ def test_many_tokens(api):
     assert torch.equal(e.long(), i[:, :2]) and float((w.double() / v[:, :2] - 1).abs().max()) < 2.0 ** -24 * 120
     e2, w2 = api.fs_route(p, x)
     assert torch.equal(e, e2) and torch.equal(w, w2)
+
+
+def test_tensors_elsewhere_are_refused(api):
+    """A host tensor among the arguments never becomes a pointer for the GPU."""
+    import torch
+    x, p = torch.zeros(4, 8, device="cuda"), api.route_params(8, 2)
+    e, w = api.fs_route(p, x)
+    plan = api.fs_expert_plan(e, 8)
+    host = api.ExpertPlan(plan.first.cpu(), plan.order, plan.place)
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    for call in (lambda: api.fs_route(p, x, torch.zeros(8)), lambda: api.fs_route(p, x, expert=e.cpu()),
+                 lambda: api.fs_route_backward(p, x, e.cpu(), w), lambda: api.fs_route_backward(p, x, e, w, x.cpu()),
+                 lambda: api.fs_expert_gather(x, host), lambda: api.fs_expert_gather(x, plan, torch.zeros(8, 8)),
+                 lambda: api.fs_expert_combine(torch.zeros(8, 8, device="cuda"), plan, w.cpu()),
+                 lambda: api.fs_expert_combine_backward(x, torch.zeros(8, 8), plan, w), lambda: api.fs_embed(x, ids.cpu()),
+                 lambda: api.fs_embed(x, ids, col_base=torch.zeros(1, dtype=torch.int32)),
+                 lambda: api.fs_embed_backward(x, ids.cpu(), 5), lambda: api.fs_embed_backward(x, ids, 5, d_table=torch.zeros(5, 8))):
+        with pytest.raises(api.FsError) as err:
+            call()
+        assert "GPU" in str(err.value)
