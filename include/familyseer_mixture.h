@@ -149,7 +149,7 @@ int fs_embed(int32_t n_vocab, int32_t width, const void *table /* DEVICE */, int
  * the ids alone; rows that no id names get 0.  accumulate = 1: it is added to what d_table holds.  d_table_type is d_out's
  * type or FS_F32.
  */
-size_t fs_embed_backward_workspace_bytes(int32_t n_vocab, int32_t width, int64_t n_rows, int32_t n_cols);
+size_t fs_embed_backward_workspace_bytes(int32_t n_vocab, int32_t width, int32_t d_out_type, int64_t n_rows, int32_t n_cols);
 int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_out /* DEVICE */, int32_t d_out_type, int64_t d_out_stride,
                       int64_t n_rows, int32_t n_cols, const void *ids /* DEVICE */, int32_t id_type,
                       const int32_t *col_base /* DEVICE or NULL */, float scale, int32_t accumulate, void *d_table /* DEVICE out */,

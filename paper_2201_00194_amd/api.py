@@ -511,7 +511,7 @@ for _name, _result, _args in (
         ("fs_expert_combine_backward", ctypes.c_int,
          [_i64, _i32, _i32, _i32, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp]),
         ("fs_embed", ctypes.c_int, [_i32, _i32, _vp, _i32, _i64, _i64, _i32, _vp, _i32, _vp, _f32, _vp, _i32, _i64, _vp]),
-        ("fs_embed_backward_workspace_bytes", _sz, [_i32, _i32, _i64, _i32]),
+        ("fs_embed_backward_workspace_bytes", _sz, [_i32, _i32, _i32, _i64, _i32]),
         ("fs_embed_backward", ctypes.c_int,
          [_i32, _i32, _vp, _i32, _i64, _i64, _i32, _vp, _i32, _vp, _f32, _i32, _vp, _i32, _i64, _vp, _sz, _vp])):
     getattr(_lib, _name).restype = _result
@@ -721,7 +721,7 @@ def fs_embed_backward(d_out: torch.Tensor, ids: torch.Tensor, n_vocab: int, scal
     kind = torch.float32 if d_table is None else d_table.dtype
     d_table, t_ptr, t_stride = at.matrix(d_table, "d_table", max(n_vocab, 0), width, kind)
     t_typ = _ELEMENT[d_table.dtype]
-    need = _lib.fs_embed_backward_workspace_bytes(n_vocab, width, rows, cols)
+    need = _lib.fs_embed_backward_workspace_bytes(n_vocab, width, typ, rows, cols)
     work = at.empty((need,), torch.uint8) if need else None
     _check(_lib.fs_embed_backward(n_vocab, width, ptr, typ, stride, rows, cols, i_ptr, i_typ, base, scale, int(accumulate), t_ptr,
                                   t_typ, t_stride, _ptr(work), need, at.ptr))

@@ -2,9 +2,9 @@
 //
 // The gradient of a table's row is the sum over the places that named it.  The (token, row) pairs are sorted by token,
 // stably, a digit at a time; then the sorted list is cut in chunks, and the lanes that hold a row add a chunk's rows run by run.
-// A run inside a chunk is a finished row of the table; what a chunk has of a run that goes on at either end is a partial sum,
-// two a chunk at most, and the partial sums are a sorted list themselves, of 2 / chunk the length: they go the same way
-// again until one chunk is left.  So a token named everywhere costs no more than others, and the order of additions depends on the
+// A run inside a chunk is a finished row of the table; what a workgroup's chunks have of a run that goes on beyond them is a
+// partial sum, two a workgroup at most, and the partial sums are a sorted list themselves: they go the same way
+// again until one workgroup is enough.  So a token named everywhere costs no more than others, and the order of additions depends on the
 // ids alone.
 #include "fs_slots.h"
 
@@ -16,8 +16,9 @@ constexpr int kEmbedWaves = 4;            // of a workgroup
 constexpr int kEmbedAhead = 8;            // rows on their way at once
 constexpr int kEmbedFewWaves = 2048;
 constexpr int kLookupRows = 4;            // rows of a lane
+constexpr int kSumWaves = 8;              // of a workgroup
 constexpr int kSumMostChunk = 256, kSumLeastChunk = 16;   // pairs a chunk
-constexpr int kSumNextChunk = 64;                         // partial sums a chunk
+constexpr int kSumNextChunk = 32;                         // partial sums a chunk
 
 template <int ID> struct IdOf;
 template <> struct IdOf<FS_ID_I32> { typedef int32_t type; };
@@ -224,13 +225,45 @@ struct PairDigit {
     __device__ __forceinline__ void put(const Pair &p, int64_t, int, int slot) const { to[slot] = p; }
 };
 
+// Rows that nobody names are 0: what block b of `blocks` clears.
+template <class T>
+__device__ __forceinline__ void clear_table(void *table, int64_t n_rows, int32_t width, int64_t stride, int32_t ll, int64_t b, int64_t blocks)
+{
+    constexpr int N = kChunk<T>;
+    const int lane = threadIdx.x & 63, h = lane & ((1 << ll) - 1), waves = blockDim.x >> 6;
+    RawChunk<T> zero;
+    zero.clear();
+    for (int64_t r = ((b * waves + (threadIdx.x >> 6)) << (6 - ll)) + (lane >> ll); r < n_rows; r += (blocks * waves) << (6 - ll))
+        for (int c = h * N; c < width; c += 64 * N)
+            zero.store((T *)table + r * stride + c, width - c);
+}
+struct ClearArgs {
+    void *table;                   // or NULL
+    int64_t n_rows, stride;
+    int32_t type, width, ll;
+};
+__device__ __forceinline__ void clear_table(const ClearArgs &a, int64_t b, int64_t blocks)
+{
+    if (a.type == FS_F32)
+        clear_table<float>(a.table, a.n_rows, a.width, a.stride, a.ll, b, blocks);
+    else                           // the zeros of bf16 and fp16 are the same
+        clear_table<_Float16>(a.table, a.n_rows, a.width, a.stride, a.ll, b, blocks);
+}
+static __global__ void __launch_bounds__(1024)
+embed_clear_kernel(ClearArgs a) { clear_table(a, blockIdx.x, gridDim.x); }
+constexpr int kClearBlocks = 2047;
+
 // All digits of up to kSlotFew entries in one workgroup.  LDS holds the tokens where the entries are and the entries' numbers
-// in the order so far, which a pass takes to registers and puts back.
+// in the order so far, which a pass takes to registers and puts back.  The launch's other workgroups clear the table meanwhile.
 constexpr int kFewDigitBits = 9;
 template <int ID>
 __global__ void __launch_bounds__(kSlotFewWaves * 64)
-embed_sort_few_kernel(IdDigit<ID> source, int32_t n, int32_t bits)
+embed_sort_few_kernel(IdDigit<ID> source, int32_t n, int32_t bits, ClearArgs clear)
 {
+    if (blockIdx.x > 0) {
+        clear_table(clear, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
     __shared__ int32_t token[kSlotFew], c[kSlotFewWaves << kFewDigitBits], wave_total[kSlotFewWaves];
     __shared__ uint16_t order[kSlotFew];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -288,62 +321,20 @@ struct SumArgs {
     int32_t width, ll, chunk, n_vocab, accumulate;
     float scale;
     void *out;
-    uint32_t *next_token;          // two a chunk
+    uint32_t *next_token;          // two a workgroup
     float *next;
     int64_t next_stride;
 };
+constexpr uint32_t kNoToken = 0xffffffffu;
 
-template <int IN, int OUT, bool PAIRS>
-__global__ void __launch_bounds__(kEmbedWaves * 64)
-embed_sum_kernel(SumArgs a)
-{
-    typedef typename Element<IN>::type In;
-    typedef typename Element<OUT>::type Out;
-    constexpr int N = kChunk<In>;
-    const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
-    const int64_t at = (((int64_t)blockIdx.x * kEmbedWaves + (threadIdx.x >> 6)) << (6 - ll)) + (lane >> ll);
-    const int64_t begin = at * a.chunk, end = min(begin + a.chunk, a.n);
-    if (begin >= a.n)
-        return;
-    const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
-    const In *const in = (const In *)a.in + c;
-    const auto token_at = [&](int64_t i) -> int { return PAIRS ? a.pairs[i].token : (int)(a.token[i] >> 1); };
-    const int before = begin > 0 ? token_at(begin - 1) : -1, behind = end < a.n ? token_at(end) : -1;
-    float sum[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        sum[i] = 0.0f;
-    int now = token_at(begin);
-    bool first = true, some = false;
-    const auto mark = [&](int which, bool partial) {
-        if (h == 0 && blockIdx.y == 0)
-            a.next_token[2 * at + which] = (uint32_t)now * 2u + (partial ? 0u : 1u);
-        if (partial)
-            store_chunk<N>(a.next + (2 * at + which) * a.next_stride + c, n, sum);
-    };
-    const auto done = [&](bool last) {                       // the run of `now` ends here, or the chunk does
-        const bool left = first && before == now, right = last && behind == now;
-        if (!left && !right && some) {
-            Out *const out = (Out *)a.out + (int64_t)now * a.out_stride + c;
-            float had[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                had[i] = 0.0f;
-            if (a.accumulate)
-                load_chunk<N>(out, n, had);
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                had[i] += sum[i] * a.scale;
-            store_chunk<N>(out, n, had);
-        }
-        if (first)
-            mark(0, (left || right) && some);
-        if (last)
-            mark(1, !first && right && some);
-    };
-    for (int64_t i0 = begin; i0 < end; i0 += kEmbedAhead) {
-        int token[kEmbedAhead];
-        bool add[kEmbedAhead];
+// The rows of kEmbedAhead list entries, on their way.
+template <class In, bool PAIRS>
+struct SumBatch {
+    int token[kEmbedAhead];
+    bool add[kEmbedAhead];
+    RawChunk<In> x[kEmbedAhead];
+    __device__ __forceinline__ void load(const SumArgs &a, int64_t i0, int64_t end, const In *in, int n)
+    {
         int64_t from[kEmbedAhead];
 #pragma unroll
         for (int u = 0; u < kEmbedAhead; ++u) {
@@ -360,63 +351,160 @@ embed_sum_kernel(SumArgs a)
                 add[u] = i0 + u < end && !(t & 1);
             }
         }
-        float x[kEmbedAhead][N];
 #pragma unroll
         for (int u = 0; u < kEmbedAhead; ++u)
-            load_chunk<N>(in + from[u] * a.in_stride, add[u] ? n : 0, x[u]);
+            x[u].load(in + from[u] * a.in_stride, add[u] ? n : 0);
+    }
+};
+
+// A chunk of the list is added by the lanes of one row, in fp32.  What a workgroup's chunks have of runs that go on beyond
+// them, two sums a chunk at most, meets in LDS, where the lanes of a run's first sum add them up, in 64 bits; what the workgroup
+// has of runs that go on beyond it goes to memory.
+template <int IN, int OUT, bool PAIRS>
+__global__ void __launch_bounds__(kSumWaves * 64)
+embed_sum_kernel(SumArgs a)
+{
+    typedef typename Element<IN>::type In;
+    typedef typename Element<OUT>::type Out;
+    constexpr int N = kChunk<In>;
+    __shared__ uint32_t slot_token[2 * kSumWaves * 64];
+    __shared__ float slot_sum[2 * kSumWaves * 64 * N];
+    const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
+    const int units = kSumWaves << (6 - ll), unit = ((threadIdx.x >> 6) << (6 - ll)) + (lane >> ll), slots = 2 * units;
+    const int64_t group_begin = (int64_t)blockIdx.x * units * a.chunk, group_end = min(group_begin + (int64_t)units * a.chunk, a.n);
+    const int64_t begin = group_begin + (int64_t)unit * a.chunk, end = min(begin + a.chunk, a.n);
+    const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
+    const In *const in = (const In *)a.in + c;
+    const auto token_at = [&](int64_t i) -> int { return PAIRS ? a.pairs[i].token : (int)(a.token[i] >> 1); };
+    // A whole row of the table.
+    const auto put = [&](int token, const float (&sum)[N]) {
+        Out *const out = (Out *)a.out + (int64_t)token * a.out_stride + c;
+        float had[N];
 #pragma unroll
-        for (int u = 0; u < kEmbedAhead; ++u) {
-            if (token[u] != now) {
-                done(false);
-                first = false;
-                some = false;
-                now = token[u];
+        for (int i = 0; i < N; ++i)
+            had[i] = 0.0f;
+        if (a.accumulate)
+            load_chunk<N>(out, n, had);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            had[i] += sum[i] * a.scale;
+        store_chunk<N>(out, n, had);
+    };
+    if (begin < a.n) {
+        const int before = begin > 0 ? token_at(begin - 1) : -1, behind = end < a.n ? token_at(end) : -1;
+        float sum[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            sum[i] = 0.0f;
+        int now = token_at(begin);
+        bool first = true, some = false;
+        const auto mark = [&](int which, bool partial) {
+            if (h == 0)
+                slot_token[2 * unit + which] = (uint32_t)now * 2u + (partial ? 0u : 1u);
+            if (partial)
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    sum[i] = 0.0f;
+                    slot_sum[(((2 * unit + which) << ll) + h) * N + i] = sum[i];
+        };
+        const auto done = [&](bool last) {                       // the run of `now` ends here, or the chunk does
+            const bool left = first && before == now, right = last && behind == now;
+            if (!left && !right && some)
+                put(now, sum);
+            if (first)
+                mark(0, (left || right) && some);
+            if (last)
+                mark(1, !first && right && some);
+        };
+        for (int64_t i0 = begin; i0 < end; i0 += kEmbedAhead) {
+            SumBatch<In, PAIRS> batch;
+            batch.load(a, i0, end, in, n);
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u) {
+                if (batch.token[u] != now) {
+                    done(false);
+                    first = false;
+                    some = false;
+                    now = batch.token[u];
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        sum[i] = 0.0f;
+                }
+                if (batch.add[u]) {
+                    some = true;
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        sum[i] += batch.x[u][i];
+                }
             }
-            if (add[u]) {
+        }
+        done(true);
+    } else if (h == 0) {
+        slot_token[2 * unit] = slot_token[2 * unit + 1] = kNoToken;
+    }
+    __syncthreads();
+    const int before = group_begin > 0 ? token_at(group_begin - 1) : -1, behind = group_end < a.n ? token_at(group_end) : -1;
+    for (int which = 0; which < 2; ++which) {
+        const int s = 2 * unit + which;
+        const uint32_t token = slot_token[s] >> 1;
+        if (s > 0 && slot_token[s - 1] >> 1 == token)
+            continue;                                            // not a run's first sum
+        double all[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            all[i] = 0.0;
+        bool some = false;
+        int e = s;
+        do {
+            if (!(slot_token[e] & 1)) {
                 some = true;
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    sum[i] += x[u][i];
+                    all[i] += (double)slot_sum[((e << ll) + h) * N + i];
             }
-        }
+            ++e;
+        } while (e < slots && slot_token[e] >> 1 == token);
+        const bool left = s == 0 && before == (int)token, right = e == slots && behind == (int)token;
+        float sum[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            sum[i] = (float)all[i];
+        if (!left && !right && some)
+            put((int)token, sum);
+        const auto mark = [&](int at, bool partial) {
+            const int64_t next = 2 * (int64_t)blockIdx.x + at;
+            if (h == 0 && blockIdx.y == 0)
+                a.next_token[next] = token * 2u + (partial ? 0u : 1u);
+            if (partial)
+                store_chunk<N>(a.next + next * a.next_stride + c, n, sum);
+        };
+        if (s == 0)
+            mark(0, (left || right) && some);
+        if (e == slots)
+            mark(1, s != 0 && right && some);
     }
-    done(true);
-}
-
-// Rows that nobody names are 0.
-template <int TYPE>
-__global__ void __launch_bounds__(256)
-embed_clear_kernel(void *table, int64_t n_rows, int32_t width, int64_t stride, int32_t ll)
-{
-    typedef typename Element<TYPE>::type T;
-    constexpr int N = kChunk<T>;
-    const int lane = threadIdx.x & 63, h = lane & ((1 << ll) - 1);
-    const int c = ((int)blockIdx.y * 64 + h) * N;
-    const float zero[N] = {};
-    for (int64_t r = (((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) << (6 - ll)) + (lane >> ll); r < n_rows; r += ((int64_t)gridDim.x * 4) << (6 - ll))
-        store_chunk<N>((T *)table + r * stride + c, width - c, zero);
 }
 
 struct SumPlan {
-    int64_t n[2];                  // rows of partial sums behind the first and the second sum
+    int64_t n[2];                  // partial sums behind the first and the second kernel
     int64_t stride;
     int32_t chunk;
 };
+inline int64_t sum_groups(int64_t n, int32_t chunk, int32_t ll)      // workgroups
+{
+    const int64_t each = ((int64_t)kSumWaves << (6 - ll)) * chunk;
+    return (n + each - 1) / each;
+}
 // More, shorter chunks where there are few pairs to a wavefront: down to kSumLeastChunk for 4096 wavefronts.
-static SumPlan sum_plan(int64_t n, int32_t width)
+static SumPlan sum_plan(int64_t n, int32_t width, int32_t type)
 {
     SumPlan p;
-    const int64_t lanes = (width + 3) / 4;           // of 16 bytes in fp32
+    const int elements = 16 / (int)type_bytes(type), ll = row_lanes_log(width, elements), columns = column_blocks(width, elements);
     p.chunk = kSumMostChunk;
-    while (p.chunk > kSumLeastChunk && n / p.chunk * lanes < 4096 * 64)
+    while (p.chunk > kSumLeastChunk && ((n / p.chunk * columns) << ll) < 4096 * 64)
         p.chunk /= 2;
     p.stride = (width + 3) / 4 * 4;
-    const int64_t chunks = (n + p.chunk - 1) / p.chunk;
-    p.n[0] = chunks > 1 ? 2 * chunks : 2;
-    p.n[1] = 2 * ((p.n[0] + kSumNextChunk - 1) / kSumNextChunk);
+    p.n[0] = 2 * sum_groups(n, p.chunk, ll);
+    p.n[1] = 2 * sum_groups(p.n[0], kSumNextChunk, row_lanes_log(width, kChunk<float>));
     return p;
 }
 
@@ -426,7 +514,7 @@ struct SortPlan {
     SumPlan sum;
     size_t list_bytes, token_bytes[2], sum_bytes[2], bytes;
 };
-static SortPlan sort_plan(int32_t n_vocab, int32_t width, int64_t n)
+static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t n)
 {
     SortPlan p;
     int bits = 1;                                  // of 0 .. n_vocab
@@ -436,7 +524,7 @@ static SortPlan sort_plan(int32_t n_vocab, int32_t width, int64_t n)
     p.passes = (bits + 9) / 10;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.shape = slot_shape(n, 1 << p.bits);
-    p.sum = sum_plan(n, width);
+    p.sum = sum_plan(n, width, type);
     p.list_bytes = ((size_t)n * sizeof(Pair) + 255) / 256 * 256;
     p.bytes = 2 * p.list_bytes + slot_count_bytes(p.shape);
     for (int i = 0; i < 2; ++i) {
@@ -526,11 +614,16 @@ extern "C" int fs_embed(int32_t n_vocab, int32_t width, const void *table, int32
     return launched("embedding kernel launch");
 }
 
-extern "C" size_t fs_embed_backward_workspace_bytes(int32_t n_vocab, int32_t width, int64_t n_rows, int32_t n_cols)
+extern "C" size_t fs_embed_backward_workspace_bytes(int32_t n_vocab, int32_t width, int32_t d_out_type, int64_t n_rows, int32_t n_cols)
 {
-    if (check_embed("fs_embed_backward_workspace_bytes", n_vocab, width, n_rows, n_cols) != FS_OK)
+    static const char who[] = "fs_embed_backward_workspace_bytes";
+    if (check_embed(who, n_vocab, width, n_rows, n_cols) != FS_OK)
         return 0;
-    return sort_plan(n_vocab, width, n_rows * n_cols).bytes;
+    if (!type_ok(d_out_type)) {
+        fail(FS_EINVAL, "%s: unknown element type %d of d_out", who, d_out_type);
+        return 0;
+    }
+    return sort_plan(n_vocab, width, d_out_type, n_rows * n_cols).bytes;
 }
 
 extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_out, int32_t d_out_type, int64_t d_out_stride, int64_t n_rows,
@@ -547,7 +640,7 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
     if (accumulate != 0 && accumulate != 1)
         return fail(FS_EINVAL, "%s: accumulate is %d", who, accumulate);
     const int64_t n = n_rows * n_cols;
-    const SortPlan p = sort_plan(n_vocab, width, n);
+    const SortPlan p = sort_plan(n_vocab, width, d_out_type, n);
     FS_TRY(check_array(who, "work", work, (int64_t)p.bytes, 256));
     if (work_bytes < p.bytes)
         return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, p.bytes);
@@ -567,42 +660,38 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
     }
     int32_t *const count = (int32_t *)at;
     prof_start(kKernTrainOther, stream);
-    if (!accumulate)
-        with_type(d_table_type, [&](auto t) {
-            typedef typename Element<decltype(t)::value>::type T;
-            const int ll = row_lanes_log(width, kChunk<T>);
-            const int64_t rows = (int64_t)4 << (6 - ll), blocks = (n_vocab + rows - 1) / rows;
-            hipLaunchKernelGGL(embed_clear_kernel<decltype(t)::value>,
-                               dim3((unsigned)(blocks < 8192 ? blocks : 8192), (unsigned)column_blocks(width, kChunk<T>)), dim3(256), 0, stream, d_table,
-                               (int64_t)n_vocab, width, d_table_stride, ll);
-        });
+    const ClearArgs clear = {d_table, n_vocab, d_table_stride, d_table_type, width, row_lanes_log(width, 16 / (int)type_bytes(d_table_type))};
+    const int64_t rows = (int64_t)16 << (6 - clear.ll), all = accumulate ? 0 : (n_vocab + rows - 1) / rows;
+    const unsigned blocks = (unsigned)(all < kClearBlocks ? all : kClearBlocks);
+    const bool few = n > 0 && n <= kSlotFew;
+    if (blocks > 0 && !few)
+        hipLaunchKernelGGL(embed_clear_kernel, dim3(blocks), dim3(1024), 0, stream, clear);
     if (n > 0) {
         const int mask = (1 << p.bits) - 1;
         int now = 0;
         with_id_type(id_type, [&](auto type) {
             constexpr int id = decltype(type)::value;
             const IdDigit<id> of = {embed_ids(ids, col_base, n_cols, n_vocab), list[0], mask};
-            if (n <= kSlotFew)
-                hipLaunchKernelGGL(embed_sort_few_kernel<id>, dim3(1), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n, p.token_bits);
+            if (few)
+                hipLaunchKernelGGL(embed_sort_few_kernel<id>, dim3(1 + blocks), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n, p.token_bits, clear);
             else
                 launch_slots(of, p.shape, count, stream);
         });
-        if (n > kSlotFew)
+        if (!few)
             for (int pass = 1; pass < p.passes; ++pass, now ^= 1)
                 launch_slots(PairDigit{list[now], list[now ^ 1], pass * p.bits, mask}, p.shape, count, stream);
         SumArgs a = {list[now], nullptr, d_out, d_out_stride, d_table_stride, n, width, 0, p.sum.chunk, n_vocab, accumulate, scale, d_table,
                      token[0], sum[0], p.sum.stride};
-        const auto grid_of = [&](int chunk_elements) {
-            a.ll = row_lanes_log(width, chunk_elements);
-            const int64_t chunks = (a.n + a.chunk - 1) / a.chunk, each = (int64_t)kEmbedWaves << (6 - a.ll);
-            return dim3((unsigned)((chunks + each - 1) / each), (unsigned)column_blocks(width, chunk_elements));
+        const auto grid_of = [&](int elements) {
+            a.ll = row_lanes_log(width, elements);
+            return dim3((unsigned)sum_groups(a.n, a.chunk, a.ll), (unsigned)column_blocks(width, elements));
         };
         with_types(d_out_type, d_table_type, [&](auto i, auto o) {
             constexpr int in = decltype(i)::value, out = decltype(o)::value;
             dim3 grid = grid_of(kChunk<typename Element<in>::type>);
-            hipLaunchKernelGGL((embed_sum_kernel<in, out, true>), grid, dim3(kEmbedWaves * 64), 0, stream, a);
-            for (int from = 0; a.n > a.chunk; from ^= 1) {
-                a.n = 2 * ((a.n + a.chunk - 1) / a.chunk);
+            hipLaunchKernelGGL((embed_sum_kernel<in, out, true>), grid, dim3(kSumWaves * 64), 0, stream, a);
+            for (int from = 0; grid.x > 1; from ^= 1) {
+                a.n = 2 * (int64_t)grid.x;
                 a.chunk = kSumNextChunk;
                 a.pairs = nullptr;
                 a.token = token[from];
@@ -611,7 +700,7 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
                 a.next_token = token[from ^ 1];
                 a.next = sum[from ^ 1];
                 grid = grid_of(kChunk<float>);
-                hipLaunchKernelGGL((embed_sum_kernel<FS_F32, out, false>), grid, dim3(kEmbedWaves * 64), 0, stream, a);
+                hipLaunchKernelGGL((embed_sum_kernel<FS_F32, out, false>), grid, dim3(kSumWaves * 64), 0, stream, a);
             }
         });
     }

@@ -49,7 +49,7 @@ int main(void) {
     if (strlen(fs_last_error()) == 0) return 2;
     if (fs_expert_plan_workspace_bytes(-1, 1, 1) != 0) return 3;
     if (fs_expert_plan_workspace_bytes(100000, 2, 8) == 0) return 4;
-    if (fs_embed_backward_workspace_bytes(100, 8, 10, 2) == 0) return 5;
+    if (fs_embed_backward_workspace_bytes(100, 8, FS_F32, 10, 2) == 0) return 5;
     printf("ok %d\n", FS_MAX_EXPERTS);
     return 0;
 }
