@@ -16,9 +16,13 @@ constexpr int kEmbedWaves = 4;            // of a workgroup
 constexpr int kEmbedAhead = 8;            // rows on their way at once
 constexpr int kEmbedFewWaves = 2048;
 constexpr int kLookupRows = 4;            // rows of a lane
-constexpr int kSumWaves = 8;              // of a workgroup
+constexpr int kSumMostWaves = 4096;
 constexpr int kSumMostChunk = 256, kSumLeastChunk = 16;   // pairs a chunk
-constexpr int kSumNextChunk = 32;                         // partial sums a chunk
+constexpr int kSumNextChunk = 16;                         // partial sums a chunk
+// Wavefronts of a workgroup and rows on their way at once, for pairs and for partial sums: of these there are few, and all of
+// a chunk come at once.
+template <bool PAIRS> constexpr int kSumWaves = PAIRS ? 8 : 16;
+template <bool PAIRS> constexpr int kSumAhead = PAIRS ? 8 : 16;
 
 template <int ID> struct IdOf;
 template <> struct IdOf<FS_ID_I32> { typedef int32_t type; };
@@ -185,44 +189,63 @@ embed_lookup_kernel(EmbedArgs a)
 
 // ---- sorting by token, the lowest digit first: the first pass takes ids, the others what the pass before left ------------
 
+// A token and the row that named it, in 32 bits where both fit, which halves what sorting moves.
 struct Pair {
     int32_t token, row;
 };
-template <int ID>
+struct Packing {                   // of 32 bits: how many are the row's
+    int32_t row_bits;
+};
+template <class P> __device__ __forceinline__ P make_pair(const Packing &k, int token, uint32_t row);
+template <> __device__ __forceinline__ Pair make_pair<Pair>(const Packing &, int token, uint32_t row) { return Pair{token, (int32_t)row}; }
+template <> __device__ __forceinline__ uint32_t make_pair<uint32_t>(const Packing &k, int token, uint32_t row) { return (uint32_t)token << k.row_bits | row; }
+__device__ __forceinline__ int token_of(const Packing &, const Pair &p) { return p.token; }
+__device__ __forceinline__ int token_of(const Packing &k, uint32_t p) { return (int)(p >> k.row_bits); }
+__device__ __forceinline__ uint32_t row_of(const Packing &, const Pair &p) { return (uint32_t)p.row; }
+__device__ __forceinline__ uint32_t row_of(const Packing &k, uint32_t p) { return p & ((1u << k.row_bits) - 1u); }
+
+template <int ID, class P>
 struct IdDigit {
-    typedef Pair Item;
+    typedef P Item, What;
     EmbedIds ids;
-    Pair *to;
+    P *to;
     int32_t mask;
+    Packing packing;
     template <int N>
-    __device__ __forceinline__ void load(Pair (&item)[N], int64_t i, int64_t end) const
+    __device__ __forceinline__ void load(P (&item)[N], int64_t i, int64_t end) const
     {
-        int row[N];
+        int token[N];
         const auto entry = [&](int u) { return (uint32_t)min(i + u * 64, end - 1); };
-        ids.template rows<ID>(row, entry, [&](int u) { return entry(u) - ids.row_of(entry(u)) * (uint32_t)ids.n_cols; });
+        ids.template rows<ID>(token, entry, [&](int u) { return entry(u) - ids.row_of(entry(u)) * (uint32_t)ids.n_cols; });
 #pragma unroll
         for (int u = 0; u < N; ++u)
-            item[u] = Pair{row[u] < 0 ? ids.n_vocab : row[u], (int32_t)ids.row_of(entry(u))};
+            item[u] = make_pair<P>(packing, token[u] < 0 ? ids.n_vocab : token[u], ids.row_of(entry(u)));
     }
-    __device__ __forceinline__ int number(const Pair &p) const { return p.token & mask; }
+    __device__ __forceinline__ int number(const P &p) const { return token_of(packing, p) & mask; }
     __device__ __forceinline__ void start(int, int) const {}
-    __device__ __forceinline__ void put(const Pair &p, int64_t, int, int slot) const { to[slot] = p; }
+    __device__ __forceinline__ void place(int64_t, int, int) const {}
+    __device__ __forceinline__ P what(const P &p, int64_t) const { return p; }
+    __device__ __forceinline__ void put(const P &p, int, int slot) const { to[slot] = p; }
 };
+template <class P>
 struct PairDigit {
-    typedef Pair Item;
-    const Pair *from;
-    Pair *to;
+    typedef P Item, What;
+    const P *from;
+    P *to;
     int32_t shift, mask;
+    Packing packing;
     template <int N>
-    __device__ __forceinline__ void load(Pair (&item)[N], int64_t i, int64_t end) const
+    __device__ __forceinline__ void load(P (&item)[N], int64_t i, int64_t end) const
     {
 #pragma unroll
         for (int u = 0; u < N; ++u)
             item[u] = from[min(i + u * 64, end - 1)];
     }
-    __device__ __forceinline__ int number(const Pair &p) const { return (p.token >> shift) & mask; }
+    __device__ __forceinline__ int number(const P &p) const { return (token_of(packing, p) >> shift) & mask; }
     __device__ __forceinline__ void start(int, int) const {}
-    __device__ __forceinline__ void put(const Pair &p, int64_t, int, int slot) const { to[slot] = p; }
+    __device__ __forceinline__ void place(int64_t, int, int) const {}
+    __device__ __forceinline__ P what(const P &p, int64_t) const { return p; }
+    __device__ __forceinline__ void put(const P &p, int, int slot) const { to[slot] = p; }
 };
 
 // Rows that nobody names are 0: what block b of `blocks` clears.
@@ -256,9 +279,9 @@ constexpr int kClearBlocks = 2047;
 // All digits of up to kSlotFew entries in one workgroup.  LDS holds the tokens where the entries are and the entries' numbers
 // in the order so far, which a pass takes to registers and puts back.  The launch's other workgroups clear the table meanwhile.
 constexpr int kFewDigitBits = 9;
-template <int ID>
+template <int ID, class P>
 __global__ void __launch_bounds__(kSlotFewWaves * 64)
-embed_sort_few_kernel(IdDigit<ID> source, int32_t n, int32_t bits, ClearArgs clear)
+embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits, ClearArgs clear)
 {
     if (blockIdx.x > 0) {
         clear_table(clear, blockIdx.x - 1, gridDim.x - 1);
@@ -269,13 +292,13 @@ embed_sort_few_kernel(IdDigit<ID> source, int32_t n, int32_t bits, ClearArgs cle
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int steps = (n + kSlotFewWaves * 64 - 1) / (kSlotFewWaves * 64);
     const int begin = wave * steps * 64 + lane;
-    Pair item[kSlotFewPer];
+    P item[kSlotFewPer];
     source.load(item, begin, n);
 #pragma unroll
     for (int u = 0; u < kSlotFewPer; ++u) {
         const int i = begin + u * 64;
         if (u < steps && i < n) {
-            token[i] = item[u].token;
+            token[i] = token_of(source.packing, item[u]);
             order[i] = (uint16_t)i;
         }
     }
@@ -307,15 +330,15 @@ embed_sort_few_kernel(IdDigit<ID> source, int32_t n, int32_t bits, ClearArgs cle
     }
     for (int s = threadIdx.x; s < n; s += kSlotFewWaves * 64) {
         const int i = order[s];
-        source.to[s] = Pair{token[i], (int32_t)source.ids.row_of((uint32_t)i)};
+        source.to[s] = make_pair<P>(source.packing, token[i], source.ids.row_of((uint32_t)i));
     }
 }
 
 // ---- sums of the runs -----------------------------------------------------------------------------------------------------
 
 struct SumArgs {
-    const Pair *pairs;             // the list, or
-    const uint32_t *token;         // partial sums: token * 2, + 1 where there is nothing to add
+    const void *list;              // pairs; of partial sums: token * 2, + 1 where there is nothing to add
+    Packing packing;
     const void *in;
     int64_t in_stride, out_stride, n;
     int32_t width, ll, chunk, n_vocab, accumulate;
@@ -326,33 +349,37 @@ struct SumArgs {
     int64_t next_stride;
 };
 constexpr uint32_t kNoToken = 0xffffffffu;
+struct PartialSum {};              // in the place of a pair's type
+template <class P> constexpr bool kIsPairs = true;
+template <> constexpr bool kIsPairs<PartialSum> = false;
 
-// The rows of kEmbedAhead list entries, on their way.
-template <class In, bool PAIRS>
+// The rows of some list entries, on their way.
+template <class In, class P>
 struct SumBatch {
-    int token[kEmbedAhead];
-    bool add[kEmbedAhead];
-    RawChunk<In> x[kEmbedAhead];
+    static constexpr bool PAIRS = kIsPairs<P>;
+    int token[kSumAhead<PAIRS>];
+    bool add[kSumAhead<PAIRS>];
+    RawChunk<In> x[kSumAhead<PAIRS>];
     __device__ __forceinline__ void load(const SumArgs &a, int64_t i0, int64_t end, const In *in, int n)
     {
-        int64_t from[kEmbedAhead];
+        int64_t from[kSumAhead<PAIRS>];
 #pragma unroll
-        for (int u = 0; u < kEmbedAhead; ++u) {
+        for (int u = 0; u < kSumAhead<PAIRS>; ++u) {
             const int64_t i = min(i0 + u, end - 1);
             if constexpr (PAIRS) {
-                const Pair p = a.pairs[i];
-                token[u] = p.token;
-                from[u] = p.row;
-                add[u] = i0 + u < end && p.token < a.n_vocab;
+                const P p = ((const P *)a.list)[i];
+                token[u] = token_of(a.packing, p);
+                from[u] = row_of(a.packing, p);
+                add[u] = i0 + u < end && token[u] < a.n_vocab;
             } else {
-                const uint32_t t = a.token[i];
+                const uint32_t t = ((const uint32_t *)a.list)[i];
                 token[u] = (int)(t >> 1);
                 from[u] = i;
                 add[u] = i0 + u < end && !(t & 1);
             }
         }
 #pragma unroll
-        for (int u = 0; u < kEmbedAhead; ++u)
+        for (int u = 0; u < kSumAhead<PAIRS>; ++u)
             x[u].load(in + from[u] * a.in_stride, add[u] ? n : 0);
     }
 };
@@ -360,22 +387,28 @@ struct SumBatch {
 // A chunk of the list is added by the lanes of one row, in fp32.  What a workgroup's chunks have of runs that go on beyond
 // them, two sums a chunk at most, meets in LDS, where the lanes of a run's first sum add them up, in 64 bits; what the workgroup
 // has of runs that go on beyond it goes to memory.
-template <int IN, int OUT, bool PAIRS>
-__global__ void __launch_bounds__(kSumWaves * 64)
+template <int IN, int OUT, class P>
+__global__ void __launch_bounds__(kSumWaves<kIsPairs<P>> * 64)
 embed_sum_kernel(SumArgs a)
 {
+    constexpr bool PAIRS = kIsPairs<P>;
     typedef typename Element<IN>::type In;
     typedef typename Element<OUT>::type Out;
     constexpr int N = kChunk<In>;
-    __shared__ uint32_t slot_token[2 * kSumWaves * 64];
-    __shared__ float slot_sum[2 * kSumWaves * 64 * N];
+    __shared__ uint32_t slot_token[2 * kSumWaves<PAIRS> * 64];
+    __shared__ float slot_sum[2 * kSumWaves<PAIRS> * 64 * N];
     const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
-    const int units = kSumWaves << (6 - ll), unit = ((threadIdx.x >> 6) << (6 - ll)) + (lane >> ll), slots = 2 * units;
+    const int units = kSumWaves<PAIRS> << (6 - ll), unit = ((threadIdx.x >> 6) << (6 - ll)) + (lane >> ll), slots = 2 * units;
     const int64_t group_begin = (int64_t)blockIdx.x * units * a.chunk, group_end = min(group_begin + (int64_t)units * a.chunk, a.n);
     const int64_t begin = group_begin + (int64_t)unit * a.chunk, end = min(begin + a.chunk, a.n);
     const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
     const In *const in = (const In *)a.in + c;
-    const auto token_at = [&](int64_t i) -> int { return PAIRS ? a.pairs[i].token : (int)(a.token[i] >> 1); };
+    const auto token_at = [&](int64_t i) -> int {
+        if constexpr (PAIRS)
+            return token_of(a.packing, ((const P *)a.list)[i]);
+        else
+            return (int)(((const uint32_t *)a.list)[i] >> 1);
+    };
     // A whole row of the table.
     const auto put = [&](int token, const float (&sum)[N]) {
         Out *const out = (Out *)a.out + (int64_t)token * a.out_stride + c;
@@ -415,11 +448,11 @@ embed_sum_kernel(SumArgs a)
             if (last)
                 mark(1, !first && right && some);
         };
-        for (int64_t i0 = begin; i0 < end; i0 += kEmbedAhead) {
-            SumBatch<In, PAIRS> batch;
+        for (int64_t i0 = begin; i0 < end; i0 += kSumAhead<PAIRS>) {
+            SumBatch<In, P> batch;
             batch.load(a, i0, end, in, n);
 #pragma unroll
-            for (int u = 0; u < kEmbedAhead; ++u) {
+            for (int u = 0; u < kSumAhead<PAIRS>; ++u) {
                 if (batch.token[u] != now) {
                     done(false);
                     first = false;
@@ -489,33 +522,37 @@ struct SumPlan {
     int64_t stride;
     int32_t chunk;
 };
-inline int64_t sum_groups(int64_t n, int32_t chunk, int32_t ll)      // workgroups
+template <bool PAIRS>
+int64_t sum_groups(int64_t n, int32_t chunk, int32_t ll)      // workgroups
 {
-    const int64_t each = ((int64_t)kSumWaves << (6 - ll)) * chunk;
+    const int64_t each = ((int64_t)kSumWaves<PAIRS> << (6 - ll)) * chunk;
     return (n + each - 1) / each;
 }
-// More, shorter chunks where there are few pairs to a wavefront: down to kSumLeastChunk for 4096 wavefronts.
+// More, shorter chunks where there are few pairs to a wavefront: down to kSumLeastChunk for kSumMostWaves.
 static SumPlan sum_plan(int64_t n, int32_t width, int32_t type)
 {
     SumPlan p;
     const int elements = 16 / (int)type_bytes(type), ll = row_lanes_log(width, elements), columns = column_blocks(width, elements);
     p.chunk = kSumMostChunk;
-    while (p.chunk > kSumLeastChunk && ((n / p.chunk * columns) << ll) < 4096 * 64)
+    while (p.chunk > kSumLeastChunk && ((n / p.chunk * columns) << ll) < (int64_t)kSumMostWaves * 64)
         p.chunk /= 2;
     p.stride = (width + 3) / 4 * 4;
-    p.n[0] = 2 * sum_groups(n, p.chunk, ll);
-    p.n[1] = 2 * sum_groups(p.n[0], kSumNextChunk, row_lanes_log(width, kChunk<float>));
+    p.n[0] = 2 * sum_groups<true>(n, p.chunk, ll);
+    p.n[1] = 2 * sum_groups<false>(p.n[0], kSumNextChunk, row_lanes_log(width, kChunk<float>));
     return p;
 }
 
 struct SortPlan {
     int token_bits, passes, bits;      // of all digits, of one
+    Packing packing;
+    bool packed;
     SlotShape shape;
     SumPlan sum;
     size_t list_bytes, token_bytes[2], sum_bytes[2], bytes;
 };
-static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t n)
+static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t n_rows, int32_t n_cols)
 {
+    const int64_t n = n_rows * n_cols;
     SortPlan p;
     int bits = 1;                                  // of 0 .. n_vocab
     while (((int64_t)1 << bits) <= n_vocab)
@@ -523,9 +560,11 @@ static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t 
     p.token_bits = bits;
     p.passes = (bits + 9) / 10;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.shape = slot_shape(n, 1 << p.bits);
     p.sum = sum_plan(n, width, type);
-    p.list_bytes = ((size_t)n * sizeof(Pair) + 255) / 256 * 256;
+    p.packing.row_bits = bits_of((int)n_rows);
+    p.packed = p.packing.row_bits + bits <= 32 && p.packing.row_bits < 32;
+    p.shape = slot_shape(n, 1 << p.bits, p.packed ? sizeof(uint32_t) : sizeof(Pair));
+    p.list_bytes = ((size_t)n * (p.packed ? sizeof(uint32_t) : sizeof(Pair)) + 255) / 256 * 256;
     p.bytes = 2 * p.list_bytes + slot_count_bytes(p.shape);
     for (int i = 0; i < 2; ++i) {
         p.token_bytes[i] = ((size_t)p.sum.n[i] * 4 + 255) / 256 * 256;
@@ -623,7 +662,7 @@ extern "C" size_t fs_embed_backward_workspace_bytes(int32_t n_vocab, int32_t wid
         fail(FS_EINVAL, "%s: unknown element type %d of d_out", who, d_out_type);
         return 0;
     }
-    return sort_plan(n_vocab, width, d_out_type, n_rows * n_cols).bytes;
+    return sort_plan(n_vocab, width, d_out_type, n_rows, n_cols).bytes;
 }
 
 extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_out, int32_t d_out_type, int64_t d_out_stride, int64_t n_rows,
@@ -640,7 +679,7 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
     if (accumulate != 0 && accumulate != 1)
         return fail(FS_EINVAL, "%s: accumulate is %d", who, accumulate);
     const int64_t n = n_rows * n_cols;
-    const SortPlan p = sort_plan(n_vocab, width, d_out_type, n);
+    const SortPlan p = sort_plan(n_vocab, width, d_out_type, n_rows, n_cols);
     FS_TRY(check_array(who, "work", work, (int64_t)p.bytes, 256));
     if (work_bytes < p.bytes)
         return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, p.bytes);
@@ -650,11 +689,11 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
         at += bytes;
         return here;
     };
-    Pair *list[2];
+    void *list[2];
     uint32_t *token[2];
     float *sum[2];
     for (int i = 0; i < 2; ++i) {
-        list[i] = (Pair *)take(p.list_bytes);
+        list[i] = take(p.list_bytes);
         token[i] = (uint32_t *)take(p.token_bytes[i]);
         sum[i] = (float *)take(p.sum_bytes[i]);
     }
@@ -669,38 +708,49 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
     if (n > 0) {
         const int mask = (1 << p.bits) - 1;
         int now = 0;
-        with_id_type(id_type, [&](auto type) {
-            constexpr int id = decltype(type)::value;
-            const IdDigit<id> of = {embed_ids(ids, col_base, n_cols, n_vocab), list[0], mask};
-            if (few)
-                hipLaunchKernelGGL(embed_sort_few_kernel<id>, dim3(1 + blocks), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n, p.token_bits, clear);
-            else
-                launch_slots(of, p.shape, count, stream);
-        });
-        if (!few)
-            for (int pass = 1; pass < p.passes; ++pass, now ^= 1)
-                launch_slots(PairDigit{list[now], list[now ^ 1], pass * p.bits, mask}, p.shape, count, stream);
-        SumArgs a = {list[now], nullptr, d_out, d_out_stride, d_table_stride, n, width, 0, p.sum.chunk, n_vocab, accumulate, scale, d_table,
+        const auto sort = [&](auto pair) {
+            typedef decltype(pair) P;
+            P *const lists[2] = {(P *)list[0], (P *)list[1]};
+            with_id_type(id_type, [&](auto type) {
+                constexpr int id = decltype(type)::value;
+                const IdDigit<id, P> of = {embed_ids(ids, col_base, n_cols, n_vocab), lists[0], mask, p.packing};
+                if (few)
+                    hipLaunchKernelGGL((embed_sort_few_kernel<id, P>), dim3(1 + blocks), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n,
+                                       p.token_bits, clear);
+                else
+                    launch_slots(of, p.shape, count, stream);
+            });
+            if (!few)
+                for (int pass = 1; pass < p.passes; ++pass, now ^= 1)
+                    launch_slots(PairDigit<P>{lists[now], lists[now ^ 1], pass * p.bits, mask, p.packing}, p.shape, count, stream);
+        };
+        if (p.packed)
+            sort(uint32_t());
+        else
+            sort(Pair());
+        SumArgs a = {list[now], p.packing, d_out, d_out_stride, d_table_stride, n, width, 0, p.sum.chunk, n_vocab, accumulate, scale, d_table,
                      token[0], sum[0], p.sum.stride};
-        const auto grid_of = [&](int elements) {
+        const auto grid_of = [&](auto pairs, int elements) {
             a.ll = row_lanes_log(width, elements);
-            return dim3((unsigned)sum_groups(a.n, a.chunk, a.ll), (unsigned)column_blocks(width, elements));
+            return dim3((unsigned)sum_groups<decltype(pairs)::value != 0>(a.n, a.chunk, a.ll), (unsigned)column_blocks(width, elements));
         };
         with_types(d_out_type, d_table_type, [&](auto i, auto o) {
             constexpr int in = decltype(i)::value, out = decltype(o)::value;
-            dim3 grid = grid_of(kChunk<typename Element<in>::type>);
-            hipLaunchKernelGGL((embed_sum_kernel<in, out, true>), grid, dim3(kSumWaves * 64), 0, stream, a);
+            dim3 grid = grid_of(TypeTag<1>(), kChunk<typename Element<in>::type>);
+            if (p.packed)
+                hipLaunchKernelGGL((embed_sum_kernel<in, out, uint32_t>), grid, dim3(kSumWaves<true> * 64), 0, stream, a);
+            else
+                hipLaunchKernelGGL((embed_sum_kernel<in, out, Pair>), grid, dim3(kSumWaves<true> * 64), 0, stream, a);
             for (int from = 0; grid.x > 1; from ^= 1) {
                 a.n = 2 * (int64_t)grid.x;
                 a.chunk = kSumNextChunk;
-                a.pairs = nullptr;
-                a.token = token[from];
+                a.list = token[from];
                 a.in = sum[from];
                 a.in_stride = p.sum.stride;
                 a.next_token = token[from ^ 1];
                 a.next = sum[from ^ 1];
-                grid = grid_of(kChunk<float>);
-                hipLaunchKernelGGL((embed_sum_kernel<FS_F32, out, false>), grid, dim3(kSumWaves * 64), 0, stream, a);
+                grid = grid_of(TypeTag<0>(), kChunk<float>);
+                hipLaunchKernelGGL((embed_sum_kernel<FS_F32, out, PartialSum>), grid, dim3(kSumWaves<false> * 64), 0, stream, a);
             }
         });
     }

@@ -4,9 +4,9 @@
 namespace fs {
 
 struct Choices {
-    typedef int32_t Item;
+    typedef int32_t Item, What;
     const int32_t *expert;
-    int32_t *first, *order, *place;
+    int32_t *first, *order, *places;
     int32_t n_experts;
     template <int N>
     __device__ __forceinline__ void load(int32_t (&item)[N], int64_t i, int64_t end) const
@@ -17,11 +17,9 @@ struct Choices {
     }
     __device__ __forceinline__ int number(int32_t e) const { return e >= 0 && e < n_experts ? e : n_experts; }
     __device__ __forceinline__ void start(int e, int slot) const { first[e] = slot; }
-    __device__ __forceinline__ void put(int32_t, int64_t i, int e, int slot) const
-    {
-        order[slot] = e < n_experts ? (int32_t)i : -1;
-        place[i] = e < n_experts ? slot : -1;
-    }
+    __device__ __forceinline__ int32_t what(int32_t, int64_t i) const { return (int32_t)i; }
+    __device__ __forceinline__ void place(int64_t i, int e, int slot) const { places[i] = e < n_experts ? slot : -1; }
+    __device__ __forceinline__ void put(int32_t i, int e, int slot) const { order[slot] = e < n_experts ? i : -1; }
 };
 
 // No choices: no slots.
@@ -214,7 +212,7 @@ extern "C" size_t fs_expert_plan_workspace_bytes(int64_t n_tokens, int32_t k, in
     static const char who[] = "fs_expert_plan_workspace_bytes";
     if (check_tokens(who, n_tokens, k) != FS_OK || check_experts(who, n_experts) != FS_OK)
         return 0;
-    return slot_count_bytes(slot_shape(n_tokens * k, n_experts + 1));
+    return slot_count_bytes(slot_shape(n_tokens * k, n_experts + 1, sizeof(Choices::What)));
 }
 
 extern "C" int fs_expert_plan(int64_t n_tokens, int32_t k, int32_t n_experts, const int32_t *expert, int32_t *first, int32_t *order,
@@ -228,7 +226,7 @@ extern "C" int fs_expert_plan(int64_t n_tokens, int32_t k, int32_t n_experts, co
     FS_TRY(check_array(who, "first", first, 1, 4));
     FS_TRY(check_array(who, "order", order, n_tokens, 4));
     FS_TRY(check_array(who, "place", place, n_tokens, 4));
-    const SlotShape s = slot_shape(n_tokens * k, n_experts + 1);
+    const SlotShape s = slot_shape(n_tokens * k, n_experts + 1, sizeof(Choices::What));
     const size_t need = slot_count_bytes(s);
     FS_TRY(check_array(who, "work", work, (int64_t)need, 256));
     if (work_bytes < need)

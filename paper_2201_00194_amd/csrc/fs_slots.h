@@ -1,10 +1,12 @@
-// A stable counting sort of n entries by a number below `buckets`.  Long lists take three kernels: every wavefront counts the
-// numbers in its stretch of entries; a number's counts are summed along the stretches; every wavefront places its stretch's
-// entries.  Up to kSlotFew entries are one workgroup's, in one kernel.  No atomics on memory, and the same result
-// whatever runs first.  Used for the slots of experts and for the table's gradient.
+// A stable counting sort of n entries by a number below `buckets`.  Long lists take three kernels: every workgroup counts the
+// numbers in its stretch of entries; a number's counts are summed along the stretches; every workgroup places its stretch's
+// entries, a tile after the other, which it puts in order in LDS so that they leave in runs.  Up to kSlotFew entries are
+// one workgroup's, in one kernel.  No atomics on memory, and the same result whatever runs first.  Used for the slots of
+// experts and for the table's gradient.
 //
 // A Source says what the entries are: load(items, i) takes entries i, i + 64, ... (the last one, where that is past it), int
-// number(item), put(item, i, number, slot), and start(number, slot of its first), called once for every number.
+// number(item), place(i, number, slot) tells where entry i goes, put(what(item, i), number, slot) puts it there, and start(number, slot
+// of its first) is called once for every number.
 #ifndef FS_SLOTS_H
 #define FS_SLOTS_H
 
@@ -12,36 +14,46 @@
 
 namespace fs {
 
-constexpr int kSlotWaves = 4;               // of a workgroup
+constexpr int kSlotWaves = 8;               // of a workgroup
+constexpr int kSlotThreads = kSlotWaves * 64;
 constexpr int kSlotMostBuckets = 1025;      // experts, and one for choices without a slot
 constexpr int kSlotMostBits = 11;
-constexpr int kSlotMostStretches = 4096;
+constexpr int kSlotMostPer = 8;             // entries of a lane in a tile
+constexpr int kSlotManyGroups = 512;
+constexpr int kSlotMostGroups = 2048;
 constexpr int kSlotScanThreads = 256;
-constexpr int kSlotScanPer = kSlotMostStretches / kSlotScanThreads;
-constexpr int kSlotAhead = 8;               // loads of a lane on their way at once
+constexpr int kSlotScanPer = kSlotMostGroups / kSlotScanThreads;
 constexpr int kSlotFew = 16384;
 constexpr int kSlotFewWaves = 16;
 constexpr int kSlotFewPer = kSlotFew / (kSlotFewWaves * 64);
 
 struct SlotShape {
-    int32_t n, buckets, stretch, stretches;
+    int32_t n, buckets, per, tiles, groups;      // groups of `tiles` tiles of per * kSlotThreads entries
 };
-// Stretches as short as 128 entries, for as many wavefronts, but not shorter than the numbers are many: the counts then
-// are no more than the entries.
-inline SlotShape slot_shape(int64_t n, int buckets)
+constexpr size_t slot_place_bytes(int per, int buckets, int what_bytes)
 {
-    SlotShape s = {(int32_t)n, buckets, 0, 0};
-    int64_t stretch = (n + kSlotMostStretches - 1) / kSlotMostStretches;
-    stretch = stretch < buckets ? buckets : stretch;
-    stretch = stretch < 128 ? 128 : stretch;
-    s.stretch = (int32_t)((stretch + 63) / 64 * 64);
-    s.stretches = (int32_t)((n + s.stretch - 1) / s.stretch);
+    return (size_t)per * kSlotThreads * (what_bytes + 2) + ((size_t)(kSlotWaves + 2) * buckets + kSlotWaves) * 4;
+}
+// Tiles short enough for kSlotManyGroups workgroups, but not shorter than the numbers are many: the counts then are no more
+// than the entries.  A tile and its counts stay within 64 KB of LDS.  what_bytes: of what a tile puts in order.
+inline SlotShape slot_shape(int64_t n, int buckets, int what_bytes)
+{
+    SlotShape s = {(int32_t)n, buckets, 0, 0, 0};
+    int64_t per = (n + kSlotThreads * kSlotManyGroups - 1) / (kSlotThreads * kSlotManyGroups);
+    const int64_t least = (buckets + kSlotThreads - 1) / kSlotThreads;
+    per = per < least ? least : per;
+    s.per = (int32_t)(per < 1 ? 1 : per > kSlotMostPer ? kSlotMostPer : per);
+    while (s.per > 1 && slot_place_bytes(s.per, buckets, what_bytes) > 65536)
+        --s.per;
+    const int64_t tiles = (n + s.per * kSlotThreads - 1) / (s.per * kSlotThreads);
+    s.tiles = (int32_t)((tiles + kSlotMostGroups - 1) / kSlotMostGroups);
+    s.groups = s.tiles ? (int32_t)((tiles + s.tiles - 1) / s.tiles) : 0;
     return s;
 }
 // The counts, and behind them every number's total.
 inline size_t slot_count_bytes(const SlotShape &s)
 {
-    return s.n <= kSlotFew ? 0 : ((size_t)s.buckets * (s.stretches + 1) * 4 + 255) / 256 * 256;
+    return s.n <= kSlotFew ? 0 : ((size_t)s.buckets * (s.groups + 1) * 4 + 255) / 256 * 256;
 }
 
 // The lanes whose number is this lane's, among the lanes that are there.
@@ -64,7 +76,7 @@ __device__ __forceinline__ uint64_t same_number(int number, int bits, bool there
 __host__ __device__ inline int bits_of(int n)        // of numbers below n
 {
     int b = 0;
-    while ((1 << b) < n)
+    while (b < 31 && (1 << b) < n)
         ++b;
     return b;
 }
@@ -98,32 +110,35 @@ __device__ __forceinline__ int32_t wave_inclusive_sum(int32_t v, int lane)
     return v;
 }
 
-// count[number * stretches + stretch]
+// count[number * groups + group]
 template <class Source>
-__global__ void __launch_bounds__(kSlotWaves * 64)
+__global__ void __launch_bounds__(kSlotThreads)
 slot_count_kernel(Source source, SlotShape s, int32_t *count)
 {
-    __shared__ int32_t lds[kSlotWaves * kSlotMostBuckets];
+    extern __shared__ int32_t slot_lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int mine = (int)blockIdx.x * kSlotWaves + wave;
-    int32_t *c = lds + wave * s.buckets;
-    for (int b = lane; b < s.buckets; b += 64)
-        c[b] = 0;
-    lds_sync();
-    if (mine >= s.stretches)
-        return;
-    const int64_t begin = (int64_t)mine * s.stretch, end = min(begin + s.stretch, (int64_t)s.n);
-    for (int64_t i0 = begin; i0 < end; i0 += kSlotAhead * 64) {
-        typename Source::Item item[kSlotAhead];
+    for (int b = threadIdx.x; b < kSlotWaves * s.buckets; b += kSlotThreads)
+        slot_lds[b] = 0;
+    __syncthreads();
+    int32_t *const c = slot_lds + wave * s.buckets;
+    const int64_t begin = (int64_t)blockIdx.x * s.tiles * s.per * kSlotThreads;
+    const int64_t end = min(begin + (int64_t)s.tiles * s.per * kSlotThreads, (int64_t)s.n);
+    for (int64_t i0 = begin + wave * kSlotMostPer * 64; i0 < end; i0 += kSlotMostPer * kSlotThreads) {
+        typename Source::Item item[kSlotMostPer];
         source.load(item, i0 + lane, end);
 #pragma unroll
-        for (int u = 0; u < kSlotAhead; ++u)
+        for (int u = 0; u < kSlotMostPer; ++u)
             if (i0 + u * 64 + lane < end)
                 atomicAdd(&c[source.number(item[u])], 1);
     }
-    lds_sync();
-    for (int b = lane; b < s.buckets; b += 64)
-        count[(int64_t)b * s.stretches + mine] = c[b];
+    __syncthreads();
+    for (int b = threadIdx.x; b < s.buckets; b += kSlotThreads) {
+        int32_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < kSlotWaves; ++w)
+            sum += slot_lds[w * s.buckets + b];
+        count[(int64_t)b * s.groups + blockIdx.x] = sum;
+    }
 }
 
 // A workgroup a number: its counts become the sums of those before them, and their total goes behind all counts.
@@ -132,12 +147,12 @@ slot_scan_kernel(int32_t *count, SlotShape s)
 {
     __shared__ int32_t wave_total[kSlotScanThreads / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int32_t *const row = count + (int64_t)blockIdx.x * s.stretches;
-    const int per = (s.stretches + kSlotScanThreads - 1) / kSlotScanThreads, first = threadIdx.x * per;
+    int32_t *const row = count + (int64_t)blockIdx.x * s.groups;
+    const int per = (s.groups + kSlotScanThreads - 1) / kSlotScanThreads, first = threadIdx.x * per;
     int32_t v[kSlotScanPer], sum = 0;
 #pragma unroll
     for (int i = 0; i < kSlotScanPer; ++i) {
-        v[i] = i < per && first + i < s.stretches ? row[first + i] : 0;
+        v[i] = i < per && first + i < s.groups ? row[first + i] : 0;
         sum += v[i];
     }
     const int32_t upto = wave_inclusive_sum(sum, lane);
@@ -152,28 +167,25 @@ slot_scan_kernel(int32_t *count, SlotShape s)
     }
 #pragma unroll
     for (int i = 0; i < kSlotScanPer; ++i) {
-        if (i < per && first + i < s.stretches)
+        if (i < per && first + i < s.groups)
             row[first + i] = at;
         at += v[i];
     }
     if (threadIdx.x == 0)
-        count[(int64_t)s.buckets * s.stretches + blockIdx.x] = total;
+        count[(int64_t)s.buckets * s.groups + blockIdx.x] = total;
 }
 
-template <class Source>
-__global__ void __launch_bounds__(kSlotWaves * 64)
-slot_place_kernel(Source source, SlotShape s, const int32_t *count)
+// f(number, sum of value(numbers before it)) by all threads of a workgroup of kSlotThreads; a barrier at the end.
+template <class V, class F>
+__device__ __forceinline__ void over_numbers(int buckets, int32_t *wave_total, V value, F f)
 {
-    constexpr int kThreads = kSlotWaves * 64, kPer = (kSlotMostBuckets + kThreads - 1) / kThreads;
-    __shared__ int32_t lds[kSlotWaves * kSlotMostBuckets], base[kSlotMostBuckets], wave_total[kSlotWaves];
+    constexpr int kPer = (kSlotMostBuckets + kSlotThreads - 1) / kSlotThreads;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int mine = (int)blockIdx.x * kSlotWaves + wave;
-    const int32_t *const total = count + (int64_t)s.buckets * s.stretches;
-    const int first = threadIdx.x * kPer;
+    const int per = (buckets + kSlotThreads - 1) / kSlotThreads, first = threadIdx.x * per;
     int32_t v[kPer], sum = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        v[i] = first + i < s.buckets ? total[first + i] : 0;
+        v[i] = i < per && first + i < buckets ? value(first + i) : 0;
         sum += v[i];
     }
     const int32_t upto = wave_inclusive_sum(sum, lane);
@@ -181,40 +193,85 @@ slot_place_kernel(Source source, SlotShape s, const int32_t *count)
         wave_total[wave] = upto;
     __syncthreads();
     int32_t at = upto - sum;
-#pragma unroll
-    for (int w = 0; w < kSlotWaves; ++w)
-        at += w < wave ? wave_total[w] : 0;
+    for (int w = 0; w < wave; ++w)
+        at += wave_total[w];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        if (first + i < s.buckets) {
-            base[first + i] = at;
-            if (blockIdx.x == 0)
-                source.start(first + i, at);
-        }
+        if (i < per && first + i < buckets)
+            f(first + i, at);
         at += v[i];
     }
     __syncthreads();
-    if (mine >= s.stretches)
-        return;
-    int32_t *next = lds + wave * s.buckets;
-    for (int b = lane; b < s.buckets; b += 64)
-        next[b] = base[b] + count[(int64_t)b * s.stretches + mine];
-    lds_sync();
-    const int bits = bits_of(s.buckets);
-    const int64_t begin = (int64_t)mine * s.stretch, end = min(begin + s.stretch, (int64_t)s.n);
-    for (int64_t i0 = begin; i0 < end; i0 += kSlotAhead * 64) {
-        typename Source::Item item[kSlotAhead];
-        source.load(item, i0 + lane, end);
+}
+
+template <class Source>
+__global__ void __launch_bounds__(kSlotThreads)
+slot_place_kernel(Source source, SlotShape s, const int32_t *count)
+{
+    extern __shared__ int32_t slot_lds[];
+    typename Source::What *const staged = (typename Source::What *)slot_lds;         // the tile in order
+    const int tile = s.per * kSlotThreads;
+    int32_t *const c = (int32_t *)(staged + tile);          // of every wavefront: how often it met a number, then where in the tile
+    int32_t *const to = c + kSlotWaves * s.buckets;         // a number's next slot, less its place in the tile
+    int32_t *const met_all = to + s.buckets;                // how often the tile met it
+    int32_t *const wave_total = met_all + s.buckets;
+    uint16_t *const staged_number = (uint16_t *)(wave_total + kSlotWaves);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bits = bits_of(s.buckets);
+    const int32_t *const total = count + (int64_t)s.buckets * s.groups;
+    over_numbers(s.buckets, wave_total, [&](int b) { return total[b]; }, [&](int b, int32_t at) {
+        to[b] = at + count[(int64_t)b * s.groups + blockIdx.x];
+        met_all[b] = 0;
+        if (blockIdx.x == 0)
+            source.start(b, at);
+    });
+    const int64_t begin = (int64_t)blockIdx.x * s.tiles * tile;
+    const int64_t end = min(begin + (int64_t)s.tiles * tile, (int64_t)s.n);
+    for (int64_t t0 = begin; t0 < end; t0 += tile) {
+        const int64_t i0 = t0 + wave * s.per * 64 + lane;
+        typename Source::Item item[kSlotMostPer];
+        source.load(item, i0, end);
+        for (int b = threadIdx.x; b < kSlotWaves * s.buckets; b += kSlotThreads)
+            c[b] = 0;
+        __syncthreads();
+        int rank[kSlotMostPer];
 #pragma unroll
-        for (int u = 0; u < kSlotAhead; ++u) {
-            const int64_t i = i0 + u * 64 + lane;
-            if (i0 + u * 64 < end) {
-                const int number = source.number(item[u]);
-                const int slot = take_slot(next, number, bits, i < end);
-                if (i < end)
-                    source.put(item[u], i, number, slot);
+        for (int u = 0; u < kSlotMostPer; ++u)
+            if (u < s.per)
+                rank[u] = take_slot(c + wave * s.buckets, source.number(item[u]), bits, i0 + u * 64 < end);
+        __syncthreads();
+        const auto met_in = [&](int b) {
+            int32_t sum = 0;
+#pragma unroll
+            for (int w = 0; w < kSlotWaves; ++w)
+                sum += c[w * s.buckets + b];
+            return sum;
+        };
+        over_numbers(s.buckets, wave_total, met_in, [&](int b, int32_t at) {
+            to[b] += met_all[b] - at;                        // on past the tile before, less the place in this one
+            int32_t sum = 0;
+#pragma unroll
+            for (int w = 0; w < kSlotWaves; ++w) {
+                const int32_t n = c[w * s.buckets + b];
+                c[w * s.buckets + b] = at + sum;
+                sum += n;
             }
+            met_all[b] = at + sum;
+        });
+#pragma unroll
+        for (int u = 0; u < kSlotMostPer; ++u)
+            if (u < s.per && i0 + u * 64 < end) {
+                const int number = source.number(item[u]), at = c[wave * s.buckets + number] + rank[u];
+                staged[at] = source.what(item[u], i0 + u * 64);
+                staged_number[at] = (uint16_t)number;
+                source.place(i0 + u * 64, number, to[number] + at);
+            }
+        __syncthreads();
+        const int n = (int)min((int64_t)tile, end - t0);
+        for (int at = threadIdx.x; at < n; at += kSlotThreads) {
+            const int number = staged_number[at];
+            source.put(staged[at], number, to[number] + at);
         }
+        __syncthreads();
     }
 }
 
@@ -280,8 +337,10 @@ slot_few_kernel(Source source, int32_t n, int32_t buckets)
             const bool there = begin + u * 64 < n;
             const int number = source.number(item[u]);
             const int slot = take_slot(c + wave * buckets, number, bits, there);
-            if (there)
-                source.put(item[u], begin + u * 64, number, slot);
+            if (there) {
+                source.place(begin + u * 64, number, slot);
+                source.put(source.what(item[u], begin + u * 64), number, slot);
+            }
         }
 }
 
@@ -293,10 +352,11 @@ void launch_few_slots(const Source &source, const SlotShape &s, hipStream_t stre
 template <class Source>
 void launch_slots(const Source &source, const SlotShape &s, int32_t *count, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((s.stretches + kSlotWaves - 1) / kSlotWaves)), block(kSlotWaves * 64);
-    hipLaunchKernelGGL(slot_count_kernel<Source>, grid, block, 0, stream, source, s, count);
+    hipLaunchKernelGGL(slot_count_kernel<Source>, dim3((unsigned)s.groups), dim3(kSlotThreads), (size_t)kSlotWaves * s.buckets * 4, stream, source, s,
+                       count);
     hipLaunchKernelGGL(slot_scan_kernel, dim3((unsigned)s.buckets), dim3(kSlotScanThreads), 0, stream, count, s);
-    hipLaunchKernelGGL(slot_place_kernel<Source>, grid, block, 0, stream, source, s, (const int32_t *)count);
+    hipLaunchKernelGGL(slot_place_kernel<Source>, dim3((unsigned)s.groups), dim3(kSlotThreads), slot_place_bytes(s.per, s.buckets, sizeof(typename Source::What)),
+                       stream, source, s, (const int32_t *)count);
 }
 
 }  // namespace fs
