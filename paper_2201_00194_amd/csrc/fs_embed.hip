@@ -3,9 +3,7 @@
 // The gradient of a table's row is the sum over the places that named it.  The (token, row) pairs are sorted by token,
 // stably, a digit at a time; then the sorted list is cut in chunks, and the lanes that hold a row add a chunk's rows run by run.
 // A run inside a chunk is a finished row of the table; what a workgroup's chunks have of a run that goes on beyond them is a
-// partial sum, two a workgroup at most, and the partial sums are a sorted list themselves: they go the same way
-// again until one workgroup is enough.  So a token named everywhere costs no more than others, and the order of additions depends on the
-// ids alone.
+// partial sum, two a workgroup at most, and a last kernel joins them.  The order of additions depends on the ids alone.
 #include "fs_slots.h"
 
 #include <math.h>
@@ -18,11 +16,8 @@ constexpr int kEmbedFewWaves = 2048;
 constexpr int kLookupRows = 4;            // rows of a lane
 constexpr int kSumMostWaves = 4096;
 constexpr int kSumMostChunk = 256, kSumLeastChunk = 16;   // pairs a chunk
-constexpr int kSumNextChunk = 16;                         // partial sums a chunk
-// Wavefronts of a workgroup and rows on their way at once, for pairs and for partial sums: of these there are few, and all of
-// a chunk come at once.
-template <bool PAIRS> constexpr int kSumWaves = PAIRS ? 8 : 16;
-template <bool PAIRS> constexpr int kSumAhead = PAIRS ? 8 : 16;
+constexpr int kSumWaves = 8;              // of a workgroup
+constexpr int kJoinAhead = 16;            // partial sums on their way at once
 
 template <int ID> struct IdOf;
 template <> struct IdOf<FS_ID_I32> { typedef int32_t type; };
@@ -337,92 +332,56 @@ embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits, ClearArgs 
 // ---- sums of the runs -----------------------------------------------------------------------------------------------------
 
 struct SumArgs {
-    const void *list;              // pairs; of partial sums: token * 2, + 1 where there is nothing to add
+    const void *list;              // pairs
     Packing packing;
     const void *in;
     int64_t in_stride, out_stride, n;
     int32_t width, ll, chunk, n_vocab, accumulate;
     float scale;
     void *out;
-    uint32_t *next_token;          // two a workgroup
-    float *next;
-    int64_t next_stride;
+    uint32_t *part_token;          // partial sums, two a workgroup: token * 2, + 1 where there is nothing to add
+    float *part;
+    int64_t part_stride;
 };
 constexpr uint32_t kNoToken = 0xffffffffu;
-struct PartialSum {};              // in the place of a pair's type
-template <class P> constexpr bool kIsPairs = true;
-template <> constexpr bool kIsPairs<PartialSum> = false;
 
-// The rows of some list entries, on their way.
-template <class In, class P>
-struct SumBatch {
-    static constexpr bool PAIRS = kIsPairs<P>;
-    int token[kSumAhead<PAIRS>];
-    bool add[kSumAhead<PAIRS>];
-    RawChunk<In> x[kSumAhead<PAIRS>];
-    __device__ __forceinline__ void load(const SumArgs &a, int64_t i0, int64_t end, const In *in, int n)
-    {
-        int64_t from[kSumAhead<PAIRS>];
+// A whole row of the table.
+template <class Out, int N>
+__device__ __forceinline__ void put_row(const SumArgs &a, int token, int c, int n, const float (&sum)[N])
+{
+    Out *const out = (Out *)a.out + (int64_t)token * a.out_stride + c;
+    float had[N];
 #pragma unroll
-        for (int u = 0; u < kSumAhead<PAIRS>; ++u) {
-            const int64_t i = min(i0 + u, end - 1);
-            if constexpr (PAIRS) {
-                const P p = ((const P *)a.list)[i];
-                token[u] = token_of(a.packing, p);
-                from[u] = row_of(a.packing, p);
-                add[u] = i0 + u < end && token[u] < a.n_vocab;
-            } else {
-                const uint32_t t = ((const uint32_t *)a.list)[i];
-                token[u] = (int)(t >> 1);
-                from[u] = i;
-                add[u] = i0 + u < end && !(t & 1);
-            }
-        }
+    for (int i = 0; i < N; ++i)
+        had[i] = 0.0f;
+    if (a.accumulate)
+        load_chunk<N>(out, n, had);
 #pragma unroll
-        for (int u = 0; u < kSumAhead<PAIRS>; ++u)
-            x[u].load(in + from[u] * a.in_stride, add[u] ? n : 0);
-    }
-};
+    for (int i = 0; i < N; ++i)
+        had[i] += sum[i] * a.scale;
+    store_chunk<N>(out, n, had);
+}
 
 // A chunk of the list is added by the lanes of one row, in fp32.  What a workgroup's chunks have of runs that go on beyond
 // them, two sums a chunk at most, meets in LDS, where the lanes of a run's first sum add them up, in 64 bits; what the workgroup
 // has of runs that go on beyond it goes to memory.
 template <int IN, int OUT, class P>
-__global__ void __launch_bounds__(kSumWaves<kIsPairs<P>> * 64)
+__global__ void __launch_bounds__(kSumWaves * 64)
 embed_sum_kernel(SumArgs a)
 {
-    constexpr bool PAIRS = kIsPairs<P>;
     typedef typename Element<IN>::type In;
     typedef typename Element<OUT>::type Out;
     constexpr int N = kChunk<In>;
-    __shared__ uint32_t slot_token[2 * kSumWaves<PAIRS> * 64];
-    __shared__ float slot_sum[2 * kSumWaves<PAIRS> * 64 * N];
+    __shared__ uint32_t slot_token[2 * kSumWaves * 64];
+    __shared__ float slot_sum[2 * kSumWaves * 64 * N];
     const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
-    const int units = kSumWaves<PAIRS> << (6 - ll), unit = ((threadIdx.x >> 6) << (6 - ll)) + (lane >> ll), slots = 2 * units;
+    const int units = kSumWaves << (6 - ll), unit = ((threadIdx.x >> 6) << (6 - ll)) + (lane >> ll), slots = 2 * units;
     const int64_t group_begin = (int64_t)blockIdx.x * units * a.chunk, group_end = min(group_begin + (int64_t)units * a.chunk, a.n);
     const int64_t begin = group_begin + (int64_t)unit * a.chunk, end = min(begin + a.chunk, a.n);
     const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
     const In *const in = (const In *)a.in + c;
-    const auto token_at = [&](int64_t i) -> int {
-        if constexpr (PAIRS)
-            return token_of(a.packing, ((const P *)a.list)[i]);
-        else
-            return (int)(((const uint32_t *)a.list)[i] >> 1);
-    };
-    // A whole row of the table.
-    const auto put = [&](int token, const float (&sum)[N]) {
-        Out *const out = (Out *)a.out + (int64_t)token * a.out_stride + c;
-        float had[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            had[i] = 0.0f;
-        if (a.accumulate)
-            load_chunk<N>(out, n, had);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            had[i] += sum[i] * a.scale;
-        store_chunk<N>(out, n, had);
-    };
+    const P *const list = (const P *)a.list;
+    const auto token_at = [&](int64_t i) { return token_of(a.packing, list[i]); };
     if (begin < a.n) {
         const int before = begin > 0 ? token_at(begin - 1) : -1, behind = end < a.n ? token_at(end) : -1;
         float sum[N];
@@ -430,7 +389,7 @@ embed_sum_kernel(SumArgs a)
         for (int i = 0; i < N; ++i)
             sum[i] = 0.0f;
         int now = token_at(begin);
-        bool first = true, some = false;
+        bool first = true;
         const auto mark = [&](int which, bool partial) {
             if (h == 0)
                 slot_token[2 * unit + which] = (uint32_t)now * 2u + (partial ? 0u : 1u);
@@ -440,34 +399,39 @@ embed_sum_kernel(SumArgs a)
                     slot_sum[(((2 * unit + which) << ll) + h) * N + i] = sum[i];
         };
         const auto done = [&](bool last) {                       // the run of `now` ends here, or the chunk does
-            const bool left = first && before == now, right = last && behind == now;
+            const bool left = first && before == now, right = last && behind == now, some = now < a.n_vocab;
             if (!left && !right && some)
-                put(now, sum);
+                put_row<Out>(a, now, c, n, sum);
             if (first)
                 mark(0, (left || right) && some);
             if (last)
                 mark(1, !first && right && some);
         };
-        for (int64_t i0 = begin; i0 < end; i0 += kSumAhead<PAIRS>) {
-            SumBatch<In, P> batch;
-            batch.load(a, i0, end, in, n);
+        for (int64_t i0 = begin; i0 < end; i0 += kEmbedAhead) {
+            int token[kEmbedAhead];
+            RawChunk<In> x[kEmbedAhead];
+            P pair[kEmbedAhead];
 #pragma unroll
-            for (int u = 0; u < kSumAhead<PAIRS>; ++u) {
-                if (batch.token[u] != now) {
+            for (int u = 0; u < kEmbedAhead; ++u)
+                pair[u] = list[min(i0 + u, end - 1)];
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u) {
+                token[u] = token_of(a.packing, pair[u]);
+                x[u].load(in + (int64_t)row_of(a.packing, pair[u]) * a.in_stride, token[u] < a.n_vocab && i0 + u < end ? n : 0);
+            }
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u) {
+                if (token[u] != now) {
                     done(false);
                     first = false;
-                    some = false;
-                    now = batch.token[u];
+                    now = token[u];
 #pragma unroll
                     for (int i = 0; i < N; ++i)
                         sum[i] = 0.0f;
                 }
-                if (batch.add[u]) {
-                    some = true;
 #pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        sum[i] += batch.x[u][i];
-                }
+                for (int i = 0; i < N; ++i)
+                    sum[i] += x[u][i];
             }
         }
         done(true);
@@ -502,13 +466,13 @@ embed_sum_kernel(SumArgs a)
         for (int i = 0; i < N; ++i)
             sum[i] = (float)all[i];
         if (!left && !right && some)
-            put((int)token, sum);
+            put_row<Out>(a, (int)token, c, n, sum);
         const auto mark = [&](int at, bool partial) {
-            const int64_t next = 2 * (int64_t)blockIdx.x + at;
+            const int64_t slot = 2 * (int64_t)blockIdx.x + at;
             if (h == 0 && blockIdx.y == 0)
-                a.next_token[next] = token * 2u + (partial ? 0u : 1u);
+                a.part_token[slot] = token * 2u + (partial ? 0u : 1u);
             if (partial)
-                store_chunk<N>(a.next + next * a.next_stride + c, n, sum);
+                store_chunk<N>(a.part + slot * a.part_stride + c, n, sum);
         };
         if (s == 0)
             mark(0, (left || right) && some);
@@ -517,28 +481,71 @@ embed_sum_kernel(SumArgs a)
     }
 }
 
-struct SumPlan {
-    int64_t n[2];                  // partial sums behind the first and the second kernel
-    int64_t stride;
-    int32_t chunk;
-};
-template <bool PAIRS>
-int64_t sum_groups(int64_t n, int32_t chunk, int32_t ll)      // workgroups
+// The partial sums of a run, mostly two, are added by the lanes of the first, in 64 bits.
+template <int OUT>
+__global__ void __launch_bounds__(kEmbedWaves * 64)
+embed_join_kernel(SumArgs a)
 {
-    const int64_t each = ((int64_t)kSumWaves<PAIRS> << (6 - ll)) * chunk;
-    return (n + each - 1) / each;
+    typedef typename Element<OUT>::type Out;
+    constexpr int N = kChunk<float>;
+    const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
+    const int64_t s = (((int64_t)blockIdx.x * kEmbedWaves + (threadIdx.x >> 6)) << (6 - ll)) + (lane >> ll);
+    if (s >= a.n)
+        return;
+    const uint32_t token = a.part_token[s] >> 1;
+    if (token >= (uint32_t)a.n_vocab || (s > 0 && a.part_token[s - 1] >> 1 == token))
+        return;
+    const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
+    double all[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        all[i] = 0.0;
+    bool some = false, on = true;
+    for (int64_t e = s; on; e += kJoinAhead) {
+        uint32_t met[kJoinAhead];
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u)
+            met[u] = e + u < a.n ? a.part_token[e + u] : kNoToken;
+        RawChunk<float> x[kJoinAhead];
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u) {
+            on = on && met[u] >> 1 == token;
+            const bool add = on && !(met[u] & 1);
+            some |= add;
+            x[u].load(a.part + (e + u) * a.part_stride + c, add ? n : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                all[i] += (double)x[u][i];
+    }
+    if (!some)
+        return;
+    float sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        sum[i] = (float)all[i];
+    put_row<Out>(a, (int)token, c, n, sum);
 }
+
+struct SumPlan {
+    int64_t groups, part_stride;   // workgroups; elements
+    int32_t chunk, ll, columns;
+};
 // More, shorter chunks where there are few pairs to a wavefront: down to kSumLeastChunk for kSumMostWaves.
 static SumPlan sum_plan(int64_t n, int32_t width, int32_t type)
 {
     SumPlan p;
-    const int elements = 16 / (int)type_bytes(type), ll = row_lanes_log(width, elements), columns = column_blocks(width, elements);
+    const int elements = 16 / (int)type_bytes(type);
+    p.ll = row_lanes_log(width, elements);
+    p.columns = column_blocks(width, elements);
     p.chunk = kSumMostChunk;
-    while (p.chunk > kSumLeastChunk && ((n / p.chunk * columns) << ll) < (int64_t)kSumMostWaves * 64)
+    while (p.chunk > kSumLeastChunk && ((n / p.chunk * p.columns) << p.ll) < (int64_t)kSumMostWaves * 64)
         p.chunk /= 2;
-    p.stride = (width + 3) / 4 * 4;
-    p.n[0] = 2 * sum_groups<true>(n, p.chunk, ll);
-    p.n[1] = 2 * sum_groups<false>(p.n[0], kSumNextChunk, row_lanes_log(width, kChunk<float>));
+    p.part_stride = (width + 3) / 4 * 4;
+    const int64_t each = ((int64_t)kSumWaves << (6 - p.ll)) * p.chunk;
+    p.groups = (n + each - 1) / each;
     return p;
 }
 
@@ -548,7 +555,7 @@ struct SortPlan {
     bool packed;
     SlotShape shape;
     SumPlan sum;
-    size_t list_bytes, token_bytes[2], sum_bytes[2], bytes;
+    size_t list_bytes, token_bytes, part_bytes, bytes;
 };
 static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t n_rows, int32_t n_cols)
 {
@@ -565,12 +572,9 @@ static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t 
     p.packed = p.packing.row_bits + bits <= 32 && p.packing.row_bits < 32;
     p.shape = slot_shape(n, 1 << p.bits, p.packed ? sizeof(uint32_t) : sizeof(Pair));
     p.list_bytes = ((size_t)n * (p.packed ? sizeof(uint32_t) : sizeof(Pair)) + 255) / 256 * 256;
-    p.bytes = 2 * p.list_bytes + slot_count_bytes(p.shape);
-    for (int i = 0; i < 2; ++i) {
-        p.token_bytes[i] = ((size_t)p.sum.n[i] * 4 + 255) / 256 * 256;
-        p.sum_bytes[i] = ((size_t)p.sum.n[i] * p.sum.stride * 4 + 255) / 256 * 256;
-        p.bytes += p.token_bytes[i] + p.sum_bytes[i];
-    }
+    p.token_bytes = ((size_t)p.sum.groups * 2 * 4 + 255) / 256 * 256;
+    p.part_bytes = ((size_t)p.sum.groups * 2 * p.sum.part_stride * 4 + 255) / 256 * 256;
+    p.bytes = 2 * p.list_bytes + p.token_bytes + p.part_bytes + slot_count_bytes(p.shape);
     return p;
 }
 
@@ -689,14 +693,9 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
         at += bytes;
         return here;
     };
-    void *list[2];
-    uint32_t *token[2];
-    float *sum[2];
-    for (int i = 0; i < 2; ++i) {
-        list[i] = take(p.list_bytes);
-        token[i] = (uint32_t *)take(p.token_bytes[i]);
-        sum[i] = (float *)take(p.sum_bytes[i]);
-    }
+    void *const list[2] = {take(p.list_bytes), take(p.list_bytes)};
+    uint32_t *const part_token = (uint32_t *)take(p.token_bytes);
+    float *const part = (float *)take(p.part_bytes);
     int32_t *const count = (int32_t *)at;
     prof_start(kKernTrainOther, stream);
     const ClearArgs clear = {d_table, n_vocab, d_table_stride, d_table_type, width, row_lanes_log(width, 16 / (int)type_bytes(d_table_type))};
@@ -728,29 +727,21 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
             sort(uint32_t());
         else
             sort(Pair());
-        SumArgs a = {list[now], p.packing, d_out, d_out_stride, d_table_stride, n, width, 0, p.sum.chunk, n_vocab, accumulate, scale, d_table,
-                     token[0], sum[0], p.sum.stride};
-        const auto grid_of = [&](auto pairs, int elements) {
-            a.ll = row_lanes_log(width, elements);
-            return dim3((unsigned)sum_groups<decltype(pairs)::value != 0>(a.n, a.chunk, a.ll), (unsigned)column_blocks(width, elements));
-        };
+        SumArgs a = {list[now], p.packing, d_out, d_out_stride, d_table_stride, n, width, p.sum.ll, p.sum.chunk, n_vocab, accumulate, scale,
+                     d_table, part_token, part, p.sum.part_stride};
         with_types(d_out_type, d_table_type, [&](auto i, auto o) {
             constexpr int in = decltype(i)::value, out = decltype(o)::value;
-            dim3 grid = grid_of(TypeTag<1>(), kChunk<typename Element<in>::type>);
+            const dim3 grid((unsigned)p.sum.groups, (unsigned)p.sum.columns);
             if (p.packed)
-                hipLaunchKernelGGL((embed_sum_kernel<in, out, uint32_t>), grid, dim3(kSumWaves<true> * 64), 0, stream, a);
+                hipLaunchKernelGGL((embed_sum_kernel<in, out, uint32_t>), grid, dim3(kSumWaves * 64), 0, stream, a);
             else
-                hipLaunchKernelGGL((embed_sum_kernel<in, out, Pair>), grid, dim3(kSumWaves<true> * 64), 0, stream, a);
-            for (int from = 0; grid.x > 1; from ^= 1) {
-                a.n = 2 * (int64_t)grid.x;
-                a.chunk = kSumNextChunk;
-                a.list = token[from];
-                a.in = sum[from];
-                a.in_stride = p.sum.stride;
-                a.next_token = token[from ^ 1];
-                a.next = sum[from ^ 1];
-                grid = grid_of(TypeTag<0>(), kChunk<float>);
-                hipLaunchKernelGGL((embed_sum_kernel<FS_F32, out, PartialSum>), grid, dim3(kSumWaves<false> * 64), 0, stream, a);
+                hipLaunchKernelGGL((embed_sum_kernel<in, out, Pair>), grid, dim3(kSumWaves * 64), 0, stream, a);
+            if (p.sum.groups > 1) {
+                a.n = 2 * p.sum.groups;
+                a.ll = row_lanes_log(width, kChunk<float>);
+                const int64_t each = (int64_t)kEmbedWaves << (6 - a.ll);
+                hipLaunchKernelGGL(embed_join_kernel<out>, dim3((unsigned)((a.n + each - 1) / each), (unsigned)column_blocks(width, kChunk<float>)),
+                                   dim3(kEmbedWaves * 64), 0, stream, a);
             }
         });
     }
