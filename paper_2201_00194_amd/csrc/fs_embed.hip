@@ -188,8 +188,10 @@ embed_lookup_kernel(EmbedArgs a)
 struct Pair {
     int32_t token, row;
 };
-struct Packing {                   // of 32 bits: how many are the row's
-    int32_t row_bits;
+struct Packing {
+    int32_t row_bits;              // of a packed pair's
+    int32_t token_bits;            // of a token's: those above are the band's
+    uint32_t band_magic;           // a row's band: the high word of row * band_magic
 };
 template <class P> __device__ __forceinline__ P make_pair(const Packing &k, int token, uint32_t row);
 template <> __device__ __forceinline__ Pair make_pair<Pair>(const Packing &, int token, uint32_t row) { return Pair{token, (int32_t)row}; }
@@ -198,6 +200,10 @@ __device__ __forceinline__ int token_of(const Packing &, const Pair &p) { return
 __device__ __forceinline__ int token_of(const Packing &k, uint32_t p) { return (int)(p >> k.row_bits); }
 __device__ __forceinline__ uint32_t row_of(const Packing &, const Pair &p) { return (uint32_t)p.row; }
 __device__ __forceinline__ uint32_t row_of(const Packing &k, uint32_t p) { return p & ((1u << k.row_bits) - 1u); }
+
+// Bands: see bands_for.  From here on a token is the token in its row's band.
+__device__ __forceinline__ int banded(const Packing &k, int token, uint32_t row) { return token | (int)(__umulhi(row, k.band_magic) << k.token_bits); }
+__device__ __forceinline__ int plain_token(const Packing &k, int token) { return token & (int)((1u << k.token_bits) - 1u); }
 
 template <int ID, class P>
 struct IdDigit {
@@ -214,7 +220,7 @@ struct IdDigit {
         ids.template rows<ID>(token, entry, [&](int u) { return entry(u) - ids.row_of(entry(u)) * (uint32_t)ids.n_cols; });
 #pragma unroll
         for (int u = 0; u < N; ++u)
-            item[u] = make_pair<P>(packing, token[u] < 0 ? ids.n_vocab : token[u], ids.row_of(entry(u)));
+            item[u] = make_pair<P>(packing, banded(packing, token[u] < 0 ? ids.n_vocab : token[u], ids.row_of(entry(u))), ids.row_of(entry(u)));
     }
     __device__ __forceinline__ int number(const P &p) const { return token_of(packing, p) & mask; }
     __device__ __forceinline__ void start(int, int) const {}
@@ -325,7 +331,7 @@ embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits, ClearArgs 
     }
     for (int s = threadIdx.x; s < n; s += kSlotFewWaves * 64) {
         const int i = order[s];
-        source.to[s] = make_pair<P>(source.packing, token[i], source.ids.row_of((uint32_t)i));
+        source.to[s] = make_pair<P>(source.packing, token[i], source.ids.row_of((uint32_t)i));       // one band
     }
 }
 
@@ -342,14 +348,21 @@ struct SumArgs {
     uint32_t *part_token;          // partial sums, two a workgroup: token * 2, + 1 where there is nothing to add
     float *part;
     int64_t part_stride;
+    int32_t groups, bands;         // workgroups' stretches of the list
 };
 constexpr uint32_t kNoToken = 0xffffffffu;
+constexpr int kXcds = 8;           // workgroups go round them
+// The row of the result for a token: with bands, of a table for each.
+__device__ __forceinline__ int64_t row_for(const SumArgs &a, int token)
+{
+    return (int64_t)(token >> a.packing.token_bits) * a.n_vocab + plain_token(a.packing, token);
+}
 
 // A whole row of the table.
 template <class Out, int N>
 __device__ __forceinline__ void put_row(const SumArgs &a, int token, int c, int n, const float (&sum)[N])
 {
-    Out *const out = (Out *)a.out + (int64_t)token * a.out_stride + c;
+    Out *const out = (Out *)a.out + row_for(a, token) * a.out_stride + c;
     float had[N];
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -376,19 +389,32 @@ embed_sum_kernel(SumArgs a)
     __shared__ float slot_sum[2 * kSumWaves * 64 * N];
     const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
     const int units = kSumWaves << (6 - ll), unit = ((threadIdx.x >> 6) << (6 - ll)) + (lane >> ll), slots = 2 * units;
-    const int64_t group_begin = (int64_t)blockIdx.x * units * a.chunk, group_end = min(group_begin + (int64_t)units * a.chunk, a.n);
+    // With bands, an XCD takes stretches of one of them.
+    int64_t group = blockIdx.x;
+    if (a.bands > 1) {
+        const int xcd = blockIdx.x % kXcds, per = kXcds / a.bands, each = (a.groups + a.bands - 1) / a.bands;
+        const int in_band = blockIdx.x / kXcds * per + xcd / a.bands;
+        group = (int64_t)(xcd % a.bands) * each + in_band;
+        if (in_band >= each || group >= a.groups)
+            return;
+    }
+    const int64_t group_begin = group * units * a.chunk, group_end = min(group_begin + (int64_t)units * a.chunk, a.n);
     const int64_t begin = group_begin + (int64_t)unit * a.chunk, end = min(begin + a.chunk, a.n);
     const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
     const In *const in = (const In *)a.in + c;
     const P *const list = (const P *)a.list;
-    const auto token_at = [&](int64_t i) { return token_of(a.packing, list[i]); };
+    // The tokens before and behind the group and the chunk, on their way together.
+    const auto token_at = [&](int64_t i) { return token_of(a.packing, list[min(max(i, (int64_t)0), a.n - 1)]); };
+    const int group_left = token_at(group_begin - 1), group_right = token_at(group_end);
+    const int chunk_left = token_at(begin - 1), chunk_right = token_at(end), chunk_first = token_at(begin);
+    const int group_before = group_begin > 0 ? group_left : -1, group_behind = group_end < a.n ? group_right : -1;
     if (begin < a.n) {
-        const int before = begin > 0 ? token_at(begin - 1) : -1, behind = end < a.n ? token_at(end) : -1;
+        const int before = begin > 0 ? chunk_left : -1, behind = end < a.n ? chunk_right : -1;
         float sum[N];
 #pragma unroll
         for (int i = 0; i < N; ++i)
             sum[i] = 0.0f;
-        int now = token_at(begin);
+        int now = chunk_first;
         bool first = true;
         const auto mark = [&](int which, bool partial) {
             if (h == 0)
@@ -399,7 +425,7 @@ embed_sum_kernel(SumArgs a)
                     slot_sum[(((2 * unit + which) << ll) + h) * N + i] = sum[i];
         };
         const auto done = [&](bool last) {                       // the run of `now` ends here, or the chunk does
-            const bool left = first && before == now, right = last && behind == now, some = now < a.n_vocab;
+            const bool left = first && before == now, right = last && behind == now, some = plain_token(a.packing, now) < a.n_vocab;
             if (!left && !right && some)
                 put_row<Out>(a, now, c, n, sum);
             if (first)
@@ -417,7 +443,7 @@ embed_sum_kernel(SumArgs a)
 #pragma unroll
             for (int u = 0; u < kEmbedAhead; ++u) {
                 token[u] = token_of(a.packing, pair[u]);
-                x[u].load(in + (int64_t)row_of(a.packing, pair[u]) * a.in_stride, token[u] < a.n_vocab && i0 + u < end ? n : 0);
+                x[u].load(in + (int64_t)row_of(a.packing, pair[u]) * a.in_stride, plain_token(a.packing, token[u]) < a.n_vocab && i0 + u < end ? n : 0);
             }
 #pragma unroll
             for (int u = 0; u < kEmbedAhead; ++u) {
@@ -439,7 +465,6 @@ embed_sum_kernel(SumArgs a)
         slot_token[2 * unit] = slot_token[2 * unit + 1] = kNoToken;
     }
     __syncthreads();
-    const int before = group_begin > 0 ? token_at(group_begin - 1) : -1, behind = group_end < a.n ? token_at(group_end) : -1;
     for (int which = 0; which < 2; ++which) {
         const int s = 2 * unit + which;
         const uint32_t token = slot_token[s] >> 1;
@@ -460,7 +485,7 @@ embed_sum_kernel(SumArgs a)
             }
             ++e;
         } while (e < slots && slot_token[e] >> 1 == token);
-        const bool left = s == 0 && before == (int)token, right = e == slots && behind == (int)token;
+        const bool left = s == 0 && group_before == (int)token, right = e == slots && group_behind == (int)token;
         float sum[N];
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -468,7 +493,7 @@ embed_sum_kernel(SumArgs a)
         if (!left && !right && some)
             put_row<Out>(a, (int)token, c, n, sum);
         const auto mark = [&](int at, bool partial) {
-            const int64_t slot = 2 * (int64_t)blockIdx.x + at;
+            const int64_t slot = 2 * group + at;
             if (h == 0 && blockIdx.y == 0)
                 a.part_token[slot] = token * 2u + (partial ? 0u : 1u);
             if (partial)
@@ -493,7 +518,7 @@ embed_join_kernel(SumArgs a)
     if (s >= a.n)
         return;
     const uint32_t token = a.part_token[s] >> 1;
-    if (token >= (uint32_t)a.n_vocab || (s > 0 && a.part_token[s - 1] >> 1 == token))
+    if (token == kNoToken >> 1 || plain_token(a.packing, (int)token) >= a.n_vocab || (s > 0 && a.part_token[s - 1] >> 1 == token))
         return;
     const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
     double all[N];
@@ -529,6 +554,35 @@ embed_join_kernel(SumArgs a)
     put_row<Out>(a, (int)token, c, n, sum);
 }
 
+// The bands' tables become one.
+template <int OUT>
+__global__ void __launch_bounds__(256)
+embed_bands_kernel(SumArgs a, const float *tables)
+{
+    typedef typename Element<OUT>::type Out;
+    constexpr int N = kChunk<float>;
+    const int lane = threadIdx.x & 63, h = lane & ((1 << a.ll) - 1);
+    const int64_t row = (((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) << (6 - a.ll)) + (lane >> a.ll);
+    if (row >= a.n_vocab)
+        return;
+    for (int c = h * N; c < a.width; c += 64 * N) {
+        const int n = a.width - c;
+        float sum[N], more[kXcds][N];
+#pragma unroll
+        for (int b = 0; b < kXcds; ++b)
+            load_chunk<N>(tables + (min(b, a.bands - 1) * (int64_t)a.n_vocab + row) * a.part_stride + c, b < a.bands ? n : 0, more[b]);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            sum[i] = 0.0f;
+#pragma unroll
+        for (int b = 0; b < kXcds; ++b)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                sum[i] += more[b][i];
+        put_row<Out>(a, (int)row, c, n, sum);
+    }
+}
+
 struct SumPlan {
     int64_t groups, part_stride;   // workgroups; elements
     int32_t chunk, ll, columns;
@@ -552,11 +606,30 @@ static SumPlan sum_plan(int64_t n, int32_t width, int32_t type)
 struct SortPlan {
     int token_bits, passes, bits;      // of all digits, of one
     Packing packing;
+    int bands;
     bool packed;
     SlotShape shape;
     SumPlan sum;
-    size_t list_bytes, token_bytes, part_bytes, bytes;
+    size_t list_bytes, token_bytes, part_bytes, table_bytes, bytes;
 };
+// Bands of rows: the sum reads a row once for every token that it names, in the order of the tokens, so that rows come from the
+// L2 cache of an XCD only if all of them fit there.  Where they do not, but a half to an eighth of them does, the list is
+// sorted by band first, every XCD sums tokens over the rows of one band, and the bands' tables are added.  32768 rows of
+// 256 bytes, 100 tokens each: 102 us without bands; 8192 such rows with 400 each 60.  The tables are written twice and read
+// once, which a thirtieth as many rows as there are pairs does not outweigh.
+constexpr int64_t kBandBytes = 5 << 19, kL2Bytes = 4 << 20;
+constexpr int kBandLeastRun = 30;
+static int bands_for(int32_t n_vocab, int32_t width, int32_t type, int64_t n_rows, int64_t n)
+{
+    const int64_t bytes = n_rows * width * (int64_t)type_bytes(type);
+    if (n <= kSlotFew || n_rows <= kXcds || bytes <= kL2Bytes || bytes > kXcds * kL2Bytes)
+        return 1;
+    int bands = 2;
+    while (bands < kXcds && bytes > bands * kBandBytes)
+        bands *= 2;
+    return n / n_vocab >= (int64_t)kBandLeastRun * bands ? bands : 1;
+}
+
 static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t n_rows, int32_t n_cols)
 {
     const int64_t n = n_rows * n_cols;
@@ -564,17 +637,23 @@ static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t 
     int bits = 1;                                  // of 0 .. n_vocab
     while (((int64_t)1 << bits) <= n_vocab)
         ++bits;
+    p.packing = Packing{bits_of((int)n_rows), bits, 0};
+    p.bands = bits + 3 <= 30 ? bands_for(n_vocab, width, type, n_rows, n) : 1;
+    if (p.bands > 1) {
+        p.packing.band_magic = (uint32_t)(((uint64_t)p.bands << 32) / (uint64_t)n_rows);
+        bits += bits_of(p.bands);
+    }
     p.token_bits = bits;
     p.passes = (bits + 9) / 10;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.sum = sum_plan(n, width, type);
-    p.packing.row_bits = bits_of((int)n_rows);
     p.packed = p.packing.row_bits + bits <= 32 && p.packing.row_bits < 32;
     p.shape = slot_shape(n, 1 << p.bits, p.packed ? sizeof(uint32_t) : sizeof(Pair));
     p.list_bytes = ((size_t)n * (p.packed ? sizeof(uint32_t) : sizeof(Pair)) + 255) / 256 * 256;
     p.token_bytes = ((size_t)p.sum.groups * 2 * 4 + 255) / 256 * 256;
     p.part_bytes = ((size_t)p.sum.groups * 2 * p.sum.part_stride * 4 + 255) / 256 * 256;
-    p.bytes = 2 * p.list_bytes + p.token_bytes + p.part_bytes + slot_count_bytes(p.shape);
+    p.table_bytes = p.bands > 1 ? ((size_t)p.bands * n_vocab * p.sum.part_stride * 4 + 255) / 256 * 256 : 0;
+    p.bytes = 2 * p.list_bytes + p.token_bytes + p.part_bytes + p.table_bytes + slot_count_bytes(p.shape);
     return p;
 }
 
@@ -695,11 +774,13 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
     };
     void *const list[2] = {take(p.list_bytes), take(p.list_bytes)};
     uint32_t *const part_token = (uint32_t *)take(p.token_bytes);
-    float *const part = (float *)take(p.part_bytes);
+    float *const part = (float *)take(p.part_bytes), *const tables = (float *)take(p.table_bytes);
     int32_t *const count = (int32_t *)at;
     prof_start(kKernTrainOther, stream);
-    const ClearArgs clear = {d_table, n_vocab, d_table_stride, d_table_type, width, row_lanes_log(width, 16 / (int)type_bytes(d_table_type))};
-    const int64_t rows = (int64_t)16 << (6 - clear.ll), all = accumulate ? 0 : (n_vocab + rows - 1) / rows;
+    ClearArgs clear = {d_table, n_vocab, d_table_stride, d_table_type, width, row_lanes_log(width, 16 / (int)type_bytes(d_table_type))};
+    if (p.bands > 1)
+        clear = ClearArgs{tables, (int64_t)p.bands * n_vocab, p.sum.part_stride, FS_F32, width, row_lanes_log(width, kChunk<float>)};
+    const int64_t rows = (int64_t)16 << (6 - clear.ll), all = p.bands == 1 && accumulate ? 0 : (clear.n_rows + rows - 1) / rows;
     const unsigned blocks = (unsigned)(all < kClearBlocks ? all : kClearBlocks);
     const bool few = n > 0 && n <= kSlotFew;
     if (blocks > 0 && !few)
@@ -728,22 +809,37 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
         else
             sort(Pair());
         SumArgs a = {list[now], p.packing, d_out, d_out_stride, d_table_stride, n, width, p.sum.ll, p.sum.chunk, n_vocab, accumulate, scale,
-                     d_table, part_token, part, p.sum.part_stride};
-        with_types(d_out_type, d_table_type, [&](auto i, auto o) {
+                     d_table, part_token, part, p.sum.part_stride, (int32_t)p.sum.groups, p.bands};
+        SumArgs to = a;                // of what adds the bands' tables
+        if (p.bands > 1) {
+            a.out = tables;
+            a.out_stride = p.sum.part_stride;
+            a.accumulate = 0;
+            a.scale = 1.0f;
+        }
+        with_types(d_out_type, p.bands > 1 ? FS_F32 : d_table_type, [&](auto i, auto o) {
             constexpr int in = decltype(i)::value, out = decltype(o)::value;
-            const dim3 grid((unsigned)p.sum.groups, (unsigned)p.sum.columns);
+            const int64_t each = (p.sum.groups + p.bands - 1) / p.bands, per = kXcds / p.bands;
+            const dim3 grid((unsigned)(p.bands > 1 ? (each + per - 1) / per * kXcds : p.sum.groups), (unsigned)p.sum.columns);
             if (p.packed)
                 hipLaunchKernelGGL((embed_sum_kernel<in, out, uint32_t>), grid, dim3(kSumWaves * 64), 0, stream, a);
             else
                 hipLaunchKernelGGL((embed_sum_kernel<in, out, Pair>), grid, dim3(kSumWaves * 64), 0, stream, a);
+            a.ll = to.ll = row_lanes_log(width, kChunk<float>);
             if (p.sum.groups > 1) {
                 a.n = 2 * p.sum.groups;
-                a.ll = row_lanes_log(width, kChunk<float>);
-                const int64_t each = (int64_t)kEmbedWaves << (6 - a.ll);
-                hipLaunchKernelGGL(embed_join_kernel<out>, dim3((unsigned)((a.n + each - 1) / each), (unsigned)column_blocks(width, kChunk<float>)),
+                const int64_t rows = (int64_t)kEmbedWaves << (6 - a.ll);
+                hipLaunchKernelGGL(embed_join_kernel<out>, dim3((unsigned)((a.n + rows - 1) / rows), (unsigned)column_blocks(width, kChunk<float>)),
                                    dim3(kEmbedWaves * 64), 0, stream, a);
             }
         });
+        if (p.bands > 1)
+            with_type(d_table_type, [&](auto t) {
+                const int64_t each = (int64_t)4 << (6 - to.ll);
+                to.packing.token_bits = 31;             // rows of one table
+                hipLaunchKernelGGL(embed_bands_kernel<decltype(t)::value>, dim3((unsigned)((n_vocab + each - 1) / each)), dim3(256), 0, stream, to,
+                                   (const float *)tables);
+            });
     }
     prof_stop(stream);
     return launched("embedding gradient kernels launch");

@@ -126,6 +126,33 @@ def test_gradient_of_long_runs(api, rows, vocab):
     assert torch.equal(d, api.fs_embed_backward(g, ids, vocab, scale=0.5))
 
 
+@pytest.mark.parametrize("typ,rows,cols,vocab,width", [("fp32", 17000, 20, 700, 64), ("bf16", 70001, 7, 1500, 40), ("fp16", 41000, 9, 610, 65),
+                                                       ("fp32", 4500, 100, 900, 256), ("fp32", 130000, 3, 60, 60)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_many_rows(api, typ, rows, cols, vocab, width, accumulate):
+    """More rows than an XCD's L2 cache holds, each token named often: rows are taken in bands."""
+    import torch
+    gen = torch.Generator("cuda").manual_seed(rows)
+    ids = torch.randint(-1, vocab + 1, (rows, cols), device="cuda", generator=gen, dtype=torch.int32)
+    g = torch.randn(rows, width, device="cuda", generator=gen).to(torch_type(typ))
+    there = (ids >= 0) & (ids < vocab)
+    exp, size = (torch.zeros(vocab + 1, width, dtype=torch.float64, device="cuda") for _ in range(2))
+    for c in range(cols):
+        at = torch.where(there[:, c], ids[:, c], vocab).long()
+        exp.index_add_(0, at, g.double())
+        size.index_add_(0, at, g.double().abs())
+    exp, size = exp[:vocab] * 0.5, size[:vocab] * 0.5
+    for out_typ in dict.fromkeys((typ, "fp32")):
+        d = torch.ones(vocab, width, dtype=torch_type(out_typ), device="cuda")
+        api.fs_embed_backward(g, ids, vocab, scale=0.5, d_table=d, accumulate=accumulate)
+        e = exp + 1 if accumulate else exp
+        off = 520 * 2.0 ** -24 * size + 2.0 ** -23 * (e.abs() + exp.abs())
+        assert bool(((d.double() - e).abs() <= off + HALF[out_typ] * (e.abs() + off)).all())
+        again = torch.ones_like(d)
+        api.fs_embed_backward(g, ids, vocab, scale=0.5, d_table=again, accumulate=accumulate)
+        assert torch.equal(d, again)
+
+
 def test_gradient_against_differences(api):
     """out is linear in the table."""
     import torch
