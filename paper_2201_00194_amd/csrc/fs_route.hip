@@ -179,9 +179,24 @@ __device__ __forceinline__ int expert_of(double v) { return 1023 - (__double2loi
 __device__ __forceinline__ float key_of(double v)
 {
     const uint32_t order = __builtin_amdgcn_alignbit((uint32_t)__double2hiint(v), (uint32_t)__double2loint(v), 20);
-    return __uint_as_float(order ^ ((uint32_t)((int)~order >> 31) | 0x80000000u));
+    return __uint_as_float(order ^ (~(uint32_t)((int)order >> 31) | 0x80000000u));
 }
 
+// 1 where a > b, else 0, from b * -kFar: one instruction, where a compare leaves a mask that the next may only read two cycles
+// later.  The difference of two floats of common size times kFar is at least 1, or 0 or less; where sizes are not common, or
+// infinite, it may be 0.
+constexpr float kFar = 1.2676506e30f;     // 2^100
+__device__ __forceinline__ float one_if_more(float a, float minus_b_far)
+{
+    float r;
+    asm("v_fma_f32 %0, %1, %2, %3 clamp" : "=v"(r) : "v"(a), "s"(kFar), "v"(minus_b_far));
+    return r;
+}
+__device__ __forceinline__ float least(float a, float b)
+{
+    asm("v_min_f32 %0, %0, %1" : "+v"(a) : "v"(b));
+    return a;
+}
 // Two of the largest so far, and another value.
 __device__ __forceinline__ void best_two(float &first, float &second, float v)
 {
@@ -466,7 +481,8 @@ route_kernel(RouteArgs a)
                 // chunks every chunk's best two keys, else all keys; then their sums.
                 const bool whole = a.group_size % kChunk<T> == 0;
                 const int width = whole ? n / kChunk<T> * 2 : n, per = width / a.p.n_groups;      // per: of a group
-                float *keys = (float *)own + (lane >> ll) * width, *sums = (float *)own + ((n << (6 - ll)) + (lane >> ll) * a.p.n_groups);
+                const int padded = (a.p.n_groups + 3) & ~3;         // sums of nobody's groups behind
+                float *keys = (float *)own + (lane >> ll) * width, *sums = (float *)own + ((((n + 3) & ~3) << (6 - ll)) + (lane >> ll) * padded);
                 if (whole) {
 #pragma unroll
                     for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
@@ -488,10 +504,11 @@ route_kernel(RouteArgs a)
                 }
                 lds_sync();
                 float size = 0.0f;                                  // of the sums
-                for (int g = h; g < a.p.n_groups; g += 1 << ll) {
+                for (int g = h; g < padded; g += 1 << ll) {
                     float first = none, second = none;
-                    for (int i = 0; i < per; ++i)
-                        best_two(first, second, keys[g * per + i]);
+                    if (g < a.p.n_groups)
+                        for (int i = 0; i < per; ++i)
+                            best_two(first, second, keys[g * per + i]);
                     first = a.p.group_best == 2 && second > none ? first + second : first;
                     sums[g] = first;
                     size = first > none ? fmaxf(size, fabsf(first)) : size;
@@ -501,16 +518,18 @@ route_kernel(RouteArgs a)
                 const float near = 4.0f * off + 8.0f * kStep * size;
                 int taken = 0;
                 for (int g = h; g < a.p.n_groups; g += 1 << ll) {
-                    const float mine = sums[g], high = mine + near, low = mine - near;
-                    int surely = 0, maybe = -1;                     // groups before this one; it is one of the second
-                    for (int o = 0; o < a.p.n_groups; ++o) {
-                        surely += sums[o] > high;
-                        maybe += !(sums[o] < low);
+                    // Groups surely before this one, and surely behind it: too few of either where it is not clear.
+                    const float mine = sums[g], high = -kFar * (mine + near), low = -kFar * (near - mine);
+                    float before = 0.0f, behind = 0.0f;
+                    for (int o = 0; o < padded; o += 4) {
+                        const float4 v = *(const float4 *)(sums + o);
+                        before += one_if_more(v.x, high) + one_if_more(v.y, high) + (one_if_more(v.z, high) + one_if_more(v.w, high));
+                        behind += one_if_more(-v.x, low) + one_if_more(-v.y, low) + (one_if_more(-v.z, low) + one_if_more(-v.w, low));
                     }
                     if (mine > none) {
-                        if (maybe < a.p.top_groups)
+                        if ((float)(padded - 1) - behind < (float)a.p.top_groups)
                             taken |= 1 << g;
-                        else if (surely < a.p.top_groups)
+                        else if (before < (float)a.p.top_groups)
                             again = true;
                     }
                 }
@@ -572,11 +591,12 @@ route_kernel(RouteArgs a)
                 const bool full = last > none;
                 const float near = 2.0f * off + 4.0f * kStep * fmaxf(fabsf(best), full ? fabsf(last) : 0.0f);
                 const float border = full ? last - 1.0001f * near : __builtin_inff();
-                bool doubt = !full || !(near < __builtin_inff());
+                float gap = __builtin_inff();
 #pragma unroll
                 for (int j = 0; j + 1 < KP; ++j)
                     if (j + 1 < a.p.k)
-                        doubt |= !(key_of(list[j]) - key_of(list[j + 1]) > near);
+                        gap = least(gap, key_of(list[j]) - key_of(list[j + 1]));
+                const bool doubt = !full || !(near < __builtin_inff()) || !(gap > near);
                 int above = 0;
 #pragma unroll
                 for (int u = 0; u < kRoutePer; ++u)
@@ -808,7 +828,7 @@ extern "C" int fs_route(const fs_route_params *params, int64_t n_tokens, const v
     const bool exact = bias || groups > 1;
     size_t wave_lds = 0;
     if (exact) {
-        const size_t wide = (size_t)(n + (groups > 1 ? groups : 0)) * 8, rows = groups > 1 ? ((size_t)(n + groups) << (6 - ll)) * 4 : 0;
+        const size_t wide = (size_t)(n + (groups > 1 ? groups : 0)) * 8, rows = groups > 1 ? ((size_t)((n + 3) / 4 + (groups + 3) / 4) << (6 - ll)) * 16 : 0;
         wave_lds = ((wide > rows && wide > 0 ? wide : rows) + 15) / 16 * 16;
     }
     RouteArgs a = {*params, n_tokens, logit_stride, 0, logits, bias, expert, weight, nullptr, nullptr, nullptr, ll, n / groups,
