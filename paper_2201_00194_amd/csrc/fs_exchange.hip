@@ -31,7 +31,6 @@ expert_none_kernel(int32_t n_experts, int32_t *first)
 }
 
 constexpr int kExchangeWaves = 4;      // of a workgroup
-constexpr int kExchangeAhead = 8;      // rows on their way at once
 
 struct ExchangeArgs {
     int64_t n_tokens, in_stride, y_stride, out_stride;
@@ -91,7 +90,7 @@ expert_gather_kernel(ExchangeArgs a)
     clear_slots_behind<T>(a, l.token, c, n);
 }
 
-template <int TYPE>
+template <int TYPE, int AHEAD>
 __global__ void __launch_bounds__(kExchangeWaves * 64)
 expert_combine_kernel(ExchangeArgs a)
 {
@@ -107,18 +106,18 @@ expert_combine_kernel(ExchangeArgs a)
 #pragma unroll
     for (int i = 0; i < N; ++i)
         sum[i] = 0.0f;
-    for (int j0 = 0; j0 < a.k; j0 += kExchangeAhead) {
-        RawChunk<T> x[kExchangeAhead];
-        float w[kExchangeAhead];
+    for (int j0 = 0; j0 < a.k; j0 += AHEAD) {
+        RawChunk<T> x[AHEAD];
+        float w[AHEAD];
 #pragma unroll
-        for (int u = 0; u < kExchangeAhead; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             const int j = min(j0 + u, a.k - 1), p = a.place[l.token * a.k + j];
             const bool there = j0 + u < a.k && p >= 0 && p < slots;
             w[u] = !there ? 0.0f : a.weight ? a.weight[l.token * a.k + j] : 1.0f;
             x[u].load(y + (int64_t)(there ? p : 0) * a.y_stride, there ? n : 0);
         }
 #pragma unroll
-        for (int u = 0; u < kExchangeAhead; ++u)
+        for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 sum[i] = fmaf(w[u], x[u][i], sum[i]);
@@ -127,7 +126,7 @@ expert_combine_kernel(ExchangeArgs a)
 }
 
 // The products need a token's whole width, so that its lanes go over the column blocks themselves.
-template <int TYPE>
+template <int TYPE, int AHEAD>
 __global__ void __launch_bounds__(kExchangeWaves * 64)
 expert_combine_backward_kernel(ExchangeArgs a)
 {
@@ -138,11 +137,11 @@ expert_combine_backward_kernel(ExchangeArgs a)
     const int64_t slots = a.n_tokens * a.k, token = there ? l.token : a.n_tokens - 1;
     if (__ballot(there) == 0)
         return;
-    for (int j0 = 0; j0 < a.k; j0 += kExchangeAhead) {
-        int p[kExchangeAhead];
-        float w[kExchangeAhead], dot[kExchangeAhead];
+    for (int j0 = 0; j0 < a.k; j0 += AHEAD) {
+        int p[AHEAD];
+        float w[AHEAD], dot[AHEAD];
 #pragma unroll
-        for (int u = 0; u < kExchangeAhead; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             const int j = min(j0 + u, a.k - 1);
             p[u] = a.place[token * a.k + j];
             if (!there || j0 + u >= a.k || p[u] < 0 || p[u] >= slots)
@@ -152,13 +151,13 @@ expert_combine_backward_kernel(ExchangeArgs a)
         }
         for (int c = l.h * N; c < a.width; c += 64 * N) {
             const int n = a.width - c;
-            RawChunk<T> g, y[kExchangeAhead];
+            RawChunk<T> g, y[AHEAD];
             g.load((const T *)a.in + token * a.in_stride + c, n);
 #pragma unroll
-            for (int u = 0; u < kExchangeAhead; ++u)
+            for (int u = 0; u < AHEAD; ++u)
                 y[u].load((const T *)a.y + (int64_t)max(p[u], 0) * a.y_stride + c, p[u] >= 0 ? n : 0);
 #pragma unroll
-            for (int u = 0; u < kExchangeAhead; ++u) {
+            for (int u = 0; u < AHEAD; ++u) {
                 if (p[u] < 0)
                     continue;
                 float d[N];
@@ -171,7 +170,7 @@ expert_combine_backward_kernel(ExchangeArgs a)
             }
         }
 #pragma unroll
-        for (int u = 0; u < kExchangeAhead; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             const float all = row_sum(dot[u], a.ll);
             if (there && l.h == 0 && j0 + u < a.k)
                 a.d_weight[token * a.k + j0 + u] = all;
@@ -286,7 +285,8 @@ extern "C" int fs_expert_combine(int64_t n_tokens, int32_t k, int32_t width, con
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
         over_tokens(a, type, false, [&](unsigned blocks) {
-            hipLaunchKernelGGL(expert_combine_kernel<decltype(t)::value>, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
+            const auto kernel = k <= 4 ? expert_combine_kernel<decltype(t)::value, 4> : expert_combine_kernel<decltype(t)::value, 8>;
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
         });
     });
     prof_stop(stream);
@@ -315,7 +315,8 @@ extern "C" int fs_expert_combine_backward(int64_t n_tokens, int32_t k, int32_t n
     prof_start(kKernTrainOther, stream);
     with_type(type, [&](auto t) {
         over_tokens(a, type, true, [&](unsigned blocks) {
-            hipLaunchKernelGGL(expert_combine_backward_kernel<decltype(t)::value>, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
+            const auto kernel = k <= 4 ? expert_combine_backward_kernel<decltype(t)::value, 4> : expert_combine_backward_kernel<decltype(t)::value, 8>;
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
         });
     });
     prof_stop(stream);
