@@ -151,7 +151,7 @@ embed_kernel(EmbedArgs a)
 }
 
 // One id a row: kLookupRows of them a lane.
-template <int IN, int OUT, int ID>
+template <int IN, int OUT, int ID, bool PAST>
 __global__ void __launch_bounds__(kEmbedWaves * 64)
 embed_lookup_kernel(EmbedArgs a)
 {
@@ -178,7 +178,7 @@ embed_lookup_kernel(EmbedArgs a)
 #pragma unroll
         for (int i = 0; i < N; ++i)
             y[i] = x[u][i] * a.scale;
-        store_chunk<N>((Out *)a.out + row(u) * a.out_stride + c, row(u) < a.n_rows ? n : 0, y);
+        store_chunk<N, PAST>((Out *)a.out + row(u) * a.out_stride + c, row(u) < a.n_rows ? n : 0, y);
     }
 }
 
@@ -725,10 +725,10 @@ extern "C" int fs_embed(int32_t n_vocab, int32_t width, const void *table, int32
             constexpr int in = decltype(i)::value, to = decltype(o)::value, id = decltype(d)::value;
             in_pieces((waves + kEmbedWaves - 1) / kEmbedWaves, [&](int64_t at, unsigned n) {
                 a.block0 = at;
-                if (n_cols == 1)
-                    hipLaunchKernelGGL((embed_lookup_kernel<in, to, id>), dim3(n), dim3(kEmbedWaves * 64), 0, stream, a);
-                else
-                    hipLaunchKernelGGL((embed_kernel<in, to, id>), dim3(n), dim3(kEmbedWaves * 64), 0, stream, a);
+                const auto kernel = n_cols > 1                             ? embed_kernel<in, to, id>
+                                    : past_caches(n_rows, width, out_type) ? embed_lookup_kernel<in, to, id, true>
+                                                                           : embed_lookup_kernel<in, to, id, false>;
+                hipLaunchKernelGGL(kernel, dim3(n), dim3(kEmbedWaves * 64), 0, stream, a);
             });
         });
     });

@@ -58,18 +58,18 @@ struct TokenLanes {
 };
 
 // The slots behind the last expert's: the tokens' lanes share them.
-template <class T>
+template <class T, bool PAST = false>
 __device__ __forceinline__ void clear_slots_behind(const ExchangeArgs &a, int64_t token, int c, int n)
 {
     RawChunk<T> zero;
     zero.clear();
     const int64_t slots = a.n_tokens * a.k;
     for (int64_t s = max(a.first[a.n_experts], 0) + token; s < slots; s += a.n_tokens)
-        zero.store((T *)a.out + s * a.out_stride + c, n);
+        zero.template store<PAST>((T *)a.out + s * a.out_stride + c, n);
 }
 
 // A row is read once and written k times.
-template <int TYPE>
+template <int TYPE, bool PAST>
 __global__ void __launch_bounds__(kExchangeWaves * 64)
 expert_gather_kernel(ExchangeArgs a)
 {
@@ -85,9 +85,9 @@ expert_gather_kernel(ExchangeArgs a)
     for (int j = 0; j < a.k; ++j) {
         const int p = place[j];
         if (p >= 0 && p < slots)
-            x.store((T *)a.out + (int64_t)p * a.out_stride + c, n);
+            x.template store<PAST>((T *)a.out + (int64_t)p * a.out_stride + c, n);
     }
-    clear_slots_behind<T>(a, l.token, c, n);
+    clear_slots_behind<T, PAST>(a, l.token, c, n);
 }
 
 template <int TYPE, int AHEAD>
@@ -261,7 +261,9 @@ extern "C" int fs_expert_gather(int64_t n_tokens, int32_t k, int32_t n_experts, 
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
         over_tokens(a, type, false, [&](unsigned blocks) {
-            hipLaunchKernelGGL(expert_gather_kernel<decltype(t)::value>, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
+            const auto kernel = past_caches(n_tokens * k, width, type) ? expert_gather_kernel<decltype(t)::value, true>
+                                                                       : expert_gather_kernel<decltype(t)::value, false>;
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
         });
     });
     prof_stop(stream);

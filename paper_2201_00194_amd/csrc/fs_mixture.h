@@ -165,7 +165,8 @@ __device__ __forceinline__ void load_chunk(const T *p, int n, float (&v)[N], flo
         }
     }
 }
-template <int N, class T>
+// PAST: the stores ask the caches not to keep what they bring; see past_caches.
+template <int N, bool PAST = false, class T>
 __device__ __forceinline__ void store_chunk(T *p, int n, const float (&v)[N])
 {
     if (n >= N) {
@@ -173,7 +174,10 @@ __device__ __forceinline__ void store_chunk(T *p, int n, const float (&v)[N])
 #pragma unroll
         for (int i = 0; i < N; ++i)
             c[i] = (T)v[i];
-        *(typename ChunkOf<T, N>::type *)p = c;
+        if constexpr (PAST)
+            __builtin_nontemporal_store(c, (typename ChunkOf<T, N>::type *)p);
+        else
+            *(typename ChunkOf<T, N>::type *)p = c;
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -210,10 +214,14 @@ struct RawChunk {
             c[i] = (T)0.0f;
     }
     __device__ __forceinline__ float operator[](int i) const { return (float)c[i]; }
+    template <bool PAST = false>
     __device__ __forceinline__ void store(T *p, int n) const
     {
         if (n >= N) {
-            *(Chunk *)p = c;
+            if constexpr (PAST)
+                __builtin_nontemporal_store(c, (Chunk *)p);
+            else
+                *(Chunk *)p = c;
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -222,6 +230,13 @@ struct RawChunk {
         }
     }
 };
+
+// Looked-up and gathered rows of this many bytes leave past the caches: whoever reads them next would find few of them there, and
+// the table's rows stay.  268 MB of looked-up rows 85 us and 58 so, with a pass that reads them next 173 and 168; of gathered
+// ones 63 and 51, 153 and 151; 134 MB 36 and 35, 78 and 80.  Gradients of results stay ordinary stores (268 MB 118 and 109, with
+// their reader 207 and 217).
+constexpr int64_t kPastCaches = 200 << 20;
+inline bool past_caches(int64_t rows, int32_t width, int32_t type) { return rows * width * (int64_t)type_bytes(type) >= kPastCaches; }
 
 // The hardware's reciprocal, one step off at most.
 __device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }
