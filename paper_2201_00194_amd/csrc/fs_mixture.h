@@ -192,10 +192,14 @@ struct RawChunk {
     static constexpr int N = kChunk<T>;
     typedef typename ChunkOf<T, N>::type Chunk;
     Chunk c;
+    template <bool PAST = false>
     __device__ __forceinline__ void load(const T *p, int n)
     {
         if (n >= N) {
-            c = *(const Chunk *)p;
+            if constexpr (PAST)
+                c = __builtin_nontemporal_load((const Chunk *)p);
+            else
+                c = *(const Chunk *)p;
         } else {
             clear();
             if (n > 0) {
