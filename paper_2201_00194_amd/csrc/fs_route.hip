@@ -477,78 +477,108 @@ route_kernel(RouteArgs a)
                 key[u] = x[u] > none ? v : none;
             }
             if (a.p.n_groups > 1) {
-                // A lane ranks groups h, h + (1 << ll), ... of its row.  What they are made of meets in LDS: of groups of whole
-                // chunks every chunk's best two keys, else all keys; then their sums.
-                const bool whole = a.group_size % kChunk<T> == 0;
-                const int width = whole ? n / kChunk<T> * 2 : n, per = width / a.p.n_groups;      // per: of a group
+                // A lane ranks groups h, h + (1 << ll), ... of its row by the sums of all, in LDS.  Of groups of one chunk these are
+                // its own chunks; else what they are made of meets in LDS too: of groups of whole chunks every chunk's best two
+                // keys, else all keys.  A group is taken if fewer than top_groups have more; where more are taken so, or one that is
+                // not is too near to one that is, nothing is decided here.
+                constexpr int kChunks = kRoutePer / kChunk<T>;
                 const int padded = (a.p.n_groups + 3) & ~3;         // sums of nobody's groups behind
-                float *keys = (float *)own + (lane >> ll) * width, *sums = (float *)own + ((((n + 3) & ~3) << (6 - ll)) + (lane >> ll) * padded);
+                float *const sums = (float *)own + ((((n + 3) & ~3) << (6 - ll)) + (lane >> ll) * padded);
+                const bool one = a.group_size == kChunk<T>, whole = a.group_size % kChunk<T> == 0;
+                float best[kChunks][2];
                 if (whole) {
 #pragma unroll
-                    for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
-                        const int e = expert_at<T>(c * kChunk<T>, ll, h);
-                        float first = key[c * kChunk<T>], second = none;
+                    for (int c = 0; c < kChunks; ++c) {
+                        best[c][0] = key[c * kChunk<T>];
+                        best[c][1] = none;
 #pragma unroll
                         for (int i = 1; i < kChunk<T>; ++i)
-                            best_two(first, second, key[c * kChunk<T> + i]);
-                        if (e < n)
-                            *(float2 *)(keys + e / kChunk<T> * 2) = make_float2(first, second);
-                    }
-                } else {
-#pragma unroll
-                    for (int u = 0; u < kRoutePer; ++u) {
-                        const int e = expert_at<T>(u, ll, h);
-                        if (e < n)
-                            keys[e] = key[u];
+                            best_two(best[c][0], best[c][1], key[c * kChunk<T> + i]);
                     }
                 }
-                lds_sync();
-                float size = 0.0f;                                  // of the sums
-                for (int g = h; g < padded; g += 1 << ll) {
-                    float first = none, second = none;
-                    if (g < a.p.n_groups)
-                        for (int i = 0; i < per; ++i)
-                            best_two(first, second, keys[g * per + i]);
-                    first = a.p.group_best == 2 && second > none ? first + second : first;
-                    sums[g] = first;
-                    size = first > none ? fmaxf(size, fabsf(first)) : size;
-                }
-                lds_sync();
-                size = row_max(size, ll);
-                const float near = 4.0f * off + 8.0f * kStep * size;
-                int taken = 0;
-                for (int g = h; g < a.p.n_groups; g += 1 << ll) {
-                    // Groups surely before this one, and surely behind it: too few of either where it is not clear.
-                    const float mine = sums[g], high = -kFar * (mine + near), low = -kFar * (near - mine);
-                    float before = 0.0f, behind = 0.0f;
+                const auto sum_of = [&](float first, float second) { return a.p.group_best == 2 && second > none ? first + second : first; };
+                const auto more_than = [&](float mine) {
+                    const float minus = -kFar * mine;
+                    float n = 0.0f;
                     for (int o = 0; o < padded; o += 4) {
                         const float4 v = *(const float4 *)(sums + o);
-                        before += one_if_more(v.x, high) + one_if_more(v.y, high) + (one_if_more(v.z, high) + one_if_more(v.w, high));
-                        behind += one_if_more(-v.x, low) + one_if_more(-v.y, low) + (one_if_more(-v.z, low) + one_if_more(-v.w, low));
+                        n += one_if_more(v.x, minus) + one_if_more(v.y, minus) + (one_if_more(v.z, minus) + one_if_more(v.w, minus));
                     }
-                    if (mine > none) {
-                        if ((float)(padded - 1) - behind < (float)a.p.top_groups)
-                            taken |= 1 << g;
-                        else if (before < (float)a.p.top_groups)
-                            again = true;
-                    }
-                }
-                taken = row_or(taken, ll);
-                if (whole) {
+                    return n;
+                };
+                const float top_groups = (float)a.p.top_groups;
+                float size = 0.0f, lowest = __builtin_inff(), highest = none, count = 0.0f;     // of the taken, of the others
+                if (one) {
+                    float sum[kChunks];
 #pragma unroll
-                    for (int c = 0; c < kRoutePer / kChunk<T>; ++c) {
-                        const bool in = taken >> ((uint32_t)expert_at<T>(c * kChunk<T>, ll, h) * a.group_magic >> 22 & 31) & 1;
+                    for (int c = 0; c < kChunks; ++c) {
+                        sum[c] = sum_of(best[c][0], best[c][1]);
+                        if ((c << ll) + h < padded)
+                            sums[(c << ll) + h] = sum[c];
+                    }
+                    lds_sync();
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) {
+                        const bool in = sum[c] > none && more_than(sum[c]) < top_groups;
+                        size = sum[c] > none ? fmaxf(size, fabsf(sum[c])) : size;
+                        lowest = in ? fminf(lowest, sum[c]) : lowest;
+                        highest = in ? highest : fmaxf(highest, sum[c]);
+                        count += in ? 1.0f : 0.0f;
 #pragma unroll
                         for (int i = 0; i < kChunk<T>; ++i)
                             key[c * kChunk<T> + i] = in ? key[c * kChunk<T> + i] : none;
                     }
+                    count = row_sum(count, ll);
                 } else {
+                    const int width = whole ? n / kChunk<T> * 2 : n, per = width / a.p.n_groups;      // per: of a group
+                    float *const keys = (float *)own + (lane >> ll) * width;
+                    if (whole) {
+#pragma unroll
+                        for (int c = 0; c < kChunks; ++c) {
+                            const int e = expert_at<T>(c * kChunk<T>, ll, h);
+                            if (e < n)
+                                *(float2 *)(keys + e / kChunk<T> * 2) = make_float2(best[c][0], best[c][1]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < kRoutePer; ++u) {
+                            const int e = expert_at<T>(u, ll, h);
+                            if (e < n)
+                                keys[e] = key[u];
+                        }
+                    }
+                    lds_sync();
+                    for (int g = h; g < padded; g += 1 << ll) {
+                        float first = none, second = none;
+                        if (g < a.p.n_groups)
+                            for (int i = 0; i < per; ++i)
+                                best_two(first, second, keys[g * per + i]);
+                        sums[g] = sum_of(first, second);
+                    }
+                    lds_sync();
+                    int taken = 0;
+                    for (int g = h; g < a.p.n_groups; g += 1 << ll) {
+                        const float mine = sums[g];
+                        const bool in = mine > none && more_than(mine) < top_groups;
+                        size = mine > none ? fmaxf(size, fabsf(mine)) : size;
+                        lowest = in ? fminf(lowest, mine) : lowest;
+                        highest = in ? highest : fmaxf(highest, mine);
+                        taken |= in ? 1 << g : 0;
+                    }
+                    taken = row_or(taken, ll);
+                    count = (float)__popc(taken);
 #pragma unroll
                     for (int u = 0; u < kRoutePer; ++u) {
-                        const bool in = taken >> ((uint32_t)expert_at<T>(u, ll, h) * a.group_magic >> 22 & 31) & 1;
+                        const int e = whole ? expert_at<T>(u / kChunk<T> * kChunk<T>, ll, h) : expert_at<T>(u, ll, h);
+                        const bool in = taken >> ((uint32_t)e * a.group_magic >> 22 & 31) & 1;
                         key[u] = in ? key[u] : none;
                     }
                 }
+                size = row_max(size, ll);
+                lowest = -row_max(-lowest, ll);
+                highest = row_max(highest, ll);
+                const float near = 4.0f * off + 8.0f * kStep * size;
+                again |= count > top_groups || !(lowest - highest > near);
             }
             if (!a.bias)
 #pragma unroll
