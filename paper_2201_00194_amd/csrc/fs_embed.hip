@@ -15,7 +15,7 @@ constexpr int kEmbedAhead = 8;            // rows on their way at once
 constexpr int kEmbedFewWaves = 2048;
 constexpr int kLookupRows = 4;            // rows of a lane
 constexpr int kSumMostWaves = 4096;
-constexpr int kSumMostChunk = 256, kSumLeastChunk = 16;   // pairs a chunk
+constexpr int kSumMostChunk = 256, kSumLeastChunk = 8;    // pairs a chunk
 constexpr int kSumWaves = 8;              // of a workgroup
 constexpr int kJoinAhead = 16;            // partial sums on their way at once
 
