@@ -37,13 +37,13 @@ struct RouteArgs {
     int64_t block0;                      // of this launch
 };
 
-// The value between -infinity and `most`; -infinity for a quiet NaN, as the instruction is defined.  (The compiler's own
-// median lets a NaN be anything.)
+// The value between -infinity and `most`; -infinity for a quiet NaN, as the median of three is defined on this hardware.  The
+// compiler, where it sees the -infinity, takes the minimum of the other two instead, which is not.
 __device__ __forceinline__ float bounded(float v, float most)
 {
-    float r;
-    asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(v), "v"(-__builtin_inff()), "s"(most));
-    return r;
+    float least = -__builtin_inff();
+    asm("" : "+v"(least));
+    return __builtin_amdgcn_fmed3f(v, least, most);
 }
 // NaN masks an expert as -infinity does; +infinity counts as the largest float.
 __device__ __forceinline__ float route_logit(float l) { return bounded(__builtin_canonicalizef(l), 3.402823466e38f); }
@@ -186,24 +186,15 @@ __device__ __forceinline__ float key_of(double v)
 // later.  The difference of two floats of common size times kFar is at least 1, or 0 or less; where sizes are not common, or
 // infinite, it may be 0.
 constexpr float kFar = 1.2676506e30f;     // 2^100
-__device__ __forceinline__ float one_if_more(float a, float minus_b_far)
-{
-    float r;
-    asm("v_fma_f32 %0, %1, %2, %3 clamp" : "=v"(r) : "v"(a), "s"(kFar), "v"(minus_b_far));
-    return r;
-}
-__device__ __forceinline__ float least(float a, float b)
-{
-    asm("v_min_f32 %0, %0, %1" : "+v"(a) : "v"(b));
-    return a;
-}
+__device__ __forceinline__ float one_if_more(float a, float minus_b_far) { return __builtin_amdgcn_fmed3f(fmaf(a, kFar, minus_b_far), 0.0f, 1.0f); }
 // Two of the largest so far, and another value.
 __device__ __forceinline__ void best_two(float &first, float &second, float v)
 {
-    asm("v_med3_f32 %0, %1, %0, %2" : "+v"(second) : "v"(first), "v"(v));
-    asm("v_max_f32 %0, %0, %1" : "+v"(first) : "v"(v));
+    second = __builtin_amdgcn_fmed3f(first, second, v);
+    first = fmaxf(first, v);
 }
-// __builtin_fmax would first make signalling NaNs quiet; there are none.
+// __builtin_fmax would first make signalling NaNs quiet; there are none.  The compiler does not know of the wait that a value
+// made so needs before another lane takes it: settled() is that wait.
 __device__ __forceinline__ double larger(double a, double b)
 {
     double r;
@@ -259,9 +250,25 @@ __device__ __forceinline__ void merge_list(double (&list)[KP], const double (&ot
             if ((i & q) == 0)
                 in_order(list[i], list[i + q]);
 }
+template <int KP>
+__device__ __forceinline__ void settled(double (&list)[KP])
+{
+    if constexpr (KP == 2) {
+        asm volatile("s_nop 1" : "+v"(list[0]), "+v"(list[1]));
+    } else if constexpr (KP == 4) {
+        asm volatile("s_nop 1" : "+v"(list[0]), "+v"(list[1]), "+v"(list[2]), "+v"(list[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < KP; i += 8)
+            asm volatile("s_nop 1"
+                         : "+v"(list[i]), "+v"(list[i + 1]), "+v"(list[i + 2]), "+v"(list[i + 3]), "+v"(list[i + 4]), "+v"(list[i + 5]),
+                           "+v"(list[i + 6]), "+v"(list[i + 7]));
+    }
+}
 template <int STEP, int KP>
 __device__ __forceinline__ void merge_met(double (&list)[KP])
 {
+    settled<KP>(list);
     double other[KP];
 #pragma unroll
     for (int i = 0; i < KP; ++i)
@@ -625,7 +632,7 @@ route_kernel(RouteArgs a)
 #pragma unroll
                 for (int j = 0; j + 1 < KP; ++j)
                     if (j + 1 < a.p.k)
-                        gap = least(gap, key_of(list[j]) - key_of(list[j + 1]));
+                        gap = fminf(gap, key_of(list[j]) - key_of(list[j + 1]));
                 const bool doubt = !full || !(near < __builtin_inff()) || !(gap > near);
                 int above = 0;
 #pragma unroll
