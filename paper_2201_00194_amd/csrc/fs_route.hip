@@ -523,6 +523,8 @@ route_kernel(RouteArgs a)
                         if ((c << ll) + h < padded)
                             sums[(c << ll) + h] = sum[c];
                     }
+                    for (int g = (kChunks << ll) + h; g < padded; g += 1 << ll)       // 2 groups of 8: nobody's, behind the last chunk
+                        sums[g] = none;
                     lds_sync();
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) {

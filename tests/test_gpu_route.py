@@ -101,6 +101,17 @@ def test_groups(api, typ, score, experts, groups, top, best, k):
             assert np.all(e[:, top * (experts // groups):] == -1)
 
 
+@pytest.mark.parametrize("typ", list(TYPES))
+@pytest.mark.parametrize("groups,per", [(2, 8), (3, 8), (5, 8), (2, 4), (3, 4), (7, 4), (2, 16), (3, 1)])
+def test_few_groups_after_a_call_with_larger_keys(api, typ, groups, per):
+    """Groups that do not fill the lanes' last chunks rank by their own keys, whatever an earlier call left where sums are kept."""
+    n = groups * per
+    for level in (-40.0, 40.0):
+        check(api, normal(1, 700, 256), 8, bias=np.full(256, 40.0), n_groups=32, top_groups=3, group_best=2)
+        bias = np.random.default_rng(6).standard_normal(n) * 0.05 + level
+        check(api, normal(n, 300, n, typ), min(4, n), score="sigmoid", bias=bias, n_groups=groups, top_groups=1, group_best=2)
+
+
 def special(experts):
     """Rows of masks and extreme values."""
     low, inf, nan = float(np.finfo(np.float32).min), np.inf, np.nan
