@@ -486,8 +486,9 @@ route_kernel(RouteArgs a)
             if (a.p.n_groups > 1) {
                 // A lane ranks groups h, h + (1 << ll), ... of its row by the sums of all, in LDS.  Of groups of one chunk these are
                 // its own chunks; else what they are made of meets in LDS too: of groups of whole chunks every chunk's best two
-                // keys, else all keys.  A group is taken if fewer than top_groups have more; where more are taken so, or one that is
-                // not is too near to one that is, nothing is decided here.
+                // keys, else all keys.  A group is taken if fewer than top_groups have more; where more are taken so, or fewer though
+                // others are there (sums of 2^28 and more are not compared), or one that is not is too near to one that is, nothing is
+                // decided here.
                 constexpr int kChunks = kRoutePer / kChunk<T>;
                 const int padded = (a.p.n_groups + 3) & ~3;         // sums of nobody's groups behind
                 float *const sums = (float *)own + ((((n + 3) & ~3) << (6 - ll)) + (lane >> ll) * padded);
@@ -503,7 +504,8 @@ route_kernel(RouteArgs a)
                             best_two(best[c][0], best[c][1], key[c * kChunk<T> + i]);
                     }
                 }
-                const auto sum_of = [&](float first, float second) { return a.p.group_best == 2 && second > none ? first + second : first; };
+                // Two keys of finite size have a sum, whatever fp32 makes of it.
+                const auto sum_of = [&](float first, float second) { return a.p.group_best == 2 && second > none ? fmaxf(first + second, -3.402823466e38f) : first; };
                 const auto more_than = [&](float mine) {
                     const float minus = -kFar * mine;
                     float n = 0.0f;
@@ -587,7 +589,7 @@ route_kernel(RouteArgs a)
                 lowest = -row_max(-lowest, ll);
                 highest = row_max(highest, ll);
                 const float near = 4.0f * off + 8.0f * kStep * size;
-                again |= count > top_groups || !(lowest - highest > near);
+                again |= (highest > none ? count != top_groups : count > top_groups) || !(lowest - highest > near);
             }
             if (!a.bias)
 #pragma unroll

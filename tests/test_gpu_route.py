@@ -112,6 +112,20 @@ def test_few_groups_after_a_call_with_larger_keys(api, typ, groups, per):
         check(api, normal(n, 300, n, typ), min(4, n), score="sigmoid", bias=bias, n_groups=groups, top_groups=1, group_best=2)
 
 
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+@pytest.mark.parametrize("experts,groups,top", [(64, 8, 4), (64, 16, 5), (30, 5, 3), (16, 2, 1), (256, 4, 2)])
+@pytest.mark.parametrize("level", [-3.4028235e38, -1e30, -3e8, 3e8, 1e30])
+def test_groups_with_biases_far_from_each_other(api, typ, experts, groups, top, level):
+    """Biases that stand for 'last resort' or 'always': their experts are eligible all the same."""
+    rng = np.random.default_rng(7)
+    near = rng.standard_normal(experts) * 0.05
+    of_group = np.repeat(np.arange(groups), experts // groups)
+    for far in (of_group >= 1, of_group == 0, np.full(experts, True), rng.random(experts) < 0.5):
+        for best in (1, 2):
+            check(api, normal(5, 37, experts, typ), min(8, top * (experts // groups)), score="sigmoid", bias=np.where(far, level, near),
+                  n_groups=groups, top_groups=top, group_best=best)
+
+
 def special(experts):
     """Rows of masks and extreme values."""
     low, inf, nan = float(np.finfo(np.float32).min), np.inf, np.nan
