@@ -18,6 +18,7 @@ constexpr int kSumMostWaves = 4096;
 constexpr int kSumMostChunk = 256, kSumLeastChunk = 8;    // pairs a chunk
 constexpr int kSumWaves = 8;              // of a workgroup
 constexpr int kJoinAhead = 16;            // partial sums on their way at once
+constexpr int kBlockSlots = 16;           // a wavefront's sums, where one row takes all its lanes
 
 template <int ID> struct IdOf;
 template <> struct IdOf<FS_ID_I32> { typedef int32_t type; };
@@ -104,7 +105,8 @@ embed_kernel(EmbedArgs a)
         return;
     const bool there = row0 + (lane >> (ll + a.split)) < a.n_rows;
     const int64_t row = there ? row0 + (lane >> (ll + a.split)) : a.n_rows - 1;
-    const int c = ((a.columns == 1 ? 0 : (int)(wave % a.columns)) * 64 + h) * N, n = a.width - c;
+    const Span at = span_of<N>(((a.columns == 1 ? 0 : (int)(wave % a.columns)) * 64 + h) * N, a.width);
+    const int c = at.c, n = at.n;
     const int cols = a.ids.n_cols, per = (cols + (1 << a.split) - 1) >> a.split;
     const int begin = min(part * per, cols), end = min(begin + per, cols);
     const In *const in = (const In *)a.in + c;
@@ -163,7 +165,8 @@ embed_lookup_kernel(EmbedArgs a)
     const int64_t row0 = ((a.columns == 1 ? wave : wave / a.columns) * kLookupRows) << (6 - ll);
     if (row0 >= a.n_rows)
         return;
-    const int c = ((a.columns == 1 ? 0 : (int)(wave % a.columns)) * 64 + h) * N, n = a.width - c;
+    const Span at = span_of<N>(((a.columns == 1 ? 0 : (int)(wave % a.columns)) * 64 + h) * N, a.width);
+    const int c = at.c, n = at.n;
     const In *const in = (const In *)a.in + c;
     const auto row = [&](int u) { return row0 + (u << (6 - ll)) + (lane >> ll); };
     int v[kLookupRows];
@@ -258,8 +261,11 @@ __device__ __forceinline__ void clear_table(void *table, int64_t n_rows, int32_t
     RawChunk<T> zero;
     zero.clear();
     for (int64_t r = ((b * waves + (threadIdx.x >> 6)) << (6 - ll)) + (lane >> ll); r < n_rows; r += (blocks * waves) << (6 - ll))
-        for (int c = h * N; c < width; c += 64 * N)
-            zero.store((T *)table + r * stride + c, width - c);
+        for (int c0 = h * N; c0 < width; c0 += 64 * N) {
+            const Span at = span_of<N>(c0, width);
+            const int c = at.c, n = at.n;
+            zero.store((T *)table + r * stride + c, n);
+        }
 }
 struct ClearArgs {
     void *table;                   // or NULL
@@ -376,8 +382,8 @@ __device__ __forceinline__ void put_row(const SumArgs &a, int token, int c, int 
 }
 
 // A chunk of the list is added by the lanes of one row, in fp32.  What a workgroup's chunks have of runs that go on beyond
-// them, two sums a chunk at most, meets in LDS, where the lanes of a run's first sum add them up, in 64 bits; what the workgroup
-// has of runs that go on beyond it goes to memory.
+// them, two sums a chunk at most, meets in LDS, where the lanes of a run's first sum add them up, in 64 bits (blocks of sixteen
+// are rounded between); what the workgroup has of runs that go on beyond it goes to memory.
 template <int IN, int OUT, class P>
 __global__ void __launch_bounds__(kSumWaves * 64)
 embed_sum_kernel(SumArgs a)
@@ -387,6 +393,7 @@ embed_sum_kernel(SumArgs a)
     constexpr int N = kChunk<In>;
     __shared__ uint32_t slot_token[2 * kSumWaves * 64];
     __shared__ float slot_sum[2 * kSumWaves * 64 * N];
+    __shared__ uint32_t whole[2 * kSumWaves * 64 / kBlockSlots];
     const int lane = threadIdx.x & 63, ll = a.ll, h = lane & ((1 << ll) - 1);
     const int units = kSumWaves << (6 - ll), unit = ((threadIdx.x >> 6) << (6 - ll)) + (lane >> ll), slots = 2 * units;
     // With bands, an XCD takes stretches of one of them.
@@ -400,7 +407,8 @@ embed_sum_kernel(SumArgs a)
     }
     const int64_t group_begin = group * units * a.chunk, group_end = min(group_begin + (int64_t)units * a.chunk, a.n);
     const int64_t begin = group_begin + (int64_t)unit * a.chunk, end = min(begin + a.chunk, a.n);
-    const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
+    const Span at = span_of<N>(((int)blockIdx.y * 64 + h) * N, a.width, !a.accumulate);
+    const int c = at.c, n = at.n;
     const In *const in = (const In *)a.in + c;
     const P *const list = (const P *)a.list;
     // The tokens before and behind the group and the chunk, on their way together.
@@ -465,11 +473,51 @@ embed_sum_kernel(SumArgs a)
         slot_token[2 * unit] = slot_token[2 * unit + 1] = kNoToken;
     }
     __syncthreads();
+    // A long run's sums would be one lane's after the other: blocks of them that are all of one run become one sum first.
+    if (unit % (kBlockSlots / 2) == 0) {
+        const int s = 2 * unit;
+        uint32_t met[kBlockSlots];
+#pragma unroll
+        for (int u = 0; u < kBlockSlots; ++u)
+            met[u] = slot_token[s + u];
+        bool same = met[0] != kNoToken;
+#pragma unroll
+        for (int u = 1; u < kBlockSlots; ++u)
+            same = same && met[u] >> 1 == met[0] >> 1;
+        if (same) {
+            double all[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                all[i] = 0.0;
+            bool some = false;
+#pragma unroll
+            for (int u = 0; u < kBlockSlots; ++u)
+                if (!(met[u] & 1)) {
+                    some = true;
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        all[i] += (double)slot_sum[(((s + u) << ll) + h) * N + i];
+                }
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                slot_sum[((s << ll) + h) * N + i] = (float)all[i];
+            if (h == 0)
+                slot_token[s] = (met[0] & ~1u) | (some ? 0u : 1u);
+        }
+        if (h == 0)
+            whole[s / kBlockSlots] = same;
+    }
+    __syncthreads();
     for (int which = 0; which < 2; ++which) {
         const int s = 2 * unit + which;
         const uint32_t token = slot_token[s] >> 1;
         if (s > 0 && slot_token[s - 1] >> 1 == token)
             continue;                                            // not a run's first sum
+        if (token == kNoToken >> 1) {                            // the list has ended: from here on nobody's
+            if (h == 0 && blockIdx.y == 0)
+                a.part_token[2 * group + 1] = kNoToken;
+            continue;
+        }
         double all[N];
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -483,7 +531,7 @@ embed_sum_kernel(SumArgs a)
                 for (int i = 0; i < N; ++i)
                     all[i] += (double)slot_sum[((e << ll) + h) * N + i];
             }
-            ++e;
+            e += e % kBlockSlots == 0 && whole[e / kBlockSlots] ? kBlockSlots : 1;
         } while (e < slots && slot_token[e] >> 1 == token);
         const bool left = s == 0 && group_before == (int)token, right = e == slots && group_behind == (int)token;
         float sum[N];
@@ -520,7 +568,8 @@ embed_join_kernel(SumArgs a)
     const uint32_t token = a.part_token[s] >> 1;
     if (token == kNoToken >> 1 || plain_token(a.packing, (int)token) >= a.n_vocab || (s > 0 && a.part_token[s - 1] >> 1 == token))
         return;
-    const int c = ((int)blockIdx.y * 64 + h) * N, n = a.width - c;
+    const Span at = span_of<N>(((int)blockIdx.y * 64 + h) * N, a.width, !a.accumulate);
+    const int c = at.c, n = at.n;
     double all[N];
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -565,8 +614,9 @@ embed_bands_kernel(SumArgs a, const float *tables)
     const int64_t row = (((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) << (6 - a.ll)) + (lane >> a.ll);
     if (row >= a.n_vocab)
         return;
-    for (int c = h * N; c < a.width; c += 64 * N) {
-        const int n = a.width - c;
+    for (int c0 = h * N; c0 < a.width; c0 += 64 * N) {
+        const Span at = span_of<N>(c0, a.width, !a.accumulate);
+        const int c = at.c, n = at.n;
         float sum[N], more[kXcds][N];
 #pragma unroll
         for (int b = 0; b < kXcds; ++b)

@@ -31,6 +31,8 @@ expert_none_kernel(int32_t n_experts, int32_t *first)
 }
 
 constexpr int kExchangeWaves = 4;      // of a workgroup
+// From so many bytes of results on, which is more wavefronts than run at once, a lane works on two tokens of up to four choices.
+constexpr int64_t kTwoTokens = 16 << 20;
 
 struct ExchangeArgs {
     int64_t n_tokens, in_stride, y_stride, out_stride;
@@ -43,17 +45,19 @@ struct ExchangeArgs {
     float *d_weight;
     int64_t block0;                  // of this launch
 };
-// Lanes (1 << ll) to a token; of a wide row, `columns` neighbouring wavefronts, so that they read a row at one time.
+// Lanes (1 << ll) to a token; of a wide row, `columns` neighbouring wavefronts, so that they read a row at one time.  A lane
+// works on tokens token, token + step, ...: `tokens` of them.
 struct TokenLanes {
-    int h, column;
+    int h, column, step;
     int64_t token;
-    __device__ __forceinline__ explicit TokenLanes(const ExchangeArgs &a)
+    __device__ __forceinline__ explicit TokenLanes(const ExchangeArgs &a, int tokens = 1)
     {
         const int lane = threadIdx.x & 63;
         h = lane & ((1 << a.ll) - 1);
         const int64_t wave = (a.block0 + blockIdx.x) * kExchangeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         column = a.columns == 1 ? 0 : (int)(wave % a.columns);
-        token = a.columns == 1 ? (wave << (6 - a.ll)) + (lane >> a.ll) : wave / a.columns;
+        token = a.columns == 1 ? ((wave * tokens) << (6 - a.ll)) + (lane >> a.ll) : wave / a.columns * tokens;
+        step = 1 << (6 - a.ll);
     }
 };
 
@@ -77,7 +81,8 @@ expert_gather_kernel(ExchangeArgs a)
     const TokenLanes l(a);
     if (l.token >= a.n_tokens)
         return;
-    const int c = (l.column * 64 + l.h) * kChunk<T>, n = a.width - c;
+    const Span at = span_of<kChunk<T>>((l.column * 64 + l.h) * kChunk<T>, a.width);
+    const int c = at.c, n = at.n;
     const int64_t slots = a.n_tokens * a.k;
     RawChunk<T> x;
     x.load((const T *)a.in + l.token * a.in_stride + c, n);
@@ -92,39 +97,58 @@ expert_gather_kernel(ExchangeArgs a)
 
 // Results are read once and not kept in the caches: 32768 rows of 164 features, slots, gather and this in turn, 66 us with them
 // kept and 60 so.
-template <int TYPE, int AHEAD>
+template <int TYPE, int AHEAD, int TOKENS>
 __global__ void __launch_bounds__(kExchangeWaves * 64)
 expert_combine_kernel(ExchangeArgs a)
 {
     typedef typename Element<TYPE>::type T;
     constexpr int N = kChunk<T>;
-    const TokenLanes l(a);
+    const TokenLanes l(a, TOKENS);
     if (l.token >= a.n_tokens)
         return;
-    const int c = (l.column * 64 + l.h) * N, n = a.width - c;
+    const Span at = span_of<N>((l.column * 64 + l.h) * N, a.width);
+    const int c = at.c, n = at.n;
     const int64_t slots = a.n_tokens * a.k;
     const T *const y = (const T *)a.y + c;
-    float sum[N];
+    float sum[TOKENS][N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        sum[i] = 0.0f;
+    for (int t = 0; t < TOKENS; ++t)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            sum[t][i] = 0.0f;
     for (int j0 = 0; j0 < a.k; j0 += AHEAD) {
-        RawChunk<T> x[AHEAD];
-        float w[AHEAD];
+        int p[TOKENS][AHEAD];
+        float w[TOKENS][AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int j = min(j0 + u, a.k - 1), p = a.place[l.token * a.k + j];
-            const bool there = j0 + u < a.k && p >= 0 && p < slots;
-            w[u] = !there ? 0.0f : a.weight ? a.weight[l.token * a.k + j] : 1.0f;
-            x[u].template load<true>(y + (int64_t)(there ? p : 0) * a.y_stride, there ? n : 0);
-        }
+        for (int t = 0; t < TOKENS; ++t)
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t at = min(l.token + t * l.step, a.n_tokens - 1) * a.k + min(j0 + u, a.k - 1);
+                p[t][u] = a.place[at];
+                w[t][u] = a.weight ? a.weight[at] : 1.0f;
+            }
+        RawChunk<T> x[TOKENS][AHEAD];
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                sum[i] = fmaf(w[u], x[u][i], sum[i]);
+        for (int t = 0; t < TOKENS; ++t)
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const bool there = j0 + u < a.k && p[t][u] >= 0 && p[t][u] < slots && l.token + t * l.step < a.n_tokens;
+                w[t][u] = there ? w[t][u] : 0.0f;
+                x[t][u].template load<true>(y + (int64_t)(there ? p[t][u] : 0) * a.y_stride, there ? n : 0);
+            }
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t)
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    sum[t][i] = fmaf(w[t][u], x[t][u][i], sum[t][i]);
     }
-    store_chunk<N>((T *)a.out + l.token * a.out_stride + c, n, sum);
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+        const int64_t token = l.token + t * l.step;
+        store_chunk<N>((T *)a.out + token * a.out_stride + c, token < a.n_tokens ? n : 0, sum[t]);
+    }
 }
 
 // The products need a token's whole width, so that its lanes go over the column blocks themselves.
@@ -151,8 +175,9 @@ expert_combine_backward_kernel(ExchangeArgs a)
             w[u] = a.weight[token * a.k + j];
             dot[u] = 0.0f;
         }
-        for (int c = l.h * N; c < a.width; c += 64 * N) {
-            const int n = a.width - c;
+        for (int c0 = l.h * N; c0 < a.width; c0 += 64 * N) {
+            const Span at = span_of<N>(c0, a.width);
+            const int c = at.c, n = at.n;
             RawChunk<T> g, y[AHEAD];
             g.load((const T *)a.in + token * a.in_stride + c, n);
 #pragma unroll
@@ -165,7 +190,7 @@ expert_combine_backward_kernel(ExchangeArgs a)
                 float d[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    dot[u] = fmaf(g[i], y[u][i], dot[u]);
+                    dot[u] = i < at.skip ? dot[u] : fmaf(g[i], y[u][i], dot[u]);
                     d[i] = w[u] * g[i];
                 }
                 store_chunk<N>((T *)a.out + (int64_t)p[u] * a.out_stride + c, n, d);
@@ -179,18 +204,21 @@ expert_combine_backward_kernel(ExchangeArgs a)
         }
     }
     if (there)
-        for (int c = l.h * N; c < a.width; c += 64 * N)
-            clear_slots_behind<T>(a, token, c, a.width - c);
+        for (int c0 = l.h * N; c0 < a.width; c0 += 64 * N) {
+            const Span at = span_of<N>(c0, a.width);
+            const int c = at.c, n = at.n;
+            clear_slots_behind<T>(a, token, c, n);
+        }
 }
 
 // f(workgroups) launches what one launch holds; a's numbers of lanes, columns and workgroups are set.
 template <class F>
-void over_tokens(ExchangeArgs &a, int32_t type, bool whole_rows, F f)
+void over_tokens(ExchangeArgs &a, int32_t type, bool whole_rows, int tokens, F f)
 {
     const int chunk = 16 / (int)type_bytes(type);
     a.ll = row_lanes_log(a.width, chunk);
     a.columns = whole_rows ? 1 : column_blocks(a.width, chunk);
-    const int64_t waves = (a.n_tokens * a.columns + ((int64_t)1 << (6 - a.ll)) - 1) >> (6 - a.ll);
+    const int64_t each = (int64_t)tokens << (6 - a.ll), waves = (a.n_tokens + each - 1) / each * a.columns;
     in_pieces((waves + kExchangeWaves - 1) / kExchangeWaves, [&](int64_t at, unsigned blocks) {
         a.block0 = at;
         f(blocks);
@@ -262,7 +290,7 @@ extern "C" int fs_expert_gather(int64_t n_tokens, int32_t k, int32_t n_experts, 
     ExchangeArgs a = {n_tokens, x_stride, 0, xs_stride, k, n_experts, width, 0, 1, x, nullptr, first, place, nullptr, xs, nullptr, 0};
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
-        over_tokens(a, type, false, [&](unsigned blocks) {
+        over_tokens(a, type, false, 1, [&](unsigned blocks) {
             const auto kernel = past_caches(n_tokens * k, width, type) ? expert_gather_kernel<decltype(t)::value, true>
                                                                        : expert_gather_kernel<decltype(t)::value, false>;
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
@@ -288,8 +316,12 @@ extern "C" int fs_expert_combine(int64_t n_tokens, int32_t k, int32_t width, con
     ExchangeArgs a = {n_tokens, 0, y_stride, out_stride, k, 0, width, 0, 1, nullptr, y, nullptr, place, weight, out, nullptr, 0};
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
-        over_tokens(a, type, false, [&](unsigned blocks) {
-            const auto kernel = k <= 4 ? expert_combine_kernel<decltype(t)::value, 4> : expert_combine_kernel<decltype(t)::value, 8>;
+        constexpr int element = decltype(t)::value;
+        const bool two = k <= 4 && n_tokens * width * (int64_t)type_bytes(type) >= kTwoTokens;
+        over_tokens(a, type, false, two ? 2 : 1, [&](unsigned blocks) {
+            const auto kernel = two      ? expert_combine_kernel<element, 4, 2>
+                                : k <= 4 ? expert_combine_kernel<element, 4, 1>
+                                         : expert_combine_kernel<element, 8, 1>;
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
         });
     });
@@ -318,7 +350,7 @@ extern "C" int fs_expert_combine_backward(int64_t n_tokens, int32_t k, int32_t n
     ExchangeArgs a = {n_tokens, d_out_stride, y_stride, d_y_stride, k, n_experts, width, 0, 1, d_out, y, first, place, weight, d_y, d_weight, 0};
     prof_start(kKernTrainOther, stream);
     with_type(type, [&](auto t) {
-        over_tokens(a, type, true, [&](unsigned blocks) {
+        over_tokens(a, type, true, 1, [&](unsigned blocks) {
             const auto kernel = k <= 4 ? expert_combine_backward_kernel<decltype(t)::value, 4> : expert_combine_backward_kernel<decltype(t)::value, 8>;
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kExchangeWaves * 64), 0, stream, a);
         });

@@ -186,6 +186,19 @@ __device__ __forceinline__ void store_chunk(T *p, int n, const float (&v)[N])
     }
 }
 
+// Elements c .. c + N - 1 of a row, n of them there.  The last chunk of a row moves back until it is whole, where the row has so many
+// elements: its first `skip` are its neighbour's too, and both write the same.  (Element by element it costs twice as many
+// loads as all other chunks together.)  `whole` false: it stays where it is, for sums onto what is there.
+struct Span {
+    int c, n, skip;
+};
+template <int N>
+__device__ __forceinline__ Span span_of(int c, int width, bool whole = true)
+{
+    const int n = width - c, skip = whole && n > 0 && n < N && width >= N ? N - n : 0;
+    return Span{c - skip, n + skip, skip};
+}
+
 // The same elements as they are: a quarter or half of the registers of load_chunk's, for what is on its way for long.
 template <class T>
 struct RawChunk {

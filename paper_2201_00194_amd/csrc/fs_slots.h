@@ -175,6 +175,36 @@ slot_scan_kernel(int32_t *count, SlotShape s)
         count[(int64_t)s.buckets * s.groups + blockIdx.x] = total;
 }
 
+// Where all counts are few, every workgroup that places entries sums them itself: a kernel less.
+constexpr int kSlotFewCounts = 8192;
+__host__ __device__ inline bool slots_scan_alone(const SlotShape &s) { return s.buckets * s.groups <= kSlotFewCounts; }
+// Every number's total, and its count in the workgroups before this one; a barrier at the end.
+__device__ __forceinline__ void sum_counts(const int32_t *count, const SlotShape &s, int32_t *total, int32_t *before)
+{
+    constexpr int kAtOnce = 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int b0 = wave * kAtOnce; b0 < s.buckets; b0 += kSlotWaves * kAtOnce) {
+        int32_t all[kAtOnce] = {}, mine[kAtOnce] = {};
+#pragma unroll 4
+        for (int g = lane; g < s.groups; g += 64)
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int32_t v = count[min(b0 + u, s.buckets - 1) * s.groups + g];
+                all[u] += v;
+                mine[u] += g < (int)blockIdx.x ? v : 0;
+            }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int32_t a = row_sum(all[u], 6), m = row_sum(mine[u], 6);
+            if (lane == 0 && b0 + u < s.buckets) {
+                total[b0 + u] = a;
+                before[b0 + u] = m;
+            }
+        }
+    }
+    __syncthreads();
+}
+
 // f(number, sum of value(numbers before it)) by all threads of a workgroup of kSlotThreads; a barrier at the end.
 template <class V, class F>
 __device__ __forceinline__ void over_numbers(int buckets, int32_t *wave_total, V value, F f)
@@ -218,8 +248,11 @@ slot_place_kernel(Source source, SlotShape s, const int32_t *count)
     uint16_t *const staged_number = (uint16_t *)(wave_total + kSlotWaves);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bits = bits_of(s.buckets);
     const int32_t *const total = count + (int64_t)s.buckets * s.groups;
-    over_numbers(s.buckets, wave_total, [&](int b) { return total[b]; }, [&](int b, int32_t at) {
-        to[b] = at + count[(int64_t)b * s.groups + blockIdx.x];
+    const bool scanned = !slots_scan_alone(s);
+    if (!scanned)
+        sum_counts(count, s, met_all, to);
+    over_numbers(s.buckets, wave_total, [&](int b) { return scanned ? total[b] : met_all[b]; }, [&](int b, int32_t at) {
+        to[b] = at + (scanned ? count[(int64_t)b * s.groups + blockIdx.x] : to[b]);
         met_all[b] = 0;
         if (blockIdx.x == 0)
             source.start(b, at);
@@ -354,7 +387,8 @@ void launch_slots(const Source &source, const SlotShape &s, int32_t *count, hipS
 {
     hipLaunchKernelGGL(slot_count_kernel<Source>, dim3((unsigned)s.groups), dim3(kSlotThreads), (size_t)kSlotWaves * s.buckets * 4, stream, source, s,
                        count);
-    hipLaunchKernelGGL(slot_scan_kernel, dim3((unsigned)s.buckets), dim3(kSlotScanThreads), 0, stream, count, s);
+    if (!slots_scan_alone(s))
+        hipLaunchKernelGGL(slot_scan_kernel, dim3((unsigned)s.buckets), dim3(kSlotScanThreads), 0, stream, count, s);
     hipLaunchKernelGGL(slot_place_kernel<Source>, dim3((unsigned)s.groups), dim3(kSlotThreads), slot_place_bytes(s.per, s.buckets, sizeof(typename Source::What)),
                        stream, source, s, (const int32_t *)count);
 }
