@@ -153,6 +153,48 @@ def test_gradient_of_many_rows(api, typ, rows, cols, vocab, width, accumulate):
         assert torch.equal(d, again)
 
 
+@pytest.mark.parametrize("typ", list(HALF))
+@pytest.mark.parametrize("rows,cols", [(1, 1), (2, 3), (64, 1), (65, 1), (85, 3), (255, 1), (256, 1), (257, 1), (1, 256), (128, 2)])
+@pytest.mark.parametrize("vocab,width", [(1, 5), (3, 8), (40, 1), (300, 91), (9000, 12), (70, 1100)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_few_ids(api, typ, rows, cols, vocab, width, accumulate):
+    """Few ids, every one of them once, or a token many times: at most 256 additions in fp32, a factor, a sum with what was there."""
+    import torch
+    gen = torch.Generator("cuda").manual_seed(rows * 1000 + vocab)
+    ids = torch.randint(-1, vocab + 1, (rows, cols), device="cuda", generator=gen, dtype=torch.int32)
+    g = torch.randn(rows, width + 1, device="cuda", generator=gen).to(torch_type(typ))[:, 1:]
+    exp, size = (torch.zeros(vocab + 1, width, dtype=torch.float64, device="cuda") for _ in range(2))
+    for c in range(cols):
+        at = torch.where((ids[:, c] >= 0) & (ids[:, c] < vocab), ids[:, c], vocab).long()
+        exp.index_add_(0, at, g.double())
+        size.index_add_(0, at, g.double().abs())
+    exp, size = exp[:vocab] * 0.5, size[:vocab] * 0.5
+    for out_typ in dict.fromkeys((typ, "fp32")):
+        buf = torch.ones(vocab, width + 3, dtype=torch_type(out_typ), device="cuda")
+        d = api.fs_embed_backward(g, ids if cols > 1 else ids[:, 0], vocab, scale=0.5, d_table=buf[:, 1:width + 1], accumulate=accumulate)
+        e = exp + 1 if accumulate else exp
+        off = 258 * 2.0 ** -24 * size + 2.0 ** -23 * (e.abs() + exp.abs())
+        tiny = 2.0 ** -25 if out_typ == "fp16" else 1e-36
+        assert bool(((d.double() - e).abs() <= off + HALF[out_typ] * (e.abs() + off) + tiny).all())
+        assert bool((buf[:, 0] == 1).all()) and bool((buf[:, width + 1:] == 1).all())
+
+
+def test_few_ids_captured_into_a_graph(api):
+    import torch
+    ids = torch.randint(0, 90, (200,), device="cuda", dtype=torch.int64)
+    g = torch.randn(200, 33, device="cuda")
+    d = api.fs_embed_backward(g, ids, 90)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        api.fs_embed_backward(g, ids, 90, d_table=d)
+    for _ in range(3):
+        ids.copy_(torch.randint(0, 90, (200,)))
+        g.copy_(torch.randn(200, 33))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(d, api.fs_embed_backward(g, ids, 90))
+
+
 def test_gradient_against_differences(api):
     """out is linear in the table."""
     import torch
