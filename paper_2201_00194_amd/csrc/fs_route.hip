@@ -286,13 +286,13 @@ __device__ __forceinline__ double entry_at(const double (&list)[KP], int j)
     int lo = __double2loint(list[0]), hi = __double2hiint(list[0]);
 #pragma unroll
     for (int i = 1; i < KP; ++i) {
-        lo = j == i ? __double2loint(list[i]) : lo + 0;
-        hi = j == i ? __double2hiint(list[i]) : hi + 0;
+        lo = j == i ? __double2loint(list[i]) : lo;
+        hi = j == i ? __double2hiint(list[i]) : hi;
     }
     return __hiloint2double(hi, lo);
 }
 template <int KP>
-__device__ __forceinline__ float key_at(const double (&list)[KP], int j) { return key_of(j == KP - 1 ? list[KP - 1] + 0.0 : entry_at<KP>(list, j)); }
+__device__ __forceinline__ float key_at(const double (&list)[KP], int j) { return key_of(entry_at<KP>(list, j)); }
 
 // Whether two keys of this lane's row that matter are too near to be told apart by what they are in fp32 (each off by at most
 // `off`, the sum's rounding on top), unless the same logit and bias made both: that is one key then, and the lower expert goes
