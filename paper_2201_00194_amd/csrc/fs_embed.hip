@@ -390,7 +390,7 @@ __device__ __forceinline__ void put_row(const SumArgs &a, int token, int c, int 
 // A chunk of the list is added by the lanes of one row, in fp32.  What a workgroup's chunks have of runs that go on beyond
 // them, two sums a chunk at most, meets in LDS, where the lanes of a run's first sum add them up, in 64 bits (blocks of sixteen
 // are rounded between); what the workgroup has of runs that go on beyond it goes to memory.
-template <int IN, int OUT, class P>
+template <int IN, int OUT, class P, bool NEAR>
 __global__ void __launch_bounds__(kSumWaves * 64)
 embed_sum_kernel(SumArgs a)
 {
@@ -447,24 +447,21 @@ embed_sum_kernel(SumArgs a)
             if (last)
                 mark(1, !first && right && some);
         };
-        for (int64_t i0 = begin; i0 < end; i0 += kEmbedAhead) {
-            int token[kEmbedAhead];
-            RawChunk<In> x[kEmbedAhead];
-            P pair[kEmbedAhead];
-#pragma unroll
-            for (int u = 0; u < kEmbedAhead; ++u)
-                pair[u] = list[min(i0 + u, end - 1)];
-#pragma unroll
-            for (int u = 0; u < kEmbedAhead; ++u) {
-                token[u] = token_of(a.packing, pair[u]);
-                x[u].load(in + (int64_t)row_of(a.packing, pair[u]) * a.in_stride, plain_token(a.packing, token[u]) < a.n_vocab && i0 + u < end ? n : 0);
-            }
+        // NEAR: offsets from the rows' start fit in 32 bits, one multiplication instead of four.
+        const auto row_at = [&](const P &p) {
+            if constexpr (NEAR)
+                return (const In *)((const char *)a.in + (row_of(a.packing, p) * (uint32_t)(a.in_stride * (int64_t)sizeof(In)) + (uint32_t)c * (uint32_t)sizeof(In)));
+            else
+                return in + (int64_t)row_of(a.packing, p) * a.in_stride;
+        };
+        const auto add = [&](const P (&pair)[kEmbedAhead], const RawChunk<In> (&x)[kEmbedAhead]) {
 #pragma unroll
             for (int u = 0; u < kEmbedAhead; ++u) {
-                if (token[u] != now) {
+                const int token = token_of(a.packing, pair[u]);
+                if (token != now) {
                     done(false);
                     first = false;
-                    now = token[u];
+                    now = token;
 #pragma unroll
                     for (int i = 0; i < N; ++i)
                         sum[i] = 0.0f;
@@ -473,6 +470,30 @@ embed_sum_kernel(SumArgs a)
                 for (int i = 0; i < N; ++i)
                     sum[i] += x[u][i];
             }
+        };
+        // Every pair's row is there, also one whose token names none of the table: its sum goes nowhere.
+        int64_t i0 = begin;
+        for (; i0 + kEmbedAhead <= end; i0 += kEmbedAhead) {
+            P pair[kEmbedAhead];
+            RawChunk<In> x[kEmbedAhead];
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u)
+                pair[u] = list[i0 + u];
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u)
+                x[u].load(row_at(pair[u]), n);
+            add(pair, x);
+        }
+        if (i0 < end) {
+            P pair[kEmbedAhead];
+            RawChunk<In> x[kEmbedAhead];
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u)
+                pair[u] = list[min(i0 + u, end - 1)];
+#pragma unroll
+            for (int u = 0; u < kEmbedAhead; ++u)
+                x[u].load(row_at(pair[u]), i0 + u < end ? n : 0);
+            add(pair, x);
         }
         done(true);
     } else if (h == 0) {
@@ -976,10 +997,10 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
             constexpr int in = decltype(i)::value, out = decltype(o)::value;
             const int64_t each = (p.sum.groups + p.bands - 1) / p.bands, per = kXcds / p.bands;
             const dim3 grid((unsigned)(p.bands > 1 ? (each + per - 1) / per * kXcds : p.sum.groups), (unsigned)p.sum.columns);
-            if (p.packed)
-                hipLaunchKernelGGL((embed_sum_kernel<in, out, uint32_t>), grid, dim3(kSumWaves * 64), 0, stream, a);
-            else
-                hipLaunchKernelGGL((embed_sum_kernel<in, out, Pair>), grid, dim3(kSumWaves * 64), 0, stream, a);
+            const bool near = d_out_stride < ((int64_t)1 << 31) && n_rows * d_out_stride * (int64_t)type_bytes(d_out_type) < ((int64_t)1 << 32);
+            const auto kernel = p.packed ? near ? embed_sum_kernel<in, out, uint32_t, true> : embed_sum_kernel<in, out, uint32_t, false>
+                                         : near ? embed_sum_kernel<in, out, Pair, true> : embed_sum_kernel<in, out, Pair, false>;
+            hipLaunchKernelGGL(kernel, grid, dim3(kSumWaves * 64), 0, stream, a);
             a.ll = to.ll = row_lanes_log(width, kChunk<float>);
             if (p.sum.groups > 1) {
                 a.n = 2 * p.sum.groups;
