@@ -210,50 +210,6 @@ __device__ __forceinline__ uint32_t row_of(const Packing &k, uint32_t p) { retur
 __device__ __forceinline__ int banded(const Packing &k, int token, uint32_t row) { return token | (int)(__umulhi(row, k.band_magic) << k.token_bits); }
 __device__ __forceinline__ int plain_token(const Packing &k, int token) { return token & (int)((1u << k.token_bits) - 1u); }
 
-template <int ID, class P>
-struct IdDigit {
-    typedef P Item, What;
-    EmbedIds ids;
-    P *to;
-    int32_t mask;
-    Packing packing;
-    template <int N>
-    __device__ __forceinline__ void load(P (&item)[N], int64_t i, int64_t end) const
-    {
-        int token[N];
-        const auto entry = [&](int u) { return (uint32_t)min(i + u * 64, end - 1); };
-        ids.template rows<ID>(token, entry, [&](int u) { return entry(u) - ids.row_of(entry(u)) * (uint32_t)ids.n_cols; });
-#pragma unroll
-        for (int u = 0; u < N; ++u)
-            item[u] = make_pair<P>(packing, banded(packing, token[u] < 0 ? ids.n_vocab : token[u], ids.row_of(entry(u))), ids.row_of(entry(u)));
-    }
-    __device__ __forceinline__ int number(const P &p) const { return token_of(packing, p) & mask; }
-    __device__ __forceinline__ void start(int, int) const {}
-    __device__ __forceinline__ void place(int64_t, int, int) const {}
-    __device__ __forceinline__ P what(const P &p, int64_t) const { return p; }
-    __device__ __forceinline__ void put(const P &p, int, int slot) const { to[slot] = p; }
-};
-template <class P>
-struct PairDigit {
-    typedef P Item, What;
-    const P *from;
-    P *to;
-    int32_t shift, mask;
-    Packing packing;
-    template <int N>
-    __device__ __forceinline__ void load(P (&item)[N], int64_t i, int64_t end) const
-    {
-#pragma unroll
-        for (int u = 0; u < N; ++u)
-            item[u] = from[min(i + u * 64, end - 1)];
-    }
-    __device__ __forceinline__ int number(const P &p) const { return (token_of(packing, p) >> shift) & mask; }
-    __device__ __forceinline__ void start(int, int) const {}
-    __device__ __forceinline__ void place(int64_t, int, int) const {}
-    __device__ __forceinline__ P what(const P &p, int64_t) const { return p; }
-    __device__ __forceinline__ void put(const P &p, int, int slot) const { to[slot] = p; }
-};
-
 struct ClearArgs {
     void *table;
     int64_t n_rows, stride;
@@ -285,6 +241,57 @@ __device__ __forceinline__ void clear_table(const ClearArgs &a, int64_t b, int64
     else                           // the zeros of bf16 and fp16 are the same
         clear_rows<_Float16>(a, b, blocks);
 }
+
+template <int ID, class P>
+struct IdDigit {
+    typedef P Item, What;
+    EmbedIds ids;
+    P *to;
+    int32_t mask;
+    Packing packing;
+    ClearArgs clear;               // beside the first pass
+    int32_t clear_blocks;
+    int more_blocks() const { return clear_blocks; }
+    __device__ __forceinline__ void beside(int block, int blocks) const { clear_table(clear, block, blocks); }
+    template <int N>
+    __device__ __forceinline__ void load(P (&item)[N], int64_t i, int64_t end) const
+    {
+        int token[N];
+        const auto entry = [&](int u) { return (uint32_t)min(i + u * 64, end - 1); };
+        ids.template rows<ID>(token, entry, [&](int u) { return entry(u) - ids.row_of(entry(u)) * (uint32_t)ids.n_cols; });
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            item[u] = make_pair<P>(packing, banded(packing, token[u] < 0 ? ids.n_vocab : token[u], ids.row_of(entry(u))), ids.row_of(entry(u)));
+    }
+    __device__ __forceinline__ int number(const P &p) const { return token_of(packing, p) & mask; }
+    __device__ __forceinline__ void start(int, int) const {}
+    __device__ __forceinline__ void place(int64_t, int, int) const {}
+    __device__ __forceinline__ P what(const P &p, int64_t) const { return p; }
+    __device__ __forceinline__ void put(const P &p, int, int slot) const { to[slot] = p; }
+};
+template <class P>
+struct PairDigit {
+    typedef P Item, What;
+    const P *from;
+    P *to;
+    int32_t shift, mask;
+    Packing packing;
+    int more_blocks() const { return 0; }
+    __device__ __forceinline__ void beside(int, int) const {}
+    template <int N>
+    __device__ __forceinline__ void load(P (&item)[N], int64_t i, int64_t end) const
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            item[u] = from[min(i + u * 64, end - 1)];
+    }
+    __device__ __forceinline__ int number(const P &p) const { return (token_of(packing, p) >> shift) & mask; }
+    __device__ __forceinline__ void start(int, int) const {}
+    __device__ __forceinline__ void place(int64_t, int, int) const {}
+    __device__ __forceinline__ P what(const P &p, int64_t) const { return p; }
+    __device__ __forceinline__ void put(const P &p, int, int slot) const { to[slot] = p; }
+};
+
 static __global__ void __launch_bounds__(1024)
 embed_clear_kernel(ClearArgs a) { clear_table(a, blockIdx.x, gridDim.x); }
 constexpr int kClearBlocks = 2047;
@@ -294,10 +301,10 @@ constexpr int kClearBlocks = 2047;
 constexpr int kFewDigitBits = 9;
 template <int ID, class P>
 __global__ void __launch_bounds__(kSlotFewWaves * 64)
-embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits, ClearArgs clear)
+embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits)
 {
     if (blockIdx.x > 0) {
-        clear_table(clear, blockIdx.x - 1, gridDim.x - 1);
+        source.beside(blockIdx.x - 1, gridDim.x - 1);
         return;
     }
     __shared__ int32_t token[kSlotFew], c[kSlotFewWaves << kFewDigitBits], wave_total[kSlotFewWaves];
@@ -940,7 +947,7 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
     ClearArgs clear = {d_table, n_vocab, d_table_stride, d_table_type, width, row_lanes_log(width, 16 / (int)type_bytes(d_table_type))};
     if (p.bands > 1)
         clear = ClearArgs{tables, (int64_t)p.bands * n_vocab, p.sum.part_stride, FS_F32, width, row_lanes_log(width, kChunk<float>)};
-    const int64_t rows = (int64_t)16 << (6 - clear.ll), all = p.bands == 1 && accumulate ? 0 : (clear.n_rows + rows - 1) / rows;
+    const int64_t rows = (int64_t)kSlotWaves << (6 - clear.ll), all = p.bands == 1 && accumulate ? 0 : (clear.n_rows + rows - 1) / rows;
     const unsigned blocks = (unsigned)(all < kClearBlocks ? all : kClearBlocks);
     const bool few = n > 0 && n <= kSlotFew;
     const int64_t rows_once = (int64_t)kDirectWaves << (6 - clear.ll), apart = min((n_vocab + rows_once - 1) / rows_once, (int64_t)kClearBlocks);
@@ -959,7 +966,7 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
         prof_stop(stream);
         return launched("embedding gradient kernel launch");
     }
-    if (blocks > 0 && !few)
+    if (blocks > 0 && n == 0)
         hipLaunchKernelGGL(embed_clear_kernel, dim3(blocks), dim3(1024), 0, stream, clear);
     if (n > 0) {
         const int mask = (1 << p.bits) - 1;
@@ -969,10 +976,10 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
             P *const lists[2] = {(P *)list[0], (P *)list[1]};
             with_id_type(id_type, [&](auto type) {
                 constexpr int id = decltype(type)::value;
-                const IdDigit<id, P> of = {embed_ids(ids, col_base, n_cols, n_vocab), lists[0], mask, p.packing};
+                const IdDigit<id, P> of = {embed_ids(ids, col_base, n_cols, n_vocab), lists[0], mask, p.packing, clear, (int32_t)blocks};
                 if (few)
                     hipLaunchKernelGGL((embed_sort_few_kernel<id, P>), dim3(1 + blocks), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n,
-                                       p.token_bits, clear);
+                                       p.token_bits);
                 else
                     launch_slots(of, p.shape, count, stream);
             });

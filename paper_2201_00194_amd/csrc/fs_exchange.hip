@@ -15,6 +15,8 @@ struct Choices {
         for (int u = 0; u < N; ++u)
             item[u] = expert[min(i + u * 64, end - 1)];
     }
+    int more_blocks() const { return 0; }
+    __device__ __forceinline__ void beside(int, int) const {}
     __device__ __forceinline__ int number(int32_t e) const { return e >= 0 && e < n_experts ? e : n_experts; }
     __device__ __forceinline__ void start(int e, int slot) const { first[e] = slot; }
     __device__ __forceinline__ int32_t what(int32_t, int64_t i) const { return (int32_t)i; }

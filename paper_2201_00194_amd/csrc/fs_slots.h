@@ -6,7 +6,8 @@
 //
 // A Source says what the entries are: load(items, i) takes entries i, i + 64, ... (the last one, where that is past it), int
 // number(item), place(i, number, slot) tells where entry i goes, put(what(item, i), number, slot) puts it there, and start(number, slot
-// of its first) is called once for every number.
+// of its first) is called once for every number.  The counting launch has more_blocks() more workgroups, for what can be done
+// beside it: beside(which, of how many).
 #ifndef FS_SLOTS_H
 #define FS_SLOTS_H
 
@@ -116,6 +117,10 @@ __global__ void __launch_bounds__(kSlotThreads)
 slot_count_kernel(Source source, SlotShape s, int32_t *count)
 {
     extern __shared__ int32_t slot_lds[];
+    if ((int)blockIdx.x >= s.groups) {
+        source.beside(blockIdx.x - s.groups, gridDim.x - s.groups);
+        return;
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int b = threadIdx.x; b < kSlotWaves * s.buckets; b += kSlotThreads)
         slot_lds[b] = 0;
@@ -385,8 +390,8 @@ void launch_few_slots(const Source &source, const SlotShape &s, hipStream_t stre
 template <class Source>
 void launch_slots(const Source &source, const SlotShape &s, int32_t *count, hipStream_t stream)
 {
-    hipLaunchKernelGGL(slot_count_kernel<Source>, dim3((unsigned)s.groups), dim3(kSlotThreads), (size_t)kSlotWaves * s.buckets * 4, stream, source, s,
-                       count);
+    hipLaunchKernelGGL(slot_count_kernel<Source>, dim3((unsigned)(s.groups + source.more_blocks())), dim3(kSlotThreads),
+                       (size_t)kSlotWaves * s.buckets * 4, stream, source, s, count);
     if (!slots_scan_alone(s))
         hipLaunchKernelGGL(slot_scan_kernel, dim3((unsigned)s.buckets), dim3(kSlotScanThreads), 0, stream, count, s);
     hipLaunchKernelGGL(slot_place_kernel<Source>, dim3((unsigned)s.groups), dim3(kSlotThreads), slot_place_bytes(s.per, s.buckets, sizeof(typename Source::What)),
