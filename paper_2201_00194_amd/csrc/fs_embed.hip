@@ -241,18 +241,23 @@ __device__ __forceinline__ void clear_table(const ClearArgs &a, int64_t b, int64
     else                           // the zeros of bf16 and fp16 are the same
         clear_rows<_Float16>(a, b, blocks);
 }
+// A pass of the sort clears two parts of the table.
+struct ClearBeside {
+    ClearArgs counting, placing;
+    int32_t count_blocks, place_blocks;
+    int more_counting() const { return count_blocks; }
+    int more_placing() const { return place_blocks; }
+    __device__ __forceinline__ void beside_count(int block, int blocks) const { clear_table(counting, block, blocks); }
+    __device__ __forceinline__ void beside_place(int block, int blocks) const { clear_table(placing, block, blocks); }
+};
 
 template <int ID, class P>
-struct IdDigit {
+struct IdDigit : ClearBeside {
     typedef P Item, What;
     EmbedIds ids;
     P *to;
     int32_t mask;
     Packing packing;
-    ClearArgs clear;               // beside the first pass
-    int32_t clear_blocks;
-    int more_blocks() const { return clear_blocks; }
-    __device__ __forceinline__ void beside(int block, int blocks) const { clear_table(clear, block, blocks); }
     template <int N>
     __device__ __forceinline__ void load(P (&item)[N], int64_t i, int64_t end) const
     {
@@ -270,14 +275,12 @@ struct IdDigit {
     __device__ __forceinline__ void put(const P &p, int, int slot) const { to[slot] = p; }
 };
 template <class P>
-struct PairDigit {
+struct PairDigit : ClearBeside {
     typedef P Item, What;
     const P *from;
     P *to;
     int32_t shift, mask;
     Packing packing;
-    int more_blocks() const { return 0; }
-    __device__ __forceinline__ void beside(int, int) const {}
     template <int N>
     __device__ __forceinline__ void load(P (&item)[N], int64_t i, int64_t end) const
     {
@@ -292,30 +295,35 @@ struct PairDigit {
     __device__ __forceinline__ void put(const P &p, int, int slot) const { to[slot] = p; }
 };
 
-static __global__ void __launch_bounds__(1024)
+static __global__ void __launch_bounds__(kSlotThreads)
 embed_clear_kernel(ClearArgs a) { clear_table(a, blockIdx.x, gridDim.x); }
 constexpr int kClearBlocks = 2047;
 
-// All digits of up to kSlotFew entries in one workgroup.  LDS holds the tokens where the entries are and the entries' numbers
+// All digits of up to PER * 1024 entries in one workgroup.  LDS holds the tokens where the entries are and the entries' numbers
 // in the order so far, which a pass takes to registers and puts back.  The launch's other workgroups clear the table meanwhile.
 constexpr int kFewDigitBits = 9;
-template <int ID, class P>
+// 8192 entries 21 us, 16384 37, and 29 by the six kernels of a long list; but where clearing takes longer than that (268 MB: 50 us),
+// it is better beside one kernel of 51 than in four parts beside the others (57 with the scans).
+constexpr int kEmbedFew = 8192;
+constexpr int64_t kClearLong = 160 << 20;
+static bool sort_in_one(int64_t n, int64_t clear_bytes) { return n <= kEmbedFew || (n <= 2 * kEmbedFew && clear_bytes >= kClearLong); }
+template <int ID, class P, int PER>
 __global__ void __launch_bounds__(kSlotFewWaves * 64)
 embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits)
 {
     if (blockIdx.x > 0) {
-        source.beside(blockIdx.x - 1, gridDim.x - 1);
+        source.beside_count(blockIdx.x - 1, gridDim.x - 1);
         return;
     }
-    __shared__ int32_t token[kSlotFew], c[kSlotFewWaves << kFewDigitBits], wave_total[kSlotFewWaves];
-    __shared__ uint16_t order[kSlotFew];
+    __shared__ int32_t token[PER * 1024], c[kSlotFewWaves << kFewDigitBits], wave_total[kSlotFewWaves];
+    __shared__ uint16_t order[PER * 1024];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int steps = (n + kSlotFewWaves * 64 - 1) / (kSlotFewWaves * 64);
     const int begin = wave * steps * 64 + lane;
-    P item[kSlotFewPer];
+    P item[PER];
     source.load(item, begin, n);
 #pragma unroll
-    for (int u = 0; u < kSlotFewPer; ++u) {
+    for (int u = 0; u < PER; ++u) {
         const int i = begin + u * 64;
         if (u < steps && i < n) {
             token[i] = token_of(source.packing, item[u]);
@@ -327,10 +335,10 @@ embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits)
         for (int b = threadIdx.x; b < kSlotFewWaves * buckets; b += kSlotFewWaves * 64)
             c[b] = 0;
         __syncthreads();
-        uint16_t mine[kSlotFewPer];
-        int number[kSlotFewPer];
+        uint16_t mine[PER];
+        int number[PER];
 #pragma unroll
-        for (int u = 0; u < kSlotFewPer; ++u)
+        for (int u = 0; u < PER; ++u)
             if (u < steps && begin + u * 64 < n) {
                 mine[u] = order[begin + u * 64];
                 number[u] = (token[mine[u]] >> shift) & (buckets - 1);
@@ -339,7 +347,7 @@ embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits)
         __syncthreads();
         first_slots(c, buckets, wave_total, [](int, int) {});
 #pragma unroll
-        for (int u = 0; u < kSlotFewPer; ++u)
+        for (int u = 0; u < PER; ++u)
             if (u < steps) {
                 const bool there = begin + u * 64 < n;
                 const int slot = take_slot(c + wave * buckets, there ? number[u] : 0, digit, there);
@@ -789,7 +797,7 @@ constexpr int kBandLeastRun = 30;
 static int bands_for(int32_t n_vocab, int32_t width, int32_t type, int64_t n_rows, int64_t n)
 {
     const int64_t bytes = n_rows * width * (int64_t)type_bytes(type);
-    if (n <= kSlotFew || n_rows <= kXcds || bytes <= kL2Bytes || bytes > kXcds * kL2Bytes)
+    if (n <= kEmbedFew || n_rows <= kXcds || bytes <= kL2Bytes || bytes > kXcds * kL2Bytes)
         return 1;
     int bands = 2;
     while (bands < kXcds && bytes > bands * kBandBytes)
@@ -820,7 +828,7 @@ static SortPlan sort_plan(int32_t n_vocab, int32_t width, int32_t type, int64_t 
     p.token_bytes = ((size_t)p.sum.groups * 2 * 4 + 255) / 256 * 256;
     p.part_bytes = ((size_t)p.sum.groups * 2 * p.sum.part_stride * 4 + 255) / 256 * 256;
     p.table_bytes = p.bands > 1 ? ((size_t)p.bands * n_vocab * p.sum.part_stride * 4 + 255) / 256 * 256 : 0;
-    p.bytes = 2 * p.list_bytes + p.token_bytes + p.part_bytes + p.table_bytes + slot_count_bytes(p.shape);
+    p.bytes = 2 * p.list_bytes + p.token_bytes + p.part_bytes + p.table_bytes + slot_count_bytes(p.shape, kEmbedFew);
     return p;
 }
 
@@ -947,9 +955,23 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
     ClearArgs clear = {d_table, n_vocab, d_table_stride, d_table_type, width, row_lanes_log(width, 16 / (int)type_bytes(d_table_type))};
     if (p.bands > 1)
         clear = ClearArgs{tables, (int64_t)p.bands * n_vocab, p.sum.part_stride, FS_F32, width, row_lanes_log(width, kChunk<float>)};
-    const int64_t rows = (int64_t)kSlotWaves << (6 - clear.ll), all = p.bands == 1 && accumulate ? 0 : (clear.n_rows + rows - 1) / rows;
-    const unsigned blocks = (unsigned)(all < kClearBlocks ? all : kClearBlocks);
-    const bool few = n > 0 && n <= kSlotFew;
+    const bool keep = p.bands == 1 && accumulate;
+    const bool few = n > 0 && sort_in_one(n, keep ? 0 : clear.n_rows * width * (int64_t)type_bytes(clear.type));
+    // Part `which` of `parts` of what is to be cleared, and the workgroups for it.
+    const auto clear_part = [&](int which, int parts, int32_t &blocks) {
+        const int64_t begin = clear.n_rows * which / parts, end = clear.n_rows * (which + 1) / parts, rows = (int64_t)kSlotWaves << (6 - clear.ll);
+        ClearArgs part = clear;
+        part.table = (char *)clear.table + begin * clear.stride * (int64_t)type_bytes(clear.type);
+        part.n_rows = end - begin;
+        blocks = keep ? 0 : (int32_t)min((end - begin + rows - 1) / rows, (int64_t)kClearBlocks);
+        return part;
+    };
+    const auto beside = [&](int pass) {
+        ClearBeside c;
+        c.counting = clear_part(few ? 0 : 2 * pass, few ? 1 : 2 * p.passes, c.count_blocks);
+        c.placing = clear_part(few ? 0 : 2 * pass + 1, few ? 1 : 2 * p.passes, c.place_blocks);
+        return c;
+    };
     const int64_t rows_once = (int64_t)kDirectWaves << (6 - clear.ll), apart = min((n_vocab + rows_once - 1) / rows_once, (int64_t)kClearBlocks);
     const int64_t rows_each = (n_vocab + apart - 1) / apart;
     if (n > 0 && n <= kDirectIds && rows_each <= kDirectRows) {
@@ -966,8 +988,11 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
         prof_stop(stream);
         return launched("embedding gradient kernel launch");
     }
-    if (blocks > 0 && n == 0)
-        hipLaunchKernelGGL(embed_clear_kernel, dim3(blocks), dim3(1024), 0, stream, clear);
+    if (n == 0 && !keep) {
+        int32_t blocks;
+        const ClearArgs all = clear_part(0, 1, blocks);
+        hipLaunchKernelGGL(embed_clear_kernel, dim3((unsigned)blocks), dim3(kSlotThreads), 0, stream, all);
+    }
     if (n > 0) {
         const int mask = (1 << p.bits) - 1;
         int now = 0;
@@ -976,16 +1001,16 @@ extern "C" int fs_embed_backward(int32_t n_vocab, int32_t width, const void *d_o
             P *const lists[2] = {(P *)list[0], (P *)list[1]};
             with_id_type(id_type, [&](auto type) {
                 constexpr int id = decltype(type)::value;
-                const IdDigit<id, P> of = {embed_ids(ids, col_base, n_cols, n_vocab), lists[0], mask, p.packing, clear, (int32_t)blocks};
+                const IdDigit<id, P> of = {beside(0), embed_ids(ids, col_base, n_cols, n_vocab), lists[0], mask, p.packing};
                 if (few)
-                    hipLaunchKernelGGL((embed_sort_few_kernel<id, P>), dim3(1 + blocks), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n,
-                                       p.token_bits);
+                    hipLaunchKernelGGL((n <= kEmbedFew ? embed_sort_few_kernel<id, P, kEmbedFew / 1024> : embed_sort_few_kernel<id, P, kEmbedFew / 512>),
+                                       dim3((unsigned)(1 + of.count_blocks)), dim3(kSlotFewWaves * 64), 0, stream, of, (int32_t)n, p.token_bits);
                 else
                     launch_slots(of, p.shape, count, stream);
             });
             if (!few)
                 for (int pass = 1; pass < p.passes; ++pass, now ^= 1)
-                    launch_slots(PairDigit<P>{lists[now], lists[now ^ 1], pass * p.bits, mask, p.packing}, p.shape, count, stream);
+                    launch_slots(PairDigit<P>{beside(pass), lists[now], lists[now ^ 1], pass * p.bits, mask, p.packing}, p.shape, count, stream);
         };
         if (p.packed)
             sort(uint32_t());

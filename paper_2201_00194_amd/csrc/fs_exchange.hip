@@ -15,8 +15,10 @@ struct Choices {
         for (int u = 0; u < N; ++u)
             item[u] = expert[min(i + u * 64, end - 1)];
     }
-    int more_blocks() const { return 0; }
-    __device__ __forceinline__ void beside(int, int) const {}
+    int more_counting() const { return 0; }
+    int more_placing() const { return 0; }
+    __device__ __forceinline__ void beside_count(int, int) const {}
+    __device__ __forceinline__ void beside_place(int, int) const {}
     __device__ __forceinline__ int number(int32_t e) const { return e >= 0 && e < n_experts ? e : n_experts; }
     __device__ __forceinline__ void start(int e, int slot) const { first[e] = slot; }
     __device__ __forceinline__ int32_t what(int32_t, int64_t i) const { return (int32_t)i; }
@@ -243,7 +245,7 @@ extern "C" size_t fs_expert_plan_workspace_bytes(int64_t n_tokens, int32_t k, in
     static const char who[] = "fs_expert_plan_workspace_bytes";
     if (check_tokens(who, n_tokens, k) != FS_OK || check_experts(who, n_experts) != FS_OK)
         return 0;
-    return slot_count_bytes(slot_shape(n_tokens * k, n_experts + 1, sizeof(Choices::What)));
+    return slot_count_bytes(slot_shape(n_tokens * k, n_experts + 1, sizeof(Choices::What)), kSlotFew);
 }
 
 extern "C" int fs_expert_plan(int64_t n_tokens, int32_t k, int32_t n_experts, const int32_t *expert, int32_t *first, int32_t *order,
@@ -258,7 +260,7 @@ extern "C" int fs_expert_plan(int64_t n_tokens, int32_t k, int32_t n_experts, co
     FS_TRY(check_array(who, "order", order, n_tokens, 4));
     FS_TRY(check_array(who, "place", place, n_tokens, 4));
     const SlotShape s = slot_shape(n_tokens * k, n_experts + 1, sizeof(Choices::What));
-    const size_t need = slot_count_bytes(s);
+    const size_t need = slot_count_bytes(s, kSlotFew);
     FS_TRY(check_array(who, "work", work, (int64_t)need, 256));
     if (work_bytes < need)
         return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, need);

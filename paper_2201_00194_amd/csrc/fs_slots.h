@@ -6,8 +6,8 @@
 //
 // A Source says what the entries are: load(items, i) takes entries i, i + 64, ... (the last one, where that is past it), int
 // number(item), place(i, number, slot) tells where entry i goes, put(what(item, i), number, slot) puts it there, and start(number, slot
-// of its first) is called once for every number.  The counting launch has more_blocks() more workgroups, for what can be done
-// beside it: beside(which, of how many).
+// of its first) is called once for every number.  The launches that count and that place have more workgroups, for what can
+// be done beside them: more_counting() that call beside_count(which, of how many), and the same for placing.
 #ifndef FS_SLOTS_H
 #define FS_SLOTS_H
 
@@ -52,9 +52,9 @@ inline SlotShape slot_shape(int64_t n, int buckets, int what_bytes)
     return s;
 }
 // The counts, and behind them every number's total.
-inline size_t slot_count_bytes(const SlotShape &s)
+inline size_t slot_count_bytes(const SlotShape &s, int few)       // up to `few` entries need none
 {
-    return s.n <= kSlotFew ? 0 : ((size_t)s.buckets * (s.groups + 1) * 4 + 255) / 256 * 256;
+    return s.n <= few ? 0 : ((size_t)s.buckets * (s.groups + 1) * 4 + 255) / 256 * 256;
 }
 
 // The lanes whose number is this lane's, among the lanes that are there.
@@ -118,7 +118,7 @@ slot_count_kernel(Source source, SlotShape s, int32_t *count)
 {
     extern __shared__ int32_t slot_lds[];
     if ((int)blockIdx.x >= s.groups) {
-        source.beside(blockIdx.x - s.groups, gridDim.x - s.groups);
+        source.beside_count(blockIdx.x - s.groups, gridDim.x - s.groups);
         return;
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -244,6 +244,10 @@ __global__ void __launch_bounds__(kSlotThreads)
 slot_place_kernel(Source source, SlotShape s, const int32_t *count)
 {
     extern __shared__ int32_t slot_lds[];
+    if ((int)blockIdx.x >= s.groups) {
+        source.beside_place(blockIdx.x - s.groups, gridDim.x - s.groups);
+        return;
+    }
     typename Source::What *const staged = (typename Source::What *)slot_lds;         // the tile in order
     const int tile = s.per * kSlotThreads;
     int32_t *const c = (int32_t *)(staged + tile);          // of every wavefront: how often it met a number, then where in the tile
@@ -390,12 +394,12 @@ void launch_few_slots(const Source &source, const SlotShape &s, hipStream_t stre
 template <class Source>
 void launch_slots(const Source &source, const SlotShape &s, int32_t *count, hipStream_t stream)
 {
-    hipLaunchKernelGGL(slot_count_kernel<Source>, dim3((unsigned)(s.groups + source.more_blocks())), dim3(kSlotThreads),
+    hipLaunchKernelGGL(slot_count_kernel<Source>, dim3((unsigned)(s.groups + source.more_counting())), dim3(kSlotThreads),
                        (size_t)kSlotWaves * s.buckets * 4, stream, source, s, count);
     if (!slots_scan_alone(s))
         hipLaunchKernelGGL(slot_scan_kernel, dim3((unsigned)s.buckets), dim3(kSlotScanThreads), 0, stream, count, s);
-    hipLaunchKernelGGL(slot_place_kernel<Source>, dim3((unsigned)s.groups), dim3(kSlotThreads), slot_place_bytes(s.per, s.buckets, sizeof(typename Source::What)),
-                       stream, source, s, (const int32_t *)count);
+    hipLaunchKernelGGL(slot_place_kernel<Source>, dim3((unsigned)(s.groups + source.more_placing())), dim3(kSlotThreads),
+                       slot_place_bytes(s.per, s.buckets, sizeof(typename Source::What)), stream, source, s, (const int32_t *)count);
 }
 
 }  // namespace fs

@@ -179,6 +179,24 @@ def test_gradient_of_few_ids(api, typ, rows, cols, vocab, width, accumulate):
         assert bool((buf[:, 0] == 1).all()) and bool((buf[:, width + 1:] == 1).all())
 
 
+@pytest.mark.parametrize("rows,vocab,width", [(8192, 40000, 4), (8193, 40000, 4), (16384, 900, 33), (16384, 45001, 1024), (9001, 45001, 1024), (16385, 45001, 1024)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_at_the_borders_of_the_sorts(api, rows, vocab, width, accumulate):
+    """One workgroup or several sort, and the table is cleared beside one kernel or in parts beside several."""
+    import torch
+    gen = torch.Generator("cuda").manual_seed(rows)
+    ids = torch.randint(-1, vocab + 1, (rows,), device="cuda", generator=gen, dtype=torch.int64)
+    g = torch.randn(rows, width, device="cuda", generator=gen)
+    exp, size = (torch.zeros(vocab + 1, width, dtype=torch.float64, device="cuda") for _ in range(2))
+    at = torch.where((ids >= 0) & (ids < vocab), ids, vocab)
+    exp.index_add_(0, at, g.double())
+    size.index_add_(0, at, g.double().abs())
+    d = torch.full((vocab, width), 2.0, device="cuda")
+    api.fs_embed_backward(g, ids, vocab, d_table=d, accumulate=accumulate)
+    e = exp[:vocab] + (2 if accumulate else 0)
+    assert bool(((d.double() - e).abs() <= 516 * 2.0 ** -24 * size[:vocab] + 2.0 ** -23 * e.abs()).all())
+
+
 def test_few_ids_captured_into_a_graph(api):
     import torch
     ids = torch.randint(0, 90, (200,), device="cuda", dtype=torch.int64)
