@@ -10,6 +10,9 @@
 // Keys with a bias (score + bias) and the sums of groups have to compare as in 64 bits.  They are computed in 32, with a bound
 // on their error; a row where two keys or sums that matter are nearer than the bounds say, and not equal by their inputs, is
 // taken again by the whole wavefront in 64 bits.
+//
+// What bounds it is issue: 2 000 000 rows of 64 bf16 experts in 8 groups with a bias, k = 8, take 223 us (1.7 TB/s) at 1038 vector
+// instructions a wavefront of 16 rows, with the vector units busy all the time.  Without bias and groups, 262 144 rows of 30 fp32 experts, k = 4: 13 us (3.1 TB/s).
 #include "fs_mixture.h"
 
 #include <math.h>
@@ -525,8 +528,9 @@ route_kernel(RouteArgs a)
                         if ((c << ll) + h < padded)
                             sums[(c << ll) + h] = sum[c];
                     }
-                    for (int g = (kChunks << ll) + h; g < padded; g += 1 << ll)       // 2 groups of 8: nobody's, behind the last chunk
-                        sums[g] = none;
+                    if constexpr (kChunks < 4)                                        // 2 groups of 8: nobody's, behind the last chunk
+                        for (int g = (kChunks << ll) + h; g < padded; g += 1 << ll)
+                            sums[g] = none;
                     lds_sync();
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) {
@@ -672,7 +676,8 @@ route_kernel(RouteArgs a)
 // ---- the gradient ---------------------------------------------------------------------------------------------------------
 
 // The choices' gradients go to the row's logits through LDS; a row's experts lie in its lanes as above, its choices j in lane
-// j mod (1 << LL).
+// j mod (1 << LL).  262 144 rows of 30 fp32 experts, a dense gradient: 21 us (3.4 TB/s), the chain of loads, LDS and moves between
+// lanes (vector units 41 % busy).
 template <int TYPE, int LL>
 __global__ void __launch_bounds__(kRouteWaves * 64)
 route_backward_kernel(RouteArgs a)
