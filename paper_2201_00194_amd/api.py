@@ -523,15 +523,18 @@ def _matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optio
     """(pointer, element type, row stride) of a matrix argument whose rows' elements are adjacent; `on`: the call's GPU."""
     if on is not None and t.get_device() != on:
         raise FsError(FS_EINVAL, f"{what} is not on the call's GPU")
-    if t.dim() != 2 or t.dtype not in _ELEMENT:
+    kind = _ELEMENT.get(t.dtype)
+    if kind is None or t.dim() != 2:
         raise FsError(FS_EINVAL, f"{what} is not a matrix of fp32, bf16 or fp16")
-    if (width is not None and t.shape[1] != width) or (rows is not None and t.shape[0] != rows):
-        raise FsError(FS_EINVAL, f"{what} is {tuple(t.shape)}, not {(rows, width)}")
+    n, w = t.shape
+    if (width is not None and w != width) or (rows is not None and n != rows):
+        raise FsError(FS_EINVAL, f"{what} is {(n, w)}, not {(rows, width)}")
     if dtype is not None and t.dtype != dtype:
         raise FsError(FS_EINVAL, f"{what} is {t.dtype}, not {dtype}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    step, between = t.stride()
+    if between != 1 and w > 1:
         raise FsError(FS_EINVAL, f"{what}: the elements of a row are not adjacent")
-    return t.data_ptr(), _ELEMENT[t.dtype], (t.stride(0) if t.shape[0] > 1 else max(1, t.shape[1]))
+    return t.data_ptr(), kind, (step if n > 1 else max(1, w))
 
 
 def _array(t: Optional[torch.Tensor], what: str, n: int, dtype: torch.dtype, on: Optional[int] = None) -> Optional[int]:
@@ -561,10 +564,12 @@ class _Place:
         self.ptr = _raw_stream(self.index) if stream is None else stream.cuda_stream
 
     def empty(self, shape, dtype: torch.dtype) -> torch.Tensor:
+        # empty_strided takes 1.3 us, empty 1.65.
+        steps = (1,) if len(shape) == 1 else (max(1, shape[1]), 1)
         if self.stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return torch.empty_strided(shape, steps, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return torch.empty_strided(shape, steps, dtype=dtype, device=self.device)
 
     def matrix(self, out: Optional[torch.Tensor], what: str, rows: int, width: int, dtype: torch.dtype):
         """(the tensor, its pointer, its row stride): `out`, checked, or a new one."""
