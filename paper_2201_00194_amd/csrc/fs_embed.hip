@@ -18,7 +18,7 @@ constexpr int kSumMostWaves = 4096;
 constexpr int kSumMostChunk = 256, kSumLeastChunk = 8;    // pairs a chunk
 constexpr int kSumWaves = 8;              // of a workgroup
 constexpr int kJoinAhead = 16;            // partial sums on their way at once
-// Ids that need no sorting.  79 of a 3891 x 11 table: 16.2 us sorted, 11.1 so (a call of one empty kernel: 8.5).  Past this
+// Ids that need no sorting.  79 of a 3891 x 11 table: 16.2 us sorted, 11.1 so (8.5 of which any call takes).  Past this
 // number, one token in all places would cost its one wavefront more than sorting does.
 constexpr int kDirectIds = 256;
 constexpr int kDirectWaves = 4, kDirectRows = 8192;       // rows of the table that a workgroup clears, at most
