@@ -490,8 +490,10 @@ route_kernel(RouteArgs a)
                 // A lane ranks groups h, h + (1 << ll), ... of its row by the sums of all, in LDS.  Of groups of one chunk these are
                 // its own chunks; else what they are made of meets in LDS too: of groups of whole chunks every chunk's best two
                 // keys, else all keys.  A group is taken if fewer than top_groups have more; where more are taken so, or fewer though
-                // others are there (sums of 2^28 and more are not compared), or one that is not is too near to one that is, nothing is
-                // decided here.
+                // others are there (sums of 2^28 and more are not compared), or one that is not may have as much as one that is, nothing
+                // is decided here.  A sum is off by what its own keys are: `off` and a rounding of each, which is large beside the
+                // sum where the keys have opposite signs, and by the rounding of the sum itself; the least and the most that it may be
+                // round once more.
                 constexpr int kChunks = kRoutePer / kChunk<T>;
                 const int padded = (a.p.n_groups + 3) & ~3;         // sums of nobody's groups behind
                 float *const sums = (float *)own + ((((n + 3) & ~3) << (6 - ll)) + (lane >> ll) * padded);
@@ -508,7 +510,12 @@ route_kernel(RouteArgs a)
                     }
                 }
                 // Two keys of finite size have a sum, whatever fp32 makes of it.
-                const auto sum_of = [&](float first, float second) { return a.p.group_best == 2 && second > none ? fmaxf(first + second, -3.402823466e38f) : first; };
+                const float most = 3.402823466e38f, of_best = (float)a.p.group_best;
+                const auto sum_of = [&](float first, float second, float &wide) {
+                    const bool both = a.p.group_best == 2 && second > none;
+                    wide = of_best * fmaf(4.0f * kStep, both ? fmaxf(fabsf(first), fabsf(second)) : fabsf(first), off);
+                    return both ? __builtin_amdgcn_fmed3f(first + second, -most, most) : first;
+                };
                 const auto more_than = [&](float mine) {
                     const float minus = -kFar * mine;
                     float n = 0.0f;
@@ -519,12 +526,14 @@ route_kernel(RouteArgs a)
                     return n;
                 };
                 const float top_groups = (float)a.p.top_groups;
-                float size = 0.0f, lowest = __builtin_inff(), highest = none, count = 0.0f;     // of the taken, of the others
+                // The least that a taken group may have, the most that another may.  A sum that is infinite is so in 64 bits too: its
+                // bounds are NaN and count for nothing.
+                float lowest = __builtin_inff(), highest = none, count = 0.0f;
                 if (one) {
-                    float sum[kChunks];
+                    float sum[kChunks], wide[kChunks];
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) {
-                        sum[c] = sum_of(best[c][0], best[c][1]);
+                        sum[c] = sum_of(best[c][0], best[c][1], wide[c]);
                         if ((c << ll) + h < padded)
                             sums[(c << ll) + h] = sum[c];
                     }
@@ -535,9 +544,8 @@ route_kernel(RouteArgs a)
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) {
                         const bool in = sum[c] > none && more_than(sum[c]) < top_groups;
-                        size = sum[c] > none ? fmaxf(size, fabsf(sum[c])) : size;
-                        lowest = in ? fminf(lowest, sum[c]) : lowest;
-                        highest = in ? highest : fmaxf(highest, sum[c]);
+                        lowest = in ? fminf(lowest, sum[c] - wide[c]) : lowest;
+                        highest = in ? highest : fmaxf(highest, sum[c] + wide[c]);
                         count += in ? 1.0f : 0.0f;
 #pragma unroll
                         for (int i = 0; i < kChunk<T>; ++i)
@@ -568,16 +576,18 @@ route_kernel(RouteArgs a)
                         if (g < a.p.n_groups)
                             for (int i = 0; i < per; ++i)
                                 best_two(first, second, keys[g * per + i]);
-                        sums[g] = sum_of(first, second);
+                        float wide;
+                        sums[g] = sum_of(first, second, wide);
+                        if (g < a.p.n_groups)
+                            keys[g * per] = wide;                   // this lane's, as its keys were
                     }
                     lds_sync();
                     int taken = 0;
                     for (int g = h; g < a.p.n_groups; g += 1 << ll) {
-                        const float mine = sums[g];
+                        const float mine = sums[g], wide = keys[g * per];
                         const bool in = mine > none && more_than(mine) < top_groups;
-                        size = mine > none ? fmaxf(size, fabsf(mine)) : size;
-                        lowest = in ? fminf(lowest, mine) : lowest;
-                        highest = in ? highest : fmaxf(highest, mine);
+                        lowest = in ? fminf(lowest, mine - wide) : lowest;
+                        highest = in ? highest : fmaxf(highest, mine + wide);
                         taken |= in ? 1 << g : 0;
                     }
                     taken = row_or(taken, ll);
@@ -589,11 +599,9 @@ route_kernel(RouteArgs a)
                         key[u] = in ? key[u] : none;
                     }
                 }
-                size = row_max(size, ll);
                 lowest = -row_max(-lowest, ll);
                 highest = row_max(highest, ll);
-                const float near = 4.0f * off + 8.0f * kStep * size;
-                again |= (highest > none ? count != top_groups : count > top_groups) || !(lowest - highest > near);
+                again |= (highest > none ? count != top_groups : count > top_groups) || !(lowest > highest);
             }
             if (!a.bias)
 #pragma unroll

@@ -312,3 +312,30 @@ def test_tensors_elsewhere_are_refused(api):
         with pytest.raises(api.FsError) as err:
             call()
         assert "GPU" in str(err.value)
+
+
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("per,top,k", [(8, 1, 1), (2, 1, 1), (4, 3, 4), (16, 2, 3)])
+@pytest.mark.parametrize("level", [1e2, 1e4, 1e5, 1e6, 1e7])
+def test_groups_whose_two_best_keys_have_opposite_signs(api, typ, score, per, top, k, level):
+    """Biases of +level for a group's first expert and -level for the others: a group's sum is small, and what fp32 loses of its
+    two keys is not.  The definition in 64 bits, in the order of additions that it names: score + bias, then the two keys."""
+    import torch
+    rows, groups = 60000, 8
+    x = normal(int(level) + per, rows, groups * per, typ).cuda()
+    bias = torch.full((groups, per), -level, device="cuda")
+    bias[:, 0] = level
+    bias = bias.view(-1)
+    params = api.route_params(groups * per, k, score=api.FS_SCORE_SIGMOID if score == "sigmoid" else api.FS_SCORE_SOFTMAX, n_groups=groups,
+                              top_groups=top, group_best=2)
+    e, _ = api.fs_route(params, x, bias)
+    s = torch.softmax(x.double(), 1) if score == "softmax" else torch.sigmoid(x.double())
+    key = s + bias.double()
+    best = key.view(rows, groups, per).topk(2, dim=2).values
+    taken = (best[:, :, 0] + best[:, :, 1]).sort(dim=1, descending=True, stable=True).indices[:, :top]
+    there = torch.zeros(rows, groups, dtype=torch.bool, device="cuda").scatter_(1, taken, True)
+    key = torch.where(there.repeat_interleave(per, dim=1), key, -float("inf"))
+    want = key.sort(dim=1, descending=True, stable=True).indices[:, :k]
+    wrong = int((e.long() != want).any(dim=1).sum())
+    assert wrong == 0, "%d of %d rows" % (wrong, rows)
