@@ -13,6 +13,7 @@ namespace fs {
 constexpr int kEmbedWaves = 4;            // of a workgroup
 constexpr int kEmbedAhead = 8;            // rows on their way at once
 constexpr int kEmbedFewWaves = 2048;
+constexpr int kEmbedMostFp32 = 256;       // rows of a bag that are added in fp32 one after the other
 constexpr int kLookupRows = 4;            // rows of a lane
 constexpr int kSumMostWaves = 4096;
 constexpr int kSumMostChunk = 256, kSumLeastChunk = 8;    // pairs a chunk
@@ -96,8 +97,9 @@ struct EmbedArgs {
 };
 
 // Bags.  A row of the result in neighbouring lanes, eight rows of the table on their way at once; bags of few rows are split over
-// lanes.  320 bags of 100 rows of 64 fp32: 9 us, three rounds of dependent loads and the launch.
-template <int IN, int OUT, int ID>
+// lanes.  320 bags of 100 rows of 64 fp32: 9 us, three rounds of dependent loads and the launch.  LONG: a lane has more than
+// kEmbedMostFp32 of a bag's rows; sums of so many are added in 64 bits, so that what is lost does not grow with the bag.
+template <int IN, int OUT, int ID, bool LONG>
 __global__ void __launch_bounds__(kEmbedWaves * 64)
 embed_kernel(EmbedArgs a)
 {
@@ -120,6 +122,7 @@ embed_kernel(EmbedArgs a)
 #pragma unroll
     for (int i = 0; i < N; ++i)
         sum[i] = 0.0f;
+    double all[N] = {};
     for (int j0 = 0; j0 < per; j0 += kEmbedAhead) {          // the same number of times in all lanes
         int v[kEmbedAhead];
         if (ll >= 3) {                                       // eight lanes fetch an id each
@@ -145,7 +148,17 @@ embed_kernel(EmbedArgs a)
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 sum[i] += x[u][i];
+        if (LONG && (j0 + kEmbedAhead) % kEmbedMostFp32 == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                all[i] += (double)sum[i];
+                sum[i] = 0.0f;
+            }
     }
+    if (LONG)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            sum[i] = (float)(all[i] + (double)sum[i]);
     for (int s = 0; s < a.split; ++s)
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -910,9 +923,10 @@ extern "C" int fs_embed(int32_t n_vocab, int32_t width, const void *table, int32
             constexpr int in = decltype(i)::value, to = decltype(o)::value, id = decltype(d)::value;
             in_pieces((waves + kEmbedWaves - 1) / kEmbedWaves, [&](int64_t at, unsigned n) {
                 a.block0 = at;
-                const auto kernel = n_cols > 1                             ? embed_kernel<in, to, id>
-                                    : past_caches(n_rows, width, out_type) ? embed_lookup_kernel<in, to, id, true>
-                                                                           : embed_lookup_kernel<in, to, id, false>;
+                const auto kernel = (n_cols - 1) >> split >= kEmbedMostFp32 ? embed_kernel<in, to, id, true>
+                                    : n_cols > 1                            ? embed_kernel<in, to, id, false>
+                                    : past_caches(n_rows, width, out_type)  ? embed_lookup_kernel<in, to, id, true>
+                                                                            : embed_lookup_kernel<in, to, id, false>;
                 hipLaunchKernelGGL(kernel, dim3(n), dim3(kEmbedWaves * 64), 0, stream, a);
             });
         });

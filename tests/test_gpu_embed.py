@@ -319,3 +319,18 @@ def test_refusals_reach_the_caller(api):
                  lambda: api.fs_embed_backward(table[:3], ids, 6, accumulate=True)):
         with pytest.raises(api.FsError):
             call()
+
+
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,width", [(1, 300001, 1), (2, 300000, 8), (3, 300000, 512), (1, 2000003, 512), (70, 100000, 130)])
+def test_long_bags(api, typ, rows, cols, width):
+    """Values of one sign, the same in every row of the table: what fp32 loses of them does not average out.  At most 256 are added in
+    fp32 one after the other, then in 64 bits; joining up to 64 lanes' sums, the factor and the result round eight times more."""
+    import torch
+    gen = torch.Generator("cuda").manual_seed(cols + width)
+    value = (torch.rand(width, device="cuda", generator=gen) + 0.1).to(torch_type(typ))
+    table = value.expand(700, width).contiguous()
+    ids = torch.randint(0, 703, (rows, cols), device="cuda", generator=gen, dtype=torch.int32)
+    out = api.fs_embed(table, ids, scale=0.7, out=torch.empty(rows, width, device="cuda"))
+    exp = (ids < 700).sum(dim=1, dtype=torch.float64)[:, None] * value.double() * float(np.float32(0.7))
+    assert bool(((out.double() - exp).abs() <= (256 + 8) * 2.0 ** -24 * exp).all()), float((out.double() / exp - 1).abs().max())
