@@ -156,8 +156,10 @@ expert_combine_kernel(ExchangeArgs a)
     }
 }
 
-// The products need a token's whole width, so that its lanes go over the column blocks themselves.  65 536 tokens of 1024 bf16,
-// k = 4: 215 us, 5.6 TB/s.
+// The products need a token's whole width, so that its lanes go over the column blocks themselves.  At most kMostProducts of a lane
+// are added one after the other; a wide row has many such sums, whose sum is another, so that 2^20 columns are 256 and 64
+// additions long.  65 536 tokens of 1024 bf16, k = 4: 215 us, 5.6 TB/s.
+constexpr int kMostProducts = 256;
 template <int TYPE, int AHEAD>
 __global__ void __launch_bounds__(kExchangeWaves * 64)
 expert_combine_backward_kernel(ExchangeArgs a)
@@ -171,7 +173,7 @@ expert_combine_backward_kernel(ExchangeArgs a)
         return;
     for (int j0 = 0; j0 < a.k; j0 += AHEAD) {
         int p[AHEAD];
-        float w[AHEAD], dot[AHEAD];
+        float w[AHEAD], dot[AHEAD], dots[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int j = min(j0 + u, a.k - 1);
@@ -179,8 +181,9 @@ expert_combine_backward_kernel(ExchangeArgs a)
             if (!there || j0 + u >= a.k || p[u] < 0 || p[u] >= slots)
                 p[u] = -1;
             w[u] = a.weight[token * a.k + j];
-            dot[u] = 0.0f;
+            dot[u] = dots[u] = 0.0f;
         }
+        int products = 0;
         for (int c0 = l.h * N; c0 < a.width; c0 += 64 * N) {
             const Span at = span_of<N>(c0, a.width);
             const int c = at.c, n = at.n;
@@ -201,10 +204,19 @@ expert_combine_backward_kernel(ExchangeArgs a)
                 }
                 store_chunk<N>((T *)a.out + (int64_t)p[u] * a.out_stride + c, n, d);
             }
+            products += N;
+            if (products == kMostProducts) {
+                products = 0;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    dots[u] += dot[u];
+                    dot[u] = 0.0f;
+                }
+            }
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const float all = row_sum(dot[u], a.ll);
+            const float all = row_sum(dots[u] + dot[u], a.ll);
             if (there && l.h == 0 && j0 + u < a.k)
                 a.d_weight[token * a.k + j0 + u] = all;
         }

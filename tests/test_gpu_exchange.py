@@ -228,3 +228,20 @@ def test_refusals_reach_the_caller(api):
     with pytest.raises(api.FsError):
         api.fs_expert_combine_backward(torch.zeros(4, 8, device="cuda"), torch.zeros(8, 8, device="cuda", dtype=torch.float16), p,
                                        torch.zeros(4, 2, device="cuda"))
+
+
+@pytest.mark.parametrize("typ", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("k", [2, 7])
+def test_weights_gradients_of_very_wide_rows(api, typ, k):
+    """Products of one sign and size, so that what fp32 loses does not average out: a lane adds at most 256 of them one after the
+    other, the lane's 64 such sums too, then 64 lanes meet; each product rounds once."""
+    import torch
+    tokens, width = 3, 1 << 20
+    t = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[typ]
+    p = plan_of(api, choices(9, tokens, k, 5, missing=0.2), 5)
+    g = torch.linspace(0.1, 0.7, tokens, device="cuda")[:, None].expand(tokens, width).to(t).contiguous()
+    y = torch.linspace(0.2, 0.9, tokens * k, device="cuda")[:, None].expand(tokens * k, width).to(t).contiguous()
+    _, d_w = api.fs_expert_combine_backward(g, y, p, torch.ones(tokens, k, device="cuda"))
+    there = p.place >= 0
+    exp = torch.where(there, g[:, :1].double() * y[:, 0].double()[p.place.clamp(min=0).long()] * width, 0.0)
+    assert bool(((d_w.double() - exp).abs() <= (256 + 64 + 6 + 2) * 2.0 ** -24 * exp).all()), float((d_w.double() / exp - 1)[there].abs().max())
