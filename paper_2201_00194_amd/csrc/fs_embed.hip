@@ -62,12 +62,13 @@ struct EmbedIds {
                 base[u] = col_base[column(u)];
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            int64_t v = (int64_t)id[u];
-            bool fits = true;
-            if constexpr (ID == FS_ID_I64)
-                fits = v == (int64_t)(int32_t)v;
-            v = (int64_t)(int32_t)v + base[u];
-            row[u] = fits && v >= 0 && v < n_vocab ? (int)v : -1;
+            if constexpr (ID == FS_ID_I64) {       // id + base in [0, n_vocab), without a sum that 64 bits might not hold
+                const int64_t v = id[u], least = -(int64_t)base[u];
+                row[u] = v >= least && v < least + n_vocab ? (int)(v - least) : -1;
+            } else {
+                const int64_t v = (int64_t)(int32_t)id[u] + base[u];
+                row[u] = v >= 0 && v < n_vocab ? (int)v : -1;
+            }
         }
     }
     __device__ __forceinline__ uint32_t row_of(uint32_t i) const { return n_cols == 1 ? i : __umulhi(i, magic) >> shift; }

@@ -334,3 +334,26 @@ def test_long_bags(api, typ, rows, cols, width):
     out = api.fs_embed(table, ids, scale=0.7, out=torch.empty(rows, width, device="cuda"))
     exp = (ids < 700).sum(dim=1, dtype=torch.float64)[:, None] * value.double() * float(np.float32(0.7))
     assert bool(((out.double() - exp).abs() <= (256 + 8) * 2.0 ** -24 * exp).all()), float((out.double() / exp - 1).abs().max())
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 1), (100, 2), (300, 3), (9000, 1), (20000, 2)])
+def test_ids_and_bases_whose_sum_alone_fits(api, rows, cols):
+    """The row is the column's base plus the id, also where the id by itself has more than 32 bits."""
+    import torch
+    vocab = 40
+    base = torch.tensor([-2147483648, 2147483647, -5][:cols], dtype=torch.int32, device="cuda")
+    row = torch.randint(-3, vocab + 3, (rows, cols), device="cuda")
+    ids = row - base.long()
+    far = torch.rand(rows, cols, device="cuda") < 0.2
+    ids = torch.where(far & (row % 2 == 0), 9223372036854775807, torch.where(far, -9223372036854775807 - 1, ids))
+    at = torch.where(far | (row < 0) | (row >= vocab), vocab, row)
+    table = torch.randint(-9, 10, (vocab + 1, 12), device="cuda").float()
+    table[vocab] = 0
+    out = api.fs_embed(table[:vocab], ids, col_base=base)
+    assert torch.equal(out, table[at].sum(dim=1))
+    g = torch.randint(-9, 10, (rows, 12), device="cuda").float()          # sums of whole numbers are exact
+    d = api.fs_embed_backward(g, ids, vocab, col_base=base)
+    exp = torch.zeros(vocab + 1, 12, dtype=torch.float64, device="cuda")
+    for c in range(cols):
+        exp.index_add_(0, at[:, c], g.double())
+    assert torch.equal(d.double(), exp[:vocab])
