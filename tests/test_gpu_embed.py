@@ -357,3 +357,16 @@ def test_ids_and_bases_whose_sum_alone_fits(api, rows, cols):
     for c in range(cols):
         exp.index_add_(0, at[:, c], g.double())
     assert torch.equal(d.double(), exp[:vocab])
+
+
+def test_the_longest_bag(api):
+    """2^31 - 1 ids in one bag: the first, the last and those where its 64 parts meet are in the sum, and nothing behind them."""
+    import torch
+    n = 2147483647
+    ids = torch.zeros(n + 1, dtype=torch.int16, device="cuda")
+    per = (n + 63) // 64
+    at = torch.tensor([0, 1, n - 1, n - 2] + [p * per + d for p in range(1, 64) for d in (-1, 0)], device="cuda")
+    ids[at] = 1
+    ids[n] = 2
+    table = torch.tensor([[0.0], [1.0], [float("nan")]], device="cuda")
+    assert float(api.fs_embed(table, ids[:n].view(1, n))) == at.numel()
