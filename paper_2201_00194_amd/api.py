@@ -537,13 +537,18 @@ def _matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optio
     return t.data_ptr(), kind, (step if n > 1 else max(1, w))
 
 
-def _array(t: Optional[torch.Tensor], what: str, n: int, dtype: torch.dtype, on: Optional[int] = None) -> Optional[int]:
+def _array(t: Optional[torch.Tensor], what: str, shape, dtype: torch.dtype, on: Optional[int] = None) -> Optional[int]:
+    """The pointer of an array argument; `shape`: so many elements, or a shape, which the array has or, laid flat, would have."""
     if t is None:
         return None
     if on is not None and t.get_device() != on:
         raise FsError(FS_EINVAL, f"{what} is not on the call's GPU")
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-        raise FsError(FS_EINVAL, f"{what} is not a contiguous array of {n} {dtype}")
+    if type(shape) is tuple:
+        fits = t.shape == shape or (t.dim() == 1 and t.numel() == math.prod(shape))
+    else:
+        fits = t.numel() == shape
+    if t.dtype != dtype or not fits or not t.is_contiguous():
+        raise FsError(FS_EINVAL, f"{what} is not a contiguous array of {shape} {dtype}")
     return t.data_ptr()
 
 
@@ -583,7 +588,7 @@ class _Place:
         if out is None:
             out = self.empty(shape, dtype)
             return out, out.data_ptr()
-        return out, _array(out, what, math.prod(shape), dtype, self.index)
+        return out, _array(out, what, shape, dtype, self.index)
 
 
 def route_params(n_experts: int, k: int, score: int = FS_SCORE_SOFTMAX, renormalise: bool = True, n_groups: int = 1,
@@ -611,8 +616,8 @@ def fs_route_backward(params: _FsRouteParams, logits: torch.Tensor, expert: torc
     ptr, typ, stride = _matrix(logits, "logits", params.n_experts, on=at.index)
     n, k = logits.shape[0], params.k
     d_logits, d_ptr, d_stride = at.matrix(d_logits, "d_logits", n, params.n_experts, logits.dtype)
-    _check(_lib.fs_route_backward(params, n, ptr, typ, stride, _array(expert, "expert", n * k, torch.int32, at.index),
-                                  _array(d_weight, "d_weight", n * k, torch.float32, at.index), d_ptr, d_stride, at.ptr))
+    _check(_lib.fs_route_backward(params, n, ptr, typ, stride, _array(expert, "expert", (n, k), torch.int32, at.index),
+                                  _array(d_weight, "d_weight", (n, k), torch.float32, at.index), d_ptr, d_stride, at.ptr))
     return d_logits
 
 
@@ -637,6 +642,8 @@ def fs_expert_plan(expert: torch.Tensor, n_experts: int, plan: Optional[ExpertPl
     if expert.dim() != 2:
         raise FsError(FS_EINVAL, "expert is not [tokens, k]")
     n, k = expert.shape
+    if plan is not None and (plan.n_tokens, plan.k, plan.n_experts) != (n, k, n_experts):
+        raise FsError(FS_EINVAL, f"plan is of {(plan.n_tokens, plan.k, plan.n_experts)} tokens, choices and experts, not {(n, k, n_experts)}")
     src = _array(expert, "expert", n * k, torch.int32, at.index)
     old = (None, None, None) if plan is None else (plan.first, plan.order, plan.place)
     first, f_ptr = at.array(old[0], "first", (max(n_experts, 0) + 1,), torch.int32)
@@ -667,7 +674,7 @@ def fs_expert_combine(y: torch.Tensor, plan: ExpertPlan, weight: Optional[torch.
     width = y.shape[1]
     out, o_ptr, o_stride = at.matrix(out, "out", plan.n_tokens, width, y.dtype)
     _check(_lib.fs_expert_combine(plan.n_tokens, plan.k, width, ptr, typ, stride, plan._lists(at)[1],
-                                  _array(weight, "weight", plan.n_tokens * plan.k, torch.float32, at.index), o_ptr, o_stride, at.ptr))
+                                  _array(weight, "weight", (plan.n_tokens, plan.k), torch.float32, at.index), o_ptr, o_stride, at.ptr))
     return out
 
 
@@ -682,7 +689,7 @@ def fs_expert_combine_backward(d_out: torch.Tensor, y: torch.Tensor, plan: Exper
     d_y, o_ptr, o_stride = at.matrix(d_y, "d_y", n * k, width, d_out.dtype)
     d_weight, w_ptr = at.array(d_weight, "d_weight", (n, k), torch.float32)
     _check(_lib.fs_expert_combine_backward(n, k, plan.n_experts, width, ptr, typ, stride, y_ptr, y_stride, *plan._lists(at),
-                                           _array(weight, "weight", n * k, torch.float32, at.index), o_ptr, o_stride, w_ptr, at.ptr))
+                                           _array(weight, "weight", (n, k), torch.float32, at.index), o_ptr, o_stride, w_ptr, at.ptr))
     return d_y, d_weight
 
 

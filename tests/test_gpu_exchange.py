@@ -245,3 +245,30 @@ def test_weights_gradients_of_very_wide_rows(api, typ, k):
     there = p.place >= 0
     exp = torch.where(there, g[:, :1].double() * y[:, 0].double()[p.place.clamp(min=0).long()] * width, 0.0)
     assert bool(((d_w.double() - exp).abs() <= (256 + 64 + 6 + 2) * 2.0 ** -24 * exp).all()), float((d_w.double() / exp - 1)[there].abs().max())
+
+
+def test_plans_and_arrays_of_another_shape_are_refused(api):
+    """As many choices, but not the same tokens: lists written for the one would be read as the other's."""
+    import torch
+    p = plan_of(api, choices(1, 4, 3, 8), 8)
+    kept = p.place.clone()
+    for e, experts in ((choices(2, 6, 2, 8), 8), (choices(2, 12, 1, 8), 8), (choices(2, 4, 3, 7), 7)):
+        with pytest.raises(api.FsError):
+            api.fs_expert_plan(torch.from_numpy(e).cuda(), experts, plan=p)
+    assert torch.equal(p.place, kept)
+    e = torch.from_numpy(choices(3, 4, 3, 8)).cuda()
+    assert api.fs_expert_plan(e, 8, plan=p) is p and torch.equal(p.place, api.fs_expert_plan(e, 8).place)
+    x, y, w = torch.zeros(4, 5, device="cuda"), torch.zeros(12, 5, device="cuda"), torch.ones(4, 3, device="cuda")
+    logits, params = torch.randn(4, 8, device="cuda"), api.route_params(8, 3)
+    turned, turned_e = torch.ones(3, 4, device="cuda"), torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+    for call in (lambda: api.fs_expert_combine(y, p, turned), lambda: api.fs_expert_combine_backward(x, y, p, turned),
+                 lambda: api.fs_expert_combine_backward(x, y, p, w, d_weight=turned), lambda: api.fs_route(params, logits, expert=turned_e),
+                 lambda: api.fs_route(params, logits, weight=turned), lambda: api.fs_route_backward(params, logits, turned_e, w),
+                 lambda: api.fs_route_backward(params, logits, e, turned)):
+        with pytest.raises(api.FsError):
+            call()
+    flat_e, flat_w = torch.empty(12, dtype=torch.int32, device="cuda"), torch.empty(12, device="cuda")
+    e2, w2 = api.fs_route(params, logits)
+    api.fs_route(params, logits, expert=flat_e, weight=flat_w)                     # the same memory, laid flat
+    assert torch.equal(flat_e.view(4, 3), e2) and torch.equal(flat_w.view(4, 3), w2)
+    assert torch.equal(api.fs_expert_combine(y + 1, p, flat_w), api.fs_expert_combine(y + 1, p, w2))

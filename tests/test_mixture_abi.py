@@ -284,3 +284,18 @@ def test_oracle_embedding_is_a_product_with_counts():
     np.testing.assert_allclose(MO.embed(table, rows, 0.5)[0], 0.5 * count @ table, atol=1e-12)
     np.testing.assert_allclose(MO.embed_backward(g, rows, 10, 0.5)[0], 0.5 * count.T @ g, atol=1e-12)
     assert MO.rows_of([[3, 3]], [0, 100], 50).tolist() == [[3, -1]]
+
+
+# ---- the binding -------------------------------------------------------------------------------------
+
+
+def test_binding_refuses_arrays_of_another_shape(api):
+    import torch
+    t = torch.zeros(6, 2)
+    for bad in ((2, 6), (4, 3), (6, 1), 13):
+        with pytest.raises(api.FsError):
+            api._array(t, "w", bad, torch.float32)
+    assert api._array(t, "w", (6, 2), torch.float32) == api._array(t, "w", 12, torch.float32) == t.data_ptr()
+    assert api._array(t.view(-1), "w", (6, 2), torch.float32) == t.data_ptr()
+    with pytest.raises(api.FsError):
+        api._array(t.view(1, 12), "w", (6, 2), torch.float32)
