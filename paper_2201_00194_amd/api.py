@@ -518,6 +518,13 @@ for _name, _result, _args in (
     getattr(_lib, _name).argtypes = _args
 
 
+def _int32(v: int, what: str) -> int:
+    """A number for an int32_t: ctypes would pass on its low 32 bits."""
+    if not -2147483648 <= v <= 2147483647:
+        raise FsError(FS_EINVAL, f"{what}: {v} does not fit 32 bits")
+    return v
+
+
 def _matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optional[int] = None,
             dtype: Optional[torch.dtype] = None, on: Optional[int] = None):
     """(pointer, element type, row stride) of a matrix argument whose rows' elements are adjacent; `on`: the call's GPU."""
@@ -531,6 +538,8 @@ def _matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optio
         raise FsError(FS_EINVAL, f"{what} is {(n, w)}, not {(rows, width)}")
     if dtype is not None and t.dtype != dtype:
         raise FsError(FS_EINVAL, f"{what} is {t.dtype}, not {dtype}")
+    if w > 2147483647:
+        raise FsError(FS_EINVAL, f"{what}: a row of {w} elements")
     step, between = t.stride()
     if between != 1 and w > 1:
         raise FsError(FS_EINVAL, f"{what}: the elements of a row are not adjacent")
@@ -593,7 +602,8 @@ class _Place:
 
 def route_params(n_experts: int, k: int, score: int = FS_SCORE_SOFTMAX, renormalise: bool = True, n_groups: int = 1,
                  top_groups: int = 1, group_best: int = 1, scale: float = 1.0) -> _FsRouteParams:
-    return _FsRouteParams(n_experts, k, score, int(renormalise), n_groups, top_groups, group_best, scale)
+    return _FsRouteParams(_int32(n_experts, "n_experts"), _int32(k, "k"), _int32(score, "score"), _int32(int(renormalise), "renormalise"),
+                          _int32(n_groups, "n_groups"), _int32(top_groups, "top_groups"), _int32(group_best, "group_best"), scale)
 
 
 def fs_route(params: _FsRouteParams, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -642,6 +652,7 @@ def fs_expert_plan(expert: torch.Tensor, n_experts: int, plan: Optional[ExpertPl
     if expert.dim() != 2:
         raise FsError(FS_EINVAL, "expert is not [tokens, k]")
     n, k = expert.shape
+    _int32(k, "k"), _int32(n_experts, "n_experts")
     if plan is not None and (plan.n_tokens, plan.k, plan.n_experts) != (n, k, n_experts):
         raise FsError(FS_EINVAL, f"plan is of {(plan.n_tokens, plan.k, plan.n_experts)} tokens, choices and experts, not {(n, k, n_experts)}")
     src = _array(expert, "expert", n * k, torch.int32, at.index)
@@ -683,8 +694,9 @@ def fs_expert_combine_backward(d_out: torch.Tensor, y: torch.Tensor, plan: Exper
                                stream: Optional[torch.cuda.Stream] = None):
     """(d_y, d_weight) of a weighted fs_expert_combine."""
     at = _Place(d_out, stream)
-    n, k, width = plan.n_tokens, plan.k, d_out.shape[-1]
+    n, k = plan.n_tokens, plan.k
     ptr, typ, stride = _matrix(d_out, "d_out", rows=n, on=at.index)
+    width = d_out.shape[1]
     y_ptr, _, y_stride = _matrix(y, "y", width, n * k, d_out.dtype, at.index)
     d_y, o_ptr, o_stride = at.matrix(d_y, "d_y", n * k, width, d_out.dtype)
     d_weight, w_ptr = at.array(d_weight, "d_weight", (n, k), torch.float32)
@@ -702,7 +714,7 @@ def _id_array(ids: torch.Tensor, col_base: Optional[torch.Tensor], on: Optional[
     if on is not None and ids.get_device() != on:
         raise FsError(FS_EINVAL, "ids is not on the call's GPU")
     rows, cols = ids.shape[0], (ids.shape[1] if ids.dim() == 2 else 1)
-    return rows, cols, ids.data_ptr(), _ID[ids.dtype], _array(col_base, "col_base", cols, torch.int32, on)
+    return rows, _int32(cols, "columns of ids"), ids.data_ptr(), _ID[ids.dtype], _array(col_base, "col_base", cols, torch.int32, on)
 
 
 def fs_embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, col_base: Optional[torch.Tensor] = None,
@@ -713,6 +725,7 @@ def fs_embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, col_bas
     t_ptr, typ, t_stride = _matrix(table, "table", on=at.index)
     rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base, at.index)
     vocab, width = table.shape
+    _int32(vocab, "rows of table")
     out, o_ptr, o_stride = at.matrix(out, "out", rows, width, table.dtype if out is None else out.dtype)
     o_typ = _ELEMENT[out.dtype]
     _check(_lib.fs_embed(vocab, width, t_ptr, typ, t_stride, rows, cols, i_ptr, i_typ, base, scale, o_ptr, o_typ, o_stride, at.ptr))
@@ -725,6 +738,7 @@ def fs_embed_backward(d_out: torch.Tensor, ids: torch.Tensor, n_vocab: int, scal
     """The table's gradient [n_vocab, width]: fp32 unless `d_table` (of that type or d_out's) is given; `accumulate` adds to
     what `d_table` holds."""
     at = _Place(d_out, stream)
+    _int32(n_vocab, "n_vocab")
     rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base, at.index)
     ptr, typ, stride = _matrix(d_out, "d_out", rows=rows, on=at.index)
     width = d_out.shape[1]

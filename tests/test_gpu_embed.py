@@ -370,3 +370,18 @@ def test_the_longest_bag(api):
     ids[n] = 2
     table = torch.tensor([[0.0], [1.0], [float("nan")]], device="cuda")
     assert float(api.fs_embed(table, ids[:n].view(1, n))) == at.numel()
+
+
+def test_tables_of_more_rows_than_32_bits_hold_are_refused(api):
+    """They would be taken for tables of the low 32 bits' rows."""
+    import torch
+    many = (1 << 32) + 5
+    ids = torch.zeros(3, dtype=torch.int64, device="cuda")
+    for call in (lambda: api.fs_embed(torch.empty(many, 1, dtype=torch.bfloat16, device="cuda"), ids),
+                 lambda: api.fs_embed_backward(torch.zeros(3, 1, device="cuda"), ids, many),
+                 lambda: api.fs_expert_plan(torch.zeros(3, 1, dtype=torch.int32, device="cuda"), (1 << 32) + 8)):
+        with pytest.raises(api.FsError):
+            call()
+    with pytest.raises(api.FsError):                        # no rows at all
+        api.fs_expert_combine_backward(torch.zeros((), device="cuda"), torch.zeros(3, 1, device="cuda"),
+                                       api.fs_expert_plan(torch.zeros(3, 1, dtype=torch.int32, device="cuda"), 2), torch.ones(3, 1, device="cuda"))

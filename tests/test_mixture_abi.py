@@ -299,3 +299,17 @@ def test_binding_refuses_arrays_of_another_shape(api):
     assert api._array(t.view(-1), "w", (6, 2), torch.float32) == t.data_ptr()
     with pytest.raises(api.FsError):
         api._array(t.view(1, 12), "w", (6, 2), torch.float32)
+
+
+def test_binding_refuses_numbers_that_32_bits_do_not_hold(api):
+    """Not one of them reaches the library as its low 32 bits."""
+    import torch
+    for name in ("n_experts", "k", "score", "n_groups", "top_groups", "group_best"):
+        with pytest.raises(api.FsError) as e:
+            api.route_params(**{"n_experts": 8, "k": 2, name: (1 << 32) + 2})
+        assert name in str(e.value)
+    with pytest.raises(api.FsError):
+        api._matrix(torch.empty(1, (1 << 32) + 8, device="meta"), "x")
+    with pytest.raises(api.FsError):
+        api._id_array(torch.empty(1, (1 << 32) + 1, device="meta", dtype=torch.int32), None)
+    assert api._matrix(torch.empty(1, (1 << 31) - 1, device="meta"), "x")[1:] == (api.FS_F32, (1 << 31) - 1)
