@@ -565,8 +565,22 @@ def _array(t: Optional[torch.Tensor], what: str, shape, dtype: torch.dtype, on: 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_gpus = 0        # how many there are, once a call has asked
+
+
+def _refuse_other_gpus(index: int, stream: Optional[torch.cuda.Stream]) -> None:
+    """The library launches on the current GPU, and a default stream's handle names that one's, whichever GPU it was asked of."""
+    global _gpus
+    _gpus = torch.cuda.device_count()
+    if _gpus > 1:
+        if torch.cuda.current_device() != index:
+            raise FsError(FS_EINVAL, f"the tensors are on GPU {index}, which is not the current one")
+        if stream is not None and stream.device_index != index:
+            raise FsError(FS_EINVAL, f"the stream is GPU {stream.device_index}'s, the tensors are on GPU {index}")
+
+
 class _Place:
-    """Where a call runs: results and working memory are allocated for its stream."""
+    """Where a call runs, the current GPU: results and working memory are allocated for its stream."""
 
     __slots__ = ("device", "index", "stream", "ptr")
 
@@ -575,6 +589,8 @@ class _Place:
             raise FsError(FS_EINVAL, "the tensors are not on the GPU")
         self.device, self.stream = like.device, stream
         self.index = self.device.index
+        if _gpus != 1:
+            _refuse_other_gpus(self.index, stream)
         self.ptr = _raw_stream(self.index) if stream is None else stream.cuda_stream
 
     def empty(self, shape, dtype: torch.dtype) -> torch.Tensor:

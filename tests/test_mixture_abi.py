@@ -313,3 +313,26 @@ def test_binding_refuses_numbers_that_32_bits_do_not_hold(api):
     with pytest.raises(api.FsError):
         api._id_array(torch.empty(1, (1 << 32) + 1, device="meta", dtype=torch.int32), None)
     assert api._matrix(torch.empty(1, (1 << 31) - 1, device="meta"), "x")[1:] == (api.FS_F32, (1 << 31) - 1)
+
+
+def test_binding_refuses_tensors_and_streams_of_a_gpu_that_is_not_the_current_one(api, monkeypatch):
+    """Two GPUs as torch would report them."""
+    import types
+
+    import torch
+
+    def tensor(index):
+        return types.SimpleNamespace(is_cuda=True, device=torch.device("cuda", index))
+
+    def stream(index):
+        return types.SimpleNamespace(device_index=index, cuda_stream=77)
+
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(api, "_raw_stream", lambda index: 100 + index)
+    monkeypatch.setattr(api, "_gpus", 0, raising=False)
+    assert api._Place(tensor(1), None).ptr == 101 and api._Place(tensor(1), stream(1)).ptr == 77
+    for t, s in ((tensor(0), None), (tensor(0), stream(0)), (tensor(1), stream(0)), (tensor(0), stream(1))):
+        with pytest.raises(api.FsError) as e:
+            api._Place(t, s)
+        assert "GPU" in str(e.value)
