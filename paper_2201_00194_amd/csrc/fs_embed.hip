@@ -7,6 +7,7 @@
 #include "fs_slots.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace fs {
 
@@ -98,21 +99,24 @@ struct EmbedArgs {
 };
 
 // The entries of a bag that a part of it takes: of the 1 << split parts, entries begin .. end - 1, `per` of them in all but the last.
-// A bag has up to 2^31 - 1 entries, so that steps beyond its end need the 32nd bit.
+// A bag has up to 2^31 - 1 entries, so that steps beyond its end need the 32nd bit; short ones are counted in int, which is quicker
+// (320 bags of 100 rows 8.8 us, 8.9 unsigned).
+template <class Count>
 struct BagPart {
-    uint32_t per, begin, end;
+    Count per, begin, end;
 };
-__host__ __device__ constexpr BagPart bag_part(uint32_t cols, int split, uint32_t part)
+template <class Count>
+__host__ __device__ constexpr BagPart<Count> bag_part(Count cols, int split, Count part)
 {
-    const uint32_t per = (cols >> split) + ((cols & ((1u << split) - 1u)) != 0u);
-    const uint32_t begin = part * per < cols ? part * per : cols, end = begin + per < cols ? begin + per : cols;
-    return BagPart{per, begin, end};
+    const Count per = (cols + (Count)(1 << split) - 1) >> split;
+    const Count begin = part * per < cols ? part * per : cols, end = begin + per < cols ? begin + per : cols;
+    return BagPart<Count>{per, begin, end};
 }
 constexpr uint32_t kMostBag = 2147483647u;
-static_assert(bag_part(kMostBag, 0, 0).per == kMostBag && bag_part(kMostBag, 0, 0).end == kMostBag && kMostBag + kEmbedAhead > kMostBag,
+static_assert(bag_part<uint32_t>(kMostBag, 0, 0).per == kMostBag && bag_part<uint32_t>(kMostBag, 0, 0).end == kMostBag && kMostBag + kEmbedAhead > kMostBag,
               "one part: all entries, and the step behind them is no smaller");
-static_assert(bag_part(kMostBag, 6, 63).end == kMostBag && bag_part(kMostBag, 6, 63).begin == bag_part(kMostBag, 6, 62).end &&
-                  bag_part(kMostBag - 62, 6, 63).end == kMostBag - 62 && bag_part(65, 6, 63).begin == 65,
+static_assert(bag_part<uint32_t>(kMostBag, 6, 63).end == kMostBag && bag_part<uint32_t>(kMostBag, 6, 63).begin == bag_part<uint32_t>(kMostBag, 6, 62).end &&
+                  bag_part<uint32_t>(kMostBag - 62, 6, 63).end == kMostBag - 62 && bag_part<uint32_t>(65, 6, 63).begin == 65,
               "64 parts: they meet, and the last ends with the bag");
 
 // Bags.  A row of the result in neighbouring lanes, eight rows of the table on their way at once; bags of few rows are split over
@@ -134,31 +138,32 @@ embed_kernel(EmbedArgs a)
     const int64_t row = there ? row0 + (lane >> (ll + a.split)) : a.n_rows - 1;
     const Span at = span_of<N>(((a.columns == 1 ? 0 : (int)(wave % a.columns)) * 64 + h) * N, a.width);
     const int c = at.c, n = at.n;
-    const uint32_t cols = (uint32_t)a.ids.n_cols;
-    const BagPart of = bag_part(cols, a.split, (uint32_t)part);
-    const uint32_t per = of.per, begin = of.begin, end = of.end;
+    typedef typename std::conditional<LONG, uint32_t, int>::type Count;
+    const Count cols = (Count)a.ids.n_cols;
+    const BagPart<Count> of = bag_part<Count>(cols, a.split, (Count)part);
+    const Count per = of.per, begin = of.begin, end = of.end;
     const In *const in = (const In *)a.in + c;
     float sum[N];
 #pragma unroll
     for (int i = 0; i < N; ++i)
         sum[i] = 0.0f;
     double all[N] = {};
-    for (uint32_t j0 = 0; j0 < per; j0 += kEmbedAhead) {     // the same number of times in all lanes
+    for (Count j0 = 0; j0 < per; j0 += kEmbedAhead) {     // the same number of times in all lanes
         int v[kEmbedAhead];
         if (ll >= 3) {                                       // eight lanes fetch an id each
             int id[1];
-            const uint32_t j = min(begin + j0 + (uint32_t)(h & 7), cols - 1);
-            a.ids.template rows<ID>(id, [&](int) { return row * (int64_t)cols + j; }, [&](int) { return j; });
+            const Count j = min(begin + j0 + (Count)(h & 7), cols - 1);
+            a.ids.template rows<ID>(id, [&](int) { return row * cols + j; }, [&](int) { return j; });
 #pragma unroll
             for (int u = 0; u < kEmbedAhead; ++u)
                 v[u] = __shfl(id[0], (lane & ~7) + u);
         } else {
-            const auto j = [&](int u) { return min(begin + j0 + (uint32_t)u, cols - 1); };
-            a.ids.template rows<ID>(v, [&](int u) { return row * (int64_t)cols + j(u); }, j);
+            const auto j = [&](int u) { return min(begin + j0 + (Count)u, cols - 1); };
+            a.ids.template rows<ID>(v, [&](int u) { return row * cols + j(u); }, j);
         }
 #pragma unroll
         for (int u = 0; u < kEmbedAhead; ++u)
-            v[u] = begin + j0 + (uint32_t)u < end ? v[u] : -1;
+            v[u] = begin + j0 + (Count)u < end ? v[u] : -1;
         RawChunk<In> x[kEmbedAhead];
 #pragma unroll
         for (int u = 0; u < kEmbedAhead; ++u)
