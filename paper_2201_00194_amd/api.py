@@ -518,9 +518,12 @@ for _name, _result, _args in (
     getattr(_lib, _name).argtypes = _args
 
 
+_INT32_MAX = 2147483647
+
+
 def _int32(v: int, what: str) -> int:
     """A number for an int32_t: ctypes would pass on its low 32 bits."""
-    if not -2147483648 <= v <= 2147483647:
+    if not -2147483648 <= v <= _INT32_MAX:
         raise FsError(FS_EINVAL, f"{what}: {v} does not fit 32 bits")
     return v
 
@@ -538,7 +541,7 @@ def _matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optio
         raise FsError(FS_EINVAL, f"{what} is {(n, w)}, not {(rows, width)}")
     if dtype is not None and t.dtype != dtype:
         raise FsError(FS_EINVAL, f"{what} is {t.dtype}, not {dtype}")
-    if w > 2147483647:
+    if w > _INT32_MAX:
         raise FsError(FS_EINVAL, f"{what}: a row of {w} elements")
     step, between = t.stride()
     if between != 1 and w > 1:
@@ -668,7 +671,8 @@ def fs_expert_plan(expert: torch.Tensor, n_experts: int, plan: Optional[ExpertPl
     if expert.dim() != 2:
         raise FsError(FS_EINVAL, "expert is not [tokens, k]")
     n, k = expert.shape
-    _int32(k, "k"), _int32(n_experts, "n_experts")
+    if k > _INT32_MAX or n_experts > _INT32_MAX:
+        raise FsError(FS_EINVAL, f"{k} choices or {n_experts} experts do not fit 32 bits")
     if plan is not None and (plan.n_tokens, plan.k, plan.n_experts) != (n, k, n_experts):
         raise FsError(FS_EINVAL, f"plan is of {(plan.n_tokens, plan.k, plan.n_experts)} tokens, choices and experts, not {(n, k, n_experts)}")
     src = _array(expert, "expert", n * k, torch.int32, at.index)
@@ -730,7 +734,9 @@ def _id_array(ids: torch.Tensor, col_base: Optional[torch.Tensor], on: Optional[
     if on is not None and ids.get_device() != on:
         raise FsError(FS_EINVAL, "ids is not on the call's GPU")
     rows, cols = ids.shape[0], (ids.shape[1] if ids.dim() == 2 else 1)
-    return rows, _int32(cols, "columns of ids"), ids.data_ptr(), _ID[ids.dtype], _array(col_base, "col_base", cols, torch.int32, on)
+    if cols > _INT32_MAX:
+        raise FsError(FS_EINVAL, f"ids has {cols} columns")
+    return rows, cols, ids.data_ptr(), _ID[ids.dtype], _array(col_base, "col_base", cols, torch.int32, on)
 
 
 def fs_embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, col_base: Optional[torch.Tensor] = None,
@@ -741,7 +747,8 @@ def fs_embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, col_bas
     t_ptr, typ, t_stride = _matrix(table, "table", on=at.index)
     rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base, at.index)
     vocab, width = table.shape
-    _int32(vocab, "rows of table")
+    if vocab > _INT32_MAX:
+        raise FsError(FS_EINVAL, f"table has {vocab} rows")
     out, o_ptr, o_stride = at.matrix(out, "out", rows, width, table.dtype if out is None else out.dtype)
     o_typ = _ELEMENT[out.dtype]
     _check(_lib.fs_embed(vocab, width, t_ptr, typ, t_stride, rows, cols, i_ptr, i_typ, base, scale, o_ptr, o_typ, o_stride, at.ptr))
@@ -754,7 +761,8 @@ def fs_embed_backward(d_out: torch.Tensor, ids: torch.Tensor, n_vocab: int, scal
     """The table's gradient [n_vocab, width]: fp32 unless `d_table` (of that type or d_out's) is given; `accumulate` adds to
     what `d_table` holds."""
     at = _Place(d_out, stream)
-    _int32(n_vocab, "n_vocab")
+    if n_vocab > _INT32_MAX:
+        raise FsError(FS_EINVAL, f"n_vocab {n_vocab} does not fit 32 bits")
     rows, cols, i_ptr, i_typ, base = _id_array(ids, col_base, at.index)
     ptr, typ, stride = _matrix(d_out, "d_out", rows=rows, on=at.index)
     width = d_out.shape[1]
