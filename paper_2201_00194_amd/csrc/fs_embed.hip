@@ -401,7 +401,7 @@ embed_sort_few_kernel(IdDigit<ID, P> source, int32_t n, int32_t bits)
     }
     for (int s = threadIdx.x; s < n; s += kSlotFewWaves * 64) {
         const int i = order[s];
-        source.to[s] = make_pair<P>(source.packing, token[i], source.ids.row_of((uint32_t)i));       // one band
+        source.to[s] = make_pair<P>(source.packing, token[i], source.ids.row_of((uint32_t)i));       // the token in its band, as it came
     }
 }
 
