@@ -345,10 +345,12 @@ constexpr int kClearBlocks = 2047;
 // All digits of up to PER * 1024 entries in one workgroup.  LDS holds the tokens where the entries are and the entries' numbers
 // in the order so far, which a pass takes to registers and puts back.  The launch's other workgroups clear the table meanwhile.
 constexpr int kFewDigitBits = 9;
-// 8192 entries 21 us, 16384 37, and 29 by the six kernels of a long list; but where clearing takes longer than that (268 MB: 50 us),
-// it is better beside one kernel of 51 than in four parts beside the others (57 with the scans).
+// 8192 entries 21 us, 16384 37, and 29 by the six kernels of a long list; but where there is much to clear, it is better cleared beside
+// one kernel than in four parts beside the others.  Whole gradients of 1024 bf16, one kernel and six, us: 9000 ids and 16 MB of
+// table 35 and 38, 64 MB 41 and 51, 130 MB 42 and 65, 400 MB 92 and 101; 16384 ids and 16 MB 44 and 39, 64 MB 51 and 54, 130 MB 54
+// and 68, 400 MB 93 and 105.
 constexpr int kEmbedFew = 8192;
-constexpr int64_t kClearLong = 160 << 20;
+constexpr int64_t kClearLong = 64000000;
 static bool sort_in_one(int64_t n, int64_t clear_bytes) { return n <= kEmbedFew || (n <= 2 * kEmbedFew && clear_bytes >= kClearLong); }
 template <int ID, class P, int PER>
 __global__ void __launch_bounds__(kSlotFewWaves * 64)

@@ -180,7 +180,9 @@ slot_scan_kernel(int32_t *count, SlotShape s)
         count[(int64_t)s.buckets * s.groups + blockIdx.x] = total;
 }
 
-// Where all counts are few, every workgroup that places entries sums them itself: a kernel less.
+// Where all counts are few, every workgroup that places entries sums them itself: a kernel less.  131 072 choices of 30 experts (7936
+// counts) 11.4 us so, 14.4 with the scan; past the border it depends on how many numbers there are: 80 000 choices of 64 (10 205 counts)
+// 12.8 and 14.2, 20 000 of 255 (10 240) 16.3 and 13.9.
 constexpr int kSlotFewCounts = 8192;
 __host__ __device__ inline bool slots_scan_alone(const SlotShape &s) { return s.buckets * s.groups <= kSlotFewCounts; }
 // Every number's total, and its count in the workgroups before this one; a barrier at the end.

@@ -114,7 +114,10 @@ def whole_numbers(api, ids, g, vocab, accumulate=False, out_typ="fp32"):
     (8192, 1, 300000, 5),          # one workgroup sorts three digits
     (8192, 1, 600000, 9),          # and pairs of 64 bits
     (300, 27, 1 << 21, 3),
-    (16384, 1, 700000, 64),        # 160 MB and more cleared beside it
+    (16384, 1, 700000, 64),        # 179 MB cleared beside it
+    (9000, 1, 15624, 1024),        # just under and
+    (9000, 1, 15625, 1024),        # as much as one workgroup's sort is worth it for
+    (12001, 1, 250001, 64),
     (20000, 1, 1200000, 6),        # three passes over a long list
     (20000, 2, 1 << 20, 7),
     (70000, 3, 3000000, 2)])
