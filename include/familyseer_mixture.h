@@ -26,6 +26,9 @@
  * handed in; a row's elements are adjacent.  Pointers are aligned to the size of an element, workspaces to 256 bytes.
  * Outputs must not overlap inputs, workspaces or each other.
  *
+ * fs_profile_begin counts these calls among the kernel classes of familyseer.h: routing as FS_KERNEL_TOPK, the exchange and
+ * lookups as FS_KERNEL_PACK, gradients as FS_KERNEL_TRAIN_OTHER.
+ *
  * Sums, softmax statistics and gradients are held in fp32 or wider and rounded once (to nearest, ties to
  * even) where the output has fewer bits.
  */
@@ -44,7 +47,7 @@ enum { FS_F32 = 0, FS_BF16 = 1, FS_F16 = 2 };
 enum {
     FS_ID_I32 = 0,
     FS_ID_I64 = 1,
-    FS_ID_U16 = 2   /* leaf_idx of fs_score_families */
+    FS_ID_U16 = 2   /* leaf_idx of fs_score_families; 0 to 65535, so that a -1 of 16 bits is 65535 */
 };
 /* Scores of an expert, from its logit. */
 enum {
@@ -74,8 +77,8 @@ typedef struct fs_route_params {
 /*
  * For every token the k eligible experts with the largest keys, by (key descending, expert ascending), and
  * their weights.  An expert's key is its logit, or, with a bias, score + bias: the bias balances how often
- * experts are chosen and does not enter the weights.  Keys are compared as in 64-bit arithmetic.  Not
- * eligible (masked) are experts whose logit is -infinity or NaN, or whose key is; a logit of +infinity
+ * experts are chosen and does not enter the weights.  Keys and groups' sums are compared as in 64-bit
+ * arithmetic.  Not eligible (masked) are experts whose logit is -infinity or NaN, or whose key is; a logit of +infinity
  * counts as the largest float.  Masked experts have the score 0.  Groups rank by (sum descending, group ascending);
  * a group without an eligible expert is never taken.
  * Where fewer than k experts are to be had, the remaining entries are expert -1 with the weight 0.
@@ -134,9 +137,9 @@ int fs_expert_combine_backward(int64_t n_tokens, int32_t k, int32_t n_experts, i
 
 /*
  * out[r] = scale * sum over c of table[col_base[c] + ids[r*n_cols + c]], c < n_cols, in an order that depends on the
- * sizes alone.  One column is the plain lookup; without col_base its entries count as 0.  Leaves of an ensemble: FS_ID_U16 ids with
- * col_base = the tree_off of fs_model_create, n_cols = n_trees.  Ids whose row is outside
- * [0, n_vocab) add nothing (use -1 for padding).  out_type is the table's type or FS_F32.
+ * sizes alone: at most 256 terms after each other in fp32, such sums in 64 bits.  One column is the plain lookup; without col_base its entries count as 0.  Leaves of an ensemble: FS_ID_U16 ids with
+ * col_base = the tree_off of fs_model_create, n_cols = n_trees.  Ids whose row, col_base + id, is outside
+ * [0, n_vocab) add nothing (for padding: -1 without col_base, or any id past the table; 16-bit ids have no -1).  out_type is the table's type or FS_F32.
  * n_rows*n_cols < 2^31.
  */
 int fs_embed(int32_t n_vocab, int32_t width, const void *table /* DEVICE */, int32_t table_type, int64_t table_stride,

@@ -481,6 +481,10 @@ def unpack_colblock64(x: torch.Tensor, n_rows: int, n_features: int) -> np.ndarr
 
 
 # ---- mixtures of family models (familyseer_mixture.h) ---------------------------------------------
+#
+# The calls take no part in autograd: results have no graph, also of inputs that require a gradient.  Every operator has its
+# gradient as a call of its own (fs_..._backward; fs_expert_combine without weights is fs_expert_gather's), to be made by the
+# program, as FamilyMixture.gradients does, or from a torch.autograd.Function.  They run on the current GPU.
 
 FS_F32, FS_BF16, FS_F16 = 0, 1, 2
 FS_ID_I32, FS_ID_I64, FS_ID_U16 = 0, 1, 2

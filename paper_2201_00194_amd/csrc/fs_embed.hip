@@ -451,9 +451,9 @@ __device__ __forceinline__ void put_row(const SumArgs &a, int token, int c, int 
 // them, two sums a chunk at most, meets in LDS, where the lanes of a run's first sum add them up, in 64 bits (blocks of sixteen
 // are rounded between); what the workgroup has of runs that go on beyond it goes to memory.
 //
-// 32 768 rows of 256 bytes, each named by 100 tokens: 55 us, 839 MB of rows at 15 TB/s, nearly all from the L2 caches, with 14 vector
-// instructions beside every four rows (vector units 53 % busy); the sort in front of it 70 us, of which the chains of 3.3 M
-// entries' ballots and LDS steps are 45 (51 and 57 % busy while placing).
+// 32 768 rows of 256 bytes, each named by 100 tokens: 52 us, 839 MB of rows at 16 TB/s, nearly all from the L2 caches, with 14 vector
+// instructions beside every four rows (vector units 52 % busy); the sort in front of it 67 us, of which the chains of 3.3 M
+// entries' ballots and LDS steps are 42 (51 and 57 % busy while placing).
 template <int IN, int OUT, class P, bool NEAR>
 __global__ void __launch_bounds__(kSumWaves * 64)
 embed_sum_kernel(SumArgs a)

@@ -8,11 +8,16 @@
 // KP maxima (the one against the other turned round) and a bitonic merge, in the lane first, between lanes then.
 //
 // Keys with a bias (score + bias) and the sums of groups have to compare as in 64 bits.  They are computed in 32, with a bound
-// on their error; a row where two keys or sums that matter are nearer than the bounds say, and not equal by their inputs, is
-// taken again by the whole wavefront in 64 bits.
+// on their error; a row where two keys that matter are nearer than the bounds say, and not equal by their inputs, or where a
+// group at the cut may have as much as one beyond it, is taken again by the whole wavefront in 64 bits.  What that costs depends
+// on the values.  Equal sums are taken again too: without a bias and with group_best 1, equal bf16 logits make them (262 144 rows
+// of 64 experts in 8 groups 83 us, with group_best 2 41).  And a softmax score's bound does not shrink with the score, so that small
+// scores next to each other are in doubt where the bias says nothing: a bias of zeros, 64 experts, k = 8, logits of standard
+// deviation 1.5 42 us, 5 114, 8 279 (without the bias 19).
 //
-// What bounds it is issue: 2 000 000 rows of 64 bf16 experts in 8 groups with a bias, k = 8, take 223 us (1.7 TB/s) at 1038 vector
-// instructions a wavefront of 16 rows, with the vector units busy all the time.  Without bias and groups, 262 144 rows of 30 fp32 experts, k = 4: 13 us (3.1 TB/s).
+// What bounds it: 2 000 000 rows of 64 bf16 experts in 8 groups with a bias, k = 8, take 219 us (1.7 TB/s) at 1022 vector
+// instructions a wavefront of 16 rows, with the vector units busy all the time.  Without bias and groups, 262 144 rows of 30 fp32
+// experts, k = 4: 12 to 13 us (3.1 TB/s), the vector units half busy: loads, then one chain through the lists.
 #include "fs_mixture.h"
 
 #include <math.h>
@@ -684,8 +689,8 @@ route_kernel(RouteArgs a)
 // ---- the gradient ---------------------------------------------------------------------------------------------------------
 
 // The choices' gradients go to the row's logits through LDS; a row's experts lie in its lanes as above, its choices j in lane
-// j mod (1 << LL).  262 144 rows of 30 fp32 experts, a dense gradient: 21 us (3.4 TB/s), the chain of loads, LDS and moves between
-// lanes (vector units 41 % busy).
+// j mod (1 << LL).  262 144 rows of 30 fp32 experts, a dense gradient: 20 us (3.6 TB/s), the chain of loads, LDS and moves between
+// lanes (vector units 38 % busy).
 template <int TYPE, int LL>
 __global__ void __launch_bounds__(kRouteWaves * 64)
 route_backward_kernel(RouteArgs a)
