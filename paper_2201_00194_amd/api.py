@@ -578,7 +578,7 @@ _gpus = 0        # how many there are, once a call has asked
 def _refuse_other_gpus(index: int, stream: Optional[torch.cuda.Stream]) -> None:
     """The library launches on the current GPU, and a default stream's handle names that one's, whichever GPU it was asked of."""
     global _gpus
-    _gpus = torch.cuda.device_count()
+    _gpus = _gpus or torch.cuda.device_count()
     if _gpus > 1:
         if torch.cuda.current_device() != index:
             raise FsError(FS_EINVAL, f"the tensors are on GPU {index}, which is not the current one")
