@@ -662,6 +662,10 @@ class ExpertPlan:
         self.n_experts = first.shape[0] - 1
         self.n_tokens, self.k = place.shape
 
+    def _bounds(self, at: _Place):
+        """The pointer of first."""
+        return _array(self.first, "first", self.n_experts + 1, torch.int32, at.index)
+
     def _lists(self, at: _Place):
         """The pointers of first and place."""
         return (_array(self.first, "first", self.n_experts + 1, torch.int32, at.index),
@@ -780,3 +784,203 @@ def fs_embed_backward(d_out: torch.Tensor, ids: torch.Tensor, n_vocab: int, scal
     _check(_lib.fs_embed_backward(n_vocab, width, ptr, typ, stride, rows, cols, i_ptr, i_typ, base, scale, int(accumulate), t_ptr,
                                   t_typ, t_stride, _ptr(work), need, at.ptr))
     return d_table
+
+
+# ---- networks as experts (familyseer_experts.h) ----------------------------------------------------
+#
+# As above: no autograd.  fs_expert_matmul with the other `turned` is the rows' gradient, fs_expert_matmul_backward the weights'.
+
+FS_MAX_I8_WIDTH = 131072
+FS_MAX_CLASSES = 1048576
+FS_MAX_LISTED = 1024
+
+
+class _FsDistillParams(ctypes.Structure):
+    _fields_ = [("n_classes", ctypes.c_int32), ("k", ctypes.c_int32), ("temperature", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+for _name, _result, _args in (
+        ("fs_expert_matmul", ctypes.c_int, [_i64, _i32, _i32, _i32, _vp, _i32, _i64, _vp, _vp, _i64, _i64, _i32, _vp, _i32, _i64, _vp]),
+        ("fs_expert_matmul_backward_workspace_bytes", _sz, [_i64, _i32, _i32, _i32, _i32]),
+        ("fs_expert_matmul_backward", ctypes.c_int,
+         [_i64, _i32, _i32, _i32, _vp, _i32, _i64, _vp, _i64, _vp, _i32, _vp, _i32, _i64, _i64, _vp, _sz, _vp]),
+        ("fs_quantize_rows", ctypes.c_int, [_i64, _i32, _vp, _i32, _i64, _vp, _i64, _vp, _vp]),
+        ("fs_expert_gather_i8", ctypes.c_int, [_i64, _i32, _i32, _i32, _vp, _i32, _i64, _vp, _vp, _vp, _i64, _vp, _vp]),
+        ("fs_expert_matmul_i8", ctypes.c_int, [_i64, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _i32, _i64, _vp]),
+        ("fs_distill_workspace_bytes", _sz, [ctypes.POINTER(_FsDistillParams), _i64, _i32]),
+        ("fs_distill", ctypes.c_int,
+         [ctypes.POINTER(_FsDistillParams), _i64, _vp, _i32, _i64, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+        ("fs_distill_backward", ctypes.c_int,
+         [ctypes.POINTER(_FsDistillParams), _i64, _vp, _i32, _i64, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp])):
+    getattr(_lib, _name).restype = _result
+    getattr(_lib, _name).argtypes = _args
+
+
+def _bytes_matrix(t: torch.Tensor, what: str, width: Optional[int] = None, rows: Optional[int] = None, on: Optional[int] = None):
+    """(pointer, row stride) of a matrix of 8-bit integers."""
+    if on is not None and t.get_device() != on:
+        raise FsError(FS_EINVAL, f"{what} is not on the call's GPU")
+    if t.dtype != torch.int8 or t.dim() != 2:
+        raise FsError(FS_EINVAL, f"{what} is not a matrix of int8")
+    n, w = t.shape
+    if (width is not None and w != width) or (rows is not None and n != rows):
+        raise FsError(FS_EINVAL, f"{what} is {(n, w)}, not {(rows, width)}")
+    if w > _INT32_MAX:
+        raise FsError(FS_EINVAL, f"{what}: a row of {w} elements")
+    step, between = t.stride()
+    if between != 1 and w > 1:
+        raise FsError(FS_EINVAL, f"{what}: the elements of a row are not adjacent")
+    return t.data_ptr(), (step if n > 1 else max(1, w))
+
+
+def _weights(w: torch.Tensor, what: str, n_experts: int, dtype, on: Optional[int] = None):
+    """(pointer, rows, columns, row stride, step from expert to expert) of weights [n_experts, rows, columns]."""
+    if on is not None and w.get_device() != on:
+        raise FsError(FS_EINVAL, f"{what} is not on the call's GPU")
+    if w.dim() != 3 or w.dtype not in (dtype if type(dtype) is tuple else (dtype,)):
+        raise FsError(FS_EINVAL, f"{what} is {w.dim()}-dimensional of {w.dtype}, not [experts, rows, columns] of {dtype}")
+    e, n, c = w.shape
+    if e != n_experts:
+        raise FsError(FS_EINVAL, f"{what} is of {e} experts, not {n_experts}")
+    if n > _INT32_MAX or c > _INT32_MAX:
+        raise FsError(FS_EINVAL, f"{what}: matrices of {n} x {c}")
+    between, step, adjacent = w.stride()
+    if adjacent != 1 and c > 1:
+        raise FsError(FS_EINVAL, f"{what}: the elements of a row are not adjacent")
+    step = step if n > 1 else max(1, c)
+    return w.data_ptr(), n, c, step, (between if e > 1 else n * step)
+
+
+def _slots_of(plan: ExpertPlan) -> int:
+    return plan.n_tokens * plan.k
+
+
+def fs_expert_matmul(x: torch.Tensor, plan: ExpertPlan, w: torch.Tensor, turned: bool = False, out: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Rows x [slots, in] of `plan`'s slots times their expert's weights w [experts, out, in], or `turned` [experts, in, out]: [slots, out],
+    of x's type unless `out` (of that type or fp32) is given.  With w turned, of a result's gradient, it is the rows' gradient."""
+    at = _Place(x, stream)
+    slots = _slots_of(plan)
+    ptr, typ, stride = _matrix(x, "x", rows=slots, on=at.index)
+    w_ptr, rows, cols, w_stride, w_step = _weights(w, "w", plan.n_experts, x.dtype, at.index)
+    width, out_width = (rows, cols) if turned else (cols, rows)
+    if x.shape[1] != width:
+        raise FsError(FS_EINVAL, f"x has {x.shape[1]} columns, w takes {width}")
+    out, o_ptr, o_stride = at.matrix(out, "out", slots, out_width, x.dtype if out is None else out.dtype)
+    _check(_lib.fs_expert_matmul(slots, plan.n_experts, width, out_width, ptr, typ, stride, plan._bounds(at), w_ptr, w_stride, w_step,
+                                 int(turned), o_ptr, _ELEMENT[out.dtype], o_stride, at.ptr))
+    return out
+
+
+def fs_expert_matmul_backward(d_y: torch.Tensor, x: torch.Tensor, plan: ExpertPlan, d_w: Optional[torch.Tensor] = None,
+                              accumulate: bool = False, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The gradient [experts, out, in] of weights through which x [slots, in] went to results whose gradient is d_y [slots, out] (of turned
+    weights: x and d_y change places); fp32 unless `d_w` (of that type or x's) is given; `accumulate` adds to what `d_w` holds."""
+    at = _Place(d_y, stream)
+    slots = _slots_of(plan)
+    g_ptr, typ, g_stride = _matrix(d_y, "d_y", rows=slots, on=at.index)
+    x_ptr, _, x_stride = _matrix(x, "x", rows=slots, dtype=d_y.dtype, on=at.index)
+    out_width, width = d_y.shape[1], x.shape[1]
+    if d_w is None:
+        if accumulate:
+            raise FsError(FS_EINVAL, "accumulate needs a d_w to add to")
+        d_w = at.empty((plan.n_experts * out_width, width), torch.float32).view(plan.n_experts, out_width, width)
+    d_ptr, rows, cols, d_stride, d_step = _weights(d_w, "d_w", plan.n_experts, (torch.float32, d_y.dtype), at.index)
+    if (rows, cols) != (out_width, width):
+        raise FsError(FS_EINVAL, f"d_w is of {(rows, cols)} an expert, not {(out_width, width)}")
+    need = _lib.fs_expert_matmul_backward_workspace_bytes(slots, plan.n_experts, width, out_width, typ)
+    work = at.empty((need,), torch.uint8) if need else None
+    _check(_lib.fs_expert_matmul_backward(slots, plan.n_experts, width, out_width, g_ptr, typ, g_stride, x_ptr, x_stride, plan._bounds(at),
+                                          int(accumulate), d_ptr, _ELEMENT[d_w.dtype], d_stride, d_step, _ptr(work), need, at.ptr))
+    return d_w
+
+
+def fs_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None):
+    """(q, scale): rows x [rows, width] as 8-bit integers, and what each row's are multiplied by, fp32 [rows]."""
+    at = _Place(x, stream)
+    ptr, typ, stride = _matrix(x, "x", on=at.index)
+    n, width = x.shape
+    q = at.empty((n, width), torch.int8) if q is None else q
+    q_ptr, q_stride = _bytes_matrix(q, "q", width, n, at.index)
+    scale, s_ptr = at.array(scale, "scale", (n,), torch.float32)
+    _check(_lib.fs_quantize_rows(n, width, ptr, typ, stride, q_ptr, q_stride, s_ptr, at.ptr))
+    return q, scale
+
+
+def fs_expert_gather_i8(x: torch.Tensor, plan: ExpertPlan, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None):
+    """(q [tokens*k, width], scale [tokens*k]): rows x [tokens, width] as fs_quantize_rows makes them, in the experts' slots."""
+    at = _Place(x, stream)
+    ptr, typ, stride = _matrix(x, "x", rows=plan.n_tokens, on=at.index)
+    slots, width = _slots_of(plan), x.shape[1]
+    q = at.empty((slots, width), torch.int8) if q is None else q
+    q_ptr, q_stride = _bytes_matrix(q, "q", width, slots, at.index)
+    scale, s_ptr = at.array(scale, "scale", (slots,), torch.float32)
+    _check(_lib.fs_expert_gather_i8(plan.n_tokens, plan.k, plan.n_experts, width, ptr, typ, stride, *plan._lists(at), q_ptr, q_stride, s_ptr, at.ptr))
+    return q, scale
+
+
+def fs_expert_matmul_i8(q: torch.Tensor, scale: torch.Tensor, plan: ExpertPlan, w: torch.Tensor, w_scale: torch.Tensor,
+                        dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Rows q [slots, in] of int8 times their expert's weights w [experts, out, in] of int8, times both scales, scale [slots] and
+    w_scale [experts, out]: [slots, out] of `dtype`, or into `out`."""
+    at = _Place(q, stream)
+    slots = _slots_of(plan)
+    ptr, stride = _bytes_matrix(q, "q", rows=slots, on=at.index)
+    w_ptr, out_width, width, w_stride, w_step = _weights(w, "w", plan.n_experts, torch.int8, at.index)
+    if q.shape[1] != width:
+        raise FsError(FS_EINVAL, f"q has {q.shape[1]} columns, w takes {width}")
+    if out is None and dtype not in _ELEMENT:
+        raise FsError(FS_EINVAL, f"results of {dtype}")
+    out, o_ptr, o_stride = at.matrix(out, "out", slots, out_width, dtype if out is None else out.dtype)
+    _check(_lib.fs_expert_matmul_i8(slots, plan.n_experts, width, out_width, ptr, stride, _array(scale, "scale", slots, torch.float32, at.index),
+                                    plan._bounds(at), w_ptr, w_stride, w_step,
+                                    _array(w_scale, "w_scale", (plan.n_experts, out_width), torch.float32, at.index), o_ptr, _ELEMENT[out.dtype],
+                                    o_stride, at.ptr))
+    return out
+
+
+def distill_params(n_classes: int, k: int, temperature: float = 1.0, scale: float = 1.0) -> _FsDistillParams:
+    return _FsDistillParams(_int32(n_classes, "n_classes"), _int32(k, "k"), temperature, scale)
+
+
+def _distill(params: _FsDistillParams, at: _Place, logits, ids, teacher, total):
+    """The arguments that both distillation calls begin with, and working memory."""
+    ptr, typ, stride = _matrix(logits, "logits", params.n_classes, on=at.index)
+    n = logits.shape[0]
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise FsError(FS_EINVAL, f"ids is {ids.dtype}, neither int32 nor int64")
+    if teacher.dtype not in _ELEMENT:
+        raise FsError(FS_EINVAL, f"teacher is {teacher.dtype}, not fp32, bf16 or fp16")
+    need = _lib.fs_distill_workspace_bytes(params, n, typ)
+    work = at.empty((need,), torch.uint8) if need else None
+    return n, work, need, (params, n, ptr, typ, stride, _array(ids, "ids", (n, params.k), ids.dtype, at.index), _ID[ids.dtype],
+                           _array(teacher, "teacher", (n, params.k), teacher.dtype, at.index), _ELEMENT[teacher.dtype],
+                           _array(total, "total", (n,), torch.float32, at.index))
+
+
+def fs_distill(params: _FsDistillParams, logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, total: Optional[torch.Tensor] = None,
+               loss: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Losses [tokens] of student's logits [tokens, n_classes] against the classes `ids` [tokens, k] and logits `teacher` [tokens, k] that a teacher
+    gave; with `total` [tokens], the log of the sum of exp(logit / temperature) over all of its classes, the rest counts as a class."""
+    at = _Place(logits, stream)
+    n, work, need, args = _distill(params, at, logits, ids, teacher, total)
+    loss, l_ptr = at.array(loss, "loss", (n,), torch.float32)
+    _check(_lib.fs_distill(*args, l_ptr, _ptr(work), need, at.ptr))
+    return loss
+
+
+def fs_distill_backward(params: _FsDistillParams, logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, d_loss: torch.Tensor,
+                        total: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None, d_logits: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The logits' gradient of losses whose gradient is d_loss [tokens]; `loss` [tokens], if given, receives the losses too."""
+    at = _Place(logits, stream)
+    n, work, need, args = _distill(params, at, logits, ids, teacher, total)
+    d_logits, d_ptr, d_stride = at.matrix(d_logits, "d_logits", n, params.n_classes, logits.dtype)
+    if d_logits.dtype != logits.dtype:
+        raise FsError(FS_EINVAL, f"d_logits is {d_logits.dtype}, not {logits.dtype}")
+    _check(_lib.fs_distill_backward(*args, _array(d_loss, "d_loss", (n,), torch.float32, at.index), _array(loss, "loss", (n,), torch.float32, at.index),
+                                    d_ptr, d_stride, _ptr(work), need, at.ptr))
+    return d_logits

@@ -243,13 +243,6 @@ void over_tokens(ExchangeArgs &a, int32_t type, bool whole_rows, int tokens, F f
     });
 }
 
-static int check_experts(const char *who, int32_t n_experts)
-{
-    if (n_experts < 1 || n_experts > FS_MAX_EXPERTS)
-        return fail(n_experts < 1 ? FS_EINVAL : FS_EUNSUPPORTED, "%s: n_experts %d outside [1, %d]", who, n_experts, FS_MAX_EXPERTS);
-    return FS_OK;
-}
-
 }  // namespace fs
 
 using namespace fs;

@@ -45,6 +45,15 @@ inline int check_matrix(const char *who, const char *what, const void *p, int64_
         return fail(FS_EINVAL, "%s: %s is not aligned to its elements", who, what);
     return FS_OK;
 }
+// A matrix of 8-bit integers.
+inline int check_bytes(const char *who, const char *what, const void *p, int64_t rows, int64_t width, int64_t stride)
+{
+    if (stride < width || stride > ((int64_t)1 << 40))
+        return fail(FS_EINVAL, "%s: row stride %lld of %s, whose width is %lld: 2^40 at most", who, (long long)stride, what, (long long)width);
+    if (rows > 0 && !p)
+        return fail(FS_EINVAL, "%s: %s is NULL", who, what);
+    return FS_OK;
+}
 inline int check_width(const char *who, int32_t width)
 {
     if (width < 1 || width > FS_MAX_WIDTH)
@@ -65,6 +74,12 @@ inline int check_tokens(const char *who, int64_t n_tokens, int32_t k)
         return fail(FS_EINVAL, "%s: k %d outside [1, %d]", who, k, FS_MAX_CHOICES);
     if (n_tokens < 0 || n_tokens * k >= ((int64_t)1 << 31) || n_tokens >= ((int64_t)1 << 31))
         return fail(FS_EINVAL, "%s: %lld tokens with %d choices: 0 to 2^31 - 1 choices are taken", who, (long long)n_tokens, k);
+    return FS_OK;
+}
+inline int check_experts(const char *who, int32_t n_experts)
+{
+    if (n_experts < 1 || n_experts > FS_MAX_EXPERTS)
+        return fail(n_experts < 1 ? FS_EINVAL : FS_EUNSUPPORTED, "%s: n_experts %d outside [1, %d]", who, n_experts, FS_MAX_EXPERTS);
     return FS_OK;
 }
 inline int launched(const char *what)

@@ -1,0 +1,367 @@
+// Tiles of matrix products on the matrix units: operands through LDS, sums in registers.
+#ifndef FS_PRODUCT_H
+#define FS_PRODUCT_H
+
+#include "fs_mixture.h"
+#include "familyseer_experts.h"
+
+namespace fs {
+
+constexpr int kI8 = 3;      // beside FS_F32, FS_BF16 and FS_F16: an operand's type, not a result's
+
+typedef float F4 __attribute__((ext_vector_type(4)));
+typedef int I4 __attribute__((ext_vector_type(4)));
+typedef short S4 __attribute__((ext_vector_type(4)));
+typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+typedef _Float16 H8 __attribute__((ext_vector_type(8)));
+
+// What a type's tiles are made of.  A fragment is 16 bytes a lane: lane l holds, of row l % 16 of sixteen, the l / 16th 16 bytes of
+// 64 along the sum.  One step of the matrix units takes 64 bytes of the sum of 16 rows and 16 columns; for fp32 that is four
+// instructions, the i-th of which takes the i-th float of every lane.
+template <int TYPE> struct Unit16;
+template <> struct Unit16<FS_BF16> {
+    typedef F4 Acc;
+    static constexpr int size = 2;
+    static __device__ __forceinline__ Acc step(I4 a, I4 b, Acc c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), __builtin_bit_cast(B8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Unit16<FS_F16> {
+    typedef F4 Acc;
+    static constexpr int size = 2;
+    static __device__ __forceinline__ Acc step(I4 a, I4 b, Acc c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(H8, a), __builtin_bit_cast(H8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Unit16<FS_F32> {
+    typedef F4 Acc;
+    static constexpr int size = 4;
+};
+template <> struct Unit16<kI8> {
+    typedef I4 Acc;
+    static constexpr int size = 1;
+    static __device__ __forceinline__ Acc step(I4 a, I4 b, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+};
+
+// An operand of a tile.  `along` false: rows of elements along the sum (p at the tile's first row); true: rows of elements across
+// it, one row for each term of the sum (p at the tile's first column).
+struct Operand {
+    const char *p;
+    int64_t stride;      // bytes from row to row
+    int count;           // rows, or columns, of the tile that are there
+};
+
+constexpr int kStepBytes = 128;      // of the sum, of 1, 2 or 4 bytes an element, that a tile takes at a time
+
+// Where 16 bytes of an operand lie in LDS.  Lanes read a fragment's rows 0 1 2 3, 16 17 18 19, ... of 64 (fragment 0; the
+// next fragment 4 to 7 and so on), so that a lane's results lie side by side; the xor spreads them over the banks.
+template <int TYPE, bool ALONG, int ROWS>
+struct Place {
+    static constexpr int size = Unit16<TYPE>::size;
+    static constexpr int chunks = ROWS * kStepBytes / 16;
+    static constexpr int per_row = ALONG ? ROWS * size / 16 : kStepBytes / 16;     // 16-byte chunks
+    // Along, 16 bits: a transposing read takes eight bytes of four neighbouring rows, in four places 32 bytes apart.
+    static __device__ __forceinline__ int turn(int row)
+    {
+        if constexpr (!ALONG)
+            return (row & 3) | ((row >> 4 & 1) << 2);
+        else if constexpr (size == 2)
+            return (row & 1) | ((row >> 1 & 1) << (per_row >= 16 ? 3 : 0));
+        else
+            return 0;
+    }
+    static __device__ __forceinline__ int at(int row, int chunk) { return (row * per_row + (chunk ^ turn(row))) * 16; }
+};
+
+// 16 bytes of which n elements are there.
+template <int ALIGNED, class E = int> struct Bytes16 {
+    typedef E type __attribute__((ext_vector_type(4), aligned(ALIGNED)));
+};
+template <int SIZE>
+__device__ __forceinline__ I4 some_bytes(const char *p, int n)
+{
+    constexpr int N = 16 / SIZE;
+    I4 v = {0, 0, 0, 0};
+    if (n >= N) {
+        v = *(const typename Bytes16<SIZE>::type *)p;
+    } else if (n > 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = i < n ? i : n - 1;
+            unsigned e;
+            if constexpr (SIZE == 1)
+                e = ((const uint8_t *)p)[at];
+            else if constexpr (SIZE == 2)
+                e = ((const uint16_t *)p)[at];
+            else
+                e = ((const uint32_t *)p)[at];
+            e = i < n ? e : 0;
+            v[i * SIZE / 4] |= (int)(e << (i * SIZE % 4 * 8));
+        }
+    }
+    return v;
+}
+
+// A tile of BM x BN results by WM x WN wavefronts, each (BM / WM) x (BN / WN) of them, multiples of 64.
+template <int TYPE, int BM, int BN, int WM, int WN, bool AT, bool BT>
+struct Tile {
+    typedef Unit16<TYPE> U;
+    typedef typename U::Acc Acc;
+    static constexpr int threads = WM * WN * 64;
+    static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;      // fragments of a wavefront
+    static constexpr int a_bytes = BM * kStepBytes, b_bytes = BN * kStepBytes, stage_bytes = a_bytes + b_bytes;
+    static constexpr int lds_bytes = 2 * stage_bytes;
+    static constexpr int step = kStepBytes / U::size;               // elements of the sum
+    Acc acc[MF][NF];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+                acc[i][j] = Acc{0, 0, 0, 0};
+    }
+
+    // ---- operands through registers: any alignment, any sizes ----
+    template <bool ALONG, int ROWS>
+    struct Fetched {
+        typedef Place<TYPE, ALONG, ROWS> P;
+        static constexpr int N = P::chunks / threads;
+        I4 v[N];
+        __device__ __forceinline__ void load(const Operand &o, int k0, int k_count)
+        {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int q = threadIdx.x + i * threads, row = q / P::per_row, first = q % P::per_row * (16 / U::size);
+                if constexpr (ALONG)
+                    v[i] = some_bytes<U::size>(o.p + (k0 + row) * o.stride + first * U::size, k0 + row < k_count ? o.count - first : 0);
+                else
+                    v[i] = some_bytes<U::size>(o.p + row * o.stride + (int64_t)(k0 + first) * U::size, row < o.count ? k_count - k0 - first : 0);
+            }
+        }
+        __device__ __forceinline__ void store(char *lds) const
+        {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int q = threadIdx.x + i * threads;
+                *(I4 *)(lds + P::at(q / P::per_row, q % P::per_row)) = v[i];
+            }
+        }
+    };
+
+    // ---- fragments ----
+    // `base`: the wavefront's first row or column.  Fragment f is of block f / 4 of 64 rows; fp32 along: v[4 * block + i][f % 4]
+    // are the i-th terms of its lanes instead of v[f][i].
+    template <bool ALONG, int ROWS, int F>
+    static __device__ __forceinline__ void fragments(I4 (&v)[F], const char *lds, int base, int kk)
+    {
+        typedef Place<TYPE, ALONG, ROWS> P;
+        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+            if constexpr (!ALONG) {
+                const int row = base + (f >> 2) * 64 + (r >> 2) * 16 + (f & 3) * 4 + (r & 3);
+                v[f] = *(const I4 *)(lds + P::at(row, kk * 4 + g));
+            } else if constexpr (U::size == 4) {
+                v[f] = *(const I4 *)(lds + P::at(kk * 16 + g * 4 + (f & 3), (base + (f >> 2) * 64) / 4 + r));
+            } else {
+                const int chunk = (base + (f >> 2) * 64) / 8 + (r & 3) * 2 + (f >> 1 & 1), k = kk * 32 + g * 8 + (r >> 2);
+                typedef __attribute__((address_space(3))) S4 *Read;
+                const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k, chunk) + (f & 1) * 8));
+                const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k + 4, chunk) + (f & 1) * 8));
+                typedef short S8 __attribute__((ext_vector_type(8)));
+                v[f] = __builtin_bit_cast(I4, S8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+            }
+        }
+    }
+
+    __device__ __forceinline__ void multiply(const char *lds)
+    {
+        const int wave = threadIdx.x >> 6, m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
+#pragma unroll
+        for (int kk = 0; kk < kStepBytes / 64; ++kk) {
+            I4 a[MF], b[NF];
+            fragments<AT, BM, MF>(a, lds, m0, kk);
+            fragments<BT, BN, NF>(b, lds + a_bytes, n0, kk);
+            if constexpr (TYPE == FS_F32) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < MF; ++i)
+#pragma unroll
+                        for (int j = 0; j < NF; ++j) {
+                            const int x = AT ? a[(i & ~3) + t][i & 3] : a[i][t], y = BT ? b[(j & ~3) + t][j & 3] : b[j][t];
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(y), __int_as_float(x), acc[i][j], 0, 0, 0);
+                        }
+            } else {
+#pragma unroll
+                for (int i = 0; i < MF; ++i)
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+                        acc[i][j] = U::step(b[j], a[i], acc[i][j]);
+            }
+        }
+    }
+
+    // The sums over k_count terms.
+    __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int k_count)
+    {
+        Fetched<AT, BM> fa;
+        Fetched<BT, BN> fb;
+        fa.load(a, 0, k_count);
+        fb.load(b, 0, k_count);
+        for (int k0 = 0, half = 0; k0 < k_count; k0 += step, half ^= 1) {
+            char *const now = lds + half * stage_bytes;
+            fa.store(now);
+            fb.store(now + a_bytes);
+            if (k0 + step < k_count) {
+                fa.load(a, k0 + step, k_count);
+                fb.load(b, k0 + step, k_count);
+            }
+            __syncthreads();      // the other half was read before the last one of these
+            multiply(now);
+        }
+    }
+
+    // f(row, first column, sixteen results side by side) for each of a lane's runs of results.
+    template <class F>
+    __device__ __forceinline__ void results(F f) const
+    {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+        const int m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
+        constexpr bool a4 = AT && TYPE == FS_F32, b4 = BT && TYPE == FS_F32;
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int row = m0 + (i >> 2) * 64 + (a4 ? 4 * r + (i & 3) : (r >> 2) * 16 + (i & 3) * 4 + (r & 3));
+#pragma unroll
+            for (int block = 0; block < NF / 4; ++block) {
+                decltype(Acc{}[0] + 0) v[16];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[b4 ? 4 * e + j : 4 * j + e] = acc[i][block * 4 + j][e];
+                f(row, n0 + block * 64 + g * 16, v);
+            }
+        }
+    }
+};
+
+// Sixteen results of which n are wanted.
+template <class T>
+__device__ __forceinline__ void store_results(T *p, int n, const float (&v)[16])
+{
+    constexpr int N = kChunk<T>;
+#pragma unroll
+    for (int c = 0; c < 16; c += N) {
+        float part[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            part[i] = v[c + i];
+        store_chunk<N>(p + c, n - c, part);
+    }
+}
+// `type`: of the matrix's type or FS_F32.
+template <int TYPE>
+__device__ __forceinline__ void store_results(void *p, int64_t at, int type, int n, const float (&v)[16])
+{
+    if (TYPE != FS_F32 && type == FS_F32)
+        store_results((float *)p + at, n, v);
+    else
+        store_results((typename Element<TYPE>::type *)p + at, n, v);
+}
+template <int TYPE>
+__device__ __forceinline__ void add_to_results(const void *p, int64_t at, int type, int n, float (&v)[16])
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (i < n)
+            v[i] += TYPE != FS_F32 && type == FS_F32 ? ((const float *)p)[at + i] : (float)((const typename Element<TYPE>::type *)p)[at + i];
+}
+
+// ---- whose rows a workgroup works on ---------------------------------------------------------------
+// Experts' slots are cut into pieces of `per`; a piece is of one expert.
+struct Piece {
+    int expert, first, count;      // its slots
+    int number, of;                // which of its expert's pieces, and of how many
+    int before;                    // pieces of earlier experts that have more than one
+    int64_t pieces;                // of all experts
+};
+struct Bounds {
+    const int32_t *first;
+    int n_experts, n_slots, per;
+    // Nobody's slots are the pieces of one expert more (`nobody`); `each`: an expert without slots has an empty piece.
+    template <bool NOBODY, bool EACH>
+    __device__ __forceinline__ int pieces(int e, int &begin, int &end) const
+    {
+        const int last = NOBODY ? n_experts : n_experts - 1;
+        if (e > last)
+            return 0;
+        begin = min(max(first[e], 0), n_slots);
+        end = e == n_experts ? n_slots : max(min(first[e + 1], n_slots), begin);
+        const int n = (int)(((int64_t)end - begin + per - 1) / per);
+        return EACH ? max(n, 1) : n;
+    }
+    // Every lane's sum of the lanes up to it.
+    static __device__ __forceinline__ int sum_to(int v)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(v, d);
+            v += lane >= d ? other : 0;
+        }
+        return v;
+    }
+    template <bool NOBODY, bool EACH>
+    __device__ __forceinline__ int64_t count() const
+    {
+        int64_t all = 0;
+        for (int e0 = 0; e0 <= n_experts; e0 += 64) {
+            int begin, end;
+            all += __builtin_amdgcn_readlane(sum_to(pieces<NOBODY, EACH>(e0 + (threadIdx.x & 63), begin, end)), 63);
+        }
+        return all;
+    }
+    // The piece `id` of all; its `count` is -1 where there is none.
+    template <bool NOBODY, bool EACH>
+    __device__ __forceinline__ Piece find(int64_t id) const
+    {
+        Piece p = {0, 0, -1, 0, 0, 0, 0};
+        const int lane = threadIdx.x & 63;
+        int64_t at = 0;
+        int before = 0;
+        for (int e0 = 0; e0 <= n_experts; e0 += 64) {
+            int begin = 0, end = 0;
+            const int n = pieces<NOBODY, EACH>(e0 + lane, begin, end), upto = sum_to(n), all = __builtin_amdgcn_readlane(upto, 63);
+            const int many = n > 1 ? n : 0, many_upto = EACH ? sum_to(many) : 0;
+            if (id < at + all) {
+                const int owner = __builtin_ctzll(__ballot(id < at + upto));
+                p.expert = e0 + owner;
+                p.of = __builtin_amdgcn_readlane(n, owner);
+                p.number = (int)(id - at) - (__builtin_amdgcn_readlane(upto, owner) - p.of);
+                p.first = __builtin_amdgcn_readlane(begin, owner) + p.number * per;
+                p.count = min(per, __builtin_amdgcn_readlane(end, owner) - p.first);
+                p.before = before + (EACH ? __builtin_amdgcn_readlane(many_upto - many, owner) : 0);
+                return p;
+            }
+            at += all;
+            before += EACH ? __builtin_amdgcn_readlane(many_upto, 63) : 0;
+        }
+        return p;
+    }
+};
+
+// Workgroup b of a launch runs on XCD b % 8.  Neighbouring tiles share operands, so an XCD, which has an L2 cache of its own, gets
+// neighbouring ones: the tile of workgroup b, of `tiles`; -1 if none.
+__device__ __forceinline__ int64_t tile_of(int64_t b, int64_t tiles)
+{
+    const int64_t each = (tiles + 7) >> 3, id = (b & 7) * each + (b >> 3);
+    return (b >> 3) < each && id < tiles ? id : -1;
+}
+
+}  // namespace fs
+#endif

@@ -1,0 +1,319 @@
+// Products of rows in slots with their expert's weights, in 32, 16 and 8 bits, and the weights' gradient.
+#include "fs_product.h"
+
+namespace fs {
+
+struct ProductArgs {
+    Bounds bounds;
+    const char *x, *w;
+    int64_t x_stride, w_stride, w_step;      // bytes
+    void *y;
+    int64_t y_stride;                        // elements
+    int32_t y_type, in_width, out_width, across;      // tiles across a row of results
+    const float *scale, *w_scale;            // of 8-bit operands
+    int64_t block0;
+};
+
+// A workgroup makes BM slots of one expert times BN columns.
+template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
+__global__ void __launch_bounds__(WM *WN * 64)
+product_kernel(ProductArgs a)
+{
+    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED> T;
+    __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
+    const int64_t id = tile_of(a.block0 + blockIdx.x, a.bounds.count<true, false>() * a.across);
+    if (id < 0)
+        return;
+    const Piece piece = a.bounds.find<true, false>(id / a.across);
+    const int n0 = (int)(id % a.across) * BN;
+    if (piece.count < 0)
+        return;
+    T t;
+    t.clear();
+    const bool owned = piece.expert < a.bounds.n_experts;
+    if (owned) {
+        const Operand x = {a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count};
+        const char *const w = a.w + (int64_t)piece.expert * a.w_step;
+        const Operand b = {TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0};
+        t.run(lds, x, b, a.in_width);
+    }
+    t.results([&](int row, int column, auto &v) {
+        const int n = a.out_width - n0 - column;
+        if (row >= piece.count || n <= 0)
+            return;
+        float y[16];
+        if constexpr (TYPE == kI8) {
+            const float scale = owned ? a.scale[piece.first + row] : 0.0f;
+            const float *const w_scale = a.w_scale + (int64_t)piece.expert * a.out_width + n0 + column;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                y[i] = owned ? (float)v[i] * scale * w_scale[i < n ? i : n - 1] : 0.0f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                y[i] = v[i];
+        }
+        store_results<RESULT>(a.y, (piece.first + (int64_t)row) * a.y_stride + n0 + column, a.y_type, n, y);
+    });
+}
+
+struct WeightsArgs {
+    Bounds bounds;
+    const char *g, *x;
+    int64_t g_stride, x_stride;              // bytes
+    void *d_w;
+    int64_t d_w_stride, d_w_step;            // elements
+    int32_t d_w_type, in_width, out_width, across, tiles, accumulate;
+    float *work;
+    int64_t block0;
+};
+
+// A workgroup makes BM x BN of an expert's gradient over one piece of its slots: the gradient itself where the piece is all of them,
+// else a partial sum, whose place is that of the piece among all of experts with several.
+template <int TYPE, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(WM *WN * 64)
+weights_kernel(WeightsArgs a)
+{
+    typedef Tile<TYPE, BM, BN, WM, WN, true, true> T;
+    __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
+    const int64_t id = tile_of(a.block0 + blockIdx.x, a.bounds.count<false, true>() * a.tiles);
+    if (id < 0)
+        return;
+    const Piece piece = a.bounds.find<false, true>(id / a.tiles);
+    const int tile = (int)(id % a.tiles), m0 = tile / a.across * BM, n0 = tile % a.across * BN;
+    if (piece.count < 0)
+        return;
+    const Operand g = {a.g + (int64_t)piece.first * a.g_stride + (int64_t)m0 * T::U::size, a.g_stride, a.out_width - m0};
+    const Operand x = {a.x + (int64_t)piece.first * a.x_stride + (int64_t)n0 * T::U::size, a.x_stride, a.in_width - n0};
+    T t;
+    t.clear();
+    t.run(lds, g, x, piece.count);
+    t.results([&](int row, int column, auto &v) {
+        const int n = a.in_width - n0 - column;
+        if (m0 + row >= a.out_width || n <= 0)
+            return;
+        float y[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            y[i] = v[i];
+        if (piece.of > 1) {
+            const int64_t at = ((piece.before + (int64_t)piece.number) * a.out_width + m0 + row) * a.in_width + n0 + column;
+            store_results(a.work + at, n, y);
+            return;
+        }
+        const int64_t at = piece.expert * a.d_w_step + (m0 + (int64_t)row) * a.d_w_stride + n0 + column;
+        if (a.accumulate)
+            add_to_results<TYPE>(a.d_w, at, a.d_w_type, n, y);
+        store_results<TYPE>(a.d_w, at, a.d_w_type, n, y);
+    });
+}
+
+// The partial sums of an expert's pieces, in their order, in 64 bits.
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+weights_join_kernel(WeightsArgs a)
+{
+    typedef typename Element<TYPE>::type E;
+    const int expert = (int)(blockIdx.x / a.tiles);
+    int begin, end;
+    const int pieces = a.bounds.pieces<false, true>(expert, begin, end);
+    if (pieces <= 1)
+        return;
+    int before = 0;
+    for (int e0 = 0; e0 < expert; e0 += 64) {
+        const int e = e0 + (threadIdx.x & 63);
+        int b, c;
+        const int n = e < expert ? a.bounds.pieces<false, true>(e, b, c) : 0;
+        before += __builtin_amdgcn_readlane(Bounds::sum_to(n > 1 ? n : 0), 63);
+    }
+    const int64_t all = (int64_t)a.out_width * a.in_width;
+    for (int64_t i = (blockIdx.x % a.tiles) * (int64_t)256 + threadIdx.x; i < all; i += a.tiles * (int64_t)256) {
+        const int64_t at = expert * a.d_w_step + i / a.in_width * a.d_w_stride + i % a.in_width;
+        const bool wide = TYPE != FS_F32 && a.d_w_type == FS_F32;
+        double sum = 0;
+        if (a.accumulate)
+            sum = wide ? ((const float *)a.d_w)[at] : (float)((const E *)a.d_w)[at];
+        for (int p = 0; p < pieces; ++p)
+            sum += a.work[(before + (int64_t)p) * all + i];
+        if (wide)
+            ((float *)a.d_w)[at] = (float)sum;
+        else
+            ((E *)a.d_w)[at] = (E)(float)sum;
+    }
+}
+
+// At most so many pieces of `per`.
+static int64_t most_pieces(int64_t n_slots, int32_t n_experts, int64_t per) { return n_slots / per + n_experts + 1; }
+
+template <class F>
+static void over_tiles(int64_t tiles, F f)
+{
+    in_pieces((tiles + 7) / 8 * 8, f);
+}
+
+template <int TYPE, int RESULT, bool TURNED>
+static void launch_product(ProductArgs a, hipStream_t stream)
+{
+    constexpr int BM = 128, BN = 128, WM = 2, WN = 2;
+    a.bounds.per = BM;
+    a.across = (a.out_width + BN - 1) / BN;
+    over_tiles(most_pieces(a.bounds.n_slots, a.bounds.n_experts, BM) * a.across, [&](int64_t at, unsigned blocks) {
+        a.block0 = at;
+        hipLaunchKernelGGL((product_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
+    });
+}
+
+// How many slots a workgroup of weights_kernel adds up.
+static int piece_of_weights(int64_t n_slots, int64_t tiles)
+{
+    int64_t per = n_slots * tiles / 512;
+    per = per < 1024 ? 1024 : per > 32768 ? 32768 : per;
+    return (int)((per + 255) / 256 * 256);
+}
+static int64_t tiles_of_weights(int32_t in_width, int32_t out_width) { return ((int64_t)in_width + 127) / 128 * (((int64_t)out_width + 127) / 128); }
+
+static int check_shape(const char *who, int64_t n_slots, int32_t n_experts, int32_t in_width, int32_t out_width)
+{
+    if (n_slots < 0 || n_slots >= ((int64_t)1 << 31))
+        return fail(FS_EINVAL, "%s: %lld slots: 0 to 2^31 - 1 are taken", who, (long long)n_slots);
+    FS_TRY(check_experts(who, n_experts));
+    FS_TRY(check_width(who, in_width));
+    return check_width(who, out_width);
+}
+// n_experts matrices, `step` apart.
+static int check_matrices(const char *who, const char *what, const void *p, int64_t rows, int64_t width, int32_t type, int64_t stride, int64_t step,
+                          int64_t least_step)
+{
+    FS_TRY(check_matrix(who, what, p, rows, width, type, stride));
+    if (step < least_step || step > ((int64_t)1 << 50))
+        return fail(FS_EINVAL, "%s: %lld elements from matrix to matrix of %s, %lld at least and 2^50 at most are taken", who, (long long)step, what,
+                    (long long)least_step);
+    return FS_OK;
+}
+static int check_result(const char *who, const char *what, int32_t result, int32_t type)
+{
+    if (result != type && result != FS_F32)
+        return fail(FS_EINVAL, "%s: %s is of another type (%d) than the operands (%d) or fp32", who, what, result, type);
+    return FS_OK;
+}
+
+}  // namespace fs
+
+using namespace fs;
+
+extern "C" int fs_expert_matmul(int64_t n_slots, int32_t n_experts, int32_t in_width, int32_t out_width, const void *x, int32_t type,
+                                int64_t x_stride, const int32_t *first, const void *w, int64_t w_stride, int64_t w_step, int32_t turned,
+                                void *y, int32_t y_type, int64_t y_stride, void *stream_)
+{
+    static const char who[] = "fs_expert_matmul";
+    hipStream_t stream = (hipStream_t)stream_;
+    FS_TRY(check_shape(who, n_slots, n_experts, in_width, out_width));
+    FS_TRY(check_matrix(who, "x", x, n_slots, in_width, type, x_stride));
+    FS_TRY(check_array(who, "first", first, n_slots, 4));
+    if (turned != 0 && turned != 1)
+        return fail(FS_EINVAL, "%s: turned %d is neither 0 nor 1", who, turned);
+    FS_TRY(check_matrices(who, "w", w, n_slots, turned ? out_width : in_width, type, w_stride, w_step, 0));
+    FS_TRY(check_matrix(who, "y", y, n_slots, out_width, y_type, y_stride));
+    FS_TRY(check_result(who, "y", y_type, type));
+    if (n_slots == 0)
+        return FS_OK;
+    const int64_t b = (int64_t)type_bytes(type);
+    ProductArgs a = {{first, n_experts, (int)n_slots, 0}, (const char *)x, (const char *)w, x_stride * b, w_stride * b, w_step * b, y, y_stride, y_type,
+                     in_width, out_width, 0, nullptr, nullptr, 0};
+    prof_start(kKernPack, stream);
+    with_type(type, [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        if (turned)
+            launch_product<T, T, true>(a, stream);
+        else
+            launch_product<T, T, false>(a, stream);
+    });
+    prof_stop(stream);
+    return launched("expert product kernel launch");
+}
+
+extern "C" int fs_expert_matmul_i8(int64_t n_slots, int32_t n_experts, int32_t in_width, int32_t out_width, const int8_t *q, int64_t q_stride,
+                                   const float *scale, const int32_t *first, const int8_t *w, int64_t w_stride, int64_t w_step,
+                                   const float *w_scale, void *y, int32_t y_type, int64_t y_stride, void *stream_)
+{
+    static const char who[] = "fs_expert_matmul_i8";
+    hipStream_t stream = (hipStream_t)stream_;
+    FS_TRY(check_shape(who, n_slots, n_experts, in_width, out_width));
+    if (in_width > FS_MAX_I8_WIDTH)
+        return fail(FS_EUNSUPPORTED, "%s: width %d of a sum in 32 bits, %d at most", who, in_width, FS_MAX_I8_WIDTH);
+    FS_TRY(check_bytes(who, "q", q, n_slots, in_width, q_stride));
+    FS_TRY(check_array(who, "scale", scale, n_slots, 4));
+    FS_TRY(check_array(who, "first", first, n_slots, 4));
+    FS_TRY(check_bytes(who, "w", w, n_slots, in_width, w_stride));
+    if (w_step < 0 || w_step > ((int64_t)1 << 50))
+        return fail(FS_EINVAL, "%s: %lld bytes from matrix to matrix of w", who, (long long)w_step);
+    FS_TRY(check_array(who, "w_scale", w_scale, n_slots, 4));
+    FS_TRY(check_matrix(who, "y", y, n_slots, out_width, y_type, y_stride));
+    if (n_slots == 0)
+        return FS_OK;
+    ProductArgs a = {{first, n_experts, (int)n_slots, 0}, (const char *)q, (const char *)w, q_stride, w_stride, w_step, y, y_stride, y_type,
+                     in_width, out_width, 0, scale, w_scale, 0};
+    prof_start(kKernPack, stream);
+    with_type(y_type, [&](auto t) { launch_product<kI8, decltype(t)::value, false>(a, stream); });
+    prof_stop(stream);
+    return launched("expert product kernel launch");
+}
+
+extern "C" size_t fs_expert_matmul_backward_workspace_bytes(int64_t n_slots, int32_t n_experts, int32_t in_width, int32_t out_width, int32_t type)
+{
+    static const char who[] = "fs_expert_matmul_backward_workspace_bytes";
+    if (check_shape(who, n_slots, n_experts, in_width, out_width) != FS_OK)
+        return 0;
+    if (!type_ok(type)) {
+        fail(FS_EINVAL, "%s: unknown element type %d", who, type);
+        return 0;
+    }
+    const int64_t per = piece_of_weights(n_slots, tiles_of_weights(in_width, out_width));
+    if (n_slots <= per)
+        return 0;
+    // An expert of n > per slots has at most n / per + 1 < 2 n / per pieces.
+    return (size_t)(2 * (n_slots / per + 1)) * in_width * out_width * 4;
+}
+
+extern "C" int fs_expert_matmul_backward(int64_t n_slots, int32_t n_experts, int32_t in_width, int32_t out_width, const void *d_y, int32_t type,
+                                         int64_t d_y_stride, const void *x, int64_t x_stride, const int32_t *first, int32_t accumulate,
+                                         void *d_w, int32_t d_w_type, int64_t d_w_stride, int64_t d_w_step, void *work, size_t work_bytes,
+                                         void *stream_)
+{
+    static const char who[] = "fs_expert_matmul_backward";
+    hipStream_t stream = (hipStream_t)stream_;
+    FS_TRY(check_shape(who, n_slots, n_experts, in_width, out_width));
+    FS_TRY(check_matrix(who, "d_y", d_y, n_slots, out_width, type, d_y_stride));
+    FS_TRY(check_matrix(who, "x", x, n_slots, in_width, type, x_stride));
+    FS_TRY(check_array(who, "first", first, 1, 4));
+    if (accumulate != 0 && accumulate != 1)
+        return fail(FS_EINVAL, "%s: accumulate %d is neither 0 nor 1", who, accumulate);
+    FS_TRY(check_matrices(who, "d_w", d_w, 1, in_width, d_w_type, d_w_stride, d_w_step, n_experts > 1 ? d_w_stride * out_width : 0));
+    FS_TRY(check_result(who, "d_w", d_w_type, type));
+    const size_t need = fs_expert_matmul_backward_workspace_bytes(n_slots, n_experts, in_width, out_width, type);
+    FS_TRY(check_array(who, "work", work, (int64_t)need, 256));
+    if (work_bytes < need)
+        return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, need);
+    const int64_t b = (int64_t)type_bytes(type);
+    const int64_t tiles = tiles_of_weights(in_width, out_width);
+    if (tiles > ((int64_t)1 << 30))
+        return fail(FS_EUNSUPPORTED, "%s: a gradient of %d x %d", who, out_width, in_width);
+    const int per = piece_of_weights(n_slots, tiles);
+    WeightsArgs a = {{first, n_experts, (int)n_slots, per}, (const char *)d_y, (const char *)x, d_y_stride * b, x_stride * b, d_w, d_w_stride, d_w_step,
+                     d_w_type, in_width, out_width, (in_width + 127) / 128, (int32_t)tiles, accumulate, (float *)work, 0};
+    prof_start(kKernTrainOther, stream);
+    with_type(type, [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        over_tiles(most_pieces(n_slots, n_experts, per) * tiles, [&](int64_t at, unsigned blocks) {
+            a.block0 = at;
+            hipLaunchKernelGGL((weights_kernel<T, 128, 128, 2, 2>), dim3(blocks), dim3(256), 0, stream, a);
+        });
+        if (need) {
+            const int64_t wanted = ((int64_t)in_width * out_width + 1023) / 1024, most = 4096 / n_experts + 1;
+            a.tiles = (int32_t)(wanted < most ? wanted : most);
+            hipLaunchKernelGGL(weights_join_kernel<T>, dim3((unsigned)(a.tiles * n_experts)), dim3(256), 0, stream, a);
+        }
+    });
+    prof_stop(stream);
+    return launched("expert weights' gradient kernel launch");
+}
