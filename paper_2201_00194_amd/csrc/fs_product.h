@@ -152,6 +152,43 @@ struct Tile {
         }
     };
 
+    // ---- operands straight into LDS: rows and their 16-byte chunks aligned and whole ----
+    // A wavefront's load writes 64 chunks side by side, so it is the lanes' sources that are turned.  A lane whose chunk is not there
+    // has an offset past the buffer's end, and zeros come.
+    template <bool ALONG, int ROWS>
+    struct Streamed {
+        typedef Place<TYPE, ALONG, ROWS> P;
+        static constexpr int N = P::chunks / threads;
+        static constexpr unsigned kNowhere = 0x80000000u;
+        unsigned from[N];
+        uint64_t base;
+        int64_t stride;
+        static __device__ __forceinline__ int row_of(int i) { return (threadIdx.x + i * threads) / P::per_row; }
+        static __device__ __forceinline__ int chunk_of(int i) { return (threadIdx.x + i * threads) % P::per_row ^ P::turn(row_of(i)); }
+        __device__ __forceinline__ Streamed(const Operand &o) : base((uint64_t)o.p), stride(o.stride)
+        {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                from[i] = (ALONG ? chunk_of(i) * (16 / U::size) : row_of(i)) < o.count ? row_of(i) * (unsigned)stride + chunk_of(i) * 16 : kNowhere;
+        }
+        // The next step's chunks, of which `left` elements of the sum are there.
+        __device__ __forceinline__ void load(char *lds, int left)
+        {
+            if (left < step) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    from[i] = (ALONG ? row_of(i) : chunk_of(i) * (16 / U::size)) < left ? from[i] : kNowhere;
+            }
+            const I4 buffer = {(int)base, (int)(base >> 32) & 0xffff, (int)kNowhere, 0x00020000};
+            const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (threadIdx.x >> 6) * 1024);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * threads * 16), "v"(from[i]), "s"(buffer)
+                             : "memory");
+            base += ALONG ? (uint64_t)step * stride : kStepBytes;
+        }
+    };
+
     // ---- fragments ----
     // `base`: the wavefront's first row or column.  Fragment f is of block f / 4 of 64 rows; fp32 along: v[4 * block + i][f % 4]
     // are the i-th terms of its lanes instead of v[f][i].
@@ -207,6 +244,25 @@ struct Tile {
     }
 
     // The sums over k_count terms.
+    __device__ __forceinline__ void stream(char *lds, const Operand &a, const Operand &b, int k_count)
+    {
+        if (k_count <= 0)
+            return;
+        Streamed<AT, BM> sa(a);
+        Streamed<BT, BN> sb(b);
+        sa.load(lds, k_count);
+        sb.load(lds + a_bytes, k_count);
+        for (int k0 = 0, half = 0; k0 < k_count; k0 += step, half ^= 1) {
+            // This half has arrived, and the other one has been read, in all wavefronts.
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (k0 + step < k_count) {
+                char *const next = lds + (half ^ 1) * stage_bytes;
+                sa.load(next, k_count - k0 - step);
+                sb.load(next + a_bytes, k_count - k0 - step);
+            }
+            multiply(lds + half * stage_bytes);
+        }
+    }
     __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int k_count)
     {
         Fetched<AT, BM> fa;

@@ -15,7 +15,7 @@ struct ProductArgs {
 };
 
 // A workgroup makes BM slots of one expert times BN columns.
-template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
+template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED, bool DIRECT>
 __global__ void __launch_bounds__(WM *WN * 64)
 product_kernel(ProductArgs a)
 {
@@ -35,7 +35,10 @@ product_kernel(ProductArgs a)
         const Operand x = {a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count};
         const char *const w = a.w + (int64_t)piece.expert * a.w_step;
         const Operand b = {TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0};
-        t.run(lds, x, b, a.in_width);
+        if constexpr (DIRECT)
+            t.stream(lds, x, b, a.in_width);
+        else
+            t.run(lds, x, b, a.in_width);
     }
     t.results([&](int row, int column, auto &v) {
         const int n = a.out_width - n0 - column;
@@ -70,7 +73,7 @@ struct WeightsArgs {
 
 // A workgroup makes BM x BN of an expert's gradient over one piece of its slots: the gradient itself where the piece is all of them,
 // else a partial sum, whose place is that of the piece among all of experts with several.
-template <int TYPE, int BM, int BN, int WM, int WN>
+template <int TYPE, int BM, int BN, int WM, int WN, bool DIRECT>
 __global__ void __launch_bounds__(WM *WN * 64)
 weights_kernel(WeightsArgs a)
 {
@@ -87,7 +90,10 @@ weights_kernel(WeightsArgs a)
     const Operand x = {a.x + (int64_t)piece.first * a.x_stride + (int64_t)n0 * T::U::size, a.x_stride, a.in_width - n0};
     T t;
     t.clear();
-    t.run(lds, g, x, piece.count);
+    if constexpr (DIRECT)
+        t.stream(lds, g, x, piece.count);
+    else
+        t.run(lds, g, x, piece.count);
     t.results([&](int row, int column, auto &v) {
         const int n = a.in_width - n0 - column;
         if (m0 + row >= a.out_width || n <= 0)
@@ -151,26 +157,60 @@ static void over_tiles(int64_t tiles, F f)
     in_pieces((tiles + 7) / 8 * 8, f);
 }
 
-template <int TYPE, int RESULT, bool TURNED>
-static void launch_product(ProductArgs a, hipStream_t stream)
+template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN, bool DIRECT>
+static void launch_tiles(ProductArgs a, hipStream_t stream)
 {
-    constexpr int BM = 128, BN = 128, WM = 2, WN = 2;
     a.bounds.per = BM;
     a.across = (a.out_width + BN - 1) / BN;
     over_tiles(most_pieces(a.bounds.n_slots, a.bounds.n_experts, BM) * a.across, [&](int64_t at, unsigned blocks) {
         a.block0 = at;
-        hipLaunchKernelGGL((product_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
+        hipLaunchKernelGGL((product_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED, DIRECT>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
     });
 }
 
-// How many slots a workgroup of weights_kernel adds up.
-static int piece_of_weights(int64_t n_slots, int64_t tiles)
+// Whether rows can be loaded straight into LDS: 16-byte chunks that are aligned and whole, and a tile's rows within 2^31 bytes.
+static bool streams(const void *p, int64_t stride, int64_t step, int64_t width)
 {
-    int64_t per = n_slots * tiles / 512;
+    return aligned_to(p, 16) && stride % 16 == 0 && step % 16 == 0 && width % 16 == 0 && stride < ((int64_t)1 << 23);
+}
+
+template <int TYPE, int RESULT, bool TURNED>
+static void launch_product(ProductArgs a, hipStream_t stream)
+{
+    constexpr int size = Unit16<TYPE>::size;
+    const bool direct = streams(a.x, a.x_stride, 0, (int64_t)a.in_width * size) &&
+                        streams(a.w, a.w_stride, a.w_step, (int64_t)(TURNED ? a.out_width : a.in_width) * size);
+    if (!direct)
+        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2, false>(a, stream);
+    else if (a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192)
+        launch_tiles<TYPE, RESULT, TURNED, 256, 256, 2, 4, true>(a, stream);
+    else
+        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2, true>(a, stream);
+}
+
+// How many slots a workgroup of weights_kernel adds up.
+static bool wide_weights(int64_t n_experts, int64_t in_width, int64_t out_width)
+{
+    return in_width > 128 && out_width > 128 && in_width * out_width * n_experts >= ((int64_t)1 << 24);
+}
+static int piece_of_weights(int64_t n_slots, int32_t n_experts, int64_t in_width, int64_t out_width)
+{
+    const int side = wide_weights(n_experts, in_width, out_width) ? 256 : 128;
+    int64_t per = n_slots * ((in_width + side - 1) / side * ((out_width + side - 1) / side)) / 512;
     per = per < 1024 ? 1024 : per > 32768 ? 32768 : per;
     return (int)((per + 255) / 256 * 256);
 }
-static int64_t tiles_of_weights(int32_t in_width, int32_t out_width) { return ((int64_t)in_width + 127) / 128 * (((int64_t)out_width + 127) / 128); }
+
+template <int TYPE, int SIDE, int WM, int WN, bool DIRECT>
+static void launch_weights(WeightsArgs a, hipStream_t stream)
+{
+    a.across = (a.in_width + SIDE - 1) / SIDE;
+    a.tiles = a.across * ((a.out_width + SIDE - 1) / SIDE);
+    over_tiles(most_pieces(a.bounds.n_slots, a.bounds.n_experts, a.bounds.per) * a.tiles, [&](int64_t at, unsigned blocks) {
+        a.block0 = at;
+        hipLaunchKernelGGL((weights_kernel<TYPE, SIDE, SIDE, WM, WN, DIRECT>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
+    });
+}
 
 static int check_shape(const char *who, int64_t n_slots, int32_t n_experts, int32_t in_width, int32_t out_width)
 {
@@ -268,7 +308,7 @@ extern "C" size_t fs_expert_matmul_backward_workspace_bytes(int64_t n_slots, int
         fail(FS_EINVAL, "%s: unknown element type %d", who, type);
         return 0;
     }
-    const int64_t per = piece_of_weights(n_slots, tiles_of_weights(in_width, out_width));
+    const int64_t per = piece_of_weights(n_slots, n_experts, in_width, out_width);
     if (n_slots <= per)
         return 0;
     // An expert of n > per slots has at most n / per + 1 < 2 n / per pieces.
@@ -295,19 +335,18 @@ extern "C" int fs_expert_matmul_backward(int64_t n_slots, int32_t n_experts, int
     if (work_bytes < need)
         return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, need);
     const int64_t b = (int64_t)type_bytes(type);
-    const int64_t tiles = tiles_of_weights(in_width, out_width);
-    if (tiles > ((int64_t)1 << 30))
-        return fail(FS_EUNSUPPORTED, "%s: a gradient of %d x %d", who, out_width, in_width);
-    const int per = piece_of_weights(n_slots, tiles);
-    WeightsArgs a = {{first, n_experts, (int)n_slots, per}, (const char *)d_y, (const char *)x, d_y_stride * b, x_stride * b, d_w, d_w_stride, d_w_step,
-                     d_w_type, in_width, out_width, (in_width + 127) / 128, (int32_t)tiles, accumulate, (float *)work, 0};
+    WeightsArgs a = {{first, n_experts, (int)n_slots, piece_of_weights(n_slots, n_experts, in_width, out_width)}, (const char *)d_y, (const char *)x,
+                     d_y_stride * b, x_stride * b, d_w, d_w_stride, d_w_step, d_w_type, in_width, out_width, 0, 0, accumulate, (float *)work, 0};
+    const bool direct = streams(d_y, a.g_stride, 0, out_width * b) && streams(x, a.x_stride, 0, in_width * b);
     prof_start(kKernTrainOther, stream);
     with_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
-        over_tiles(most_pieces(n_slots, n_experts, per) * tiles, [&](int64_t at, unsigned blocks) {
-            a.block0 = at;
-            hipLaunchKernelGGL((weights_kernel<T, 128, 128, 2, 2>), dim3(blocks), dim3(256), 0, stream, a);
-        });
+        if (!direct)
+            launch_weights<T, 128, 2, 2, false>(a, stream);
+        else if (wide_weights(n_experts, in_width, out_width))
+            launch_weights<T, 256, 2, 4, true>(a, stream);
+        else
+            launch_weights<T, 128, 2, 2, true>(a, stream);
         if (need) {
             const int64_t wanted = ((int64_t)in_width * out_width + 1023) / 1024, most = 4096 / n_experts + 1;
             a.tiles = (int32_t)(wanted < most ? wanted : most);
