@@ -53,6 +53,15 @@ struct Operand {
     int count;           // rows, or columns, of the tile that are there
 };
 
+// The thread's number, as one that the compiler cannot know: what follows from it is computed where it is needed, and not kept in
+// registers beside the sums of all tiles.
+__device__ __forceinline__ int thread_here()
+{
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
 constexpr int kStepBytes = 128;      // of the sum, of 1, 2 or 4 bytes an element, that a tile takes at a time
 
 // Where 16 bytes of an operand lie in LDS.  Lanes read a fragment's rows 0 1 2 3, 16 17 18 19, ... of 64 (fragment 0; the
@@ -66,7 +75,7 @@ struct Place {
     static __device__ __forceinline__ int turn(int row)
     {
         if constexpr (!ALONG)
-            return (row & 3) | ((row >> 4 & 1) << 2);
+            return (row >> 1 & 1) | ((row >> 4 & 3) << 1);
         else if constexpr (size == 2)
             return (row & 1) | ((row >> 1 & 1) << (per_row >= 16 ? 3 : 0));
         else
@@ -163,21 +172,24 @@ struct Tile {
         unsigned from[N];
         uint64_t base;
         int64_t stride;
-        static __device__ __forceinline__ int row_of(int i) { return (threadIdx.x + i * threads) / P::per_row; }
-        static __device__ __forceinline__ int chunk_of(int i) { return (threadIdx.x + i * threads) % P::per_row ^ P::turn(row_of(i)); }
+        __device__ __forceinline__ Streamed() {}
+        static __device__ __forceinline__ int row_of(int t, int i) { return (t + i * threads) / P::per_row; }
+        static __device__ __forceinline__ int chunk_of(int t, int i) { return (t + i * threads) % P::per_row ^ P::turn(row_of(t, i)); }
         __device__ __forceinline__ Streamed(const Operand &o) : base((uint64_t)o.p), stride(o.stride)
         {
+            const int t = thread_here();
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                from[i] = (ALONG ? chunk_of(i) * (16 / U::size) : row_of(i)) < o.count ? row_of(i) * (unsigned)stride + chunk_of(i) * 16 : kNowhere;
+                from[i] = (ALONG ? chunk_of(t, i) * (16 / U::size) : row_of(t, i)) < o.count ? row_of(t, i) * (unsigned)stride + chunk_of(t, i) * 16 : kNowhere;
         }
         // The next step's chunks, of which `left` elements of the sum are there.
         __device__ __forceinline__ void load(char *lds, int left)
         {
             if (left < step) {
+                const int t = thread_here();
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    from[i] = (ALONG ? row_of(i) : chunk_of(i) * (16 / U::size)) < left ? from[i] : kNowhere;
+                    from[i] = (ALONG ? row_of(t, i) : chunk_of(t, i) * (16 / U::size)) < left ? from[i] : kNowhere;
             }
             const I4 buffer = {(int)base, (int)(base >> 32) & 0xffff, (int)kNowhere, 0x00020000};
             const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (threadIdx.x >> 6) * 1024);
@@ -243,25 +255,30 @@ struct Tile {
         }
     }
 
-    // The sums over k_count terms.
-    __device__ __forceinline__ void stream(char *lds, const Operand &a, const Operand &b, int k_count)
+    // The sums over k_count terms, whose first step is on its way to half `half`; while the last one is multiplied, next() starts
+    // the first step of another tile in the other half.  `kept`: so many younger stores need not have ended.
+    template <int KEPT, class F>
+    __device__ __forceinline__ void stream(char *lds, int &half, Streamed<AT, BM> &sa, Streamed<BT, BN> &sb, int k_count, bool keep, F next)
     {
-        if (k_count <= 0)
-            return;
-        Streamed<AT, BM> sa(a);
-        Streamed<BT, BN> sb(b);
-        sa.load(lds, k_count);
-        sb.load(lds + a_bytes, k_count);
-        for (int k0 = 0, half = 0; k0 < k_count; k0 += step, half ^= 1) {
+        for (int k0 = 0; k0 < k_count; k0 += step) {
             // This half has arrived, and the other one has been read, in all wavefronts.
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (k0 + step < k_count) {
-                char *const next = lds + (half ^ 1) * stage_bytes;
-                sa.load(next, k_count - k0 - step);
-                sb.load(next + a_bytes, k_count - k0 - step);
-            }
-            multiply(lds + half * stage_bytes);
+            if (k0 == 0 && keep)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(KEPT) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            char *const now = lds + half * stage_bytes;
+            half ^= 1;
+            if (k0 + step < k_count)
+                load(lds + half * stage_bytes, sa, sb, k_count - k0 - step);
+            else
+                next();
+            multiply(now);
         }
+    }
+    static __device__ __forceinline__ void load(char *lds, Streamed<AT, BM> &sa, Streamed<BT, BN> &sb, int left)
+    {
+        sa.load(lds, left);
+        sb.load(lds + a_bytes, left);
     }
     __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int k_count)
     {
@@ -282,60 +299,77 @@ struct Tile {
         }
     }
 
-    // f(row, first column, sixteen results side by side) for each of a lane's runs of results.
-    template <class F>
-    __device__ __forceinline__ void results(F f) const
+    // ---- results ----
+    // A lane has, of one row a fragment, sixteen results side by side for each block of 64 columns, and sixteen lanes have sixteen
+    // rows.  They change places in `rows` bytes of LDS of the wavefront's own, sixteen rows of 128 bytes at a time, so that eight lanes
+    // store a line together: where each lane stored its own results, a tile of 256 x 256 took 10 us for it.
+    // make(fragment, values, what of_column(column) gave, sixteen numbers): the results as numbers; put(row, column, chunk): 16 bytes
+    // of them, as S.
+    static constexpr int rows_bytes = 2048;
+    static __device__ __forceinline__ int row_of(int t, int r, int i)
     {
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-        const int m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
-        constexpr bool a4 = AT && TYPE == FS_F32, b4 = BT && TYPE == FS_F32;
+        return (t >> 6) / WN * (BM / WM) + (i >> 2) * 64 + (AT && TYPE == FS_F32 ? 4 * r + (i & 3) : (r >> 2) * 16 + (i & 3) * 4 + (r & 3));
+    }
+    template <class S, class G, class M, class P>
+    __device__ __forceinline__ void results(char *rows, int t, G of_column, M make, P put) const
+    {
+        typedef S Chunk __attribute__((ext_vector_type(16 / sizeof(S))));
+        constexpr bool b4 = BT && TYPE == FS_F32;
+        constexpr int passes = sizeof(S) == 4 ? 2 : 1, N = 16 / sizeof(S);      // 32 or 64 columns a pass
+        char *const own = rows + (t >> 6) * rows_bytes;
+        const int n0 = (t >> 6) % WN * (BN / WN), lane = t & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            const int row = m0 + (i >> 2) * 64 + (a4 ? 4 * r + (i & 3) : (r >> 2) * 16 + (i & 3) * 4 + (r & 3));
+        for (int block = 0; block < NF / 4; ++block) {
+            const auto c = of_column(n0 + block * 64 + g * 16);
 #pragma unroll
-            for (int block = 0; block < NF / 4; ++block) {
+            for (int i = 0; i < MF; ++i) {
                 decltype(Acc{}[0] + 0) v[16];
+                float y[16];
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         v[b4 ? 4 * e + j : 4 * j + e] = acc[i][block * 4 + j][e];
-                f(row, n0 + block * 64 + g * 16, v);
+                make(i, v, c, y);
+#pragma unroll
+                for (int pass = 0; pass < passes; ++pass) {
+                    if (passes == 1 || g >> 1 == pass) {
+#pragma unroll
+                        for (int h = 0; h < 16 / N; ++h) {
+                            Chunk part;
+#pragma unroll
+                            for (int e = 0; e < N; ++e)
+                                part[e] = (S)y[h * N + e];
+                            const int chunk = (g & (4 / passes - 1)) * (16 / N) + h;
+                            *(Chunk *)(own + r * 128 + (chunk ^ (r >> 1)) * 16) = part;
+                        }
+                    }
+                    lds_sync();
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int rr = u * 8 + (lane >> 3), chunk = lane & 7;
+                        const Chunk part = *(const Chunk *)(own + rr * 128 + (chunk ^ (rr >> 1)) * 16);
+                        put(row_of(t, rr, i), n0 + block * 64 + pass * 32 + chunk * N, part);
+                    }
+                    lds_sync();
+                }
             }
         }
     }
 };
 
-// Sixteen results of which n are wanted.
-template <class T>
-__device__ __forceinline__ void store_results(T *p, int n, const float (&v)[16])
+// A chunk of results of which n are wanted.
+template <class S, int N>
+__device__ __forceinline__ void store_part(S *p, int n, const S __attribute__((ext_vector_type(N))) &v)
 {
-    constexpr int N = kChunk<T>;
-#pragma unroll
-    for (int c = 0; c < 16; c += N) {
-        float part[N];
+    if (n >= N) {
+        *(typename ChunkOf<S, N>::type *)p = v;
+    } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            part[i] = v[c + i];
-        store_chunk<N>(p + c, n - c, part);
+            if (i < n)
+                p[i] = v[i];
     }
-}
-// `type`: of the matrix's type or FS_F32.
-template <int TYPE>
-__device__ __forceinline__ void store_results(void *p, int64_t at, int type, int n, const float (&v)[16])
-{
-    if (TYPE != FS_F32 && type == FS_F32)
-        store_results((float *)p + at, n, v);
-    else
-        store_results((typename Element<TYPE>::type *)p + at, n, v);
-}
-template <int TYPE>
-__device__ __forceinline__ void add_to_results(const void *p, int64_t at, int type, int n, float (&v)[16])
-{
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (i < n)
-            v[i] += TYPE != FS_F32 && type == FS_F32 ? ((const float *)p)[at + i] : (float)((const typename Element<TYPE>::type *)p)[at + i];
 }
 
 // ---- whose rows a workgroup works on ---------------------------------------------------------------
@@ -407,6 +441,66 @@ struct Bounds {
             at += all;
             before += EACH ? __builtin_amdgcn_readlane(many_upto, 63) : 0;
         }
+        return p;
+    }
+};
+
+// The same pieces (none of nobody's), listed once by a workgroup that looks for several.
+struct PieceTable {
+    int upto[FS_MAX_EXPERTS + 1];      // pieces of the experts before
+    int waves[16];
+    // By all THREADS of the workgroup; the number of pieces.
+    template <int THREADS, bool EACH>
+    __device__ __forceinline__ int fill(const Bounds &b)
+    {
+        constexpr int most = (FS_MAX_EXPERTS + THREADS - 1) / THREADS;
+        const int each = (b.n_experts + THREADS - 1) / THREADS, e0 = threadIdx.x * each, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        int n[most], sum = 0;
+#pragma unroll
+        for (int u = 0; u < most; ++u) {
+            n[u] = 0;
+            if (u < each && e0 + u < b.n_experts) {
+                int from, to;
+                n[u] = b.pieces<false, EACH>(e0 + u, from, to);
+            }
+            sum += n[u];
+        }
+        const int to_here = Bounds::sum_to(sum);
+        if (lane == 63)
+            waves[wave] = to_here;
+        __syncthreads();
+        int before = to_here - sum, all = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) {
+            before += w < wave ? waves[w] : 0;
+            all += waves[w];
+        }
+#pragma unroll
+        for (int u = 0; u < most; ++u)
+            if (u < each && e0 + u < b.n_experts) {
+                upto[e0 + u] = before;
+                before += n[u];
+            }
+        if (threadIdx.x == 0)
+            upto[b.n_experts] = all;
+        __syncthreads();
+        return __builtin_amdgcn_readfirstlane(all);
+    }
+    // Piece `id`, which is there: the last expert with no more than `id` before it, by 64 lanes twice.
+    __device__ __forceinline__ Piece find(const Bounds &b, int id) const
+    {
+        const int lane = threadIdx.x & 63, each = (b.n_experts + 63) >> 6;
+        const int block = __popcll(__ballot(lane * each < b.n_experts && upto[min(lane * each, b.n_experts)] <= id)) - 1;
+        const int e = block * each + lane, in_block = __popcll(__ballot(lane < each && e < b.n_experts && upto[min(e, b.n_experts)] <= id)) - 1;
+        Piece p = {};
+        p.expert = __builtin_amdgcn_readfirstlane(block * each + in_block);
+        const int before = __builtin_amdgcn_readfirstlane(upto[p.expert]);
+        p.of = __builtin_amdgcn_readfirstlane(upto[p.expert + 1]) - before;
+        p.number = id - before;
+        int begin, end;
+        b.pieces<false, false>(p.expert, begin, end);
+        p.first = __builtin_amdgcn_readfirstlane(begin) + p.number * b.per;
+        p.count = min(b.per, __builtin_amdgcn_readfirstlane(end) - p.first);
         return p;
     }
 };

@@ -11,53 +11,155 @@ struct ProductArgs {
     int64_t y_stride;                        // elements
     int32_t y_type, in_width, out_width, across;      // tiles across a row of results
     const float *scale, *w_scale;            // of 8-bit operands
-    int64_t block0;
+    int64_t block0, blocks;
 };
 
+// Results of a tile whose piece and first column are given.
+template <int TYPE, class S, class T>
+__device__ __forceinline__ void store_product(const ProductArgs &a, const T &t, char *rows, const Piece &piece, int n0)
+{
+    constexpr int N = 16 / sizeof(S);
+    const int thread = thread_here();
+    S *const y = (S *)a.y + (int64_t)piece.first * a.y_stride + n0;
+    const auto put = [&](int row, int column, const auto &part) {
+        if (row < piece.count)
+            store_part<S, N>(y + row * a.y_stride + column, a.out_width - n0 - column, part);
+    };
+    if constexpr (TYPE == kI8) {      // all scales are there before the first store
+        struct Scales {
+            float v[16];
+        };
+        float scale[T::MF];
+#pragma unroll
+        for (int i = 0; i < T::MF; ++i)
+            scale[i] = a.scale[piece.first + min(T::row_of(thread, thread & 15, i), piece.count - 1)];
+        t.template results<S>(
+            rows, thread,
+            [&](int column) {
+                Scales s;
+                const float *const from = a.w_scale + (int64_t)piece.expert * a.out_width;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s.v[i] = from[min(n0 + column + i, a.out_width - 1)];
+                return s;
+            },
+            [&](int i, const auto &v, const Scales &s, float (&out)[16]) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    out[e] = (float)v[e] * scale[i] * s.v[e];
+            },
+            put);
+    } else {
+        t.template results<S>(
+            rows, thread, [](int) { return 0; },
+            [](int, const auto &v, int, float (&out)[16]) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    out[e] = v[e];
+            },
+            put);
+    }
+}
+template <int TYPE, int RESULT, class T>
+__device__ __forceinline__ void store_product_as(const ProductArgs &a, const T &t, char *rows, const Piece &piece, int n0)
+{
+    if (RESULT != FS_F32 && a.y_type == FS_F32)
+        store_product<TYPE, float>(a, t, rows, piece, n0);
+    else
+        store_product<TYPE, typename Element<RESULT>::type>(a, t, rows, piece, n0);
+}
+
+// Nobody's slots, by all workgroups of a launch.
+template <class S, int THREADS>
+__device__ __forceinline__ void clear_nobodys_as(const ProductArgs &a)
+{
+    constexpr int N = 16 / sizeof(S), rows = THREADS / 64;
+    const S __attribute__((ext_vector_type(N))) zero = {};
+    const int from = min(max(a.bounds.first[a.bounds.n_experts], 0), a.bounds.n_slots);
+    for (int64_t s = from + (a.block0 + blockIdx.x) * rows + threadIdx.x / 64; s < a.bounds.n_slots; s += a.blocks * rows)
+        for (int c = (threadIdx.x & 63) * N; c < a.out_width; c += 64 * N)
+            store_part<S, N>((S *)a.y + s * a.y_stride + c, a.out_width - c, zero);
+}
+template <int RESULT, int THREADS>
+__device__ __forceinline__ void clear_nobodys(const ProductArgs &a)
+{
+    if (RESULT != FS_F32 && a.y_type == FS_F32)
+        clear_nobodys_as<float, THREADS>(a);
+    else
+        clear_nobodys_as<typename Element<RESULT>::type, THREADS>(a);
+}
+
 // A workgroup makes BM slots of one expert times BN columns.
-template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED, bool DIRECT>
+template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
 __global__ void __launch_bounds__(WM *WN * 64)
 product_kernel(ProductArgs a)
 {
     typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED> T;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
-    const int64_t id = tile_of(a.block0 + blockIdx.x, a.bounds.count<true, false>() * a.across);
+    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
+    clear_nobodys<RESULT, T::threads>(a);
+    const int64_t id = tile_of(a.block0 + blockIdx.x, a.bounds.count<false, false>() * a.across);
     if (id < 0)
         return;
-    const Piece piece = a.bounds.find<true, false>(id / a.across);
+    const Piece piece = a.bounds.find<false, false>(id / a.across);
     const int n0 = (int)(id % a.across) * BN;
     if (piece.count < 0)
         return;
     T t;
     t.clear();
-    const bool owned = piece.expert < a.bounds.n_experts;
-    if (owned) {
-        const Operand x = {a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count};
+    const Operand x = {a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count};
+    const char *const w = a.w + (int64_t)piece.expert * a.w_step;
+    const Operand b = {TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0};
+    t.run(lds, x, b, a.in_width);
+    store_product_as<TYPE, RESULT>(a, t, rows, piece, n0);
+}
+
+// The same with operands straight to LDS, one tile after the other: the first step of the next tile is on its way while the last
+// step of one is multiplied and its results are stored.
+template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
+__global__ void __launch_bounds__(WM *WN * 64)
+product_stream_kernel(ProductArgs a)
+{
+    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED> T;
+    __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
+    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
+    __shared__ PieceTable table;
+    clear_nobodys<RESULT, T::threads>(a);
+    // Results that fit the card's memory have fewer than 2^31 tiles.  An XCD, whose L2 cache is its own, takes neighbouring ones.
+    const int tiles = table.fill<T::threads, false>(a.bounds) * a.across, each = (tiles + 7) >> 3;
+    const int last = min((int)((blockIdx.x & 7) + 1) * each, tiles);
+    int id = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
+    if (id >= last)
+        return;
+    typename T::template Streamed<false, BM> sx;
+    typename T::template Streamed<TURNED, BN> sw;
+    Piece piece;
+    int n0;
+    const auto start = [&](char *to) {
+        piece = table.find(a.bounds, id / a.across);
+        n0 = id % a.across * BN;
+        sx = {Operand{a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count}};
         const char *const w = a.w + (int64_t)piece.expert * a.w_step;
-        const Operand b = {TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0};
-        if constexpr (DIRECT)
-            t.stream(lds, x, b, a.in_width);
-        else
-            t.run(lds, x, b, a.in_width);
+        sw = {Operand{TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0}};
+        T::load(to, sx, sw, a.in_width);
+    };
+    constexpr int stores = T::MF * T::NF / 4 * (RESULT == FS_F32 ? 4 : 2);     // of a wavefront and a whole tile, at least
+    bool whole = false;
+    int half = 0;
+    start(lds);
+    while (id < last) {
+        const Piece now = piece;
+        const int now_n0 = n0;
+        T t;
+        t.clear();
+        t.template stream<stores>(lds, half, sx, sw, a.in_width, whole, [&] {
+            id += (int)(gridDim.x >> 3);
+            if (id < last)
+                start(lds + half * T::stage_bytes);
+        });
+        store_product_as<TYPE, RESULT>(a, t, rows, now, now_n0);
+        whole = now.count == BM && now_n0 + BN <= a.out_width;
     }
-    t.results([&](int row, int column, auto &v) {
-        const int n = a.out_width - n0 - column;
-        if (row >= piece.count || n <= 0)
-            return;
-        float y[16];
-        if constexpr (TYPE == kI8) {
-            const float scale = owned ? a.scale[piece.first + row] : 0.0f;
-            const float *const w_scale = a.w_scale + (int64_t)piece.expert * a.out_width + n0 + column;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                y[i] = owned ? (float)v[i] * scale * w_scale[i < n ? i : n - 1] : 0.0f;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                y[i] = v[i];
-        }
-        store_results<RESULT>(a.y, (piece.first + (int64_t)row) * a.y_stride + n0 + column, a.y_type, n, y);
-    });
 }
 
 struct WeightsArgs {
@@ -79,6 +181,7 @@ weights_kernel(WeightsArgs a)
 {
     typedef Tile<TYPE, BM, BN, WM, WN, true, true> T;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
+    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
     const int64_t id = tile_of(a.block0 + blockIdx.x, a.bounds.count<false, true>() * a.tiles);
     if (id < 0)
         return;
@@ -90,27 +193,53 @@ weights_kernel(WeightsArgs a)
     const Operand x = {a.x + (int64_t)piece.first * a.x_stride + (int64_t)n0 * T::U::size, a.x_stride, a.in_width - n0};
     T t;
     t.clear();
-    if constexpr (DIRECT)
-        t.stream(lds, g, x, piece.count);
-    else
-        t.run(lds, g, x, piece.count);
-    t.results([&](int row, int column, auto &v) {
-        const int n = a.in_width - n0 - column;
-        if (m0 + row >= a.out_width || n <= 0)
-            return;
-        float y[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            y[i] = v[i];
-        if (piece.of > 1) {
-            const int64_t at = ((piece.before + (int64_t)piece.number) * a.out_width + m0 + row) * a.in_width + n0 + column;
-            store_results(a.work + at, n, y);
-            return;
+    if constexpr (DIRECT) {
+        if (piece.count > 0) {
+            typename T::template Streamed<true, BM> sg(g);
+            typename T::template Streamed<true, BN> sx(x);
+            int half = 0;
+            T::load(lds, sg, sx, piece.count);
+            t.template stream<0>(lds, half, sg, sx, piece.count, false, [] {});
         }
-        const int64_t at = piece.expert * a.d_w_step + (m0 + (int64_t)row) * a.d_w_stride + n0 + column;
-        if (a.accumulate)
-            add_to_results<TYPE>(a.d_w, at, a.d_w_type, n, y);
-        store_results<TYPE>(a.d_w, at, a.d_w_type, n, y);
+    } else {
+        t.run(lds, g, x, piece.count);
+    }
+    const int thread = thread_here();
+    const auto as_they_are = [](int, const auto &v, int, float (&out)[16]) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            out[e] = v[e];
+    };
+    if (piece.of > 1) {
+        float *const to = a.work + (piece.before + (int64_t)piece.number) * a.out_width * a.in_width;
+        t.template results<float>(rows, thread, [](int) { return 0; }, as_they_are, [&](int row, int column, const auto &part) {
+            if (m0 + row < a.out_width)
+                store_part<float, 4>(to + (m0 + row) * (int64_t)a.in_width + n0 + column, a.in_width - n0 - column, part);
+        });
+        return;
+    }
+    t.template results<float>(rows, thread, [](int) { return 0; }, as_they_are, [&](int row, int column, auto part) {
+        if (m0 + row >= a.out_width)
+            return;
+        const int64_t at = piece.expert * a.d_w_step + (m0 + row) * a.d_w_stride + n0 + column;
+        const int n = a.in_width - n0 - column;
+        typedef typename Element<TYPE>::type E;
+        if (TYPE == FS_F32 || a.d_w_type == FS_F32) {
+            float *const to = (float *)a.d_w + at;
+            if (a.accumulate) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    part[i] += i < n ? to[i] : 0.0f;
+            }
+            store_part<float, 4>(to, n, part);
+        } else {
+            E *const to = (E *)a.d_w + at;
+            E __attribute__((ext_vector_type(4))) half;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                half[i] = (E)(part[i] + (a.accumulate && i < n ? (float)to[i] : 0.0f));
+            store_part<E, 4>(to, n, half);
+        }
     });
 }
 
@@ -157,15 +286,30 @@ static void over_tiles(int64_t tiles, F f)
     in_pieces((tiles + 7) / 8 * 8, f);
 }
 
-template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN, bool DIRECT>
+template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN>
 static void launch_tiles(ProductArgs a, hipStream_t stream)
 {
     a.bounds.per = BM;
     a.across = (a.out_width + BN - 1) / BN;
-    over_tiles(most_pieces(a.bounds.n_slots, a.bounds.n_experts, BM) * a.across, [&](int64_t at, unsigned blocks) {
+    const int64_t tiles = (most_pieces(a.bounds.n_slots, a.bounds.n_experts, BM) * a.across + 7) / 8 * 8;
+    a.blocks = tiles;
+    in_pieces(tiles, [&](int64_t at, unsigned blocks) {
         a.block0 = at;
-        hipLaunchKernelGGL((product_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED, DIRECT>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
+        hipLaunchKernelGGL((product_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
     });
+}
+
+constexpr int kUnits = 256;      // compute units of the card
+template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN>
+static void launch_stream(ProductArgs a, hipStream_t stream)
+{
+    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED> T;
+    constexpr int resident = kUnits * (int)(163840 / (T::lds_bytes + T::rows_bytes * WM * WN + sizeof(PieceTable)));
+    a.bounds.per = BM;
+    a.across = (a.out_width + BN - 1) / BN;
+    const int64_t tiles = (most_pieces(a.bounds.n_slots, a.bounds.n_experts, BM) * a.across + 7) / 8 * 8;
+    a.blocks = tiles < resident ? tiles : resident;
+    hipLaunchKernelGGL((product_stream_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3((unsigned)a.blocks), dim3(WM * WN * 64), 0, stream, a);
 }
 
 // Whether rows can be loaded straight into LDS: 16-byte chunks that are aligned and whole, and a tile's rows within 2^31 bytes.
@@ -181,11 +325,11 @@ static void launch_product(ProductArgs a, hipStream_t stream)
     const bool direct = streams(a.x, a.x_stride, 0, (int64_t)a.in_width * size) &&
                         streams(a.w, a.w_stride, a.w_step, (int64_t)(TURNED ? a.out_width : a.in_width) * size);
     if (!direct)
-        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2, false>(a, stream);
-    else if (a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192)
-        launch_tiles<TYPE, RESULT, TURNED, 256, 256, 2, 4, true>(a, stream);
+        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2>(a, stream);
+    else if (TYPE != FS_F32 && a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192)
+        launch_stream<TYPE == FS_F32 ? FS_BF16 : TYPE, RESULT, TURNED, 256, 256, 2, 4>(a, stream);
     else
-        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2, true>(a, stream);
+        launch_stream<TYPE, RESULT, TURNED, 128, 128, 2, 2>(a, stream);
 }
 
 // How many slots a workgroup of weights_kernel adds up.
@@ -259,7 +403,7 @@ extern "C" int fs_expert_matmul(int64_t n_slots, int32_t n_experts, int32_t in_w
         return FS_OK;
     const int64_t b = (int64_t)type_bytes(type);
     ProductArgs a = {{first, n_experts, (int)n_slots, 0}, (const char *)x, (const char *)w, x_stride * b, w_stride * b, w_step * b, y, y_stride, y_type,
-                     in_width, out_width, 0, nullptr, nullptr, 0};
+                     in_width, out_width, 0, nullptr, nullptr, 0, 0};
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
@@ -292,7 +436,7 @@ extern "C" int fs_expert_matmul_i8(int64_t n_slots, int32_t n_experts, int32_t i
     if (n_slots == 0)
         return FS_OK;
     ProductArgs a = {{first, n_experts, (int)n_slots, 0}, (const char *)q, (const char *)w, q_stride, w_stride, w_step, y, y_stride, y_type,
-                     in_width, out_width, 0, scale, w_scale, 0};
+                     in_width, out_width, 0, scale, w_scale, 0, 0};
     prof_start(kKernPack, stream);
     with_type(y_type, [&](auto t) { launch_product<kI8, decltype(t)::value, false>(a, stream); });
     prof_stop(stream);
