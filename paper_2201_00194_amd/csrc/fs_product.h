@@ -62,27 +62,38 @@ __device__ __forceinline__ int thread_here()
     return t;
 }
 
-constexpr int kStepBytes = 128;      // of the sum, of 1, 2 or 4 bytes an element, that a tile takes at a time
+constexpr int kStepBytes = 64;      // of the sum, of 1, 2 or 4 bytes an element, that a tile takes at a time: a step of the matrix units
+constexpr int kStages = 4;          // steps in LDS
 
-// Where 16 bytes of an operand lie in LDS.  Lanes read a fragment's rows 0 1 2 3, 16 17 18 19, ... of 64 (fragment 0; the
-// next fragment 4 to 7 and so on), so that a lane's results lie side by side; the xor spreads them over the banks.
+// Where 16 bytes of an operand lie in LDS.  The xor spreads what sixteen lanes, or 32 with a transposing read, take at a time over the
+// banks.
 template <int TYPE, bool ALONG, int ROWS>
 struct Place {
     static constexpr int size = Unit16<TYPE>::size;
     static constexpr int chunks = ROWS * kStepBytes / 16;
     static constexpr int per_row = ALONG ? ROWS * size / 16 : kStepBytes / 16;     // 16-byte chunks
-    // Along, 16 bits: a transposing read takes eight bytes of four neighbouring rows, in four places 32 bytes apart.
     static __device__ __forceinline__ int turn(int row)
     {
         if constexpr (!ALONG)
-            return (row >> 1 & 1) | ((row >> 4 & 3) << 1);
+            return -(row >> 4) & 3;      // the four lanes of sixteen or 32 that a read takes together: 0 3 of one fragment half, 1 2 of its neighbour
         else if constexpr (size == 2)
-            return (row & 1) | ((row >> 1 & 1) << (per_row >= 16 ? 3 : 0));
+            return (row & 1) | (row >> 3 & 1) << 1 | (row >> 1 & 1) << 3;
         else
             return 0;
     }
     static __device__ __forceinline__ int at(int row, int chunk) { return (row * per_row + (chunk ^ turn(row))) * 16; }
 };
+// Which of an operand's 64 rows (columns) lane r of sixteen has in fragment f of four: such that a lane's results lie side by side.
+template <int TYPE, bool ALONG>
+__device__ __forceinline__ int member(int f, int r)
+{
+    if constexpr (!ALONG)
+        return (r >> 2) * 16 + f * 4 + (r & 3);
+    else if constexpr (Unit16<TYPE>::size == 2)
+        return (r >> 2) * 16 + (f ^ (r >> 2 & 1)) * 4 + (r & 3);      // both halves of 16 bytes are read at a time
+    else
+        return 4 * r + f;
+}
 
 // 16 bytes of which n elements are there.
 template <int ALIGNED, class E = int> struct Bytes16 {
@@ -121,7 +132,7 @@ struct Tile {
     static constexpr int threads = WM * WN * 64;
     static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;      // fragments of a wavefront
     static constexpr int a_bytes = BM * kStepBytes, b_bytes = BN * kStepBytes, stage_bytes = a_bytes + b_bytes;
-    static constexpr int lds_bytes = 2 * stage_bytes;
+    static constexpr int lds_bytes = kStages * stage_bytes;
     static constexpr int step = kStepBytes / U::size;               // elements of the sum
     Acc acc[MF][NF];
 
@@ -144,7 +155,8 @@ struct Tile {
         {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int q = threadIdx.x + i * threads, row = q / P::per_row, first = q % P::per_row * (16 / U::size);
+                const unsigned q = threadIdx.x + i * threads;
+                const int row = q / P::per_row, first = q % P::per_row * (16 / U::size);
                 if constexpr (ALONG)
                     v[i] = some_bytes<U::size>(o.p + (k0 + row) * o.stride + first * U::size, k0 + row < k_count ? o.count - first : 0);
                 else
@@ -155,7 +167,7 @@ struct Tile {
         {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int q = threadIdx.x + i * threads;
+                const unsigned q = threadIdx.x + i * threads;
                 *(I4 *)(lds + P::at(q / P::per_row, q % P::per_row)) = v[i];
             }
         }
@@ -173,8 +185,8 @@ struct Tile {
         uint64_t base;
         int64_t stride;
         __device__ __forceinline__ Streamed() {}
-        static __device__ __forceinline__ int row_of(int t, int i) { return (t + i * threads) / P::per_row; }
-        static __device__ __forceinline__ int chunk_of(int t, int i) { return (t + i * threads) % P::per_row ^ P::turn(row_of(t, i)); }
+        static __device__ __forceinline__ int row_of(unsigned t, int i) { return (t + i * threads) / P::per_row; }
+        static __device__ __forceinline__ int chunk_of(unsigned t, int i) { return (t + i * threads) % P::per_row ^ P::turn(row_of(t, i)); }
         __device__ __forceinline__ Streamed(const Operand &o) : base((uint64_t)o.p), stride(o.stride)
         {
             const int t = thread_here();
@@ -191,7 +203,7 @@ struct Tile {
                 for (int i = 0; i < N; ++i)
                     from[i] = (ALONG ? row_of(t, i) : chunk_of(t, i) * (16 / U::size)) < left ? from[i] : kNowhere;
             }
-            const I4 buffer = {(int)base, (int)(base >> 32) & 0xffff, (int)kNowhere, 0x00020000};
+            const I4 buffer = {__builtin_amdgcn_readfirstlane((int)base), __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff), (int)kNowhere, 0x00020000};
             const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (threadIdx.x >> 6) * 1024);
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -204,82 +216,176 @@ struct Tile {
     // ---- fragments ----
     // `base`: the wavefront's first row or column.  Fragment f is of block f / 4 of 64 rows; fp32 along: v[4 * block + i][f % 4]
     // are the i-th terms of its lanes instead of v[f][i].
-    template <bool ALONG, int ROWS, int F>
-    static __device__ __forceinline__ void fragments(I4 (&v)[F], const char *lds, int base, int kk)
+    template <bool ALONG, int ROWS>
+    static __device__ __forceinline__ I4 fragment(const char *lds, int base, int f)
     {
         typedef Place<TYPE, ALONG, ROWS> P;
-        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-            if constexpr (!ALONG) {
-                const int row = base + (f >> 2) * 64 + (r >> 2) * 16 + (f & 3) * 4 + (r & 3);
-                v[f] = *(const I4 *)(lds + P::at(row, kk * 4 + g));
-            } else if constexpr (U::size == 4) {
-                v[f] = *(const I4 *)(lds + P::at(kk * 16 + g * 4 + (f & 3), (base + (f >> 2) * 64) / 4 + r));
-            } else {
-                const int chunk = (base + (f >> 2) * 64) / 8 + (r & 3) * 2 + (f >> 1 & 1), k = kk * 32 + g * 8 + (r >> 2);
-                typedef __attribute__((address_space(3))) S4 *Read;
-                const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k, chunk) + (f & 1) * 8));
-                const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k + 4, chunk) + (f & 1) * 8));
-                typedef short S8 __attribute__((ext_vector_type(8)));
-                v[f] = __builtin_bit_cast(I4, S8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-            }
+        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, block = base + (f >> 2) * 64;
+        if constexpr (!ALONG) {
+            return *(const I4 *)(lds + P::at(block + member<TYPE, false>(f & 3, r), g));
+        } else if constexpr (U::size == 4) {
+            return *(const I4 *)(lds + P::at(g * 4 + (f & 3), block / 4 + r));
+        } else {
+            // Lane r brings four elements for lanes 4 (r % 4) to 4 (r % 4) + 3, of row r / 4 of four.
+            const int at = block + member<TYPE, true>(f & 3, (r & 3) * 4), k = g * 8 + (r >> 2);
+            typedef __attribute__((address_space(3))) S4 *Read;
+            const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k, at >> 3) + (at & 4) * 2));
+            const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k + 4, at >> 3) + (at & 4) * 2));
+            typedef short S8 __attribute__((ext_vector_type(8)));
+            return __builtin_bit_cast(I4, S8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
         }
     }
-
+    static __device__ __forceinline__ I4 fragment_a(const char *lds, int i) { return fragment<AT, BM>(lds, (threadIdx.x >> 6) / WN * (BM / WM), i); }
+    static __device__ __forceinline__ I4 fragment_b(const char *lds, int j)
+    {
+        return fragment<BT, BN>(lds + a_bytes, (threadIdx.x >> 6) % WN * (BN / WN), j);
+    }
     __device__ __forceinline__ void multiply(const char *lds)
     {
-        const int wave = threadIdx.x >> 6, m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
+        I4 a[MF], b[NF];
 #pragma unroll
-        for (int kk = 0; kk < kStepBytes / 64; ++kk) {
-            I4 a[MF], b[NF];
-            fragments<AT, BM, MF>(a, lds, m0, kk);
-            fragments<BT, BN, NF>(b, lds + a_bytes, n0, kk);
-            if constexpr (TYPE == FS_F32) {
+        for (int j = 0; j < NF; ++j)
+            b[j] = fragment_b(lds, j);
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+        for (int i = 0; i < MF; ++i)
+            a[i] = fragment_a(lds, i);
+        if constexpr (TYPE == FS_F32) {
 #pragma unroll
-                    for (int i = 0; i < MF; ++i)
-#pragma unroll
-                        for (int j = 0; j < NF; ++j) {
-                            const int x = AT ? a[(i & ~3) + t][i & 3] : a[i][t], y = BT ? b[(j & ~3) + t][j & 3] : b[j][t];
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(y), __int_as_float(x), acc[i][j], 0, 0, 0);
-                        }
-            } else {
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int i = 0; i < MF; ++i)
 #pragma unroll
-                    for (int j = 0; j < NF; ++j)
-                        acc[i][j] = U::step(b[j], a[i], acc[i][j]);
-            }
+                    for (int j = 0; j < NF; ++j) {
+                        const int x = AT ? a[(i & ~3) + t][i & 3] : a[i][t], y = BT ? b[(j & ~3) + t][j & 3] : b[j][t];
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(y), __int_as_float(x), acc[i][j], 0, 0, 0);
+                    }
+        } else {
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+                    acc[i][j] = U::step(b[j], a[i], acc[i][j]);
         }
     }
 
-    // The sums over k_count terms, whose first step is on its way to half `half`; while the last one is multiplied, next() starts
-    // the first step of another tile in the other half.  `kept`: so many younger stores need not have ended.
-    template <int KEPT, class F>
-    __device__ __forceinline__ void stream(char *lds, int &half, Streamed<AT, BM> &sa, Streamed<BT, BN> &sb, int k_count, bool keep, F next)
-    {
-        for (int k0 = 0; k0 < k_count; k0 += step) {
-            // This half has arrived, and the other one has been read, in all wavefronts.
-            if (k0 == 0 && keep)
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(KEPT) : "memory");
-            else
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            char *const now = lds + half * stage_bytes;
-            half ^= 1;
-            if (k0 + step < k_count)
-                load(lds + half * stage_bytes, sa, sb, k_count - k0 - step);
-            else
-                next();
-            multiply(now);
+    // ---- one tile after the other ----
+    // Loads run kAhead steps ahead of the products, across tiles.  Counted are steps since the kernel's start: step n is in place n % kStages.
+    template <int STORES>
+    struct Stream {
+        static constexpr bool kHalves = MF == 8 && TYPE != FS_F32;
+        static constexpr int kAhead = kHalves ? kStages : kStages - 1;
+        static constexpr int kLoads = Streamed<AT, BM>::N + Streamed<BT, BN>::N;      // of a wavefront and a step
+        char *lds;
+        Streamed<AT, BM> sa;
+        Streamed<BT, BN> sb;
+        int left = 0;                   // elements of the sum that the tile being loaded has left
+        int issued = 0, used = 0;       // steps
+        int mark = 0;                   // steps that were issued before the youngest stores, of which there are STORES at least
+        I4 lo[4], b[NF];                // fragments of the step that comes next
+        // next() sets sa, sb and left to another tile's; false if there is none.
+        template <class F>
+        __device__ __forceinline__ void issue(F next)
+        {
+            if (left <= 0 && !next())
+                return;
+            char *const to = lds + (issued & (kStages - 1)) * stage_bytes;
+            sa.load(to, left);
+            sb.load(to + a_bytes, left);
+            left -= step;
+            ++issued;
         }
-    }
-    static __device__ __forceinline__ void load(char *lds, Streamed<AT, BM> &sa, Streamed<BT, BN> &sb, int left)
-    {
-        sa.load(lds, left);
-        sb.load(lds + a_bytes, left);
-    }
+        // Step n has arrived in all wavefronts; loads return in their order, so that what is younger may be on its way.
+        template <int MORE>
+        static __device__ __forceinline__ void wait(int younger)
+        {
+            if (younger >= 3)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(3 * kLoads + MORE) : "memory");
+            else if (younger == 2)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kLoads + MORE) : "memory");
+            else if (younger == 1)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads + MORE) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(MORE) : "memory");
+        }
+        __device__ __forceinline__ void await(int n) const
+        {
+            if (n >= issued)                     // none: all others have come this far
+                wait<63 - 3 * kLoads>(3);
+            else if (n < mark)
+                wait<STORES>(issued - n - 1);
+            else
+                wait<0>(issued - n - 1);
+        }
+        // Begins: the first steps on their way.
+        template <class F>
+        __device__ __forceinline__ void begin(F next)
+        {
+#pragma unroll 1
+            for (int i = 0; i < kAhead; ++i)
+                issue(next);
+            if constexpr (kHalves) {
+                await(0);
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+                    b[j] = fragment_b(lds, j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    lo[i] = fragment_a(lds, i);
+            }
+        }
+        __device__ __forceinline__ const char *place() const { return lds + (used & (kStages - 1)) * stage_bytes; }
+        // The sums of the tile whose steps come next.
+        template <class F>
+        __device__ __forceinline__ void sum(Tile &t, int k_count, F next)
+        {
+            int steps = (k_count + step - 1) / step;
+            if (steps <= 0)
+                return;
+            if constexpr (kHalves) {
+                // Eight fragments of rows, four of columns.  The second four of rows are read while the first four are multiplied; the next
+                // step's first four, and its columns one after the other, while the second four are.
+#pragma unroll 1
+                do {
+                    I4 hi[4];
+                    const char *const now = place();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        hi[i] = fragment_a(now, 4 + i);
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            t.acc[i][j] = U::step(b[j], lo[i], t.acc[i][j]);
+                    await(used + 1);
+                    issue(next);                 // to where this step was, which all have read
+                    ++used;
+                    const char *const then = place();      // behind the last step of all: read, and not used
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        lo[i] = fragment_a(then, i);
+#pragma unroll
+                    for (int j = 0; j < NF; ++j) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            t.acc[4 + i][j] = U::step(b[j], hi[i], t.acc[4 + i][j]);
+                        b[j] = fragment_b(then, j);
+                    }
+                } while (--steps > 0);
+            } else {
+#pragma unroll 1
+                do {
+                    await(used);
+                    issue(next);
+                    t.multiply(place());
+                    ++used;
+                } while (--steps > 0);
+            }
+        }
+        // A tile's results have been stored: by `whole`, with STORES instructions a wavefront at least.
+        __device__ __forceinline__ void stored(bool whole) { mark = whole ? issued : 0; }
+    };
+
+    // The sums over k_count terms, through registers.
     __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int k_count)
     {
         Fetched<AT, BM> fa;
@@ -308,13 +414,12 @@ struct Tile {
     static constexpr int rows_bytes = 2048;
     static __device__ __forceinline__ int row_of(int t, int r, int i)
     {
-        return (t >> 6) / WN * (BM / WM) + (i >> 2) * 64 + (AT && TYPE == FS_F32 ? 4 * r + (i & 3) : (r >> 2) * 16 + (i & 3) * 4 + (r & 3));
+        return (t >> 6) / WN * (BM / WM) + (i >> 2) * 64 + member<TYPE, AT>(i & 3, r);
     }
     template <class S, class G, class M, class P>
     __device__ __forceinline__ void results(char *rows, int t, G of_column, M make, P put) const
     {
         typedef S Chunk __attribute__((ext_vector_type(16 / sizeof(S))));
-        constexpr bool b4 = BT && TYPE == FS_F32;
         constexpr int passes = sizeof(S) == 4 ? 2 : 1, N = 16 / sizeof(S);      // 32 or 64 columns a pass
         char *const own = rows + (t >> 6) * rows_bytes;
         const int n0 = (t >> 6) % WN * (BN / WN), lane = t & 63, g = lane >> 4, r = lane & 15;
@@ -329,7 +434,12 @@ struct Tile {
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        v[b4 ? 4 * e + j : 4 * j + e] = acc[i][block * 4 + j][e];
+                        if constexpr (BT && TYPE == FS_F32)
+                            v[4 * e + j] = acc[i][block * 4 + j][e];
+                        else if constexpr (BT)
+                            v[4 * j + e] = g & 1 ? acc[i][block * 4 + (j ^ 1)][e] : acc[i][block * 4 + j][e];
+                        else
+                            v[4 * j + e] = acc[i][block * 4 + j][e];
                 make(i, v, c, y);
 #pragma unroll
                 for (int pass = 0; pass < passes; ++pass) {
@@ -497,10 +607,12 @@ struct PieceTable {
         const int before = __builtin_amdgcn_readfirstlane(upto[p.expert]);
         p.of = __builtin_amdgcn_readfirstlane(upto[p.expert + 1]) - before;
         p.number = id - before;
-        int begin, end;
-        b.pieces<false, false>(p.expert, begin, end);
-        p.first = __builtin_amdgcn_readfirstlane(begin) + p.number * b.per;
-        p.count = min(b.per, __builtin_amdgcn_readfirstlane(end) - p.first);
+        // Through the scalar cache: a vector load's wait would be one for all operands that are on their way.
+        typedef const __attribute__((address_space(4))) int32_t *Constant;
+        const Constant first = (Constant)(uintptr_t)b.first + p.expert;
+        const int begin = min(max(first[0], 0), b.n_slots), end = max(min(first[1], b.n_slots), begin);
+        p.first = begin + p.number * b.per;
+        p.count = min(b.per, end - p.first);
         return p;
     }
 };

@@ -131,34 +131,31 @@ product_stream_kernel(ProductArgs a)
     int id = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
     if (id >= last)
         return;
-    typename T::template Streamed<false, BM> sx;
-    typename T::template Streamed<TURNED, BN> sw;
-    Piece piece;
-    int n0;
-    const auto start = [&](char *to) {
-        piece = table.find(a.bounds, id / a.across);
-        n0 = id % a.across * BN;
-        sx = {Operand{a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count}};
-        const char *const w = a.w + (int64_t)piece.expert * a.w_step;
-        sw = {Operand{TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0}};
-        T::load(to, sx, sw, a.in_width);
-    };
     constexpr int stores = T::MF * T::NF / 4 * (RESULT == FS_F32 ? 4 : 2);     // of a wavefront and a whole tile, at least
-    bool whole = false;
-    int half = 0;
-    start(lds);
-    while (id < last) {
-        const Piece now = piece;
-        const int now_n0 = n0;
+    typename T::template Stream<stores> stream;
+    stream.lds = lds;
+    int to_load = id - (int)(gridDim.x >> 3);
+    const auto next = [&] {
+        to_load += (int)(gridDim.x >> 3);
+        if (to_load >= last)
+            return false;
+        const Piece piece = table.find(a.bounds, to_load / a.across);
+        const int n0 = to_load % a.across * BN;
+        stream.sa = {Operand{a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count}};
+        const char *const w = a.w + (int64_t)piece.expert * a.w_step;
+        stream.sb = {Operand{TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0}};
+        stream.left = a.in_width;
+        return true;
+    };
+    stream.begin(next);
+    for (; id < last; id += (int)(gridDim.x >> 3)) {
+        const Piece piece = table.find(a.bounds, id / a.across);
+        const int n0 = id % a.across * BN;
         T t;
         t.clear();
-        t.template stream<stores>(lds, half, sx, sw, a.in_width, whole, [&] {
-            id += (int)(gridDim.x >> 3);
-            if (id < last)
-                start(lds + half * T::stage_bytes);
-        });
-        store_product_as<TYPE, RESULT>(a, t, rows, now, now_n0);
-        whole = now.count == BM && now_n0 + BN <= a.out_width;
+        stream.sum(t, a.in_width, next);
+        store_product_as<TYPE, RESULT>(a, t, rows, piece, n0);
+        stream.stored(piece.count == BM && n0 + BN <= a.out_width);
     }
 }
 
@@ -194,13 +191,14 @@ weights_kernel(WeightsArgs a)
     T t;
     t.clear();
     if constexpr (DIRECT) {
-        if (piece.count > 0) {
-            typename T::template Streamed<true, BM> sg(g);
-            typename T::template Streamed<true, BN> sx(x);
-            int half = 0;
-            T::load(lds, sg, sx, piece.count);
-            t.template stream<0>(lds, half, sg, sx, piece.count, false, [] {});
-        }
+        typename T::template Stream<0> stream;
+        stream.lds = lds;
+        stream.sa = {g};
+        stream.sb = {x};
+        stream.left = piece.count;
+        const auto no_more = [] { return false; };
+        stream.begin(no_more);
+        stream.sum(t, piece.count, no_more);
     } else {
         t.run(lds, g, x, piece.count);
     }
@@ -487,8 +485,8 @@ extern "C" int fs_expert_matmul_backward(int64_t n_slots, int32_t n_experts, int
         constexpr int T = decltype(t)::value;
         if (!direct)
             launch_weights<T, 128, 2, 2, false>(a, stream);
-        else if (wide_weights(n_experts, in_width, out_width))
-            launch_weights<T, 256, 2, 4, true>(a, stream);
+        else if (T != FS_F32 && wide_weights(n_experts, in_width, out_width))
+            launch_weights<T == FS_F32 ? FS_BF16 : T, 256, 2, 4, true>(a, stream);
         else
             launch_weights<T, 128, 2, 2, true>(a, stream);
         if (need) {
