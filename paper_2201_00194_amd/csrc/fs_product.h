@@ -62,19 +62,20 @@ __device__ __forceinline__ int thread_here()
     return t;
 }
 
-constexpr int kStepBytes = 64;      // of the sum, of 1, 2 or 4 bytes an element, that a tile takes at a time: a step of the matrix units
-constexpr int kStages = 4;          // steps in LDS
+constexpr int kUnitBytes = 64;      // of the sum, of 1, 2 or 4 bytes an element: a step of the matrix units
 
 // Where 16 bytes of an operand lie in LDS.  The xor spreads what sixteen lanes, or 32 with a transposing read, take at a time over the
 // banks.
-template <int TYPE, bool ALONG, int ROWS>
+template <int TYPE, bool ALONG, int ROWS, int STEP>
 struct Place {
     static constexpr int size = Unit16<TYPE>::size;
-    static constexpr int chunks = ROWS * kStepBytes / 16;
-    static constexpr int per_row = ALONG ? ROWS * size / 16 : kStepBytes / 16;     // 16-byte chunks
+    static constexpr int chunks = ROWS * STEP / 16;
+    static constexpr int per_row = ALONG ? ROWS * size / 16 : STEP / 16;     // 16-byte chunks
     static __device__ __forceinline__ int turn(int row)
     {
-        if constexpr (!ALONG)
+        if constexpr (!ALONG && STEP == 128)
+            return (row >> 1 & 1) | (row >> 4 & 3) << 1;
+        else if constexpr (!ALONG)
             return -(row >> 4) & 3;      // the four lanes of sixteen or 32 that a read takes together: 0 3 of one fragment half, 1 2 of its neighbour
         else if constexpr (size == 2)
             return (row & 1) | (row >> 3 & 1) << 1 | (row >> 1 & 1) << 3;
@@ -124,16 +125,19 @@ __device__ __forceinline__ I4 some_bytes(const char *p, int n)
     return v;
 }
 
-// A tile of BM x BN results by WM x WN wavefronts, each (BM / WM) x (BN / WN) of them, multiples of 64.
-template <int TYPE, int BM, int BN, int WM, int WN, bool AT, bool BT>
+// A tile of BM x BN results by WM x WN wavefronts, each (BM / WM) x (BN / WN) of them, multiples of 64; STEP bytes of the sum (64 or
+// 128) at a time.
+template <int TYPE, int BM, int BN, int WM, int WN, bool AT, bool BT, int STEP>
 struct Tile {
     typedef Unit16<TYPE> U;
     typedef typename U::Acc Acc;
     static constexpr int threads = WM * WN * 64;
     static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;      // fragments of a wavefront
-    static constexpr int a_bytes = BM * kStepBytes, b_bytes = BN * kStepBytes, stage_bytes = a_bytes + b_bytes;
+    static constexpr int a_bytes = BM * STEP, b_bytes = BN * STEP, stage_bytes = a_bytes + b_bytes;
+    static constexpr int kStages = 256 / STEP;                      // steps in LDS
     static constexpr int lds_bytes = kStages * stage_bytes;
-    static constexpr int step = kStepBytes / U::size;               // elements of the sum
+    static constexpr int units = STEP / kUnitBytes;
+    static constexpr int step = STEP / U::size;               // elements of the sum
     Acc acc[MF][NF];
 
     __device__ __forceinline__ void clear()
@@ -148,7 +152,7 @@ struct Tile {
     // ---- operands through registers: any alignment, any sizes ----
     template <bool ALONG, int ROWS>
     struct Fetched {
-        typedef Place<TYPE, ALONG, ROWS> P;
+        typedef Place<TYPE, ALONG, ROWS, STEP> P;
         static constexpr int N = P::chunks / threads;
         I4 v[N];
         __device__ __forceinline__ void load(const Operand &o, int k0, int k_count)
@@ -178,7 +182,7 @@ struct Tile {
     // has an offset past the buffer's end, and zeros come.
     template <bool ALONG, int ROWS>
     struct Streamed {
-        typedef Place<TYPE, ALONG, ROWS> P;
+        typedef Place<TYPE, ALONG, ROWS, STEP> P;
         static constexpr int N = P::chunks / threads;
         static constexpr unsigned kNowhere = 0x80000000u;
         unsigned from[N];
@@ -209,7 +213,7 @@ struct Tile {
             for (int i = 0; i < N; ++i)
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * threads * 16), "v"(from[i]), "s"(buffer)
                              : "memory");
-            base += ALONG ? (uint64_t)step * stride : kStepBytes;
+            base += ALONG ? (uint64_t)step * stride : STEP;
         }
     };
 
@@ -217,17 +221,17 @@ struct Tile {
     // `base`: the wavefront's first row or column.  Fragment f is of block f / 4 of 64 rows; fp32 along: v[4 * block + i][f % 4]
     // are the i-th terms of its lanes instead of v[f][i].
     template <bool ALONG, int ROWS>
-    static __device__ __forceinline__ I4 fragment(const char *lds, int base, int f)
+    static __device__ __forceinline__ I4 fragment(const char *lds, int base, int f, int unit)
     {
-        typedef Place<TYPE, ALONG, ROWS> P;
+        typedef Place<TYPE, ALONG, ROWS, STEP> P;
         const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, block = base + (f >> 2) * 64;
         if constexpr (!ALONG) {
-            return *(const I4 *)(lds + P::at(block + member<TYPE, false>(f & 3, r), g));
+            return *(const I4 *)(lds + P::at(block + member<TYPE, false>(f & 3, r), unit * 4 + g));
         } else if constexpr (U::size == 4) {
-            return *(const I4 *)(lds + P::at(g * 4 + (f & 3), block / 4 + r));
+            return *(const I4 *)(lds + P::at(unit * 16 + g * 4 + (f & 3), block / 4 + r));
         } else {
             // Lane r brings four elements for lanes 4 (r % 4) to 4 (r % 4) + 3, of row r / 4 of four.
-            const int at = block + member<TYPE, true>(f & 3, (r & 3) * 4), k = g * 8 + (r >> 2);
+            const int at = block + member<TYPE, true>(f & 3, (r & 3) * 4), k = unit * 32 + g * 8 + (r >> 2);
             typedef __attribute__((address_space(3))) S4 *Read;
             const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k, at >> 3) + (at & 4) * 2));
             const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k + 4, at >> 3) + (at & 4) * 2));
@@ -235,20 +239,29 @@ struct Tile {
             return __builtin_bit_cast(I4, S8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
         }
     }
-    static __device__ __forceinline__ I4 fragment_a(const char *lds, int i) { return fragment<AT, BM>(lds, (threadIdx.x >> 6) / WN * (BM / WM), i); }
-    static __device__ __forceinline__ I4 fragment_b(const char *lds, int j)
+    static __device__ __forceinline__ I4 fragment_a(const char *lds, int i, int unit)
     {
-        return fragment<BT, BN>(lds + a_bytes, (threadIdx.x >> 6) % WN * (BN / WN), j);
+        return fragment<AT, BM>(lds, (threadIdx.x >> 6) / WN * (BM / WM), i, unit);
+    }
+    static __device__ __forceinline__ I4 fragment_b(const char *lds, int j, int unit)
+    {
+        return fragment<BT, BN>(lds + a_bytes, (threadIdx.x >> 6) % WN * (BN / WN), j, unit);
     }
     __device__ __forceinline__ void multiply(const char *lds)
+    {
+#pragma unroll
+        for (int unit = 0; unit < units; ++unit)
+            multiply(lds, unit);
+    }
+    __device__ __forceinline__ void multiply(const char *lds, int unit)
     {
         I4 a[MF], b[NF];
 #pragma unroll
         for (int j = 0; j < NF; ++j)
-            b[j] = fragment_b(lds, j);
+            b[j] = fragment_b(lds, j, unit);
 #pragma unroll
         for (int i = 0; i < MF; ++i)
-            a[i] = fragment_a(lds, i);
+            a[i] = fragment_a(lds, i, unit);
         if constexpr (TYPE == FS_F32) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -310,7 +323,7 @@ struct Tile {
         __device__ __forceinline__ void await(int n) const
         {
             if (n >= issued)                     // none: all others have come this far
-                wait<63 - 3 * kLoads>(3);
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             else if (n < mark)
                 wait<STORES>(issued - n - 1);
             else
@@ -327,10 +340,10 @@ struct Tile {
                 await(0);
 #pragma unroll
                 for (int j = 0; j < NF; ++j)
-                    b[j] = fragment_b(lds, j);
+                    b[j] = fragment_b(lds, j, 0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    lo[i] = fragment_a(lds, i);
+                    lo[i] = fragment_a(lds, i, 0);
             }
         }
         __device__ __forceinline__ const char *place() const { return lds + (used & (kStages - 1)) * stage_bytes; }
@@ -346,29 +359,35 @@ struct Tile {
                 // step's first four, and its columns one after the other, while the second four are.
 #pragma unroll 1
                 do {
-                    I4 hi[4];
-                    const char *const now = place();
+                    const char *then = place();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        hi[i] = fragment_a(now, 4 + i);
-#pragma unroll
-                    for (int j = 0; j < NF; ++j)
+                    for (int unit = 0; unit < units; ++unit) {
+                        I4 hi[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            t.acc[i][j] = U::step(b[j], lo[i], t.acc[i][j]);
-                    await(used + 1);
-                    issue(next);                 // to where this step was, which all have read
-                    ++used;
-                    const char *const then = place();      // behind the last step of all: read, and not used
+                            hi[i] = fragment_a(then, 4 + i, unit);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        lo[i] = fragment_a(then, i);
+                        for (int j = 0; j < NF; ++j)
 #pragma unroll
-                    for (int j = 0; j < NF; ++j) {
+                            for (int i = 0; i < 4; ++i)
+                                t.acc[i][j] = U::step(b[j], lo[i], t.acc[i][j]);
+                        const int next_unit = (unit + 1) % units;
+                        if (next_unit == 0) {
+                            await(used + 1);
+                            issue(next);             // to where this step was, which all have read
+                            ++used;
+                            then = place();          // behind the last step of all: read, and not used
+                        }
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            t.acc[4 + i][j] = U::step(b[j], hi[i], t.acc[4 + i][j]);
-                        b[j] = fragment_b(then, j);
+                            lo[i] = fragment_a(then, i, next_unit);
+#pragma unroll
+                        for (int j = 0; j < NF; ++j) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                t.acc[4 + i][j] = U::step(b[j], hi[i], t.acc[4 + i][j]);
+                            b[j] = fragment_b(then, j, next_unit);
+                        }
                     }
                 } while (--steps > 0);
             } else {

@@ -14,6 +14,8 @@ struct ProductArgs {
     int64_t block0, blocks;
 };
 
+constexpr int kStreamStep = 128, kWeightStep = 64;      // bytes of a sum that a tile takes at a time
+
 // Results of a tile whose piece and first column are given.
 template <int TYPE, class S, class T>
 __device__ __forceinline__ void store_product(const ProductArgs &a, const T &t, char *rows, const Piece &piece, int n0)
@@ -94,7 +96,7 @@ template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
 __global__ void __launch_bounds__(WM *WN * 64)
 product_kernel(ProductArgs a)
 {
-    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED> T;
+    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED, 128> T;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
     __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
     clear_nobodys<RESULT, T::threads>(a);
@@ -120,7 +122,7 @@ template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
 __global__ void __launch_bounds__(WM *WN * 64)
 product_stream_kernel(ProductArgs a)
 {
-    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED> T;
+    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED, kStreamStep> T;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
     __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
     __shared__ PieceTable table;
@@ -176,7 +178,7 @@ template <int TYPE, int BM, int BN, int WM, int WN, bool DIRECT>
 __global__ void __launch_bounds__(WM *WN * 64)
 weights_kernel(WeightsArgs a)
 {
-    typedef Tile<TYPE, BM, BN, WM, WN, true, true> T;
+    typedef Tile<TYPE, BM, BN, WM, WN, true, true, kWeightStep> T;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
     __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
     const int64_t id = tile_of(a.block0 + blockIdx.x, a.bounds.count<false, true>() * a.tiles);
@@ -301,7 +303,7 @@ constexpr int kUnits = 256;      // compute units of the card
 template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN>
 static void launch_stream(ProductArgs a, hipStream_t stream)
 {
-    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED> T;
+    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED, kStreamStep> T;
     constexpr int resident = kUnits * (int)(163840 / (T::lds_bytes + T::rows_bytes * WM * WN + sizeof(PieceTable)));
     a.bounds.per = BM;
     a.across = (a.out_width + BN - 1) / BN;
