@@ -506,23 +506,19 @@ __device__ __forceinline__ void store_part(S *p, int n, const S __attribute__((e
 struct Piece {
     int expert, first, count;      // its slots
     int number, of;                // which of its expert's pieces, and of how many
-    int before;                    // pieces of earlier experts that have more than one
-    int64_t pieces;                // of all experts
 };
 struct Bounds {
     const int32_t *first;
     int n_experts, n_slots, per;
-    // Nobody's slots are the pieces of one expert more (`nobody`); `each`: an expert without slots has an empty piece.
-    template <bool NOBODY, bool EACH>
+    // The pieces of an expert (none behind the last one).
     __device__ __forceinline__ int pieces(int e, int &begin, int &end) const
     {
-        const int last = NOBODY ? n_experts : n_experts - 1;
-        if (e > last)
+        begin = end = 0;
+        if (e >= n_experts)
             return 0;
         begin = min(max(first[e], 0), n_slots);
-        end = e == n_experts ? n_slots : max(min(first[e + 1], n_slots), begin);
-        const int n = (int)(((int64_t)end - begin + per - 1) / per);
-        return EACH ? max(n, 1) : n;
+        end = max(min(first[e + 1], n_slots), begin);
+        return (int)(((int64_t)end - begin + per - 1) / per);
     }
     // Every lane's sum of the lanes up to it.
     static __device__ __forceinline__ int sum_to(int v)
@@ -535,62 +531,53 @@ struct Bounds {
         }
         return v;
     }
-    template <bool NOBODY, bool EACH>
-    __device__ __forceinline__ int64_t count() const
-    {
-        int64_t all = 0;
-        for (int e0 = 0; e0 <= n_experts; e0 += 64) {
-            int begin, end;
-            all += __builtin_amdgcn_readlane(sum_to(pieces<NOBODY, EACH>(e0 + (threadIdx.x & 63), begin, end)), 63);
-        }
-        return all;
-    }
-    // The piece `id` of all; its `count` is -1 where there is none.
-    template <bool NOBODY, bool EACH>
-    __device__ __forceinline__ Piece find(int64_t id) const
-    {
-        Piece p = {0, 0, -1, 0, 0, 0, 0};
-        const int lane = threadIdx.x & 63;
-        int64_t at = 0;
-        int before = 0;
-        for (int e0 = 0; e0 <= n_experts; e0 += 64) {
-            int begin = 0, end = 0;
-            const int n = pieces<NOBODY, EACH>(e0 + lane, begin, end), upto = sum_to(n), all = __builtin_amdgcn_readlane(upto, 63);
-            const int many = n > 1 ? n : 0, many_upto = EACH ? sum_to(many) : 0;
-            if (id < at + all) {
-                const int owner = __builtin_ctzll(__ballot(id < at + upto));
-                p.expert = e0 + owner;
-                p.of = __builtin_amdgcn_readlane(n, owner);
-                p.number = (int)(id - at) - (__builtin_amdgcn_readlane(upto, owner) - p.of);
-                p.first = __builtin_amdgcn_readlane(begin, owner) + p.number * per;
-                p.count = min(per, __builtin_amdgcn_readlane(end, owner) - p.first);
-                p.before = before + (EACH ? __builtin_amdgcn_readlane(many_upto - many, owner) : 0);
-                return p;
-            }
-            at += all;
-            before += EACH ? __builtin_amdgcn_readlane(many_upto, 63) : 0;
-        }
-        return p;
-    }
 };
 
-// The same pieces (none of nobody's), listed once by a workgroup that looks for several.
+// The pieces of all experts in a row, listed once by a workgroup.  SORTED: the experts with the most slots first, and an expert without
+// slots has an empty piece.
+template <bool SORTED>
 struct PieceTable {
-    int upto[FS_MAX_EXPERTS + 1];      // pieces of the experts before
+    int upto[FS_MAX_EXPERTS + 1];                        // pieces of the experts before
+    int16_t order[SORTED ? FS_MAX_EXPERTS : 1];
     int waves[16];
+    __device__ __forceinline__ int expert_at(int place) const { return SORTED ? order[place] : place; }
     // By all THREADS of the workgroup; the number of pieces.
-    template <int THREADS, bool EACH>
+    template <int THREADS>
     __device__ __forceinline__ int fill(const Bounds &b)
     {
         constexpr int most = (FS_MAX_EXPERTS + THREADS - 1) / THREADS;
         const int each = (b.n_experts + THREADS - 1) / THREADS, e0 = threadIdx.x * each, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         int n[most], sum = 0;
+        if constexpr (SORTED) {
+            int begin, end;
+#pragma unroll
+            for (int u = 0; u < most; ++u)
+                if (u < each && e0 + u < b.n_experts) {
+                    b.pieces(e0 + u, begin, end);
+                    n[u] = upto[e0 + u] = end - begin;
+                }
+            __syncthreads();
+            int before[most] = {};
+            for (int e = 0; e < b.n_experts; ++e) {
+                const int other = upto[e];
+#pragma unroll
+                for (int u = 0; u < most; ++u)
+                    before[u] += u < each && (other > n[u] || (other == n[u] && e < e0 + u)) ? 1 : 0;
+            }
+#pragma unroll
+            for (int u = 0; u < most; ++u)
+                if (u < each && e0 + u < b.n_experts)
+                    order[before[u]] = (int16_t)(e0 + u);
+            __syncthreads();
+        }
 #pragma unroll
         for (int u = 0; u < most; ++u) {
             n[u] = 0;
             if (u < each && e0 + u < b.n_experts) {
-                int from, to;
-                n[u] = b.pieces<false, EACH>(e0 + u, from, to);
+                int begin, end;
+                n[u] = b.pieces(expert_at(e0 + u), begin, end);
+                if constexpr (SORTED)
+                    n[u] = max(n[u], 1);
             }
             sum += n[u];
         }
@@ -621,10 +608,11 @@ struct PieceTable {
         const int lane = threadIdx.x & 63, each = (b.n_experts + 63) >> 6;
         const int block = __popcll(__ballot(lane * each < b.n_experts && upto[min(lane * each, b.n_experts)] <= id)) - 1;
         const int e = block * each + lane, in_block = __popcll(__ballot(lane < each && e < b.n_experts && upto[min(e, b.n_experts)] <= id)) - 1;
-        Piece p = {};
-        p.expert = __builtin_amdgcn_readfirstlane(block * each + in_block);
-        const int before = __builtin_amdgcn_readfirstlane(upto[p.expert]);
-        p.of = __builtin_amdgcn_readfirstlane(upto[p.expert + 1]) - before;
+        const int place = __builtin_amdgcn_readfirstlane(block * each + in_block);
+        Piece p;
+        p.expert = __builtin_amdgcn_readfirstlane(expert_at(place));
+        const int before = __builtin_amdgcn_readfirstlane(upto[place]);
+        p.of = __builtin_amdgcn_readfirstlane(upto[place + 1]) - before;
         p.number = id - before;
         // Through the scalar cache: a vector load's wait would be one for all operands that are on their way.
         typedef const __attribute__((address_space(4))) int32_t *Constant;
@@ -635,14 +623,6 @@ struct PieceTable {
         return p;
     }
 };
-
-// Workgroup b of a launch runs on XCD b % 8.  Neighbouring tiles share operands, so an XCD, which has an L2 cache of its own, gets
-// neighbouring ones: the tile of workgroup b, of `tiles`; -1 if none.
-__device__ __forceinline__ int64_t tile_of(int64_t b, int64_t tiles)
-{
-    const int64_t each = (tiles + 7) >> 3, id = (b & 7) * each + (b >> 3);
-    return (b >> 3) < each && id < tiles ? id : -1;
-}
 
 }  // namespace fs
 #endif

@@ -11,7 +11,6 @@ struct ProductArgs {
     int64_t y_stride;                        // elements
     int32_t y_type, in_width, out_width, across;      // tiles across a row of results
     const float *scale, *w_scale;            // of 8-bit operands
-    int64_t block0, blocks;
 };
 
 constexpr int kStreamStep = 128, kWeightStep = 64;      // bytes of a sum that a tile takes at a time
@@ -78,7 +77,7 @@ __device__ __forceinline__ void clear_nobodys_as(const ProductArgs &a)
     constexpr int N = 16 / sizeof(S), rows = THREADS / 64;
     const S __attribute__((ext_vector_type(N))) zero = {};
     const int from = min(max(a.bounds.first[a.bounds.n_experts], 0), a.bounds.n_slots);
-    for (int64_t s = from + (a.block0 + blockIdx.x) * rows + threadIdx.x / 64; s < a.bounds.n_slots; s += a.blocks * rows)
+    for (int64_t s = from + (int64_t)blockIdx.x * rows + threadIdx.x / 64; s < a.bounds.n_slots; s += (int64_t)gridDim.x * rows)
         for (int c = (threadIdx.x & 63) * N; c < a.out_width; c += 64 * N)
             store_part<S, N>((S *)a.y + s * a.y_stride + c, a.out_width - c, zero);
 }
@@ -91,7 +90,20 @@ __device__ __forceinline__ void clear_nobodys(const ProductArgs &a)
         clear_nobodys_as<typename Element<RESULT>::type, THREADS>(a);
 }
 
-// A workgroup makes BM slots of one expert times BN columns.
+// The tiles that a workgroup makes, of `tiles`: an XCD, whose L2 cache is its own, takes neighbouring ones.  Results that fit the card's
+// memory have fewer than 2^31 tiles.
+struct Share {
+    int id, last, by;
+    __device__ __forceinline__ explicit Share(int tiles)
+    {
+        const int each = (tiles + 7) >> 3, xcd = (int)(blockIdx.x & 7);
+        last = min((xcd + 1) * each, tiles);
+        id = xcd * each + (int)(blockIdx.x >> 3);
+        by = (int)(gridDim.x >> 3);
+    }
+};
+
+// A workgroup makes BM slots of one expert times BN columns, and then others.
 template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
 __global__ void __launch_bounds__(WM *WN * 64)
 product_kernel(ProductArgs a)
@@ -99,21 +111,20 @@ product_kernel(ProductArgs a)
     typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED, 128> T;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
     __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
+    __shared__ PieceTable<false> table;
     clear_nobodys<RESULT, T::threads>(a);
-    const int64_t id = tile_of(a.block0 + blockIdx.x, a.bounds.count<false, false>() * a.across);
-    if (id < 0)
-        return;
-    const Piece piece = a.bounds.find<false, false>(id / a.across);
-    const int n0 = (int)(id % a.across) * BN;
-    if (piece.count < 0)
-        return;
-    T t;
-    t.clear();
-    const Operand x = {a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count};
-    const char *const w = a.w + (int64_t)piece.expert * a.w_step;
-    const Operand b = {TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0};
-    t.run(lds, x, b, a.in_width);
-    store_product_as<TYPE, RESULT>(a, t, rows, piece, n0);
+    for (Share s(table.template fill<T::threads>(a.bounds) * a.across); s.id < s.last; s.id += s.by) {
+        const Piece piece = table.find(a.bounds, s.id / a.across);
+        const int n0 = s.id % a.across * BN;
+        T t;
+        t.clear();
+        const Operand x = {a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count};
+        const char *const w = a.w + (int64_t)piece.expert * a.w_step;
+        const Operand b = {TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0};
+        t.run(lds, x, b, a.in_width);
+        store_product_as<TYPE, RESULT>(a, t, rows, piece, n0);
+        __syncthreads();      // the last step has been read
+    }
 }
 
 // The same with operands straight to LDS, one tile after the other: the first step of the next tile is on its way while the last
@@ -125,21 +136,18 @@ product_stream_kernel(ProductArgs a)
     typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED, kStreamStep> T;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
     __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
-    __shared__ PieceTable table;
+    __shared__ PieceTable<false> table;
     clear_nobodys<RESULT, T::threads>(a);
-    // Results that fit the card's memory have fewer than 2^31 tiles.  An XCD, whose L2 cache is its own, takes neighbouring ones.
-    const int tiles = table.fill<T::threads, false>(a.bounds) * a.across, each = (tiles + 7) >> 3;
-    const int last = min((int)((blockIdx.x & 7) + 1) * each, tiles);
-    int id = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
-    if (id >= last)
+    Share s(table.template fill<T::threads>(a.bounds) * a.across);
+    if (s.id >= s.last)
         return;
     constexpr int stores = T::MF * T::NF / 4 * (RESULT == FS_F32 ? 4 : 2);     // of a wavefront and a whole tile, at least
     typename T::template Stream<stores> stream;
     stream.lds = lds;
-    int to_load = id - (int)(gridDim.x >> 3);
+    int to_load = s.id - s.by;
     const auto next = [&] {
-        to_load += (int)(gridDim.x >> 3);
-        if (to_load >= last)
+        to_load += s.by;
+        if (to_load >= s.last)
             return false;
         const Piece piece = table.find(a.bounds, to_load / a.across);
         const int n0 = to_load % a.across * BN;
@@ -150,9 +158,9 @@ product_stream_kernel(ProductArgs a)
         return true;
     };
     stream.begin(next);
-    for (; id < last; id += (int)(gridDim.x >> 3)) {
-        const Piece piece = table.find(a.bounds, id / a.across);
-        const int n0 = id % a.across * BN;
+    for (; s.id < s.last; s.id += s.by) {
+        const Piece piece = table.find(a.bounds, s.id / a.across);
+        const int n0 = s.id % a.across * BN;
         T t;
         t.clear();
         stream.sum(t, a.in_width, next);
@@ -167,43 +175,20 @@ struct WeightsArgs {
     int64_t g_stride, x_stride;              // bytes
     void *d_w;
     int64_t d_w_stride, d_w_step;            // elements
-    int32_t d_w_type, in_width, out_width, across, tiles, accumulate;
+    int32_t d_w_type, in_width, out_width, across, tiles, accumulate;      // tiles across and of a matrix
     float *work;
-    int64_t block0;
 };
 
-// A workgroup makes BM x BN of an expert's gradient over one piece of its slots: the gradient itself where the piece is all of them,
-// else a partial sum, whose place is that of the piece among all of experts with several.
-template <int TYPE, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ void __launch_bounds__(WM *WN * 64)
-weights_kernel(WeightsArgs a)
+// Where the partial sum of a piece lies, of an expert that has several: such experts have more than bounds.per slots, so that of each
+// bounds.per slots at most two such pieces begin there, a first one and another expert's last.
+__device__ __forceinline__ float *partial_sum(const WeightsArgs &a, int first, int number)
 {
-    typedef Tile<TYPE, BM, BN, WM, WN, true, true, kWeightStep> T;
-    __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
-    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
-    const int64_t id = tile_of(a.block0 + blockIdx.x, a.bounds.count<false, true>() * a.tiles);
-    if (id < 0)
-        return;
-    const Piece piece = a.bounds.find<false, true>(id / a.tiles);
-    const int tile = (int)(id % a.tiles), m0 = tile / a.across * BM, n0 = tile % a.across * BN;
-    if (piece.count < 0)
-        return;
-    const Operand g = {a.g + (int64_t)piece.first * a.g_stride + (int64_t)m0 * T::U::size, a.g_stride, a.out_width - m0};
-    const Operand x = {a.x + (int64_t)piece.first * a.x_stride + (int64_t)n0 * T::U::size, a.x_stride, a.in_width - n0};
-    T t;
-    t.clear();
-    if constexpr (DIRECT) {
-        typename T::template Stream<0> stream;
-        stream.lds = lds;
-        stream.sa = {g};
-        stream.sb = {x};
-        stream.left = piece.count;
-        const auto no_more = [] { return false; };
-        stream.begin(no_more);
-        stream.sum(t, piece.count, no_more);
-    } else {
-        t.run(lds, g, x, piece.count);
-    }
+    return a.work + ((int64_t)(first / a.bounds.per) * 2 + (number > 0 ? 1 : 0)) * a.out_width * a.in_width;
+}
+
+template <int TYPE, class T>
+__device__ __forceinline__ void store_weights(const WeightsArgs &a, const T &t, char *rows, const Piece &piece, int m0, int n0)
+{
     const int thread = thread_here();
     const auto as_they_are = [](int, const auto &v, int, float (&out)[16]) {
 #pragma unroll
@@ -211,7 +196,7 @@ weights_kernel(WeightsArgs a)
             out[e] = v[e];
     };
     if (piece.of > 1) {
-        float *const to = a.work + (piece.before + (int64_t)piece.number) * a.out_width * a.in_width;
+        float *const to = partial_sum(a, piece.first, piece.number);
         t.template results<float>(rows, thread, [](int) { return 0; }, as_they_are, [&](int row, int column, const auto &part) {
             if (m0 + row < a.out_width)
                 store_part<float, 4>(to + (m0 + row) * (int64_t)a.in_width + n0 + column, a.in_width - n0 - column, part);
@@ -243,7 +228,83 @@ weights_kernel(WeightsArgs a)
     });
 }
 
-// The partial sums of an expert's pieces, in their order, in 64 bits.
+// A workgroup makes BM x BN of an expert's gradient over one piece of its slots, and then others: the gradient itself where the
+// piece is all of them, else a partial sum.  Pieces differ in length.  The longest come first, and each round of tiles goes to the XCDs the
+// other way round than the one before, so that all have about the same to do; an XCD's tiles of a round are neighbours.
+template <int TYPE, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ void __launch_bounds__(WM *WN * 64)
+weights_kernel(WeightsArgs a)
+{
+    typedef Tile<TYPE, BM, BN, WM, WN, true, true, kWeightStep> T;
+    __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
+    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
+    __shared__ PieceTable<true> table;
+    const int tiles = table.template fill<T::threads>(a.bounds) * a.tiles, per_xcd = (int)(gridDim.x >> 3), xcd = (int)(blockIdx.x & 7);
+    const auto tile_of_round = [&](int round) {
+        return (round * 8 + (round & 1 ? 7 - xcd : xcd)) * per_xcd + (int)(blockIdx.x >> 3);
+    };
+    const int rounds = (tiles + (int)gridDim.x - 1) / (int)gridDim.x;
+    struct Place2 {
+        Piece piece;
+        int m0, n0;
+    };
+    const auto place_of = [&](int id) {
+        const int tile = id % a.tiles;
+        return Place2{table.find(a.bounds, id / a.tiles), tile / a.across * BM, tile % a.across * BN};
+    };
+    const auto operand_g = [&](const Place2 &p) {
+        return Operand{a.g + (int64_t)p.piece.first * a.g_stride + (int64_t)p.m0 * T::U::size, a.g_stride, a.out_width - p.m0};
+    };
+    const auto operand_x = [&](const Place2 &p) {
+        return Operand{a.x + (int64_t)p.piece.first * a.x_stride + (int64_t)p.n0 * T::U::size, a.x_stride, a.in_width - p.n0};
+    };
+    if constexpr (DIRECT) {
+        typename T::template Stream<T::MF * T::NF / 4 * 4> stream;
+        stream.lds = lds;
+        int to_load = -1;
+        const auto next = [&] {
+            while (++to_load < rounds) {
+                const int id = tile_of_round(to_load);
+                if (id >= tiles)
+                    continue;
+                const Place2 p = place_of(id);
+                if (p.piece.count <= 0)
+                    continue;
+                stream.sa = {operand_g(p)};
+                stream.sb = {operand_x(p)};
+                stream.left = p.piece.count;
+                return true;
+            }
+            return false;
+        };
+        stream.begin(next);
+        for (int round = 0; round < rounds; ++round) {
+            const int id = tile_of_round(round);
+            if (id >= tiles)
+                continue;
+            const Place2 p = place_of(id);
+            T t;
+            t.clear();
+            stream.sum(t, p.piece.count, next);
+            store_weights<TYPE>(a, t, rows, p.piece, p.m0, p.n0);
+            stream.stored(!a.accumulate && a.d_w_type == FS_F32 && p.m0 + BM <= a.out_width && p.n0 + BN <= a.in_width);
+        }
+    } else {
+        for (int round = 0; round < rounds; ++round) {
+            const int id = tile_of_round(round);
+            if (id >= tiles)
+                continue;
+            const Place2 p = place_of(id);
+            T t;
+            t.clear();
+            t.run(lds, operand_g(p), operand_x(p), p.piece.count);
+            store_weights<TYPE>(a, t, rows, p.piece, p.m0, p.n0);
+            __syncthreads();      // the last step has been read
+        }
+    }
+}
+
+// The partial sums of an expert's pieces, in their order, in 64 bits: a wavefront to a row of the gradient.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 weights_join_kernel(WeightsArgs a)
@@ -251,65 +312,60 @@ weights_join_kernel(WeightsArgs a)
     typedef typename Element<TYPE>::type E;
     const int expert = (int)(blockIdx.x / a.tiles);
     int begin, end;
-    const int pieces = a.bounds.pieces<false, true>(expert, begin, end);
+    const int pieces = a.bounds.pieces(expert, begin, end);
     if (pieces <= 1)
         return;
-    int before = 0;
-    for (int e0 = 0; e0 < expert; e0 += 64) {
-        const int e = e0 + (threadIdx.x & 63);
-        int b, c;
-        const int n = e < expert ? a.bounds.pieces<false, true>(e, b, c) : 0;
-        before += __builtin_amdgcn_readlane(Bounds::sum_to(n > 1 ? n : 0), 63);
-    }
-    const int64_t all = (int64_t)a.out_width * a.in_width;
-    for (int64_t i = (blockIdx.x % a.tiles) * (int64_t)256 + threadIdx.x; i < all; i += a.tiles * (int64_t)256) {
-        const int64_t at = expert * a.d_w_step + i / a.in_width * a.d_w_stride + i % a.in_width;
-        const bool wide = TYPE != FS_F32 && a.d_w_type == FS_F32;
-        double sum = 0;
-        if (a.accumulate)
-            sum = wide ? ((const float *)a.d_w)[at] : (float)((const E *)a.d_w)[at];
-        for (int p = 0; p < pieces; ++p)
-            sum += a.work[(before + (int64_t)p) * all + i];
-        if (wide)
-            ((float *)a.d_w)[at] = (float)sum;
-        else
-            ((E *)a.d_w)[at] = (E)(float)sum;
-    }
+    const bool wide = TYPE == FS_F32 || a.d_w_type == FS_F32;
+    for (int row = (int)(blockIdx.x % a.tiles) * 4 + (int)(threadIdx.x >> 6); row < a.out_width; row += a.tiles * 4)
+        for (int c = (threadIdx.x & 63) * 4; c < a.in_width; c += 256) {
+            const int64_t at = expert * a.d_w_step + row * a.d_w_stride + c;
+            const int n = a.in_width - c;
+            double sum[4] = {};
+            if (a.accumulate) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < n)
+                        sum[i] = wide ? ((const float *)a.d_w)[at + i] : (float)((const E *)a.d_w)[at + i];
+            }
+            for (int p = 0; p < pieces; ++p) {
+                float v[4];
+                load_chunk(partial_sum(a, begin + p * a.bounds.per, p) + (int64_t)row * a.in_width + c, n, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sum[i] += v[i];
+            }
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = (float)sum[i];
+            if (wide)
+                store_chunk<4>((float *)a.d_w + at, n, v);
+            else
+                store_chunk<4>((E *)a.d_w + at, n, v);
+        }
 }
 
-// At most so many pieces of `per`.
-static int64_t most_pieces(int64_t n_slots, int32_t n_experts, int64_t per) { return n_slots / per + n_experts + 1; }
-
-template <class F>
-static void over_tiles(int64_t tiles, F f)
+// Workgroups of a launch for at most `pieces` pieces of `tiles` tiles, of which a compute unit holds as many as its LDS does.
+constexpr int kUnits = 256;      // compute units of the card
+template <class T, class Table>
+static unsigned workgroups(int64_t n_slots, int32_t n_experts, int64_t per, int64_t tiles)
 {
-    in_pieces((tiles + 7) / 8 * 8, f);
+    constexpr int resident = kUnits * (int)(163840 / (T::lds_bytes + T::rows_bytes * (T::threads / 64) + sizeof(Table)));
+    const int64_t most = ((n_slots / per + n_experts) * tiles + 7) / 8 * 8;
+    return (unsigned)(most < resident ? most : resident);
 }
 
-template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN>
+template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN, bool DIRECT>
 static void launch_tiles(ProductArgs a, hipStream_t stream)
 {
     a.bounds.per = BM;
     a.across = (a.out_width + BN - 1) / BN;
-    const int64_t tiles = (most_pieces(a.bounds.n_slots, a.bounds.n_experts, BM) * a.across + 7) / 8 * 8;
-    a.blocks = tiles;
-    in_pieces(tiles, [&](int64_t at, unsigned blocks) {
-        a.block0 = at;
+    const unsigned blocks =
+        workgroups<Tile<TYPE, BM, BN, WM, WN, false, TURNED, 128>, PieceTable<false>>(a.bounds.n_slots, a.bounds.n_experts, BM, a.across);
+    if constexpr (DIRECT)
+        hipLaunchKernelGGL((product_stream_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
+    else
         hipLaunchKernelGGL((product_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
-    });
-}
-
-constexpr int kUnits = 256;      // compute units of the card
-template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN>
-static void launch_stream(ProductArgs a, hipStream_t stream)
-{
-    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED, kStreamStep> T;
-    constexpr int resident = kUnits * (int)(163840 / (T::lds_bytes + T::rows_bytes * WM * WN + sizeof(PieceTable)));
-    a.bounds.per = BM;
-    a.across = (a.out_width + BN - 1) / BN;
-    const int64_t tiles = (most_pieces(a.bounds.n_slots, a.bounds.n_experts, BM) * a.across + 7) / 8 * 8;
-    a.blocks = tiles < resident ? tiles : resident;
-    hipLaunchKernelGGL((product_stream_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3((unsigned)a.blocks), dim3(WM * WN * 64), 0, stream, a);
 }
 
 // Whether rows can be loaded straight into LDS: 16-byte chunks that are aligned and whole, and a tile's rows within 2^31 bytes.
@@ -325,11 +381,11 @@ static void launch_product(ProductArgs a, hipStream_t stream)
     const bool direct = streams(a.x, a.x_stride, 0, (int64_t)a.in_width * size) &&
                         streams(a.w, a.w_stride, a.w_step, (int64_t)(TURNED ? a.out_width : a.in_width) * size);
     if (!direct)
-        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2>(a, stream);
+        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2, false>(a, stream);
     else if (TYPE != FS_F32 && a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192)
-        launch_stream<TYPE == FS_F32 ? FS_BF16 : TYPE, RESULT, TURNED, 256, 256, 2, 4>(a, stream);
+        launch_tiles<TYPE == FS_F32 ? FS_BF16 : TYPE, RESULT, TURNED, 256, 256, 2, 4, true>(a, stream);
     else
-        launch_stream<TYPE, RESULT, TURNED, 128, 128, 2, 2>(a, stream);
+        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2, true>(a, stream);
 }
 
 // How many slots a workgroup of weights_kernel adds up.
@@ -340,7 +396,7 @@ static bool wide_weights(int64_t n_experts, int64_t in_width, int64_t out_width)
 static int piece_of_weights(int64_t n_slots, int32_t n_experts, int64_t in_width, int64_t out_width)
 {
     const int side = wide_weights(n_experts, in_width, out_width) ? 256 : 128;
-    int64_t per = n_slots * ((in_width + side - 1) / side * ((out_width + side - 1) / side)) / 512;
+    int64_t per = n_slots * ((in_width + side - 1) / side * ((out_width + side - 1) / side)) / 256;
     per = per < 1024 ? 1024 : per > 32768 ? 32768 : per;
     return (int)((per + 255) / 256 * 256);
 }
@@ -350,10 +406,9 @@ static void launch_weights(WeightsArgs a, hipStream_t stream)
 {
     a.across = (a.in_width + SIDE - 1) / SIDE;
     a.tiles = a.across * ((a.out_width + SIDE - 1) / SIDE);
-    over_tiles(most_pieces(a.bounds.n_slots, a.bounds.n_experts, a.bounds.per) * a.tiles, [&](int64_t at, unsigned blocks) {
-        a.block0 = at;
-        hipLaunchKernelGGL((weights_kernel<TYPE, SIDE, SIDE, WM, WN, DIRECT>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
-    });
+    const unsigned blocks =
+        workgroups<Tile<TYPE, SIDE, SIDE, WM, WN, true, true, kWeightStep>, PieceTable<true>>(a.bounds.n_slots, a.bounds.n_experts, a.bounds.per, a.tiles);
+    hipLaunchKernelGGL((weights_kernel<TYPE, SIDE, SIDE, WM, WN, DIRECT>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
 }
 
 static int check_shape(const char *who, int64_t n_slots, int32_t n_experts, int32_t in_width, int32_t out_width)
@@ -362,7 +417,13 @@ static int check_shape(const char *who, int64_t n_slots, int32_t n_experts, int3
         return fail(FS_EINVAL, "%s: %lld slots: 0 to 2^31 - 1 are taken", who, (long long)n_slots);
     FS_TRY(check_experts(who, n_experts));
     FS_TRY(check_width(who, in_width));
-    return check_width(who, out_width);
+    FS_TRY(check_width(who, out_width));
+    // Tiles are counted in 32 bits: more of them, of 128 x 128 results, would be more than the card holds.
+    const int64_t in_tiles = ((int64_t)in_width + 127) / 128, out_tiles = ((int64_t)out_width + 127) / 128;
+    const int64_t rows = n_slots / 128 + n_experts, wide = in_tiles > out_tiles ? in_tiles : out_tiles;
+    if (rows > INT32_MAX / wide || (n_slots / 1024 + n_experts) > INT32_MAX / (in_tiles * out_tiles))
+        return fail(FS_EUNSUPPORTED, "%s: %lld slots of %d experts, %d to %d columns", who, (long long)n_slots, n_experts, in_width, out_width);
+    return FS_OK;
 }
 // n_experts matrices, `step` apart.
 static int check_matrices(const char *who, const char *what, const void *p, int64_t rows, int64_t width, int32_t type, int64_t stride, int64_t step,
@@ -403,7 +464,7 @@ extern "C" int fs_expert_matmul(int64_t n_slots, int32_t n_experts, int32_t in_w
         return FS_OK;
     const int64_t b = (int64_t)type_bytes(type);
     ProductArgs a = {{first, n_experts, (int)n_slots, 0}, (const char *)x, (const char *)w, x_stride * b, w_stride * b, w_step * b, y, y_stride, y_type,
-                     in_width, out_width, 0, nullptr, nullptr, 0, 0};
+                     in_width, out_width, 0, nullptr, nullptr};
     prof_start(kKernPack, stream);
     with_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
@@ -436,7 +497,7 @@ extern "C" int fs_expert_matmul_i8(int64_t n_slots, int32_t n_experts, int32_t i
     if (n_slots == 0)
         return FS_OK;
     ProductArgs a = {{first, n_experts, (int)n_slots, 0}, (const char *)q, (const char *)w, q_stride, w_stride, w_step, y, y_stride, y_type,
-                     in_width, out_width, 0, scale, w_scale, 0, 0};
+                     in_width, out_width, 0, scale, w_scale};
     prof_start(kKernPack, stream);
     with_type(y_type, [&](auto t) { launch_product<kI8, decltype(t)::value, false>(a, stream); });
     prof_stop(stream);
@@ -480,7 +541,7 @@ extern "C" int fs_expert_matmul_backward(int64_t n_slots, int32_t n_experts, int
         return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, need);
     const int64_t b = (int64_t)type_bytes(type);
     WeightsArgs a = {{first, n_experts, (int)n_slots, piece_of_weights(n_slots, n_experts, in_width, out_width)}, (const char *)d_y, (const char *)x,
-                     d_y_stride * b, x_stride * b, d_w, d_w_stride, d_w_step, d_w_type, in_width, out_width, 0, 0, accumulate, (float *)work, 0};
+                     d_y_stride * b, x_stride * b, d_w, d_w_stride, d_w_step, d_w_type, in_width, out_width, 0, 0, accumulate, (float *)work};
     const bool direct = streams(d_y, a.g_stride, 0, out_width * b) && streams(x, a.x_stride, 0, in_width * b);
     prof_start(kKernTrainOther, stream);
     with_type(type, [&](auto t) {
@@ -492,7 +553,7 @@ extern "C" int fs_expert_matmul_backward(int64_t n_slots, int32_t n_experts, int
         else
             launch_weights<T, 128, 2, 2, true>(a, stream);
         if (need) {
-            const int64_t wanted = ((int64_t)in_width * out_width + 1023) / 1024, most = 4096 / n_experts + 1;
+            const int64_t wanted = ((int64_t)out_width + 3) / 4, most = 8192 / n_experts + 1;
             a.tiles = (int32_t)(wanted < most ? wanted : most);
             hipLaunchKernelGGL(weights_join_kernel<T>, dim3((unsigned)(a.tiles * n_experts)), dim3(256), 0, stream, a);
         }
