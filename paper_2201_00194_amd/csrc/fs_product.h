@@ -77,6 +77,8 @@ struct Place {
             return (row >> 1 & 1) | (row >> 4 & 3) << 1;
         else if constexpr (!ALONG)
             return -(row >> 4) & 3;      // the four lanes of sixteen or 32 that a read takes together: 0 3 of one fragment half, 1 2 of its neighbour
+        else if constexpr (size == 2 && per_row == 8)
+            return (row >> 3 & 1) << 1 | (row >> 1 & 1) << 2;
         else if constexpr (size == 2)
             return (row & 1) | (row >> 3 & 1) << 1 | (row >> 1 & 1) << 3;
         else
@@ -125,16 +127,20 @@ __device__ __forceinline__ I4 some_bytes(const char *p, int n)
     return v;
 }
 
-// A tile of BM x BN results by WM x WN wavefronts, each (BM / WM) x (BN / WN) of them, multiples of 64; STEP bytes of the sum (64 or
-// 128) at a time.
-template <int TYPE, int BM, int BN, int WM, int WN, bool AT, bool BT, int STEP>
+// A tile's shape: BM x BN results by WM x WN wavefronts, each (BM / WM) x (BN / WN) of them, multiples of 64; STEP bytes of the sum
+// (64 or 128) at a time, STAGES steps in LDS.
+template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_>
+struct Shape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_, threads = WM_ * WN_ * 64;
+};
+template <int TYPE, class SHAPE, bool AT, bool BT>
 struct Tile {
+    static constexpr int BM = SHAPE::BM, BN = SHAPE::BN, WM = SHAPE::WM, WN = SHAPE::WN, STEP = SHAPE::STEP, kStages = SHAPE::STAGES;
     typedef Unit16<TYPE> U;
     typedef typename U::Acc Acc;
     static constexpr int threads = WM * WN * 64;
     static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;      // fragments of a wavefront
     static constexpr int a_bytes = BM * STEP, b_bytes = BN * STEP, stage_bytes = a_bytes + b_bytes;
-    static constexpr int kStages = 256 / STEP;                      // steps in LDS
     static constexpr int lds_bytes = kStages * stage_bytes;
     static constexpr int units = STEP / kUnitBytes;
     static constexpr int step = STEP / U::size;               // elements of the sum
@@ -301,7 +307,7 @@ struct Tile {
         {
             if (left <= 0 && !next())
                 return;
-            char *const to = lds + (issued & (kStages - 1)) * stage_bytes;
+            char *const to = lds + (kStages == 3 ? issued % 3 : issued & (kStages - 1)) * stage_bytes;
             sa.load(to, left);
             sb.load(to + a_bytes, left);
             left -= step;
@@ -346,7 +352,7 @@ struct Tile {
                     lo[i] = fragment_a(lds, i, 0);
             }
         }
-        __device__ __forceinline__ const char *place() const { return lds + (used & (kStages - 1)) * stage_bytes; }
+        __device__ __forceinline__ const char *place() const { return lds + (kStages == 3 ? used % 3 : used & (kStages - 1)) * stage_bytes; }
         // The sums of the tile whose steps come next.
         template <class F>
         __device__ __forceinline__ void sum(Tile &t, int k_count, F next)
@@ -412,6 +418,7 @@ struct Tile {
         fa.load(a, 0, k_count);
         fb.load(b, 0, k_count);
         for (int k0 = 0, half = 0; k0 < k_count; k0 += step, half ^= 1) {
+            static_assert(kStages >= 2, "");
             char *const now = lds + half * stage_bytes;
             fa.store(now);
             fb.store(now + a_bytes);

@@ -13,7 +13,10 @@ struct ProductArgs {
     const float *scale, *w_scale;            // of 8-bit operands
 };
 
-constexpr int kStreamStep = 128, kWeightStep = 64;      // bytes of a sum that a tile takes at a time
+typedef Shape<256, 256, 2, 4, 128, 2> Wide;           // of rows
+typedef Shape<256, 256, 2, 4, 64, 4> WideAcross;      // of weights' gradients
+typedef Shape<128, 128, 2, 2, 128, 2> Middle;
+typedef Shape<128, 64, 2, 1, 64, 2> Small;
 
 // Results of a tile whose piece and first column are given.
 template <int TYPE, class S, class T>
@@ -104,13 +107,14 @@ struct Share {
 };
 
 // A workgroup makes BM slots of one expert times BN columns, and then others.
-template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
-__global__ void __launch_bounds__(WM *WN * 64)
+template <int TYPE, int RESULT, class SHAPE, bool TURNED>
+__global__ void __launch_bounds__(SHAPE::threads)
 product_kernel(ProductArgs a)
 {
-    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED, 128> T;
+    typedef Tile<TYPE, SHAPE, false, TURNED> T;
+    constexpr int BN = T::BN;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
-    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
+    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * (T::threads / 64)];
     __shared__ PieceTable<false> table;
     clear_nobodys<RESULT, T::threads>(a);
     for (Share s(table.template fill<T::threads>(a.bounds) * a.across); s.id < s.last; s.id += s.by) {
@@ -129,13 +133,14 @@ product_kernel(ProductArgs a)
 
 // The same with operands straight to LDS, one tile after the other: the first step of the next tile is on its way while the last
 // step of one is multiplied and its results are stored.
-template <int TYPE, int RESULT, int BM, int BN, int WM, int WN, bool TURNED>
-__global__ void __launch_bounds__(WM *WN * 64)
+template <int TYPE, int RESULT, class SHAPE, bool TURNED>
+__global__ void __launch_bounds__(SHAPE::threads)
 product_stream_kernel(ProductArgs a)
 {
-    typedef Tile<TYPE, BM, BN, WM, WN, false, TURNED, kStreamStep> T;
+    typedef Tile<TYPE, SHAPE, false, TURNED> T;
+    constexpr int BM = T::BM, BN = T::BN;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
-    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
+    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * (T::threads / 64)];
     __shared__ PieceTable<false> table;
     clear_nobodys<RESULT, T::threads>(a);
     Share s(table.template fill<T::threads>(a.bounds) * a.across);
@@ -231,13 +236,14 @@ __device__ __forceinline__ void store_weights(const WeightsArgs &a, const T &t, 
 // A workgroup makes BM x BN of an expert's gradient over one piece of its slots, and then others: the gradient itself where the
 // piece is all of them, else a partial sum.  Pieces differ in length.  The longest come first, and each round of tiles goes to the XCDs the
 // other way round than the one before, so that all have about the same to do; an XCD's tiles of a round are neighbours.
-template <int TYPE, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ void __launch_bounds__(WM *WN * 64)
+template <int TYPE, class SHAPE, bool DIRECT>
+__global__ void __launch_bounds__(SHAPE::threads)
 weights_kernel(WeightsArgs a)
 {
-    typedef Tile<TYPE, BM, BN, WM, WN, true, true, kWeightStep> T;
+    typedef Tile<TYPE, SHAPE, true, true> T;
+    constexpr int BM = T::BM, BN = T::BN;
     __shared__ __attribute__((aligned(1024))) char lds[T::lds_bytes];
-    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * WM * WN];
+    __shared__ __attribute__((aligned(1024))) char rows[T::rows_bytes * (T::threads / 64)];
     __shared__ PieceTable<true> table;
     const int tiles = table.template fill<T::threads>(a.bounds) * a.tiles, per_xcd = (int)(gridDim.x >> 3), xcd = (int)(blockIdx.x & 7);
     const auto tile_of_round = [&](int round) {
@@ -355,17 +361,16 @@ static unsigned workgroups(int64_t n_slots, int32_t n_experts, int64_t per, int6
     return (unsigned)(most < resident ? most : resident);
 }
 
-template <int TYPE, int RESULT, bool TURNED, int BM, int BN, int WM, int WN, bool DIRECT>
+template <int TYPE, int RESULT, bool TURNED, class SHAPE, bool DIRECT>
 static void launch_tiles(ProductArgs a, hipStream_t stream)
 {
-    a.bounds.per = BM;
-    a.across = (a.out_width + BN - 1) / BN;
-    const unsigned blocks =
-        workgroups<Tile<TYPE, BM, BN, WM, WN, false, TURNED, 128>, PieceTable<false>>(a.bounds.n_slots, a.bounds.n_experts, BM, a.across);
+    a.bounds.per = SHAPE::BM;
+    a.across = (a.out_width + SHAPE::BN - 1) / SHAPE::BN;
+    const unsigned blocks = workgroups<Tile<TYPE, SHAPE, false, TURNED>, PieceTable<false>>(a.bounds.n_slots, a.bounds.n_experts, SHAPE::BM, a.across);
     if constexpr (DIRECT)
-        hipLaunchKernelGGL((product_stream_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
+        hipLaunchKernelGGL((product_stream_kernel<TYPE, RESULT, SHAPE, TURNED>), dim3(blocks), dim3(SHAPE::threads), 0, stream, a);
     else
-        hipLaunchKernelGGL((product_kernel<TYPE, RESULT, BM, BN, WM, WN, TURNED>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
+        hipLaunchKernelGGL((product_kernel<TYPE, RESULT, SHAPE, TURNED>), dim3(blocks), dim3(SHAPE::threads), 0, stream, a);
 }
 
 // Whether rows can be loaded straight into LDS: 16-byte chunks that are aligned and whole, and a tile's rows within 2^31 bytes.
@@ -380,35 +385,48 @@ static void launch_product(ProductArgs a, hipStream_t stream)
     constexpr int size = Unit16<TYPE>::size;
     const bool direct = streams(a.x, a.x_stride, 0, (int64_t)a.in_width * size) &&
                         streams(a.w, a.w_stride, a.w_step, (int64_t)(TURNED ? a.out_width : a.in_width) * size);
-    if (!direct)
-        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2, false>(a, stream);
-    else if (TYPE != FS_F32 && a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192)
-        launch_tiles<TYPE == FS_F32 ? FS_BF16 : TYPE, RESULT, TURNED, 256, 256, 2, 4, true>(a, stream);
-    else
-        launch_tiles<TYPE, RESULT, TURNED, 128, 128, 2, 2, true>(a, stream);
+    // fp32 is bound by the matrix units whatever the tile, and small ones leave less idle at the edges and the end.
+    const bool small = TYPE == FS_F32 || a.out_width <= 64;
+    if constexpr (TYPE != FS_F32) {
+        if (direct && a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192)
+            return launch_tiles<TYPE, RESULT, TURNED, Wide, true>(a, stream);
+        if (!small)
+            return direct ? launch_tiles<TYPE, RESULT, TURNED, Middle, true>(a, stream) : launch_tiles<TYPE, RESULT, TURNED, Middle, false>(a, stream);
+    }
+    direct ? launch_tiles<TYPE, RESULT, TURNED, Small, true>(a, stream) : launch_tiles<TYPE, RESULT, TURNED, Small, false>(a, stream);
 }
 
-// How many slots a workgroup of weights_kernel adds up.
-static bool wide_weights(int64_t n_experts, int64_t in_width, int64_t out_width)
+// The shapes of weights' gradients, and how many slots a workgroup adds up: no more than a workgroup's share of all of them, so that the
+// longest experts end no later than the others.
+enum { kSmall, kMiddle, kWide };
+static int shape_of_weights(int32_t type, int64_t n_experts, int64_t in_width, int64_t out_width)
 {
-    return in_width > 128 && out_width > 128 && in_width * out_width * n_experts >= ((int64_t)1 << 24);
+    if (type == FS_F32 || in_width <= 64 || out_width <= 64)
+        return kSmall;
+    return in_width > 128 && out_width > 128 && in_width * out_width * n_experts >= ((int64_t)1 << 24) ? kWide : kMiddle;
 }
-static int piece_of_weights(int64_t n_slots, int32_t n_experts, int64_t in_width, int64_t out_width)
+template <class SHAPE>
+static int64_t tiles_of_weights(int64_t in_width, int64_t out_width)
 {
-    const int side = wide_weights(n_experts, in_width, out_width) ? 256 : 128;
-    int64_t per = n_slots * ((in_width + side - 1) / side * ((out_width + side - 1) / side)) / 256;
-    per = per < 1024 ? 1024 : per > 32768 ? 32768 : per;
-    return (int)((per + 255) / 256 * 256);
+    return (in_width + SHAPE::BN - 1) / SHAPE::BN * ((out_width + SHAPE::BM - 1) / SHAPE::BM);
+}
+static int piece_of_weights(int64_t n_slots, int32_t type, int32_t n_experts, int64_t in_width, int64_t out_width)
+{
+    const int shape = shape_of_weights(type, n_experts, in_width, out_width);
+    const int64_t work = n_slots * (shape == kWide     ? tiles_of_weights<Wide>(in_width, out_width)
+                                    : shape == kMiddle ? tiles_of_weights<Middle>(in_width, out_width)
+                                                       : tiles_of_weights<Small>(in_width, out_width));
+    const int64_t per = work / (shape == kWide ? kUnits : shape == kMiddle ? 2 * kUnits : 4 * kUnits);
+    return (int)(((per < 512 ? 512 : per > 32768 ? 32768 : per) + 255) / 256 * 256);
 }
 
-template <int TYPE, int SIDE, int WM, int WN, bool DIRECT>
+template <int TYPE, class SHAPE, bool DIRECT>
 static void launch_weights(WeightsArgs a, hipStream_t stream)
 {
-    a.across = (a.in_width + SIDE - 1) / SIDE;
-    a.tiles = a.across * ((a.out_width + SIDE - 1) / SIDE);
-    const unsigned blocks =
-        workgroups<Tile<TYPE, SIDE, SIDE, WM, WN, true, true, kWeightStep>, PieceTable<true>>(a.bounds.n_slots, a.bounds.n_experts, a.bounds.per, a.tiles);
-    hipLaunchKernelGGL((weights_kernel<TYPE, SIDE, SIDE, WM, WN, DIRECT>), dim3(blocks), dim3(WM * WN * 64), 0, stream, a);
+    a.across = (a.in_width + SHAPE::BN - 1) / SHAPE::BN;
+    a.tiles = (int32_t)tiles_of_weights<SHAPE>(a.in_width, a.out_width);
+    const unsigned blocks = workgroups<Tile<TYPE, SHAPE, true, true>, PieceTable<true>>(a.bounds.n_slots, a.bounds.n_experts, a.bounds.per, a.tiles);
+    hipLaunchKernelGGL((weights_kernel<TYPE, SHAPE, DIRECT>), dim3(blocks), dim3(SHAPE::threads), 0, stream, a);
 }
 
 static int check_shape(const char *who, int64_t n_slots, int32_t n_experts, int32_t in_width, int32_t out_width)
@@ -418,10 +436,10 @@ static int check_shape(const char *who, int64_t n_slots, int32_t n_experts, int3
     FS_TRY(check_experts(who, n_experts));
     FS_TRY(check_width(who, in_width));
     FS_TRY(check_width(who, out_width));
-    // Tiles are counted in 32 bits: more of them, of 128 x 128 results, would be more than the card holds.
-    const int64_t in_tiles = ((int64_t)in_width + 127) / 128, out_tiles = ((int64_t)out_width + 127) / 128;
+    // Tiles are counted in 32 bits: more of them, of 128 x 64 results, would be more than the card holds.
+    const int64_t in_tiles = ((int64_t)in_width + 63) / 64, out_tiles = ((int64_t)out_width + 63) / 64;
     const int64_t rows = n_slots / 128 + n_experts, wide = in_tiles > out_tiles ? in_tiles : out_tiles;
-    if (rows > INT32_MAX / wide || (n_slots / 1024 + n_experts) > INT32_MAX / (in_tiles * out_tiles))
+    if (rows > INT32_MAX / wide || (n_slots / 512 + n_experts) > INT32_MAX / ((in_tiles * out_tiles + 1) / 2))
         return fail(FS_EUNSUPPORTED, "%s: %lld slots of %d experts, %d to %d columns", who, (long long)n_slots, n_experts, in_width, out_width);
     return FS_OK;
 }
@@ -513,7 +531,7 @@ extern "C" size_t fs_expert_matmul_backward_workspace_bytes(int64_t n_slots, int
         fail(FS_EINVAL, "%s: unknown element type %d", who, type);
         return 0;
     }
-    const int64_t per = piece_of_weights(n_slots, n_experts, in_width, out_width);
+    const int64_t per = piece_of_weights(n_slots, type, n_experts, in_width, out_width);
     if (n_slots <= per)
         return 0;
     // An expert of n > per slots has at most n / per + 1 < 2 n / per pieces.
@@ -540,18 +558,21 @@ extern "C" int fs_expert_matmul_backward(int64_t n_slots, int32_t n_experts, int
     if (work_bytes < need)
         return fail(FS_EINVAL, "%s: %zu bytes of working memory, %zu are needed", who, work_bytes, need);
     const int64_t b = (int64_t)type_bytes(type);
-    WeightsArgs a = {{first, n_experts, (int)n_slots, piece_of_weights(n_slots, n_experts, in_width, out_width)}, (const char *)d_y, (const char *)x,
+    WeightsArgs a = {{first, n_experts, (int)n_slots, piece_of_weights(n_slots, type, n_experts, in_width, out_width)}, (const char *)d_y, (const char *)x,
                      d_y_stride * b, x_stride * b, d_w, d_w_stride, d_w_step, d_w_type, in_width, out_width, 0, 0, accumulate, (float *)work};
     const bool direct = streams(d_y, a.g_stride, 0, out_width * b) && streams(x, a.x_stride, 0, in_width * b);
     prof_start(kKernTrainOther, stream);
     with_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
-        if (!direct)
-            launch_weights<T, 128, 2, 2, false>(a, stream);
-        else if (T != FS_F32 && wide_weights(n_experts, in_width, out_width))
-            launch_weights<T == FS_F32 ? FS_BF16 : T, 256, 2, 4, true>(a, stream);
-        else
-            launch_weights<T, 128, 2, 2, true>(a, stream);
+        const int shape = shape_of_weights(type, n_experts, in_width, out_width);
+        if constexpr (T != FS_F32) {
+            if (shape == kWide && direct)
+                launch_weights<T, WideAcross, true>(a, stream);
+            else if (shape != kSmall)
+                direct ? launch_weights<T, Middle, true>(a, stream) : launch_weights<T, Middle, false>(a, stream);
+        }
+        if (shape == kSmall)
+            direct ? launch_weights<T, Small, true>(a, stream) : launch_weights<T, Small, false>(a, stream);
         if (need) {
             const int64_t wanted = ((int64_t)out_width + 3) / 4, most = 8192 / n_experts + 1;
             a.tiles = (int32_t)(wanted < most ? wanted : most);
