@@ -38,6 +38,13 @@ template <> struct Unit16<FS_F16> {
 template <> struct Unit16<FS_F32> {
     typedef F4 Acc;
     static constexpr int size = 4;
+    static __device__ __forceinline__ Acc step(I4 a, I4 b, Acc c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(a[i]), __int_as_float(b[i]), c, 0, 0, 0);
+        return c;
+    }
 };
 template <> struct Unit16<kI8> {
     typedef I4 Acc;

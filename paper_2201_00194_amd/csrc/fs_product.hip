@@ -174,6 +174,95 @@ product_stream_kernel(ProductArgs a)
     }
 }
 
+// Few rows an expert: what counts is how fast the weights arrive.  A workgroup makes sixteen columns of one expert's results; its
+// wavefronts share the sum out, 64 bytes of it each in turn, straight from memory to registers, and meet in LDS.
+constexpr int kFewWaves = 4;
+template <int TYPE, int RESULT, int MF>
+__global__ void __launch_bounds__(kFewWaves * 64)
+product_few_kernel(ProductArgs a)
+{
+    typedef Unit16<TYPE> U;
+    typedef typename Element<RESULT>::type E;
+    constexpr int AHEAD = 4, per = MF * 16;
+    __shared__ typename U::Acc others[kFewWaves - 1][MF][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int expert = blockIdx.y, n0 = blockIdx.x * 16, n_slots = a.bounds.n_slots;
+    const bool owned = expert < a.bounds.n_experts;
+    const int begin = min(max(a.bounds.first[expert], 0), n_slots), end = owned ? max(min(a.bounds.first[expert + 1], n_slots), begin) : n_slots;
+    const bool wide = RESULT == FS_F32 || a.y_type == FS_F32;
+    const int bytes = a.in_width * U::size, whole = bytes / kUnitBytes;
+    const char *const w = a.w + (owned ? expert : 0) * a.w_step + min(n0 + r, a.out_width - 1) * a.w_stride + g * 16;
+    for (int64_t s = begin + (int64_t)blockIdx.z * per; s < end; s += (int64_t)gridDim.z * per) {
+        typename U::Acc acc[MF];
+        const char *x[MF];
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            acc[f] = typename U::Acc{0, 0, 0, 0};
+            x[f] = a.x + min((int)s + f * 16 + r, end - 1) * a.x_stride + g * 16;
+        }
+        if (owned) {
+            int u = wave;
+            for (; u + (AHEAD - 1) * kFewWaves < whole; u += AHEAD * kFewWaves) {
+                I4 wv[AHEAD], xv[AHEAD][MF];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int64_t at = (int64_t)(u + i * kFewWaves) * kUnitBytes;
+                    wv[i] = *(const typename Bytes16<U::size>::type *)(w + at);
+#pragma unroll
+                    for (int f = 0; f < MF; ++f)
+                        xv[i][f] = *(const typename Bytes16<U::size>::type *)(x[f] + at);
+                }
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                    for (int f = 0; f < MF; ++f)
+                        acc[f] = U::step(wv[i], xv[i][f], acc[f]);
+            }
+            for (; u * kUnitBytes < bytes; u += kFewWaves) {
+                const int64_t at = (int64_t)u * kUnitBytes;
+                const int n = (bytes - u * kUnitBytes - g * 16) / U::size;
+                const I4 wv = some_bytes<U::size>(w + at, n);
+#pragma unroll
+                for (int f = 0; f < MF; ++f)
+                    acc[f] = U::step(wv, some_bytes<U::size>(x[f] + at, n), acc[f]);
+            }
+            __syncthreads();      // the last piece's sums have been read
+            if (wave > 0) {
+#pragma unroll
+                for (int f = 0; f < MF; ++f)
+                    others[wave - 1][f][lane] = acc[f];
+            }
+            __syncthreads();
+        }
+        if (wave > 0)
+            continue;
+        const int column = n0 + g * 4, n = a.out_width - column;
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            const int row = (int)s + f * 16 + r;
+            if (owned) {
+#pragma unroll
+                for (int i = 0; i < kFewWaves - 1; ++i)
+                    acc[f] += others[i][f][lane];
+            }
+            if (row >= end || n <= 0)
+                continue;
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[i] = (float)acc[f][i];
+                if constexpr (TYPE == kI8)
+                    y[i] = owned ? y[i] * a.scale[row] * a.w_scale[(int64_t)expert * a.out_width + min(column + i, a.out_width - 1)] : 0.0f;
+            }
+            const int64_t at = row * a.y_stride + column;
+            if (wide)
+                store_chunk<4>((float *)a.y + at, n, y);
+            else
+                store_chunk<4>((E *)a.y + at, n, y);
+        }
+    }
+}
+
 struct WeightsArgs {
     Bounds bounds;
     const char *g, *x;
@@ -373,6 +462,15 @@ static void launch_tiles(ProductArgs a, hipStream_t stream)
         hipLaunchKernelGGL((product_kernel<TYPE, RESULT, SHAPE, TURNED>), dim3(blocks), dim3(SHAPE::threads), 0, stream, a);
 }
 
+template <int TYPE, int RESULT, int MF>
+static void launch_few(const ProductArgs &a, hipStream_t stream)
+{
+    // Pieces of an expert that has more rows than most: four workgroups share them.
+    const int64_t pieces = (a.bounds.n_slots + MF * 16 - 1) / (MF * 16);
+    const dim3 grid((a.out_width + 15) / 16, a.bounds.n_experts + 1, (unsigned)(pieces < 4 ? pieces : 4));
+    hipLaunchKernelGGL((product_few_kernel<TYPE, RESULT, MF>), grid, dim3(kFewWaves * 64), 0, stream, a);
+}
+
 // Whether rows can be loaded straight into LDS: 16-byte chunks that are aligned and whole, and a tile's rows within 2^31 bytes.
 static bool streams(const void *p, int64_t stride, int64_t step, int64_t width)
 {
@@ -385,6 +483,17 @@ static void launch_product(ProductArgs a, hipStream_t stream)
     constexpr int size = Unit16<TYPE>::size;
     const bool direct = streams(a.x, a.x_stride, 0, (int64_t)a.in_width * size) &&
                         streams(a.w, a.w_stride, a.w_step, (int64_t)(TURNED ? a.out_width : a.in_width) * size);
+    // Few rows: sixteen columns a workgroup get all compute units to work, and their sums are short, but each reads its expert's rows.
+    // us, tiles of 128 x 128 and this: 30 of 164 x 256 fp32, 64 rows an expert 19.0 and 7.7, 192 19.6 and 15.1; one of 1024 x 1024 bf16,
+    // 1 row 15.1 and 7.7, 192 27.9 and 12.1; eight of 4096 x 4096, 1 row each 47 and 30, 8 rows 62 and 54, 16 rows 63 and 69; 64 of
+    // 2048 x 1024, 1 row each 28.7 and 29.2, 4 rows 42 and 59.
+    if constexpr (!TURNED) {
+        const int64_t met = a.bounds.n_slots < a.bounds.n_experts ? a.bounds.n_slots : a.bounds.n_experts;      // experts, at most
+        const int64_t mean = (a.bounds.n_slots + a.bounds.n_experts - 1) / a.bounds.n_experts, row = (int64_t)a.in_width * size;
+        const bool little = met * a.out_width * row <= (32 << 20) && (int64_t)a.bounds.n_slots * ((a.out_width + 15) / 16) * row <= (64 << 20);
+        if (little || (mean <= 8 && met * ((a.out_width + 127) / 128) <= kUnits))
+            return mean <= 16 ? launch_few<TYPE, RESULT, 1>(a, stream) : mean <= 32 ? launch_few<TYPE, RESULT, 2>(a, stream) : launch_few<TYPE, RESULT, 4>(a, stream);
+    }
     // fp32 is bound by the matrix units whatever the tile, and small ones leave less idle at the edges and the end.
     const bool small = TYPE == FS_F32 || a.out_width <= 64;
     if constexpr (TYPE != FS_F32) {
