@@ -41,58 +41,83 @@ __device__ __forceinline__ void store_bytes(int8_t *p, int n, const int (&v)[N])
     }
 }
 
-// 1 << ll lanes to a row, which is read once for its largest and once more for its integers.
-template <int TYPE>
+// 1 << ll lanes to a row.  C > 0: a lane keeps so many chunks of it; else it is read once for its largest and once more for its integers.
+template <int TYPE, int C>
 __global__ void __launch_bounds__(256)
 quantize_kernel(QuantizeArgs a)
 {
     typedef typename Element<TYPE>::type T;
     constexpr int N = kChunk<T>;
     const int lane = threadIdx.x & 63, h = lane & ((1 << a.ll) - 1), each = 64 >> a.ll;
-    const int64_t wave = (a.row0 + blockIdx.x) * 4 + (threadIdx.x >> 6), row = wave * each + (lane >> a.ll);
+    const int64_t wave = (a.row0 + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = wave * each + (lane >> a.ll);
     if (wave * each >= a.n_rows)
         return;
     const bool there = row < a.n_rows;
-    const T *const x = (const T *)a.x + (there ? row : a.n_rows - 1) * a.x_stride;
+    const int64_t from = there ? row : a.n_rows - 1;
+    const T *const x = (const T *)a.x + from * a.x_stride;
     unsigned most = 0;      // of the values without their signs, as their bits: infinities and NaN are above all others
-    for (int c = h * N; c < a.width; c += N << a.ll) {
-        float v[N];
-        load_chunk(x + c, a.width - c, v);
+    RawChunk<T> kept[C ? C : 1];
+    if constexpr (C > 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+        for (int u = 0; u < C; ++u) {
+            const int c = (u << a.ll | h) * N;
+            kept[u].load(x + c, a.width - c);
+        }
+#pragma unroll
+        for (int u = 0; u < C; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                most = max(most, __float_as_uint(kept[u][i]) & 0x7fffffffu);
+    } else {
+        for (int c = h * N; c < a.width; c += N << a.ll) {
+            float v[N];
+            load_chunk(x + c, a.width - c, v);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+        }
     }
     most = row_reduce((int)most, a.ll, [](int p, int q) { return max(p, q); });
     const bool good = most < 0x7f800000u;
     const float scale = good ? fmaxf(__uint_as_float(most) / 127.0f, 1.17549435e-38f) : __uint_as_float(0x7fc00000u);
     const float inverse_scale = 1.0f / scale;
     const int64_t slots = a.n_rows * a.k;
-    if (there && h == 0) {
-        if (!a.place)
-            a.scale[row] = scale;
-        else
-            for (int j = 0; j < a.k; ++j) {
-                const int p = a.place[row * a.k + j];
-                if (p >= 0 && p < slots)
-                    a.scale[p] = scale;
-            }
-    }
-    for (int c = h * N; c < a.width; c += N << a.ll) {
-        float v[N];
+    // f(row of q) for each row that this one goes to.
+    const auto each_place = [&](auto f) {
+        if (!there)
+            return;
+        if (!a.place) {
+            f(row);
+            return;
+        }
+        for (int j = 0; j < a.k; ++j) {
+            const int p = a.place[row * a.k + j];
+            if (p >= 0 && p < slots)
+                f((int64_t)p);
+        }
+    };
+    if (h == 0)
+        each_place([&](int64_t p) { a.scale[p] = scale; });
+    const auto put = [&](int c, const auto &v) {
         int q[N];
-        const int n = there ? a.width - c : 0;
-        load_chunk(x + c, n, v);
 #pragma unroll
         for (int i = 0; i < N; ++i)
             q[i] = good ? quotient(v[i], scale, inverse_scale) : 0;
-        if (!a.place)
-            store_bytes<N>(a.q + row * a.q_stride + c, n, q);
-        else
-            for (int j = 0; j < a.k; ++j) {
-                const int p = a.place[(there ? row : 0) * a.k + j];
-                if (p >= 0 && p < slots)
-                    store_bytes<N>(a.q + p * a.q_stride + c, n, q);
-            }
+        each_place([&](int64_t p) { store_bytes<N>(a.q + p * a.q_stride + c, a.width - c, q); });
+    };
+    if constexpr (C > 0) {
+#pragma unroll
+        for (int u = 0; u < C; ++u) {
+            const int c = (u << a.ll | h) * N;
+            if (c < a.width)
+                put(c, kept[u]);
+        }
+    } else {
+        for (int c = h * N; c < a.width; c += N << a.ll) {
+            float v[N];
+            load_chunk(x + c, a.width - c, v);
+            put(c, v);
+        }
     }
     if (a.place && there) {
         const int zero[N] = {};
@@ -107,12 +132,19 @@ quantize_kernel(QuantizeArgs a)
 
 static void launch_quantize(QuantizeArgs a, int32_t type, hipStream_t stream)
 {
-    a.ll = row_lanes_log(a.width, 16 / (int)type_bytes(type));
+    const int chunk = 16 / (int)type_bytes(type), blocks_of_row = column_blocks(a.width, chunk);
+    a.ll = row_lanes_log(a.width, chunk);
     const int64_t each = (int64_t)4 << (6 - a.ll);
     with_type(type, [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        const auto kernel = blocks_of_row <= 1   ? quantize_kernel<T, 1>
+                            : blocks_of_row <= 2 ? quantize_kernel<T, 2>
+                            : blocks_of_row <= 4 ? quantize_kernel<T, 4>
+                            : blocks_of_row <= 8 ? quantize_kernel<T, 8>
+                                                 : quantize_kernel<T, 0>;
         in_pieces((a.n_rows + each - 1) / each, [&](int64_t at, unsigned blocks) {
             a.row0 = at;
-            hipLaunchKernelGGL(quantize_kernel<decltype(t)::value>, dim3(blocks), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, stream, a);
         });
     });
 }
