@@ -73,17 +73,18 @@ constexpr int kUnitBytes = 64;      // of the sum, of 1, 2 or 4 bytes an element
 
 // Where 16 bytes of an operand lie in LDS.  The xor spreads what sixteen lanes, or 32 with a transposing read, take at a time over the
 // banks.
-template <int TYPE, bool ALONG, int ROWS, int STEP>
+template <int TYPE, bool ALONG, int ROWS, int STEP, int FOUR>
 struct Place {
     static constexpr int size = Unit16<TYPE>::size;
     static constexpr int chunks = ROWS * STEP / 16;
     static constexpr int per_row = ALONG ? ROWS * size / 16 : STEP / 16;     // 16-byte chunks
     static __device__ __forceinline__ int turn(int row)
     {
+        constexpr int shift = FOUR == 4 ? 4 : 3;
         if constexpr (!ALONG && STEP == 128)
-            return (row >> 1 & 1) | (row >> 4 & 3) << 1;
+            return (row >> 1 & 1) | (row >> shift & 3) << 1;
         else if constexpr (!ALONG)
-            return -(row >> 4) & 3;      // the four lanes of sixteen or 32 that a read takes together: 0 3 of one fragment half, 1 2 of its neighbour
+            return -(row >> shift) & 3;      // the four lanes of sixteen or 32 that a read takes together: 0 3 of one fragment half, 1 2 of its neighbour
         else if constexpr (size == 2 && per_row == 8)
             return (row >> 3 & 1) << 1 | (row >> 1 & 1) << 2;
         else if constexpr (size == 2)
@@ -94,11 +95,13 @@ struct Place {
     static __device__ __forceinline__ int at(int row, int chunk) { return (row * per_row + (chunk ^ turn(row))) * 16; }
 };
 // Which of an operand's 64 rows (columns) lane r of sixteen has in fragment f of four: such that a lane's results lie side by side.
-template <int TYPE, bool ALONG>
+// FOUR = 2: of 32, two fragments.
+template <int TYPE, bool ALONG, int FOUR>
 __device__ __forceinline__ int member(int f, int r)
 {
+    static_assert(FOUR == 4 || (FOUR == 2 && !ALONG), "");
     if constexpr (!ALONG)
-        return (r >> 2) * 16 + f * 4 + (r & 3);
+        return (r >> 2) * (4 * FOUR) + f * 4 + (r & 3);
     else if constexpr (Unit16<TYPE>::size == 2)
         return (r >> 2) * 16 + (f ^ (r >> 2 & 1)) * 4 + (r & 3);      // both halves of 16 bytes are read at a time
     else
@@ -134,8 +137,8 @@ __device__ __forceinline__ I4 some_bytes(const char *p, int n)
     return v;
 }
 
-// A tile's shape: BM x BN results by WM x WN wavefronts, each (BM / WM) x (BN / WN) of them, multiples of 64; STEP bytes of the sum
-// (64 or 128) at a time, STAGES steps in LDS.
+// A tile's shape: BM x BN results by WM x WN wavefronts, each (BM / WM) x (BN / WN) of them, multiples of 64 (of rows along the
+// sum, 32 too); STEP bytes of the sum (64 or 128) at a time, STAGES steps in LDS.
 template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_>
 struct Shape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_, threads = WM_ * WN_ * 64;
@@ -147,6 +150,7 @@ struct Tile {
     typedef typename U::Acc Acc;
     static constexpr int threads = WM * WN * 64;
     static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;      // fragments of a wavefront
+    static constexpr int MFOUR = MF < 4 ? MF : 4;
     static constexpr int a_bytes = BM * STEP, b_bytes = BN * STEP, stage_bytes = a_bytes + b_bytes;
     static constexpr int lds_bytes = kStages * stage_bytes;
     static constexpr int units = STEP / kUnitBytes;
@@ -163,9 +167,9 @@ struct Tile {
     }
 
     // ---- operands through registers: any alignment, any sizes ----
-    template <bool ALONG, int ROWS>
+    template <bool ALONG, int ROWS, int FOUR = 4>
     struct Fetched {
-        typedef Place<TYPE, ALONG, ROWS, STEP> P;
+        typedef Place<TYPE, ALONG, ROWS, STEP, FOUR> P;
         static constexpr int N = P::chunks / threads;
         I4 v[N];
         __device__ __forceinline__ void load(const Operand &o, int k0, int k_count)
@@ -193,9 +197,9 @@ struct Tile {
     // ---- operands straight into LDS: rows and their 16-byte chunks aligned and whole ----
     // A wavefront's load writes 64 chunks side by side, so it is the lanes' sources that are turned.  A lane whose chunk is not there
     // has an offset past the buffer's end, and zeros come.
-    template <bool ALONG, int ROWS>
+    template <bool ALONG, int ROWS, int FOUR = 4>
     struct Streamed {
-        typedef Place<TYPE, ALONG, ROWS, STEP> P;
+        typedef Place<TYPE, ALONG, ROWS, STEP, FOUR> P;
         static constexpr int N = P::chunks / threads;
         static constexpr unsigned kNowhere = 0x80000000u;
         unsigned from[N];
@@ -233,18 +237,18 @@ struct Tile {
     // ---- fragments ----
     // `base`: the wavefront's first row or column.  Fragment f is of block f / 4 of 64 rows; fp32 along: v[4 * block + i][f % 4]
     // are the i-th terms of its lanes instead of v[f][i].
-    template <bool ALONG, int ROWS>
+    template <bool ALONG, int ROWS, int FOUR>
     static __device__ __forceinline__ I4 fragment(const char *lds, int base, int f, int unit)
     {
-        typedef Place<TYPE, ALONG, ROWS, STEP> P;
-        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, block = base + (f >> 2) * 64;
+        typedef Place<TYPE, ALONG, ROWS, STEP, FOUR> P;
+        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, block = base + f / FOUR * (16 * FOUR);
         if constexpr (!ALONG) {
-            return *(const I4 *)(lds + P::at(block + member<TYPE, false>(f & 3, r), unit * 4 + g));
+            return *(const I4 *)(lds + P::at(block + member<TYPE, false, FOUR>(f % FOUR, r), unit * 4 + g));
         } else if constexpr (U::size == 4) {
             return *(const I4 *)(lds + P::at(unit * 16 + g * 4 + (f & 3), block / 4 + r));
         } else {
             // Lane r brings four elements for lanes 4 (r % 4) to 4 (r % 4) + 3, of row r / 4 of four.
-            const int at = block + member<TYPE, true>(f & 3, (r & 3) * 4), k = unit * 32 + g * 8 + (r >> 2);
+            const int at = block + member<TYPE, true, 4>(f & 3, (r & 3) * 4), k = unit * 32 + g * 8 + (r >> 2);
             typedef __attribute__((address_space(3))) S4 *Read;
             const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k, at >> 3) + (at & 4) * 2));
             const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(lds + P::at(k + 4, at >> 3) + (at & 4) * 2));
@@ -254,11 +258,11 @@ struct Tile {
     }
     static __device__ __forceinline__ I4 fragment_a(const char *lds, int i, int unit)
     {
-        return fragment<AT, BM>(lds, (threadIdx.x >> 6) / WN * (BM / WM), i, unit);
+        return fragment<AT, BM, MFOUR>(lds, (threadIdx.x >> 6) / WN * (BM / WM), i, unit);
     }
     static __device__ __forceinline__ I4 fragment_b(const char *lds, int j, int unit)
     {
-        return fragment<BT, BN>(lds + a_bytes, (threadIdx.x >> 6) % WN * (BN / WN), j, unit);
+        return fragment<BT, BN, 4>(lds + a_bytes, (threadIdx.x >> 6) % WN * (BN / WN), j, unit);
     }
     __device__ __forceinline__ void multiply(const char *lds)
     {
@@ -300,9 +304,9 @@ struct Tile {
     struct Stream {
         static constexpr bool kHalves = MF == 8 && TYPE != FS_F32;
         static constexpr int kAhead = kHalves ? kStages : kStages - 1;
-        static constexpr int kLoads = Streamed<AT, BM>::N + Streamed<BT, BN>::N;      // of a wavefront and a step
+        static constexpr int kLoads = Streamed<AT, BM, MFOUR>::N + Streamed<BT, BN>::N;      // of a wavefront and a step
         char *lds;
-        Streamed<AT, BM> sa;
+        Streamed<AT, BM, MFOUR> sa;
         Streamed<BT, BN> sb;
         int left = 0;                   // elements of the sum that the tile being loaded has left
         int issued = 0, used = 0;       // steps
@@ -420,7 +424,7 @@ struct Tile {
     // The sums over k_count terms, through registers.
     __device__ __forceinline__ void run(char *lds, const Operand &a, const Operand &b, int k_count)
     {
-        Fetched<AT, BM> fa;
+        Fetched<AT, BM, MFOUR> fa;
         Fetched<BT, BN> fb;
         fa.load(a, 0, k_count);
         fb.load(b, 0, k_count);
@@ -447,7 +451,7 @@ struct Tile {
     static constexpr int rows_bytes = 2048;
     static __device__ __forceinline__ int row_of(int t, int r, int i)
     {
-        return (t >> 6) / WN * (BM / WM) + (i >> 2) * 64 + member<TYPE, AT>(i & 3, r);
+        return (t >> 6) / WN * (BM / WM) + i / MFOUR * (16 * MFOUR) + member<TYPE, AT, MFOUR>(i % MFOUR, r);
     }
     template <class S, class G, class M, class P>
     __device__ __forceinline__ void results(char *rows, int t, G of_column, M make, P put) const

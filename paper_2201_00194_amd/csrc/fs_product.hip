@@ -16,7 +16,8 @@ struct ProductArgs {
 typedef Shape<256, 256, 2, 4, 128, 2> Wide;           // of rows
 typedef Shape<256, 256, 2, 4, 64, 4> WideAcross;      // of weights' gradients
 typedef Shape<128, 128, 2, 2, 128, 2> Middle;
-typedef Shape<128, 64, 2, 1, 64, 2> Small;
+typedef Shape<128, 64, 4, 1, 64, 2> Small;            // of rows
+typedef Shape<128, 64, 2, 1, 64, 2> SmallAcross;
 
 // Results of a tile whose piece and first column are given.
 template <int TYPE, class S, class T>
@@ -524,7 +525,7 @@ static int piece_of_weights(int64_t n_slots, int32_t type, int32_t n_experts, in
     const int shape = shape_of_weights(type, n_experts, in_width, out_width);
     const int64_t work = n_slots * (shape == kWide     ? tiles_of_weights<Wide>(in_width, out_width)
                                     : shape == kMiddle ? tiles_of_weights<Middle>(in_width, out_width)
-                                                       : tiles_of_weights<Small>(in_width, out_width));
+                                                       : tiles_of_weights<SmallAcross>(in_width, out_width));
     const int64_t per = work / (shape == kWide ? kUnits : shape == kMiddle ? 2 * kUnits : 4 * kUnits);
     return (int)(((per < 512 ? 512 : per > 32768 ? 32768 : per) + 255) / 256 * 256);
 }
@@ -681,7 +682,7 @@ extern "C" int fs_expert_matmul_backward(int64_t n_slots, int32_t n_experts, int
                 direct ? launch_weights<T, Middle, true>(a, stream) : launch_weights<T, Middle, false>(a, stream);
         }
         if (shape == kSmall)
-            direct ? launch_weights<T, Small, true>(a, stream) : launch_weights<T, Small, false>(a, stream);
+            direct ? launch_weights<T, SmallAcross, true>(a, stream) : launch_weights<T, SmallAcross, false>(a, stream);
         if (need) {
             const int64_t wanted = ((int64_t)out_width + 3) / 4, most = 8192 / n_experts + 1;
             a.tiles = (int32_t)(wanted < most ? wanted : most);
