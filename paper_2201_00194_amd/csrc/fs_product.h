@@ -215,8 +215,9 @@ struct Tile {
             for (int i = 0; i < N; ++i)
                 from[i] = (ALONG ? chunk_of(t, i) * (16 / U::size) : row_of(t, i)) < o.count ? row_of(t, i) * (unsigned)stride + chunk_of(t, i) * 16 : kNowhere;
         }
-        // The next step's chunks, of which `left` elements of the sum are there.
-        __device__ __forceinline__ void load(char *lds, int left)
+        // Of the next step `left` elements of the sum are there; its chunks go to `lds`.
+        unsigned to;
+        __device__ __forceinline__ void prepare(char *lds, int left)
         {
             if (left < step) {
                 const int t = thread_here();
@@ -224,13 +225,22 @@ struct Tile {
                 for (int i = 0; i < N; ++i)
                     from[i] = (ALONG ? row_of(t, i) : chunk_of(t, i) * (16 / U::size)) < left ? from[i] : kNowhere;
             }
+            to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (threadIdx.x >> 6) * 1024);
+        }
+        __device__ __forceinline__ void load(int i) const
+        {
             const I4 buffer = {__builtin_amdgcn_readfirstlane((int)base), __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff), (int)kNowhere, 0x00020000};
-            const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (threadIdx.x >> 6) * 1024);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * threads * 16), "v"(from[i]), "s"(buffer)
+                         : "memory");
+        }
+        __device__ __forceinline__ void advance() { base += ALONG ? (uint64_t)step * stride : STEP; }
+        // Nothing more: zeros come.
+        __device__ __forceinline__ void end()
+        {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * threads * 16), "v"(from[i]), "s"(buffer)
-                             : "memory");
-            base += ALONG ? (uint64_t)step * stride : STEP;
+                from[i] = kNowhere;
+            stride = 0;
         }
     };
 
@@ -312,18 +322,45 @@ struct Tile {
         int issued = 0, used = 0;       // steps
         int mark = 0;                   // steps that were issued before the youngest stores, of which there are STORES at least
         I4 lo[4], b[NF];                // fragments of the step that comes next
-        // next() sets sa, sb and left to another tile's; false if there is none.
+        // next() sets sa, sb and left to another tile's; false if there is none: then steps of zeros are loaded.
         template <class F>
-        __device__ __forceinline__ void issue(F next)
+        __device__ __forceinline__ void prepare(F next)
         {
-            if (left <= 0 && !next())
-                return;
-            char *const to = lds + (kStages == 3 ? issued % 3 : issued & (kStages - 1)) * stage_bytes;
-            sa.load(to, left);
-            sb.load(to + a_bytes, left);
+            if (left <= 0 && !next()) {
+                sa.end();
+                sb.end();
+                left = INT32_MAX;
+            }
+            char *const to = lds + (issued & (kStages - 1)) * stage_bytes;
+            sa.prepare(to, left);
+            sb.prepare(to + a_bytes, left);
+        }
+        __device__ __forceinline__ void load(int i) const
+        {
+            constexpr int of_a = Streamed<AT, BM, MFOUR>::N;
+            if (i < of_a)
+                sa.load(i);
+            else
+                sb.load(i - of_a);
+        }
+        __device__ __forceinline__ void advance()
+        {
+            sa.advance();
+            sb.advance();
             left -= step;
             ++issued;
         }
+        template <class F>
+        __device__ __forceinline__ void issue(F next)
+        {
+            prepare(next);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                load(i);
+            advance();
+        }
+        // Before the kernel's end: LDS is written no more.
+        __device__ __forceinline__ void end() const { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
         // Step n has arrived in all wavefronts; loads return in their order, so that what is younger may be on its way.
         template <int MORE>
         static __device__ __forceinline__ void wait(int younger)
@@ -339,9 +376,7 @@ struct Tile {
         }
         __device__ __forceinline__ void await(int n) const
         {
-            if (n >= issued)                     // none: all others have come this far
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            else if (n < mark)
+            if (n < mark)
                 wait<STORES>(issued - n - 1);
             else
                 wait<0>(issued - n - 1);
@@ -374,6 +409,9 @@ struct Tile {
             if constexpr (kHalves) {
                 // Eight fragments of rows, four of columns.  The second four of rows are read while the first four are multiplied; the next
                 // step's first four, and its columns one after the other, while the second four are.
+                // Loads go out one by one between products: all at once, they would hold the products up behind them until the others'
+                // have been taken too.
+                bool some = false;                   // of a step's loads are left
 #pragma unroll 1
                 do {
                     const char *then = place();
@@ -384,14 +422,22 @@ struct Tile {
                         for (int i = 0; i < 4; ++i)
                             hi[i] = fragment_a(then, 4 + i, unit);
 #pragma unroll
-                        for (int j = 0; j < NF; ++j)
+                        for (int j = 0; j < NF; ++j) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
                                 t.acc[i][j] = U::step(b[j], lo[i], t.acc[i][j]);
+                            if (unit == 0 && kLoads > NF && some) {
+                                __builtin_amdgcn_sched_barrier(0);
+                                load(NF + j);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                        if (unit == 0 && kLoads > NF && some)
+                            advance();
                         const int next_unit = (unit + 1) % units;
                         if (next_unit == 0) {
                             await(used + 1);
-                            issue(next);             // to where this step was, which all have read
+                            prepare(next);           // to where this step was, which all have read
                             ++used;
                             then = place();          // behind the last step of all: read, and not used
                         }
@@ -404,9 +450,23 @@ struct Tile {
                             for (int i = 0; i < 4; ++i)
                                 t.acc[4 + i][j] = U::step(b[j], hi[i], t.acc[4 + i][j]);
                             b[j] = fragment_b(then, j, next_unit);
+                            if (next_unit == 0) {
+                                __builtin_amdgcn_sched_barrier(0);
+                                load(j);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
                         }
+                        if (next_unit == 0 && kLoads <= NF)
+                            advance();
                     }
+                    some = true;
                 } while (--steps > 0);
+                if (kLoads > NF) {
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+                        load(NF + j);
+                    advance();
+                }
             } else {
 #pragma unroll 1
                 do {

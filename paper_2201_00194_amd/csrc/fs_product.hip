@@ -173,6 +173,7 @@ product_stream_kernel(ProductArgs a)
         store_product_as<TYPE, RESULT>(a, t, rows, piece, n0);
         stream.stored(piece.count == BM && n0 + BN <= a.out_width);
     }
+    stream.end();
 }
 
 // Few rows an expert: what counts is how fast the weights arrive.  A workgroup makes sixteen columns of one expert's results; its
@@ -385,6 +386,7 @@ weights_kernel(WeightsArgs a)
             store_weights<TYPE>(a, t, rows, p.piece, p.m0, p.n0);
             stream.stored(!a.accumulate && a.d_w_type == FS_F32 && p.m0 + BM <= a.out_width && p.n0 + BN <= a.in_width);
         }
+        stream.end();
     } else {
         for (int round = 0; round < rounds; ++round) {
             const int id = tile_of_round(round);
