@@ -493,8 +493,10 @@ static void launch_product(ProductArgs a, hipStream_t stream)
     if constexpr (!TURNED) {
         const int64_t met = a.bounds.n_slots < a.bounds.n_experts ? a.bounds.n_slots : a.bounds.n_experts;      // experts, at most
         const int64_t mean = (a.bounds.n_slots + a.bounds.n_experts - 1) / a.bounds.n_experts, row = (int64_t)a.in_width * size;
-        const bool little = met * a.out_width * row <= (32 << 20) && (int64_t)a.bounds.n_slots * ((a.out_width + 15) / 16) * row <= (64 << 20);
-        if (little || (mean <= 8 && met * ((a.out_width + 127) / 128) <= kUnits))
+        const int64_t wide = (a.out_width + 127) / 128, again = (int64_t)a.bounds.n_slots * ((a.out_width + 15) / 16) * row;      // bytes of rows
+        const bool little = met * a.out_width * row <= (32 << 20) && mean <= 192 && again <= (64 << 20);
+        const bool alone = (a.bounds.n_slots / 128 + met) * wide <= 64 && mean <= 256 && again <= (128 << 20);
+        if (little || alone || (mean <= 8 && met * wide <= kUnits))
             return mean <= 16 ? launch_few<TYPE, RESULT, 1>(a, stream) : mean <= 32 ? launch_few<TYPE, RESULT, 2>(a, stream) : launch_few<TYPE, RESULT, 4>(a, stream);
     }
     // fp32 is bound by the matrix units whatever the tile, and small ones leave less idle at the edges and the end.
