@@ -487,22 +487,28 @@ static void launch_product(ProductArgs a, hipStream_t stream)
     const bool direct = streams(a.x, a.x_stride, 0, (int64_t)a.in_width * size) &&
                         streams(a.w, a.w_stride, a.w_step, (int64_t)(TURNED ? a.out_width : a.in_width) * size);
     // Few rows: sixteen columns a workgroup get all compute units to work, and their sums are short, but each reads its expert's rows.
-    // us, tiles of 128 x 128 and this: 30 of 164 x 256 fp32, 64 rows an expert 19.0 and 7.7, 192 19.6 and 15.1; one of 1024 x 1024 bf16,
+    // us, tiles and this: 30 of 164 x 256 fp32, 64 rows an expert 19.0 and 7.7, 192 19.6 and 15.1; one of 1024 x 1024 bf16,
     // 1 row 15.1 and 7.7, 192 27.9 and 12.1; eight of 4096 x 4096, 1 row each 47 and 30, 8 rows 62 and 54, 16 rows 63 and 69; 64 of
-    // 2048 x 1024, 1 row each 28.7 and 29.2, 4 rows 42 and 59.
+    // 2048 x 1024, 1 row each 28.7 and 29.2, 4 rows 42 and 59.  Of 16 and 8 bits only where sums are long, for a tile takes as long as its sum and this
+    // as there are parts: 64 of 1024 to 64, 32 rows each, 256 parts bf16 14.7 and 7.4; 64 of 64 to 1024, 64 rows each, 4096 parts 8.0 and
+    // 15.9, int8 8.5 and 21.
     if constexpr (!TURNED) {
         const int64_t met = a.bounds.n_slots < a.bounds.n_experts ? a.bounds.n_slots : a.bounds.n_experts;      // experts, at most
         const int64_t mean = (a.bounds.n_slots + a.bounds.n_experts - 1) / a.bounds.n_experts, row = (int64_t)a.in_width * size;
         const int64_t wide = (a.out_width + 127) / 128, again = (int64_t)a.bounds.n_slots * ((a.out_width + 15) / 16) * row;      // bytes of rows
-        const bool little = met * a.out_width * row <= (32 << 20) && mean <= 192 && again <= (64 << 20);
+        const int64_t parts = (a.bounds.n_slots / 64 > met ? a.bounds.n_slots / 64 : met) * ((a.out_width + 15) / 16);
+        const bool little = met * a.out_width * row <= (32 << 20) && mean <= 192 && again <= (TYPE == kI8 ? 32 << 20 : 64 << 20);
         const bool alone = (a.bounds.n_slots / 128 + met) * wide <= 64 && mean <= 256 && again <= (128 << 20);
-        if (little || alone || (mean <= 8 && met * wide <= kUnits))
+        if ((TYPE == FS_F32 || parts <= row) && (little || alone || (mean <= 8 && met * wide <= kUnits)))
             return mean <= 16 ? launch_few<TYPE, RESULT, 1>(a, stream) : mean <= 32 ? launch_few<TYPE, RESULT, 2>(a, stream) : launch_few<TYPE, RESULT, 4>(a, stream);
     }
     // fp32 is bound by the matrix units whatever the tile, and small ones leave less idle at the edges and the end.
     const bool small = TYPE == FS_F32 || a.out_width <= 64;
     if constexpr (TYPE != FS_F32) {
-        if (direct && a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192)
+        // Tiles of 128 x 128 where the card makes all of them at once, two a compute unit: us, of 128 and of 256, in 4096 to out columns
+        // bf16: 2048 slots of 8 experts to 1024 48 and 84, to 4096 94 and 125; 4096 slots of 4 to 2048 64 and 88, to 4096 131 and 103.
+        const bool at_once = (int64_t)(a.bounds.n_slots / 128) * ((a.out_width + 127) / 128) <= 2 * kUnits;
+        if (direct && a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192 && !at_once)
             return launch_tiles<TYPE, RESULT, TURNED, Wide, true>(a, stream);
         if (!small)
             return direct ? launch_tiles<TYPE, RESULT, TURNED, Middle, true>(a, stream) : launch_tiles<TYPE, RESULT, TURNED, Middle, false>(a, stream);
