@@ -34,8 +34,8 @@ extern "C" {
 
 /*
  * The slots [first[e], first[e+1]) are expert e's, as fs_expert_plan leaves them; from first[n_experts] on nobody's.
- * Bounds are taken as max(0, min(n_slots, .)), a last one before its first as equal to it, so that no list of bounds leads
- * outside the matrices; where experts' slots overlap, results there are one of the experts', from run to run either.
+ * Bounds are taken as max(0, min(n_slots, .)), so that no list of them leads outside the matrices; of bounds that descend
+ * anywhere the results are not defined (those of fs_expert_matmul_backward too).
  *
  * Weights: turned = 0: expert e's are out_width rows of in_width elements, row o at w + e * w_step + o * w_stride, and
  *   y[s][o] = sum over i of x[s][i] * w[e][o][i];

@@ -398,7 +398,7 @@ struct Tile {
                     lo[i] = fragment_a(lds, i, 0);
             }
         }
-        __device__ __forceinline__ const char *place() const { return lds + (kStages == 3 ? used % 3 : used & (kStages - 1)) * stage_bytes; }
+        __device__ __forceinline__ const char *place() const { return lds + (used & (kStages - 1)) * stage_bytes; }
         // The sums of the tile whose steps come next.
         template <class F>
         __device__ __forceinline__ void sum(Tile &t, int k_count, F next)
@@ -619,13 +619,15 @@ struct PieceTable {
     int16_t order[SORTED ? FS_MAX_EXPERTS : 1];
     int waves[16];
     __device__ __forceinline__ int expert_at(int place) const { return SORTED ? order[place] : place; }
-    // By all THREADS of the workgroup; the number of pieces.
+    // By all THREADS of the workgroup; the number of pieces, none if bounds descend: their pieces could be more than 32 bits count.
     template <int THREADS>
     __device__ __forceinline__ int fill(const Bounds &b)
     {
         constexpr int most = (FS_MAX_EXPERTS + THREADS - 1) / THREADS;
         const int each = (b.n_experts + THREADS - 1) / THREADS, e0 = threadIdx.x * each, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        static_assert(THREADS <= 512, "");
         int n[most], sum = 0;
+        bool descends = false;
         if constexpr (SORTED) {
             int begin, end;
 #pragma unroll
@@ -654,20 +656,25 @@ struct PieceTable {
             if (u < each && e0 + u < b.n_experts) {
                 int begin, end;
                 n[u] = b.pieces(expert_at(e0 + u), begin, end);
+                descends |= b.first[e0 + u + 1] < b.first[e0 + u];
                 if constexpr (SORTED)
                     n[u] = max(n[u], 1);
             }
             sum += n[u];
         }
         const int to_here = Bounds::sum_to(sum);
-        if (lane == 63)
+        descends = __any(descends);
+        if (lane == 63) {
             waves[wave] = to_here;
+            waves[8 + wave] = descends;
+        }
         __syncthreads();
         int before = to_here - sum, all = 0;
 #pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) {
             before += w < wave ? waves[w] : 0;
             all += waves[w];
+            descends |= waves[8 + w] != 0;
         }
 #pragma unroll
         for (int u = 0; u < most; ++u)
@@ -678,7 +685,7 @@ struct PieceTable {
         if (threadIdx.x == 0)
             upto[b.n_experts] = all;
         __syncthreads();
-        return __builtin_amdgcn_readfirstlane(all);
+        return __builtin_amdgcn_readfirstlane(descends ? 0 : all);
     }
     // Piece `id`, which is there: the last expert with no more than `id` before it, by 64 lanes twice.
     __device__ __forceinline__ Piece find(const Bounds &b, int id) const

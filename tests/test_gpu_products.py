@@ -240,6 +240,22 @@ def test_bounds_that_lead_outside_are_cut(api, typ):
     torch.cuda.synchronize()
 
 
+def test_bounds_that_descend_touch_nothing_else(api):
+    # All experts claim all slots: as pieces of 128 rows they would be some 500 times as many as the slots have.
+    import torch
+    n, experts = 20000, 1024
+    first = torch.tensor([0, n] * (experts // 2) + [n], dtype=torch.int32, device="cuda")
+    plan = api.ExpertPlan(first, torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty((n, 1), dtype=torch.int32, device="cuda"))
+    x, w = torch.ones(n, 64, device="cuda"), torch.ones(experts, 64, 64, device="cuda")
+    around = torch.full((n + 2, 64), 7.0, device="cuda")
+    api.fs_expert_matmul(x, plan, w, out=around[1:-1])
+    api.fs_expert_matmul(x, plan, w, turned=True, out=around[1:-1])
+    assert bool((around[0] == 7).all()) and bool((around[-1] == 7).all())
+    grads = torch.full((experts + 2, 64, 64), 7.0, device="cuda")
+    api.fs_expert_matmul_backward(x, x, plan, d_w=grads[1:-1])
+    assert bool((grads[0] == 7).all()) and bool((grads[-1] == 7).all())
+
+
 def test_weights_of_all_experts_in_one(api):
     import torch
     plan = plan_of(api, [9, 140, 3])
