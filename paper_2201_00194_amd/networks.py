@@ -42,6 +42,8 @@ class NetworkMixture:
 
     def _programs(self, row_score, prog_off):
         lengths = (prog_off[1:] - prog_off[:-1]).long()
+        if row_score.shape[0] == 0 or lengths.shape[0] == 0:
+            return row_score.new_zeros(lengths.shape[0]), lengths
         return self.torch.segment_reduce(row_score[:, 0], "sum", lengths=lengths, initial=0.0), lengths
 
     def forward(self, rows, prog_off):
@@ -76,7 +78,7 @@ class NetworkMixture:
         self.w -= (rate * d_w).to(self.dtype)
         self.v -= (rate * d_v).to(self.dtype)
         self.served = None
-        return (off * off).mean()
+        return (off * off).sum() / max(1, off.shape[0])
 
     def teach(self, rows, ids, teacher, total=None, rate: float = 0.5, temperature: float = 1.0):
         """One step of the router towards a teacher's choice: for every row experts `ids` [rows, k] (-1: none) and their logits; the mean
@@ -89,7 +91,7 @@ class NetworkMixture:
         d_loss = torch.full((n,), 1.0 / max(1, n), device="cuda")
         d_logits = api.fs_distill_backward(params, logits, ids, teacher, d_loss, total=total, loss=loss)
         self.gate -= rate * (rows.float().t() @ d_logits)
-        return loss.mean()
+        return loss.sum() / max(1, n)
 
     def serve(self):
         """Lays the weights out in 8-bit integers, a scale for every channel."""

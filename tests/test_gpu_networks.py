@@ -171,3 +171,21 @@ def test_the_products_in_one_graph(api):
         assert torch.equal(h, api.fs_expert_matmul(xs, p, mix.w))
         d = api.fs_expert_matmul(d_y, p, mix.v, turned=True)
         assert torch.equal(d_a, d) and torch.equal(d_w, api.fs_expert_matmul_backward(d, xs, p))
+
+
+def test_no_rows_and_programs_without_rows(api):
+    import torch
+    from paper_2201_00194_amd.networks import NetworkMixture
+    mix = NetworkMixture(api, 20, 3, hidden=16)
+    none = torch.empty(0, 20, device="cuda")
+    for off in ([0], [0, 0, 0]):
+        off = torch.tensor(off, dtype=torch.int32, device="cuda")
+        programs = off.shape[0] - 1
+        score, way = mix.forward(none, off)
+        assert score.tolist() == [0.0] * programs and mix.score_served(none, off).tolist() == [0.0] * programs
+        assert all(bool((d == 0).all()) for d in mix.gradients(way, torch.ones(programs, device="cuda")))
+        assert float(mix.step(none, off, torch.zeros(programs, device="cuda"))) == 0
+    assert float(mix.teach(none, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"))) == 0
+    rows = torch.randn(5, 20, device="cuda")
+    score, _ = mix.forward(rows, torch.tensor([0, 0, 5, 5], dtype=torch.int32, device="cuda"))
+    assert float(score[0]) == 0 and float(score[2]) == 0 and float(score[1]) != 0
