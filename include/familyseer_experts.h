@@ -97,7 +97,7 @@ int fs_expert_matmul_i8(int64_t n_slots, int32_t n_experts, int32_t in_width, in
 typedef struct fs_distill_params {
     int32_t n_classes;   /* 1 .. FS_MAX_CLASSES                                  */
     int32_t k;           /* 1 .. FS_MAX_LISTED: entries of a token's list        */
-    float temperature;   /* > 0, finite: all logits are divided by it            */
+    float temperature;   /* >= 2^-126, finite: all logits are divided by it      */
     float scale;         /* factor on the loss, finite (often temperature^2)     */
 } fs_distill_params;
 

@@ -268,6 +268,9 @@ __device__ __forceinline__ float share_of(float v, float from, float rate)
     return __builtin_amdgcn_exp2f(fminf(fmaxf(v - from, -__builtin_inff()), 0.0f) * rate);
 }
 
+// Exponents of 2 are counted from a largest one that is rounded: below this, it is off by less than 1.
+constexpr float kPlain = 16777216.0f;
+
 // The same chunk, of which nothing is known: what was made of its elements before is not kept beside it.
 template <class T>
 __device__ __forceinline__ T anew(T v)
@@ -354,9 +357,9 @@ distill_row_kernel(DistillArgs a)
                 m = fmaxf(m, (float)v[i]);
         }
         const float M = clean(team.join(m, [](float p, float q) { return fmaxf(p, q); })), from = M > -__builtin_inff() ? M : 0.0f;
-        // Exponents of 2 as one product and sum, from `base`, where no logit is so large that they overflow or NaN.
+        // Exponents of 2 as one product and sum, from `base`, where it is near enough to the largest logit's and nothing is NaN.
         float base = from * a.rate, s = 0.0f;
-        bool plain = fabsf(base) < 1e30f;
+        bool plain = fabsf(base) < kPlain;
         if (plain) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -519,7 +522,7 @@ distill_long_kernel(DistillArgs a)
                 base = most * a.rate;
                 s = m > -__builtin_inff() ? s * __builtin_amdgcn_exp2f(before - base) : 0.0f;
                 m = most;
-                plain = plain && fabsf(base) < 1e30f;
+                plain = plain && fabsf(base) < kPlain;
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
@@ -529,7 +532,7 @@ distill_long_kernel(DistillArgs a)
         }
         if (m > -__builtin_inff())               // from m itself
             s *= __builtin_amdgcn_exp2f(fmaf(-m, a.rate, base));
-        if (!(plain && s == s)) {                // infinities and NaN, or logits that overflow
+        if (!(plain && s == s)) {                // infinities and NaN, or logits far above the temperature
             m = -__builtin_inff();
             s = 0.0f;
             for (int c = team.h * N; c < batches * AHEAD * threads * N; c += threads * N)
@@ -616,8 +619,8 @@ static int check_distill(const char *who, const fs_distill_params *p, int64_t n_
         return fail(p->n_classes < 1 ? FS_EINVAL : FS_EUNSUPPORTED, "%s: n_classes %d outside [1, %d]", who, p->n_classes, FS_MAX_CLASSES);
     if (p->k < 1 || p->k > FS_MAX_LISTED)
         return fail(p->k < 1 ? FS_EINVAL : FS_EUNSUPPORTED, "%s: k %d outside [1, %d]", who, p->k, FS_MAX_LISTED);
-    if (!(p->temperature > 0.0f) || p->temperature > 3.402823466e38f)
-        return fail(FS_EINVAL, "%s: temperature %g is not positive and finite", who, (double)p->temperature);
+    if (!(p->temperature >= 1.17549435e-38f) || p->temperature > 3.402823466e38f)      // below, log2(e) / T would be no fp32
+        return fail(FS_EINVAL, "%s: temperature %g is not of at least 2^-126 and finite", who, (double)p->temperature);
     if (!(fabsf(p->scale) <= 3.402823466e38f))
         return fail(FS_EINVAL, "%s: scale %g is not finite", who, (double)p->scale);
     if (n_tokens < 0 || n_tokens >= ((int64_t)1 << 31))

@@ -134,6 +134,7 @@ DISTILL = dict(n_classes=64, k=8, temperature=1.0, scale=1.0)
 @pytest.mark.parametrize("change,code,word", [
     (dict(n_classes=0), EINVAL, "n_classes"), (dict(n_classes=1048577), EUNSUPPORTED, "n_classes"), (dict(k=0), EINVAL, "k 0"), (dict(k=1025), EUNSUPPORTED, "k 1025"),
     (dict(temperature=0.0), EINVAL, "temperature"), (dict(temperature=-1.0), EINVAL, "temperature"), (dict(temperature=float("nan")), EINVAL, "temperature"),
+    (dict(temperature=1e-40), EINVAL, "temperature"),
     (dict(temperature=float("inf")), EINVAL, "temperature"), (dict(scale=float("nan")), EINVAL, "scale"), (dict(scale=float("-inf")), EINVAL, "scale")])
 def test_distillation_refuses_bad_parameters(api, change, code, word):
     p = api._FsDistillParams(**{**DISTILL, **change})

@@ -94,6 +94,15 @@ def test_temperatures_scales_and_strides(api, typ, temperature, scale, extra, at
 
 
 @pytest.mark.parametrize("typ", list(HALF))
+@pytest.mark.parametrize("temperature", [1e-20, 1e30])
+@pytest.mark.parametrize("classes", [20, 5000, 140000])
+def test_far_temperatures(api, typ, temperature, classes):
+    x, ids, teacher, total, d_loss = study(5, 6, classes, 9, typ, temperature=temperature)
+    for some in (None, total):
+        check(api, x, ids, teacher, d_loss, some, temperature, temperature)
+
+
+@pytest.mark.parametrize("typ", list(HALF))
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("classes", [20, 700, 5000])
 def test_masks_short_lists_and_bad_entries(api, typ, rest, classes):
