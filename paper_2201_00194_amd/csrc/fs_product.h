@@ -1,4 +1,8 @@
 // Tiles of matrix products on the matrix units: operands through LDS, sums in registers.
+//
+// sum over k of a[m][k] b[n][k], of operands whose rows lie along the sum or across it (ALONG: row k has all m, or all n).  Fragments are
+// 16 bytes a lane; across 16-bit operands LDS turns them as they are read.  A wavefront of 256 x 256 tiles holds 128 x 64 results, so that
+// of a fragment's read from LDS four or eight products come and LDS keeps up with the matrix units.
 #ifndef FS_PRODUCT_H
 #define FS_PRODUCT_H
 

@@ -1,4 +1,7 @@
 // Products of rows in slots with their expert's weights, in 32, 16 and 8 bits, and the weights' gradient.
+//
+// A workgroup takes tiles of one expert's slots and columns one after the other; which, it finds from the experts' bounds by itself, so that no
+// launch waits for the host to read them.
 #include "fs_product.h"
 
 namespace fs {
@@ -107,7 +110,9 @@ struct Share {
     }
 };
 
-// A workgroup makes BM slots of one expert times BN columns, and then others.
+// A workgroup makes BM slots of one expert times BN columns, and then others.  This form takes any alignment and is bound by the
+// instructions that bring operands through registers: 32 768 slots of 16 experts, 1001 columns to 1001, bf16 127 us, where 1000 to 1000 take 67
+// in the next one.
 template <int TYPE, int RESULT, class SHAPE, bool TURNED>
 __global__ void __launch_bounds__(SHAPE::threads)
 product_kernel(ProductArgs a)
@@ -133,7 +138,10 @@ product_kernel(ProductArgs a)
 }
 
 // The same with operands straight to LDS, one tile after the other: the first step of the next tile is on its way while the last
-// step of one is multiplied and its results are stored.
+// step of one is multiplied and its results are stored.  131 072 slots of 64 experts, 1024 columns to 2048, bf16: 540 us, 1017 TFLOP/s,
+// matrix units half busy; what holds it up is how long a row's first bytes take from memory, for of a quarter of the slots, which stay in the
+// last cache, the same launch makes 1370 TFLOP/s.  Tiles in the order of the pieces, bypassing stores, longer and shorter steps, sums
+// begun at other places, and loads asked for earlier changed nothing or cost time.
 template <int TYPE, int RESULT, class SHAPE, bool TURNED>
 __global__ void __launch_bounds__(SHAPE::threads)
 product_stream_kernel(ProductArgs a)
@@ -177,7 +185,8 @@ product_stream_kernel(ProductArgs a)
 }
 
 // Few rows an expert: what counts is how fast the weights arrive.  A workgroup makes sixteen columns of one expert's results; its
-// wavefronts share the sum out, 64 bytes of it each in turn, straight from memory to registers, and meet in LDS.
+// wavefronts share the sum out, 64 bytes of it each in turn, straight from memory to registers, and meet in LDS.  One row of 30
+// experts, 1024 x 1024 bf16: 5 us; 16 slots of 30 of 2048 x 2048 int8, 46 MB of weights: 12.6 us, 3.7 TB/s.
 constexpr int kFewWaves = 4;
 template <int TYPE, int RESULT, int MF>
 __global__ void __launch_bounds__(kFewWaves * 64)
@@ -327,6 +336,8 @@ __device__ __forceinline__ void store_weights(const WeightsArgs &a, const T &t, 
 // A workgroup makes BM x BN of an expert's gradient over one piece of its slots, and then others: the gradient itself where the
 // piece is all of them, else a partial sum.  Pieces differ in length.  The longest come first, and each round of tiles goes to the XCDs the
 // other way round than the one before, so that all have about the same to do; an XCD's tiles of a round are neighbours.
+// 131 072 slots of 64 experts, 1024 x 1024 bf16, a tenth nobody's: 336 us, 740 TFLOP/s, matrix units half busy: rows of both operands come
+// from memory as those of products do.  65 536 slots of 30, 164 x 256 fp32: 77 us, 71 TFLOP/s, 64 % busy.
 template <int TYPE, class SHAPE, bool DIRECT>
 __global__ void __launch_bounds__(SHAPE::threads)
 weights_kernel(WeightsArgs a)
@@ -402,7 +413,8 @@ weights_kernel(WeightsArgs a)
     }
 }
 
-// The partial sums of an expert's pieces, in their order, in 64 bits: a wavefront to a row of the gradient.
+// The partial sums of an expert's pieces, in their order, in 64 bits: a wavefront to a row of the gradient.  8 us for 164 x 256 of 30
+// experts of which each has two or three; 16 us for 64 of 1024 x 1024, most of it the start of workgroups that have nothing to join.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 weights_join_kernel(WeightsArgs a)
