@@ -111,7 +111,7 @@ struct Share {
 };
 
 // A workgroup makes BM slots of one expert times BN columns, and then others.  This form takes any alignment and is bound by the
-// instructions that bring operands through registers: 32 768 slots of 16 experts, 1001 columns to 1001, bf16 127 us, where 1000 to 1000 take 67
+// instructions that bring operands through registers: 32 768 slots of 16 experts, 1001 columns to 1001, bf16 108 us, where 1000 to 1000 take 67
 // in the next one.
 template <int TYPE, int RESULT, class SHAPE, bool TURNED>
 __global__ void __launch_bounds__(SHAPE::threads)
@@ -131,7 +131,7 @@ product_kernel(ProductArgs a)
         const Operand x = {a.x + (int64_t)piece.first * a.x_stride, a.x_stride, piece.count};
         const char *const w = a.w + (int64_t)piece.expert * a.w_step;
         const Operand b = {TURNED ? w + (int64_t)n0 * T::U::size : w + (int64_t)n0 * a.w_stride, a.w_stride, a.out_width - n0};
-        t.run(lds, x, b, a.in_width);
+        t.run(lds, x, b, a.in_width, a.in_width, TURNED ? a.out_width : a.in_width);
         store_product_as<TYPE, RESULT>(a, t, rows, piece, n0);
         __syncthreads();      // the last step has been read
     }
@@ -406,7 +406,7 @@ weights_kernel(WeightsArgs a)
             const Place2 p = place_of(id);
             T t;
             t.clear();
-            t.run(lds, operand_g(p), operand_x(p), p.piece.count);
+            t.run(lds, operand_g(p), operand_x(p), p.piece.count, a.out_width, a.in_width);
             store_weights<TYPE>(a, t, rows, p.piece, p.m0, p.n0);
             __syncthreads();      // the last step has been read
         }
