@@ -20,6 +20,7 @@ typedef Shape<256, 256, 2, 4, 128, 2> Wide;           // of rows
 typedef Shape<256, 256, 2, 4, 64, 4> WideAcross;      // of weights' gradients
 typedef Shape<128, 128, 2, 2, 128, 2> Middle;
 typedef Shape<128, 64, 4, 1, 64, 2> Small;            // of rows
+typedef Shape<64, 64, 2, 1, 128, 2> Little;           // of rows
 typedef Shape<128, 64, 2, 1, 64, 2> SmallAcross;
 
 // Results of a tile whose piece and first column are given.
@@ -504,11 +505,12 @@ static void launch_product(ProductArgs a, hipStream_t stream)
     // 2048 x 1024, 1 row each 28.7 and 29.2, 4 rows 42 and 59.  Of 16 and 8 bits only where sums are long, for a tile takes as long as its sum and this
     // as there are parts: 64 of 1024 to 64, 32 rows each, 256 parts bf16 14.7 and 7.4; 64 of 64 to 1024, 64 rows each, 4096 parts 8.0 and
     // 15.9, int8 8.5 and 21.
+    const int64_t met = a.bounds.n_slots < a.bounds.n_experts ? a.bounds.n_slots : a.bounds.n_experts;      // experts, at most
+    const int64_t pieces = a.bounds.n_slots / 64 > met ? a.bounds.n_slots / 64 : met;                       // of 64 slots, about
     if constexpr (!TURNED) {
-        const int64_t met = a.bounds.n_slots < a.bounds.n_experts ? a.bounds.n_slots : a.bounds.n_experts;      // experts, at most
         const int64_t mean = (a.bounds.n_slots + a.bounds.n_experts - 1) / a.bounds.n_experts, row = (int64_t)a.in_width * size;
         const int64_t wide = (a.out_width + 127) / 128, again = (int64_t)a.bounds.n_slots * ((a.out_width + 15) / 16) * row;      // bytes of rows
-        const int64_t parts = (a.bounds.n_slots / 64 > met ? a.bounds.n_slots / 64 : met) * ((a.out_width + 15) / 16);
+        const int64_t parts = pieces * ((a.out_width + 15) / 16);
         const bool little = met * a.out_width * row <= (32 << 20) && mean <= 192 && again <= (TYPE == kI8 ? 32 << 20 : 64 << 20);
         const bool alone = (a.bounds.n_slots / 128 + met) * wide <= 64 && mean <= 256 && again <= (128 << 20);
         if ((TYPE == FS_F32 || parts <= row) && (little || alone || (mean <= 8 && met * wide <= kUnits)))
@@ -522,6 +524,11 @@ static void launch_product(ProductArgs a, hipStream_t stream)
         const bool at_once = (int64_t)(a.bounds.n_slots / 128) * ((a.out_width + 127) / 128) <= 2 * kUnits;
         if (direct && a.out_width > 128 && a.bounds.n_slots / a.bounds.n_experts >= 192 && !at_once)
             return launch_tiles<TYPE, RESULT, TURNED, Wide, true>(a, stream);
+        // Tiles of 64 x 64 in the same case: alone on a compute unit a tile takes the time that its operands take to get there.  us, of 128
+        // and of 64, 1024 columns to out bf16: 1000 slots of one expert to 1024 16.4 and 11.7, to 2048 17.1 and 14.7; 2048 slots of 8 to 2048,
+        // 1024 tiles, 17.8 and 24.2.
+        if (direct && pieces * ((a.out_width + 63) / 64) <= 2 * kUnits)
+            return launch_tiles<TYPE, RESULT, TURNED, Little, true>(a, stream);
         if (!small)
             return direct ? launch_tiles<TYPE, RESULT, TURNED, Middle, true>(a, stream) : launch_tiles<TYPE, RESULT, TURNED, Middle, false>(a, stream);
     }
