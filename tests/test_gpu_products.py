@@ -94,7 +94,8 @@ SHAPES = [
     ([0, 0, 0], 4, 32, 32, 0, 0), ([15, 16, 17], 0, 40, 33, 0, 0), ([64, 65, 63, 1], 7, 63, 65, 0, 0), ([128, 127, 129, 0, 1], 3, 128, 128, 0, 0),
     ([130], 0, 164, 64, 0, 0), ([70, 3, 200], 5, 164, 100, 4, 0), ([70, 3, 200], 5, 96, 160, 3, 1), ([31, 300], 0, 255, 257, 0, 0),
     ([5, 4, 6, 3, 7, 2, 8, 0, 9], 0, 512, 384, 0, 0), ([256, 257, 255], 1, 256, 256, 8, 8), ([600], 0, 1000, 300, 0, 0), ([40, 600, 2], 9, 320, 520, 16, 0),
-    ([1] * 40, 0, 1024, 128, 0, 0), ([4, 4], 0, 2048, 48, 0, 0), ([1, 3], 0, 3000, 17, 0, 0), ([700, 20, 513], 0, 72, 1030, 0, 0)]
+    ([1] * 40, 0, 1024, 128, 0, 0), ([4, 4], 0, 2048, 48, 0, 0), ([1, 3], 0, 3000, 17, 0, 0), ([700, 20, 513], 0, 72, 1030, 0, 0),
+    ([1400, 0, 700, 5, 900], 3, 144, 3000, 0, 0), ([500, 64, 200, 3, 433], 2, 200, 2000, 8, 0)]
 
 
 @pytest.mark.parametrize("typ", list(HALF))

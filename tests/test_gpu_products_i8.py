@@ -123,7 +123,7 @@ def test_a_plan_of_ones_own_stays_inside(api):
 SHAPES = [([1], 0, 1, 1, 0, 0), ([3, 0, 5, 1], 2, 16, 24, 0, 0), ([2, 1], 1, 17, 3, 0, 0), ([0, 0], 4, 32, 32, 0, 0), ([15, 16, 17], 0, 40, 33, 3, 1),
           ([64, 65, 63, 1], 7, 63, 65, 0, 0), ([128, 127, 129, 0, 1], 3, 128, 128, 0, 0), ([70, 3, 200], 5, 164, 100, 12, 4), ([256, 257, 255], 1, 256, 256, 16, 16),
           ([600], 0, 1000, 300, 0, 0), ([1] * 40, 0, 1024, 128, 0, 0), ([4, 4], 0, 2048, 48, 0, 0), ([1, 3], 0, 3001, 17, 0, 0), ([700, 20, 513], 0, 72, 1030, 0, 0),
-          ([300, 300], 1, 4096, 256, 0, 0)]
+          ([300, 300], 1, 4096, 256, 0, 0), ([1400, 0, 700, 5, 900], 3, 144, 3000, 0, 0), ([500, 64, 200, 3, 433], 2, 208, 2000, 16, 16)]
 
 
 @pytest.mark.parametrize("typ", list(HALF))
