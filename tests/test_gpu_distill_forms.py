@@ -1,0 +1,180 @@
+"""Distillation of so many rows that workgroups go from one to the next, and of rows whose numbers are at the ends of fp32, against the definition
+in 64 bits on the device, every row of it.
+
+What fp32 may be off by: each exponential by 4 * 2^-23 of itself and 2^-23 for each unit of |x - m|, which is 100 at most where it counts;
+a thread adds at most 128 of them one after the other, or classes / 64, each addition off by 2^-24 of the sum, and all else is added in 64 bits.
+A loss is off by that share of what is added up in it and half a step of fp32, a gradient by twice that share (its own exponential and
+the sum that it is divided by) and half a step of its type."""
+import numpy as np
+import pytest
+
+from oracle import experts_oracle as XO
+
+HALF = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+LEAST = {"fp32": 1e-37, "bf16": 1e-37, "fp16": 2.0 ** -25}
+BIG = float(np.finfo(np.float32).max)
+
+
+@pytest.fixture(scope="module")
+def api():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    from paper_2201_00194_amd import api as A
+    return A
+
+
+def of(typ):
+    import torch
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[typ]
+
+
+def definition(x, ids, teacher, total, d_loss, temperature, scale):
+    """(loss, size of what is added up in it, gradient, size of what is added up in it) of rows whose entries name a class once."""
+    import torch
+    inf = float("inf")
+
+    def clean(v):
+        v = v.double()
+        return torch.where(torch.isnan(v), -inf, v).clamp(max=BIG) / temperature
+
+    def log_sum(v):                       # -inf where there is nothing
+        m = v.max(dim=1, keepdim=True).values
+        m = torch.where(torch.isinf(m), 0.0, m)
+        return m, torch.log(torch.exp(v - m).sum(dim=1, keepdim=True))
+
+    x = clean(x)
+    ids = ids.long()
+    at = ids.clamp(0, x.shape[1] - 1)
+    t = clean(teacher)
+    own = x.gather(1, at)
+    on = (ids >= 0) & (ids < x.shape[1]) & (own > -inf) & (t > -inf)
+    taught = on.any(dim=1, keepdim=True)
+    named = torch.zeros(x.shape[0], x.shape[1] + 1, dtype=torch.bool, device=x.device)
+    named.scatter_(1, torch.where(on, at, x.shape[1]), True)
+    named = named[:, :-1]
+    beside = torch.where(named, -inf, x)
+    m, s = log_sum(x)
+    log_p, own_log_p = (x - m) - s, (own - m) - s
+    t = torch.where(on, t, -inf)
+    mt, st = log_sum(t)
+    log_q = (t - mt) - st
+    with_rest = torch.zeros_like(taught)
+    if total is not None:
+        with_rest = torch.isfinite(total)[:, None] & (beside > -inf).any(dim=1, keepdim=True) & taught
+        log_q = torch.where(with_rest, (t - torch.where(torch.isfinite(total), total, 0.0)[:, None].double()).clamp(max=0), log_q)
+    q = torch.where(on, torch.exp(log_q), 0.0)
+    counts = on & (q > 0)
+    log_q, own_log_p, own = (torch.where(counts, v, 0.0) for v in (log_q, own_log_p, own))
+    loss = (q * (log_q - own_log_p)).sum(dim=1)
+    size = (q * (log_q.abs() + own.abs() + own_log_p.abs() + 1)).sum(dim=1)
+    q_rest = torch.where(with_rest, (1 - q.sum(dim=1, keepdim=True)).clamp(min=0), 0.0)
+    mr, sr = log_sum(beside)
+    log_p_rest = (mr - m) - s + sr
+    some = (q_rest > 0)[:, 0]
+    rest_term = torch.where(some, (q_rest * (torch.log(q_rest) - log_p_rest))[:, 0], 0.0)
+    loss = loss + rest_term
+    size = size + torch.where(some, (q_rest * (torch.log(q_rest).abs() + log_p_rest.abs()) + 1)[:, 0], 0.0)
+    f = d_loss.double()[:, None] * scale / temperature
+    p = torch.exp(log_p)
+    part = torch.where(beside > -inf, torch.exp((beside - mr) - sr) * q_rest, 0.0)
+    grad = p * (q.sum(dim=1, keepdim=True) + q_rest) - part
+    grad_size = p * (q.sum(dim=1, keepdim=True) + q_rest) + part
+    grad.scatter_add_(1, at, -q)
+    grad_size.scatter_add_(1, at, q)
+    open_ = taught & (x > -inf)
+    taught = taught[:, 0]
+    return (torch.where(taught, loss * scale, 0.0), torch.where(taught, size * abs(scale), 0.0),
+            torch.where(open_, grad * f, 0.0), torch.where(open_, grad_size * f.abs(), 0.0))
+
+
+@pytest.mark.parametrize("rest", [False, True])
+def test_the_definition_against_the_oracle(rest):
+    import torch
+    torch.manual_seed(0)
+    x = torch.randn(12, 17, dtype=torch.float64) * 3
+    ids = torch.stack([torch.randperm(17)[:5] for _ in range(12)])
+    teacher, total, d_loss = torch.randn(12, 5).double(), torch.rand(12) + 2.5, torch.randn(12)
+    inf = float("inf")
+    x[0], x[1, ::2], x[2, 3], x[3] = -inf, -inf, inf, float("nan")
+    x[4] = -inf
+    x[4].scatter_(0, ids[4], 1.0)
+    ids[5], ids[6, 1], ids[7, 0], teacher[8, 2], teacher[9, 0] = -1, -1, 99, -inf, inf
+    total[10] -= 4
+    total[11] = inf
+    got = definition(x, ids, teacher, total if rest else None, d_loss, 0.7, 1.5)
+    want = XO.distill(x.numpy(), ids.numpy(), teacher.numpy(), 0.7, 1.5, total.double().numpy() if rest else None, d_loss.double().numpy())
+    for a, b in zip(got, want):
+        np.testing.assert_allclose(a.numpy(), b, rtol=1e-11, atol=1e-11)
+
+
+def study(seed, rows, classes, k, typ, temperature=1.0):
+    """Rows that all differ, with masked classes, short lists, rows without a list, and totals that say nothing."""
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    x = torch.randn(rows, classes, generator=gen, device="cuda") * 3
+    full = x + torch.randn(rows, classes, generator=gen, device="cuda")
+    best = torch.topk(full, k, dim=1)
+    ids, teacher = best.indices.int(), best.values
+    total = torch.logsumexp(full.double() / temperature, dim=1).float()
+    x[torch.rand(rows, generator=gen, device="cuda") < 0.3, classes // 3: classes // 2] = -float("inf")
+    ids[torch.rand(rows, generator=gen, device="cuda") < 0.2, k // 2:] = -1
+    ids[torch.rand(rows, generator=gen, device="cuda") < 0.05] = -1
+    total[torch.rand(rows, generator=gen, device="cuda") < 0.1] = float("nan")
+    return x.to(of(typ)), ids, teacher, total, torch.randn(rows, generator=gen, device="cuda")
+
+
+def check(api, x, ids, teacher, d_loss, total=None, temperature=1.0, scale=1.0, gradient=True, losses=True):
+    import torch
+    rows, classes = x.shape
+    typ = {torch.float32: "fp32", torch.bfloat16: "bf16", torch.float16: "fp16"}[x.dtype]
+    p = api.distill_params(classes, ids.shape[1], temperature, scale)
+    t32, s32 = float(np.float32(temperature)), float(np.float32(scale))
+    results = [api.fs_distill(p, x, ids, teacher, total)] if losses else []
+    d = None
+    if gradient:
+        results.append(torch.full((rows,), 9.0, device="cuda"))
+        d = api.fs_distill_backward(p, x, ids, teacher, d_loss, total, loss=results[-1])
+    share = (208 + 128 + classes / 64) * 2.0 ** -24
+    step = max(1, (1 << 25) // classes)
+    for a in range(0, rows, step):
+        b = slice(a, min(rows, a + step))
+        el, sl, eg, sg = definition(x[b], ids[b], teacher[b], None if total is None else total[b], d_loss[b], t32, s32)
+        for got in results:
+            off = (got[b].double() - el).abs()
+            bad = ~(off <= (share + 2.0 ** -23) * sl + 2.0 ** -24 * el.abs() + 1e-37)
+            assert not bool(bad.any()), (a, torch.nonzero(bad)[:5].tolist(), got[b][bad][:5].tolist(), el[bad][:5].tolist())
+        if gradient:
+            lost = (d_loss[b].double() * s32 / t32).abs()[:, None] * 2.0 ** -126          # the hardware's exponential has no results below 2^-126
+            may = (2 * share + 2.0 ** -22) * sg
+            bad = ~((d[b].double() - eg).abs() <= may + HALF[typ] * (eg.abs() + may) + LEAST[typ] + lost)
+            assert not bool(bad.any()), (a, torch.nonzero(bad)[:5].tolist(), d[b][bad][:5].tolist(), eg[bad][:5].tolist())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,classes,k,typ", [(300, 9001, 20, "fp32"), (600, 20003, 33, "bf16"), (2600, 8200, 7, "fp16"), (2300, 9001, 16, "bf16"), (300, 1000, 300, "fp32"),
+                                                (300, 140000, 64, "bf16"), (257, 600001, 5, "fp16"), (9000, 5000, 8, "fp32")])
+def test_losses_of_many_long_rows(api, rest, rows, classes, k, typ):
+    x, ids, teacher, total, d_loss = study(rows + classes, rows, classes, k, typ)
+    check(api, x, ids, teacher, d_loss, total if rest else None, gradient=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,classes,k,typ", [(600, 131072, 64, "bf16"), (530, 100001, 20, "fp16"), (2500, 20001, 33, "bf16"), (2100, 12001, 12, "fp32"), (600, 65536, 40, "bf16"),
+                                                (300, 30001, 9, "fp32"), (600, 57001, 64, "fp32"), (300, 200000, 20, "bf16"), (300, 70001, 20, "fp32"), (2100, 1000, 300, "bf16")])
+def test_gradients_of_many_long_rows(api, rest, rows, classes, k, typ):
+    """Workgroups make two or three rows, the last round of which not all have."""
+    x, ids, teacher, total, d_loss = study(rows + classes, rows, classes, k, typ)
+    check(api, x, ids, teacher, d_loss, total if rest else None, losses=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("typ", list(HALF))
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,classes,k", [(70001, 30, 8), (270001, 3, 2), (40001, 700, 9), (10001, 4000, 40), (140001, 64, 20), (9001, 1500, 250)])
+def test_many_short_rows(api, typ, rest, rows, classes, k):
+    """Some lanes of a wavefront to a row, and more rows than they take at once."""
+    x, ids, teacher, total, d_loss = study(rows + classes, rows, classes, k, typ)
+    check(api, x, ids, teacher, d_loss, total if rest else None)
