@@ -358,7 +358,8 @@ distill_row_kernel(DistillArgs a)
                 m = fmaxf(m, (float)v[i]);
         }
         const float M = clean(team.join(m, [](float p, float q) { return fmaxf(p, q); })), from = M > -__builtin_inff() ? M : 0.0f;
-        // Exponents of 2 as one product and sum, from `base`, where it is near enough to the largest logit's and nothing is NaN.
+        // Exponents of 2 as one product and sum, from `base`, where it is near enough to the largest logit's and nothing is NaN or infinity: of
+        // either, the sum would tell.  (Temperatures far above 1 bring the largest float near enough too.)
         float base = from * a.rate, s = 0.0f;
         bool plain = fabsf(base) < kPlain;
         if (plain) {
@@ -373,7 +374,8 @@ distill_row_kernel(DistillArgs a)
             }
         }
         double S = team.join((double)s, [](double p, double q) { return p + q; });
-        if (WAVES ? !(plain && S == S) : __any(!(plain && S == S))) {
+        plain = plain && S < __builtin_inf();
+        if (WAVES ? !plain : __any(!plain)) {
             plain = false;
             s = 0.0f;
 #pragma unroll

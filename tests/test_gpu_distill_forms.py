@@ -178,3 +178,28 @@ def test_many_short_rows(api, typ, rest, rows, classes, k):
     """Some lanes of a wavefront to a row, and more rows than they take at once."""
     x, ids, teacher, total, d_loss = study(rows + classes, rows, classes, k, typ)
     check(api, x, ids, teacher, d_loss, total if rest else None)
+
+
+def far_study(api, typ, temperature, classes):
+    """Logits and a teacher's some temperatures apart, however many floats that is; and a factor on the loss that leaves gradients and losses in fp32."""
+    import torch
+    x, ids, teacher, total, d_loss = study(classes, 8, classes, 6, "fp32")
+    x, teacher = ((v * temperature).clamp(-BIG, BIG).to(of(t)) for v, t in ((x, typ), (teacher, "fp32")))
+    return x, ids, teacher, total, d_loss, temperature / 1024
+
+
+FAR = [(typ, temperature, classes) for typ in HALF for temperature in (1e33,) for classes in (20, 700, 5000, 40000, 140000)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("typ,temperature,classes", FAR)
+def test_infinities_at_far_temperatures(api, typ, temperature, classes):
+    """Infinity counts as the largest float, which is some temperatures from the others here."""
+    x, ids, teacher, total, d_loss, scale = far_study(api, typ, temperature, classes)
+    inf = float("inf")
+    x[0, 5], x[1, :2], x[2, int(ids[2, 0])], x[3] = inf, inf, inf, inf
+    x[4, ::2], x[4, 1] = -inf, inf
+    teacher[5, 0] = inf
+    x[6, classes - 1] = inf
+    for some in (None, total):
+        check(api, x, ids, teacher, d_loss, some, temperature, scale)
