@@ -262,10 +262,11 @@ __device__ __forceinline__ void store_entries(const DistillArgs &a, const RowLds
             d_logits[e.id] = (T)e.x;
     }
 }
-// exp((v - from) / T) of a logit whatever it holds: NaN counts as -infinity, infinity as the largest float, which is `from` then.
+// exp((v - from) / T) of a logit whatever it holds: NaN counts as -infinity, infinity as the largest float, which is `from` then.  The
+// difference is of halves, as that of two floats may be no float, and times twice the rate, which is 2^127 * 1.45 at most.
 __device__ __forceinline__ float share_of(float v, float from, float rate)
 {
-    return __builtin_amdgcn_exp2f(fminf(fmaxf(v - from, -__builtin_inff()), 0.0f) * rate);
+    return __builtin_amdgcn_exp2f(fminf(fmaxf(fmaf(v, 0.5f, -0.5f * from), -__builtin_inff()), 0.0f) * (2.0f * rate));
 }
 
 // Exponents of 2 are counted from a largest one that is rounded: below this, it is off by less than 1.

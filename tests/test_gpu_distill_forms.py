@@ -188,7 +188,7 @@ def far_study(api, typ, temperature, classes):
     return x, ids, teacher, total, d_loss, temperature / 1024
 
 
-FAR = [(typ, temperature, classes) for typ in HALF for temperature in (1e33,) for classes in (20, 700, 5000, 40000, 140000)]
+FAR = [(typ, temperature, classes) for typ in HALF for temperature in (1e33, 3e38) for classes in (20, 700, 5000, 40000, 140000)]
 
 
 @pytest.mark.gpu
@@ -201,5 +201,17 @@ def test_infinities_at_far_temperatures(api, typ, temperature, classes):
     x[4, ::2], x[4, 1] = -inf, inf
     teacher[5, 0] = inf
     x[6, classes - 1] = inf
+    for some in (None, total):
+        check(api, x, ids, teacher, d_loss, some, temperature, scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("typ,temperature,classes", [c for c in FAR if c[0] != "fp16"])
+def test_logits_whose_difference_no_float_holds(api, typ, temperature, classes):
+    x, ids, teacher, total, d_loss, scale = far_study(api, typ, temperature, classes)
+    x[0, 0], x[0, 1] = -3.3e38, 3.3e38
+    x[1, ::2], x[1, 1::2] = -2e38, 2e38
+    x[2, :3] = float("nan")
+    x[2, 3], x[2, 4] = 3e38, -3e38
     for some in (None, total):
         check(api, x, ids, teacher, d_loss, some, temperature, scale)
