@@ -18,12 +18,13 @@ struct DistillArgs {
     int64_t n_tokens, logit_stride, d_logit_stride;
     int32_t n_classes, k, id_type, teacher_type;
     int32_t n_bits, ll;         // classes that have a bit; lanes of a row
-    float rate;                 // log2(e) / T
-    double inverse_t, scale;    // of the temperature that `rate` stands for
+    float rate, twice_rate;     // log2(e) / T
+    double inverse_t, inverse_rate, scale;
 };
 
-// -infinity for NaN, the largest float for infinity.
-__device__ __forceinline__ float clean(float v) { return fminf(fmaxf(v, -__builtin_inff()), 3.402823466e38f); }
+// -infinity for NaN, the largest float for infinity.  NaN that signals is made quiet first: of it and a number the larger is NaN, of
+// quiet NaN and a number it is the number.
+__device__ __forceinline__ float clean(float v) { return fminf(fmaxf(__builtin_canonicalizef(v), -__builtin_inff()), 3.402823466e38f); }
 
 __device__ __forceinline__ int64_t id_at(const void *ids, int type, int64_t i) { return type == FS_ID_I64 ? ((const int64_t *)ids)[i] : ((const int32_t *)ids)[i]; }
 __device__ __forceinline__ float element_at(const void *p, int type, int64_t i)
@@ -264,9 +265,9 @@ __device__ __forceinline__ void store_entries(const DistillArgs &a, const RowLds
 }
 // exp((v - from) / T) of a logit whatever it holds: NaN counts as -infinity, infinity as the largest float, which is `from` then.  The
 // difference is of halves, as that of two floats may be no float, and times twice the rate, which is 2^127 * 1.45 at most.
-__device__ __forceinline__ float share_of(float v, float from, float rate)
+__device__ __forceinline__ float share_of(float v, float from, float twice_rate)
 {
-    return __builtin_amdgcn_exp2f(fminf(fmaxf(fmaf(v, 0.5f, -0.5f * from), -__builtin_inff()), 0.0f) * (2.0f * rate));
+    return __builtin_amdgcn_exp2f(fminf(fmaxf(fmaf(v, 0.5f, -0.5f * from), -__builtin_inff()), 0.0f) * twice_rate);
 }
 
 // Exponents of 2 are counted from a largest one that is rounded: below this, it is off by less than 1.
@@ -358,10 +359,13 @@ distill_row_kernel(DistillArgs a)
             for (int i = 0; i < N; ++i)
                 m = fmaxf(m, (float)v[i]);
         }
-        const float M = clean(team.join(m, [](float p, float q) { return fmaxf(p, q); })), from = M > -__builtin_inff() ? M : 0.0f;
+        const auto larger = [](float p, float q) { return fmaxf(p, q); };
+        float M = clean(team.join(m, larger));
+        const auto zero_if_none = [](float most) { return most > -__builtin_inff() ? most : 0.0f; };
         // Exponents of 2 as one product and sum, from `base`, where it is near enough to the largest logit's and nothing is NaN or infinity: of
         // either, the sum would tell.  (Temperatures far above 1 bring the largest float near enough too.)
-        float base = from * a.rate, s = 0.0f;
+        const float base = zero_if_none(M) * a.rate;
+        float s = 0.0f;
         bool plain = fabsf(base) < kPlain;
         if (plain) {
 #pragma unroll
@@ -378,6 +382,17 @@ distill_row_kernel(DistillArgs a)
         plain = plain && S < __builtin_inf();
         if (WAVES ? !plain : __any(!plain)) {
             plain = false;
+            m = -__builtin_inff();      // once more: NaN that signals hid what was larger before it
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (!has(c))
+                    continue;
+                const Chunk v = anew(x[c]);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    m = fmaxf(m, __builtin_canonicalizef((float)v[i]));
+            }
+            M = clean(team.join(m, larger));
             s = 0.0f;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -386,12 +401,13 @@ distill_row_kernel(DistillArgs a)
                 const Chunk v = anew(x[c]);
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    s += share_of((float)v[i], from, a.rate);
+                    s += share_of((float)v[i], zero_if_none(M), a.twice_rate);
             }
             S = team.join((double)s, [](double p, double q) { return p + q; });
         }
+        const float from = zero_if_none(M);
         // What the sum is one of exp((x - .) / T) from.
-        const double origin = !(M > -__builtin_inff()) ? -__builtin_inf() : plain ? (double)base / a.rate : M;
+        const double origin = !(M > -__builtin_inff()) ? -__builtin_inf() : plain ? base * a.inverse_rate : M;
         if (team.leads()) {
             // The registers do not hold all chunks and what the verdict takes: some wait in LDS.
 #pragma unroll
@@ -427,7 +443,7 @@ distill_row_kernel(DistillArgs a)
                 } else {
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const float e = share_of((float)logit[i], from, a.rate);
+                        const float e = share_of((float)logit[i], from, a.twice_rate);
                         d[i] = e > 0.0f ? e * v.factor : 0.0f;
                     }
                 }
@@ -489,12 +505,12 @@ distill_long_kernel(DistillArgs a)
                 most = fmaxf(most, v[i]);
             }
             if (most > m) {
-                s *= share_of(m, most, a.rate);
+                s *= share_of(m, most, a.twice_rate);
                 m = most;
             }
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                s += m > -__builtin_inff() ? share_of(v[i], m, a.rate) : 0.0f;
+                s += m > -__builtin_inff() ? share_of(v[i], m, a.twice_rate) : 0.0f;
         };
         if (batches > 0)
             load(0);
@@ -522,6 +538,7 @@ distill_long_kernel(DistillArgs a)
                 for (int i = 0; i < N; ++i)
                     most = fmaxf(most, (float)now[u][i]);
             }
+            plain = plain && most == most;          // NaN that signals has hidden what was larger before it
             if (most > m) {
                 const float before = base;
                 base = most * a.rate;
@@ -546,7 +563,7 @@ distill_long_kernel(DistillArgs a)
         for (int c = batches * AHEAD * threads * N + team.h * N; c < a.n_classes; c += threads * N)
             one(c);
         const float M = team.join(m, [](float p, float q) { return fmaxf(p, q); }), from = M > -__builtin_inff() ? M : 0.0f;
-        const double S = team.join((double)s * share_of(m, from, a.rate), [](double p, double q) { return p + q; });
+        const double S = team.join((double)s * share_of(m, from, a.twice_rate), [](double p, double q) { return p + q; });
         if (team.leads())
             judge<GRADIENT>(a, row, r, true, apart, bits ? *row.twice != 0 : GRADIENT || apart, total, from, M, S, 6, (int)threadIdx.x);
         if constexpr (GRADIENT) {
@@ -558,7 +575,7 @@ distill_long_kernel(DistillArgs a)
                 load_chunk(logits + c, a.n_classes - c, v, -__builtin_inff());
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float e = share_of(v[i], verdict.from, a.rate);
+                    const float e = share_of(v[i], verdict.from, a.twice_rate);
                     v[i] = e > 0.0f ? e * verdict.factor : 0.0f;
                 }
                 store_chunk<N>(d_logits + c, a.n_classes - c, v);
@@ -658,6 +675,8 @@ static int distill(const char *who, bool gradient, const fs_distill_params *p, D
     a.n_classes = p->n_classes;
     a.k = p->k;
     a.rate = (float)(1.44269504088896340736 / p->temperature);
+    a.twice_rate = 2.0f * a.rate;
+    a.inverse_rate = 1.0 / a.rate;
     a.inverse_t = 1.0 / p->temperature;
     a.scale = p->scale;
     // Bits of the classes: for a rest, and to see whether two entries name one class (comparing 64 entries with each other instead made
@@ -689,7 +708,7 @@ extern "C" int fs_distill(const fs_distill_params *params, int64_t n_tokens, con
                           const void *ids, int32_t id_type, const void *teacher, int32_t teacher_type, const float *total, float *loss,
                           void *work, size_t work_bytes, void *stream)
 {
-    const DistillArgs a = {logits, ids, teacher, total, nullptr, loss, nullptr, n_tokens, logit_stride, 0, 0, 0, id_type, teacher_type, 0, 0, 0, 0, 0};
+    const DistillArgs a = {logits, ids, teacher, total, nullptr, loss, nullptr, n_tokens, logit_stride, 0, 0, 0, id_type, teacher_type, 0, 0, 0, 0, 0, 0, 0};
     return distill("fs_distill", false, params, a, logit_type, work, work_bytes, (hipStream_t)stream);
 }
 
@@ -698,6 +717,6 @@ extern "C" int fs_distill_backward(const fs_distill_params *params, int64_t n_to
                                    const float *d_loss, float *loss, void *d_logits, int64_t d_logit_stride, void *work, size_t work_bytes,
                                    void *stream)
 {
-    const DistillArgs a = {logits, ids, teacher, total, d_loss, loss, d_logits, n_tokens, logit_stride, d_logit_stride, 0, 0, id_type, teacher_type, 0, 0, 0, 0, 0};
+    const DistillArgs a = {logits, ids, teacher, total, d_loss, loss, d_logits, n_tokens, logit_stride, d_logit_stride, 0, 0, id_type, teacher_type, 0, 0, 0, 0, 0, 0, 0};
     return distill("fs_distill_backward", true, params, a, logit_type, work, work_bytes, (hipStream_t)stream);
 }

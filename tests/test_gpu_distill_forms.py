@@ -215,3 +215,21 @@ def test_logits_whose_difference_no_float_holds(api, typ, temperature, classes):
     x[2, 3], x[2, 4] = 3e38, -3e38
     for some in (None, total):
         check(api, x, ids, teacher, d_loss, some, temperature, scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("typ", list(HALF))
+@pytest.mark.parametrize("classes", [20, 700, 5000, 40000, 140000])
+def test_bits_that_signal(api, typ, classes):
+    """NaN whose first bit of the fraction is 0, of either sign, counts as every other: a class that may not be taken."""
+    import torch
+    x, ids, teacher, total, d_loss = study(classes, 6, classes, 5, typ)
+    word = {"fp32": (torch.int32, 0x7fa00000), "bf16": (torch.int16, 0x7fa0), "fp16": (torch.int16, 0x7d00)}[typ]
+    bits = x.view(word[0])
+    bits[0, 1::3] = word[1]
+    bits[1, 0] = word[1]
+    bits[2, 3] = word[1] - (1 << 31 if typ == "fp32" else 1 << 15)
+    bits[3] = word[1]
+    assert int(torch.isnan(x).sum()) == len(range(1, classes, 3)) + 2 + classes
+    for some in (None, total):
+        check(api, x, ids, teacher, d_loss, some)
