@@ -16,7 +16,8 @@ import numpy as np
 
 
 class NetworkMixture:
-    """`dtype`: of rows and weights (fp32, bf16 or fp16); the gate, gradients and scores are fp32."""
+    """`dtype`: of rows and weights (fp32, bf16 or fp16); the gate, gradients and scores are fp32.  Training keeps what of 16-bit weights their type
+    does not hold, in fp32 beside them, so that steps smaller than the type's add up."""
 
     def __init__(self, api, n_features: int, n_experts: int, hidden: int = 64, k: int = 2, dtype=None, seed: int = 0):
         import torch
@@ -33,6 +34,7 @@ class NetworkMixture:
         self.gate = normal(n_features, n_experts, scale=1 / math.sqrt(n_features))
         self.w = normal(n_experts, hidden, n_features, scale=math.sqrt(2 / n_features)).to(self.dtype)
         self.v = normal(n_experts, 1, hidden, scale=1 / math.sqrt(hidden)).to(self.dtype)
+        self.rests = None
         self.served = None
 
     def route(self, rows):
@@ -69,14 +71,26 @@ class NetworkMixture:
         d_logits = api.fs_route_backward(self.params, way["logits"], way["expert"], d_weight)
         return way["rows"].float().t() @ d_logits, d_w, d_v
 
+    def _move(self, w, rest, by):
+        """Takes `by` from 16-bit weights w that `rest` was rounded off, in place; what is rounded off now.  A rest that w cannot have been rounded
+        from is of other weights, which were there before."""
+        whole = w.float() + rest
+        whole = self.torch.where(whole.to(w.dtype) == w, whole, w.float()) - by
+        w.copy_(whole)
+        return whole - w.float()
+
     def step(self, rows, prog_off, target, rate: float = 0.002):
         """One step of gradient descent on the mean squared error against `target`; the loss before it, on the device."""
         program, way = self.forward(rows, prog_off)
         off = program - target
         d_gate, d_w, d_v = self.gradients(way, off * (2.0 / max(1, off.shape[0])))
         self.gate -= rate * d_gate
-        self.w -= (rate * d_w).to(self.dtype)
-        self.v -= (rate * d_v).to(self.dtype)
+        if self.dtype == self.torch.float32:
+            self.w -= rate * d_w
+            self.v -= rate * d_v
+        else:
+            rests = self.rests or (0.0, 0.0)
+            self.rests = self._move(self.w, rests[0], rate * d_w), self._move(self.v, rests[1], rate * d_v)
         self.served = None
         return (off * off).sum() / max(1, off.shape[0])
 
