@@ -60,14 +60,22 @@ class NetworkMixture:
         return program, dict(rows=rows, logits=logits, expert=expert, weight=weight, plan=plan, x=x, a=a, y=y, lengths=lengths)
 
     def gradients(self, way, d_program):
-        """(d_gate, d_w, d_v), fp32, of a loss whose gradient by the programs' scores is d_program."""
-        api, plan = self.api, way["plan"]
+        """(d_gate, d_w, d_v), fp32, of a loss whose gradient by the programs' scores is d_program.  What passes through the networks on the way is
+        of their type; fp16's numbers end at 2^-24 and 2^16, so that there the results' gradient is brought to 16 at most, which leaves room
+        for output weights of up to some thousand, and the weights' gradients back."""
+        api, torch, plan = self.api, self.torch, way["plan"]
         d_rows = d_program.repeat_interleave(way["lengths"], output_size=way["rows"].shape[0])[:, None].contiguous()
         d_y, d_weight = api.fs_expert_combine_backward(d_rows, way["y"], plan, way["weight"])
+        scaled = self.dtype == torch.float16 and d_y.shape[0] > 0
+        if scaled:
+            size = d_y.abs().amax().clamp(min=2.0 ** -100) / 16
+            d_y = d_y / size
         d_y = d_y.to(self.dtype)
         d_v = api.fs_expert_matmul_backward(d_y, way["a"], plan)
         d_a = api.fs_expert_matmul(d_y, plan, self.v, turned=True) * (way["a"] > 0)
         d_w = api.fs_expert_matmul_backward(d_a, way["x"], plan)
+        if scaled:
+            d_v, d_w = d_v * size, d_w * size
         d_logits = api.fs_route_backward(self.params, way["logits"], way["expert"], d_weight)
         return way["rows"].float().t() @ d_logits, d_w, d_v
 

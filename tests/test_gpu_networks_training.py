@@ -1,7 +1,14 @@
-"""Networks as experts whose weights are of 16 bits, in training: steps that are smaller than the weights' own."""
+"""Networks as experts whose weights are of 16 bits, in training: their gradients against the same steps in 64 bits on the host, and steps that are
+smaller than the weights' own.
+
+A result's gradient is rounded to the type on its way to the weights, which is half a step of it or, of fp16's smallest, 2^-25 over what they were
+multiplied by: 16 over the largest, and 2^-100 at least.  The hidden rows' gradient is one product of it, rounded once more.  Products add
+(n + 3) * 2^-24 of their absolute sums, factors 2^-24 each."""
 import numpy as np
 import pytest
 
+from oracle import experts_oracle as XO
+from oracle import mixture_oracle as MO
 from paper_2201_00194_amd.networks import NetworkMixture
 
 pytestmark = pytest.mark.gpu
@@ -26,6 +33,35 @@ def study(api, k, experts, features, hidden, dtype, seed=3, programs=50):
 
 def host(t):
     return t.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("size", [1.0, 1e-8, 1e-20, 1e6])
+@pytest.mark.parametrize("k,experts,features,hidden", [(1, 1, 20, 16), (2, 4, 164, 64), (3, 9, 65, 33)])
+def test_gradients(api, dtype, size, k, experts, features, hidden):
+    import torch
+    typ = getattr(torch, dtype)
+    half = torch.finfo(typ).eps / 2
+    rng, off, o, rows, mix = study(api, k, experts, features, hidden, typ)
+    _, way = mix.forward(rows, o)
+    d_program = torch.from_numpy((rng.standard_normal(off.size - 1) * size).astype(np.float32)).cuda()
+    _, d_w, d_v = mix.gradients(way, d_program)
+    assert d_w.dtype == d_v.dtype == torch.float32
+
+    first, order, place = MO.plan(way["expert"].cpu().numpy(), experts)
+    x, v, a = MO.gather(host(rows), order, k), host(mix.v), host(way["a"])
+    g = np.repeat(host(d_program), np.diff(off))[:, None]
+    d_y, _, _ = MO.combine_backward(g, host(way["y"]), place, host(way["weight"]))
+    least = 2.0 ** -25 * max(np.abs(d_y).max(), 2.0 ** -100) / 16 if dtype == "float16" else 2.0 ** -134      # bf16: half its smallest
+    n = order.size
+    ev, sv = XO.matmul_backward(d_y, a, first, experts)
+    _, lost = XO.matmul_backward(np.ones_like(d_y), a, first, experts)
+    assert np.all(np.abs(host(d_v) - ev) <= (half + (n + 8) * EPS) * (1 + half) * sv + 1.01 * least * lost + 1e-44)
+    open_ = a > 0
+    d_h = XO.matmul(d_y, first, np.swapaxes(v, 1, 2))[0] * open_
+    ew, sw = XO.matmul_backward(d_h, x, first, experts)
+    _, lost = XO.matmul_backward((1 + np.abs(XO.matmul(np.ones_like(d_y), first, np.swapaxes(v, 1, 2))[0])) * open_, x, first, experts)
+    assert np.all(np.abs(host(d_w) - ew) <= (2 * half + half * half + (n + 12) * EPS) * (1 + half) * sw + 1.01 * least * lost + 1e-44)
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
