@@ -267,7 +267,7 @@ struct Tile {
         {
             const I4 buffer = {__builtin_amdgcn_readfirstlane((int)base), __builtin_amdgcn_readfirstlane((int)(base >> 32) & 0xffff), (int)kNowhere, 0x00020000};
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * threads * 16), "v"(from[i]), "s"(buffer)
-                         : "memory", "m0");
+                         : "memory");
         }
         __device__ __forceinline__ void advance() { base += ALONG ? (uint64_t)step * stride : STEP; }
         // Nothing more: zeros come.

@@ -32,8 +32,8 @@ static __device__ __forceinline__ void dma_1k(const uint8_t *src, uint32_t dst, 
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     const uint8_t *p = src + 16 * lane;
-    // m0: the LDS address of such loads
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)dst)), "v"(p) : "memory", "m0");
+    // (m0, the LDS address of such loads, has no other user in these kernels)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)dst)), "v"(p) : "memory");
 #else
     (void)src; (void)dst; (void)lane;
 #endif
