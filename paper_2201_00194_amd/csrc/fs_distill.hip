@@ -40,10 +40,11 @@ __device__ __forceinline__ double brought(double c)
     asm volatile("" : "+s"(c));
     return c;
 }
-// v = n log 2 + f, |f| <= log(2) / 2; the series of exp(f) to f^11 / 11!.
+// v = n log 2 + f, |f| <= log(2) / 2; the series of exp(f) to f^11 / 11!.  n log 2 is taken off as log 2 rounded to 64 bits, in one rounding of
+// what is left, and what that leaves of it.
 __device__ __forceinline__ double exp_of_double(double v)
 {
-    const double n = __builtin_rint(fmax(v, -740.0) * brought(1.4426950408889634)), f = fma(n, brought(-1.90821492927058770002e-10), fma(n, brought(-0.69314718036912381649), v));
+    const double n = __builtin_rint(fmax(v, -740.0) * brought(1.4426950408889634)), f = fma(n, brought(-2.3190468138462996e-17), fma(n, brought(-0.69314718055994531), v));
     double e = brought(1.0 / 39916800);
     e = fma(e, f, brought(1.0 / 3628800));
     e = fma(e, f, brought(1.0 / 362880));
