@@ -233,3 +233,67 @@ def test_bits_that_signal(api, typ, classes):
     assert int(torch.isnan(x).sum()) == len(range(1, classes, 3)) + 2 + classes
     for some in (None, total):
         check(api, x, ids, teacher, d_loss, some)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("typ", list(HALF))
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,classes,k", [(9, 5, 200), (6, 3, 700), (4, 1, 40), (5, 30, 1024), (3, 5000, 1024), (300, 11, 64)])
+def test_lists_that_name_few_classes_over_and_over(api, typ, rest, rows, classes, k):
+    """Every entry counts by itself, and its class is listed once."""
+    import torch
+    x, _, _, _, d_loss = study(rows + classes, rows, classes, min(k, classes), typ)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(k)
+    ids = torch.randint(-1, max(1, classes // 2), (rows, k), generator=gen, device="cuda", dtype=torch.int32)
+    teacher = torch.randn(rows, k, generator=gen, device="cuda")
+    total = torch.logsumexp(teacher, 1) + 0.5 if rest else None
+    p = api.distill_params(classes, k)
+    loss = torch.empty(rows, device="cuda")
+    d = api.fs_distill_backward(p, x, ids, teacher, d_loss, total, loss=loss)
+    el, sl, eg, sg = XO.distill(x.double().cpu().numpy(), ids.cpu().numpy(), teacher.double().cpu().numpy(), 1.0, 1.0,
+                                None if total is None else total.double().cpu().numpy(), d_loss.double().cpu().numpy())
+    share = (208 + 128 + classes / 64) * 2.0 ** -24
+    for got in (loss, api.fs_distill(p, x, ids, teacher, total)):
+        assert np.all(np.abs(got.double().cpu().numpy() - el) <= (share + 2.0 ** -23) * sl + 2.0 ** -24 * np.abs(el) + 1e-37)
+    may = (2 * share + 2.0 ** -22) * sg
+    lost = np.abs(d_loss.double().cpu().numpy())[:, None] * 2.0 ** -126
+    assert np.all(np.abs(d.double().cpu().numpy() - eg) <= may + HALF[typ] * (np.abs(eg) + may) + LEAST[typ] + lost)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("typ", list(HALF))
+@pytest.mark.parametrize("classes", [20, 700, 5000, 40000, 140000])
+def test_a_rest_that_is_nearly_nothing_or_all(api, typ, classes):
+    """The student's rest so far below the list that its probability is no number, or so far above; totals that leave all to the rest, and nothing."""
+    import torch
+    x, ids, teacher, total, d_loss = study(classes + 1, 8, classes, 6, typ)
+    ids = torch.topk(x.float(), 6, dim=1).indices.int()
+    at = ids.long()
+    total[:] = torch.logsumexp(teacher.double(), 1).float() + 0.1
+    for r, by in ((0, 2000.0), (1, 800.0), (2, 90.0), (3, -2000.0), (4, -90.0)):
+        x[r, at[r]] += by
+    total[5], total[6] = 3e38, -3e38
+    x[7] = -float("inf")
+    x[7, at[7]] = 1.0
+    check(api, x, ids, teacher, d_loss, total)
+
+
+@pytest.mark.gpu
+def test_the_longest_rows_in_a_graph(api):
+    """Rows whose bits take more LDS than a kernel has unasked."""
+    import torch
+    x, ids, teacher, total, d_loss = study(3, 3, 600001, 5, "fp32")
+    p = api.distill_params(600001, 5)
+    loss, d = api.fs_distill(p, x, ids, teacher, total), api.fs_distill_backward(p, x, ids, teacher, d_loss, total)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        api.fs_distill(p, x, ids, teacher, total, loss=loss)
+        api.fs_distill_backward(p, x, ids, teacher, d_loss, total, d_logits=d)
+    for _ in range(4):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, api.fs_distill(p, x, ids, teacher, total))
+        assert torch.equal(d, api.fs_distill_backward(p, x, ids, teacher, d_loss, total))

@@ -196,3 +196,42 @@ def test_wide_gradients_of_any_alignment(api, typ):
 def test_gradients_of_narrow_weights(api, typ, wide, out, extra):
     """The widths of networks on feature rows, with an output layer of one column."""
     gradient(api, typ, [4000, 0, 9000, 1, 1200] + [700] * 25, 3, wide, out, extra=extra)
+
+
+@pytest.mark.parametrize("typ", TYPES)
+def test_gradients_of_as_many_experts_as_there_are(api, typ):
+    """1024 lists, many of one length, most of them empty or in one piece."""
+    counts = [(e * 37) % 19 for e in range(1024)]
+    counts[0], counts[511], counts[1023] = 3000, 1700, 900
+    gradient(api, typ, counts, 7, 40, 72)
+    gradient(api, typ, [0] * 1023 + [5], 0, 136, 144)
+
+
+@pytest.mark.parametrize("typ", ["fp32", "bf16", "i8"])
+@pytest.mark.parametrize("pad", [0, 16])
+def test_rows_far_apart(api, typ, pad):
+    """Rows of x, of weights and of gradients 2^23 bytes and more apart: whole chunks, but beyond what a tile's loads reach from its first row."""
+    import torch
+    gen = generator(3)
+    size = torch.empty(0, dtype=of(typ)).element_size()
+    stride, wide, out, counts = (1 << 23) // size + pad, 64, 80, [150, 0, 145]
+    plan, slots = plan_of(api, counts, 5), 300
+    buf = torch.empty(slots * stride, dtype=of(typ), device="cuda")
+    x = buf.as_strided((slots, wide), (stride, 1))
+    x.copy_(whole(gen, typ, slots, wide))
+    w = whole(gen, typ, 3, out, wide)
+    want = exact(plan, x, w)
+    if typ == "i8":
+        one = torch.ones(slots, device="cuda")
+        assert torch.equal(api.fs_expert_matmul_i8(x, one, plan, w, torch.ones(3, out, device="cuda")).double(), want)
+        return
+    y = torch.empty(slots, out, device="cuda")
+    assert torch.equal(api.fs_expert_matmul(x, plan, w, out=y).double(), want)
+    turned = buf[wide * 2:].as_strided((3, wide, out), (100 * stride, stride, 1))      # behind the rows of x, in the same memory
+    turned.copy_(w.transpose(1, 2))
+    assert torch.equal(api.fs_expert_matmul(x, plan, turned, turned=True, out=y).double(), want)
+    g = whole(gen, typ, slots, out)
+    d = torch.zeros(3, out, wide, dtype=torch.float64, device="cuda")
+    for e, (a, b) in enumerate(XO.bounds(plan.first.tolist(), slots)[:-1]):
+        d[e] = g[a:b].double().t().contiguous() @ x[a:b].double()
+    assert torch.equal(api.fs_expert_matmul_backward(g, x, plan).double(), d)
