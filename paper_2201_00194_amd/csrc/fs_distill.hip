@@ -283,7 +283,7 @@ __device__ __forceinline__ T anew(T v)
 }
 
 // Rows of which a thread keeps C chunks of 16 bytes in registers, so that they are read once.  As a chunk has done its work, the next row's is
-// asked for.  4096 rows of 131 072 bf16 and their gradient: 520 us, 4.1 TB/s of reads and writes (a copy reaches 4.7), 1000 rows of 32 001
+// asked for.  4096 rows of 131 072 bf16 and their gradient: 522 us, 4.1 TB/s of reads and writes (a copy reaches 4.7), 1000 rows of 32 001
 // fp16 with a rest 36 us, 3.5 TB/s; 5120 rows of 64 fp32, losses alone, 5.9 us, the chain of one verdict.
 template <int TYPE, bool GRADIENT, int WAVES, int C>
 __global__ void __launch_bounds__(Team<WAVES>::threads, WAVES == 16 ? 4 : C < 16 ? 1 : WAVES ? 4 : 3)
@@ -459,8 +459,9 @@ distill_row_kernel(DistillArgs a)
     }
 }
 
-// Rows of any length: read for their sums, AHEAD chunks of a thread on their way at once, and once more for the gradient.  Losses of many rows
-// come at 4.5 to 6 TB/s.  One row stays in one workgroup: of 131 072 bf16 13.5 us, what a compute unit takes to issue its exponentials.
+// Rows of any length: read for their sums, AHEAD chunks of a thread on their way at once, and once more for the gradient.  Losses of many rows: 4096
+// of 131 072 bf16 191 us, 5.6 TB/s, 8192 of 32 001 145 us, 3.6 TB/s, as nothing of the next row is on its way during a verdict.  One row stays in one
+// workgroup: of 131 072 bf16 12.9 us, what a compute unit takes to issue its exponentials.
 template <int TYPE, bool GRADIENT, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 1)
 distill_long_kernel(DistillArgs a)

@@ -187,7 +187,7 @@ product_stream_kernel(ProductArgs a)
 
 // Few rows an expert: what counts is how fast the weights arrive.  A workgroup makes sixteen columns of one expert's results; its
 // wavefronts share the sum out, 64 bytes of it each in turn, straight from memory to registers, and meet in LDS.  One row of 30
-// experts, 1024 x 1024 bf16: 5 us; 16 slots of 30 of 2048 x 2048 int8, 46 MB of weights: 12.6 us, 3.7 TB/s.
+// experts, 1024 x 1024 bf16: 5 us; 16 slots of 30 of 2048 x 2048 int8, 46 MB of weights: 12.9 us, 3.6 TB/s.
 constexpr int kFewWaves = 4;
 template <int TYPE, int RESULT, int MF>
 __global__ void __launch_bounds__(kFewWaves * 64)
@@ -337,8 +337,8 @@ __device__ __forceinline__ void store_weights(const WeightsArgs &a, const T &t, 
 // A workgroup makes BM x BN of an expert's gradient over one piece of its slots, and then others: the gradient itself where the
 // piece is all of them, else a partial sum.  Pieces differ in length.  The longest come first, and each round of tiles goes to the XCDs the
 // other way round than the one before, so that all have about the same to do; an XCD's tiles of a round are neighbours.
-// 131 072 slots of 64 experts, 1024 x 1024 bf16, a tenth nobody's: 336 us, 740 TFLOP/s, matrix units half busy: rows of both operands come
-// from memory as those of products do.  65 536 slots of 30, 164 x 256 fp32: 77 us, 71 TFLOP/s, 64 % busy.
+// 131 072 slots of 64 experts, 1024 x 1024 bf16, a tenth nobody's: 343 us, 725 TFLOP/s, matrix units half busy: rows of both operands come
+// from memory as those of products do.  65 536 slots of 30, 164 x 256 fp32: 78 us, 71 TFLOP/s, 64 % busy.
 template <int TYPE, class SHAPE, bool DIRECT>
 __global__ void __launch_bounds__(SHAPE::threads)
 weights_kernel(WeightsArgs a)
@@ -536,7 +536,7 @@ static void launch_product(ProductArgs a, hipStream_t stream)
 }
 
 // The shapes of weights' gradients, and how many slots a workgroup adds up: no more than a workgroup's share of all of them, so that the
-// longest experts end no later than the others.
+// longest experts end no later than the others; and 32 768 at most, as a piece is one sum in fp32, whatever the share is, and pieces meet in 64 bits.
 enum { kSmall, kMiddle, kWide };
 static int shape_of_weights(int32_t type, int64_t n_experts, int64_t in_width, int64_t out_width)
 {

@@ -3,8 +3,8 @@
 As in `mixture`, a router gives every statement row to k experts and its score is the weighted sum of theirs.  An expert is a network of
 one hidden layer here, score = v . max(W x, 0), so that router and experts are trained together by what programs measured.  The rows that an
 expert gets differ in number from expert to expert: its products are fs_expert_matmul's, its weights' gradients
-fs_expert_matmul_backward's.  Where the families of rows are known, the router learns from them directly (fs_distill); for serving, the
-weights are laid out once in 8-bit integers.
+fs_expert_matmul_backward's.  Where the families of rows are known, the router learns from them directly
+(fs_distill_backward, which gives the losses too); for serving, the weights are laid out once in 8-bit integers.
 
 The library does the work; this module only puts the calls in order.  PyTorch multiplies by the gate, clips at 0 and sums rows to programs.
 """
