@@ -101,3 +101,15 @@ def test_other_weights_put_in_between(api):
     before = mix.w.clone()
     mix.step(rows, o, target, rate=0.0)
     assert torch.equal(mix.w, before)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_no_rows(api, dtype):
+    import torch
+    typ = getattr(torch, dtype)
+    mix = NetworkMixture(api, 20, 3, hidden=16, dtype=typ)
+    before = mix.w.clone()
+    none, off = torch.empty(0, 20, dtype=typ, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    _, way = mix.forward(none, off)
+    assert all(bool((d == 0).all()) for d in mix.gradients(way, torch.ones(2, device="cuda")))
+    assert float(mix.step(none, off, torch.zeros(2, device="cuda"))) == 0 and torch.equal(mix.w, before)

@@ -235,3 +235,28 @@ def test_rows_far_apart(api, typ, pad):
     for e, (a, b) in enumerate(XO.bounds(plan.first.tolist(), slots)[:-1]):
         d[e] = g[a:b].double().t().contiguous() @ x[a:b].double()
     assert torch.equal(api.fs_expert_matmul_backward(g, x, plan).double(), d)
+
+
+@pytest.mark.parametrize("typ,step", [("fp16", -24), ("bf16", -133), ("fp32", -149)])
+@pytest.mark.parametrize("counts,wide,out,at", [([3, 0, 5], 64, 48, 0), ([300, 200], 96, 144, 0), ([300, 200], 96, 144, 1), ([20000, 13], 256, 1024, 0), ([20000, 13], 255, 63, 0)])
+def test_numbers_below_the_normal_ones(api, typ, step, counts, wide, out, at):
+    """Operands of some of the type's smallest steps are not taken for 0, nor are such results."""
+    import torch
+    gen = generator(wide + at)
+    plan, slots = plan_of(api, counts, 0), sum(counts)
+    x, w = whole(gen, typ, slots, wide, extra=at, at=at), whole(gen, typ, len(counts), out, wide)
+    want, d_want = exact(plan, x, w), torch.zeros(len(counts), out, wide, dtype=torch.float64, device="cuda")
+    up = 0 if typ == "fp16" else 100
+    small = x.double().mul(2.0 ** step).to(of(typ))
+    assert float(small.abs().max()) == 2.0 ** (step + 1) and bool((small.double() == x.double() * 2.0 ** step).all())
+    x.copy_(small)
+    big = w * 2.0 ** up
+    got = api.fs_expert_matmul(x, plan, big, out=torch.empty(slots, out, device="cuda"))
+    assert torch.equal(got.double(), want * 2.0 ** (step + up))
+    assert torch.equal(api.fs_expert_matmul(x, plan, big.transpose(1, 2).contiguous(), turned=True, out=got).double(), want * 2.0 ** (step + up))
+    if typ == "fp16":                                    # results of the type, of some of its smallest steps
+        assert torch.equal(api.fs_expert_matmul(x, plan, w).double(), want * 2.0 ** step)
+    g = whole(gen, typ, slots, out)
+    for e, (a, b) in enumerate(XO.bounds(plan.first.tolist(), slots)[:-1]):
+        d_want[e] = g[a:b].double().t().contiguous() @ (x[a:b].double() * 2.0 ** up)
+    assert torch.equal(api.fs_expert_matmul_backward(g * 2.0 ** up, x, plan).double(), d_want)
